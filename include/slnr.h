@@ -258,6 +258,129 @@ slnr_status slnr_sddmm_spmm_noalloc(const slnr_csr *B, const float *C, const flo
 slnr_status slnr_spmm_gemm_original(const slnr_csr *B, const float *C, int32_t K, const float *D, int32_t L,
                                     float *A, void *stream);
 
+/* ======================================================================
+ * Attention over a paged key/value cache
+ *
+ * The expressions above take a sparse pattern that the host made.  These
+ * entry points make patterns of blocks on the device and contract them at
+ * once: <SDDMM,SpMM> with a softmax between, its sparse operand the pages of a
+ * cache that each new token of a request sees.  One step of a program that
+ * serves requests is: slnr_page_tables, slnr_page_append, then
+ * slnr_paged_attention, or slnr_page_select and slnr_selected_attention.
+ *
+ * Conventions beside those at the top of this file:
+ *  - Keys, values and queries are bf16 or fp16 (slnr_dtype), one type for a
+ *    call; products, sums, maxima and weights' sums are fp32, the weights are
+ *    rounded to that type before their product with the values.
+ *  - head_dim is a multiple of 8 in [8, 128]; query heads are a multiple of
+ *    key heads, consecutive query heads share one.
+ *  - Strides are in values, multiples of 8, the last axis is packed; base
+ *    pointers are 16-byte aligned.  Outputs are packed.
+ *  - The new tokens of all requests are packed one request after another:
+ *    those of request r are [q_pos[r], q_pos[r+1]).  The k_len[r] keys of a
+ *    request include its new tokens, so new token i of n lies at position
+ *    k_len[r] - n + i and sees the keys up to that position.  A token at a
+ *    negative position sees none: its output is zero, its lse -inf.
+ *  - Slots past a request's last key, and pages not in use, are not read.
+ *    A key or value that is not finite makes the rows that see it, and the
+ *    rows of the same block that do not see it yet, not finite.
+ *  - q_pos, k_len, tables, req and slots are trusted without opts->validate; a page
+ *    outside the cache is then not read or written, what its keys add to a
+ *    result is not defined.
+ *  - opts->variant and allow_tf32 have no effect.  slnr_page_tables,
+ *    slnr_page_append and slnr_page_select need a workspace (256 bytes) in
+ *    validate mode only.
+ */
+typedef enum slnr_dtype { SLNR_BF16 = 0, SLNR_FP16 = 1 } slnr_dtype;
+
+/* The requests of a step. */
+typedef struct slnr_pages {
+  int32_t nreq;         /* requests */
+  int32_t ntok;         /* new tokens in all == q_pos[nreq] */
+  int32_t max_q;        /* no request has more new tokens */
+  int32_t max_k;        /* no request has more keys; <= width * page size */
+  int32_t width;        /* columns of table */
+  int32_t reserved;     /* must be 0 */
+  int64_t table_stride; /* from one row of table to the next */
+  const int32_t *q_pos; /* [nreq + 1] */
+  const int32_t *k_len; /* [nreq] */
+  const int32_t *table; /* [nreq][width]: entry n is the page of keys [n page_size, (n + 1) page_size) */
+  const int32_t *req;   /* [ntok] request of each token */
+  const int32_t *slots; /* [ntok] page * page_size + offset of each token; read by slnr_page_append only */
+} slnr_pages;
+
+/* The cache.  The summary (codes and scales) may be NULL where no call needs it. */
+typedef struct slnr_cache {
+  int32_t npages, page_size, nheads, head_dim;
+  int32_t dtype;        /* slnr_dtype */
+  int32_t reserved;     /* must be 0 */
+  int64_t k_stride[3];  /* page, slot, head */
+  int64_t v_stride[3];
+  void *k, *v;          /* [npages][page_size][nheads][head_dim] by those strides */
+  int8_t *codes;        /* [npages][nheads][head_dim], packed */
+  float *scales;        /* [npages][nheads], packed */
+} slnr_cache;
+
+/* Rows [token][head][head_dim] of queries, new keys or new values. */
+typedef struct slnr_rows {
+  const void *p;
+  int64_t stride_tok, stride_head;
+} slnr_rows;
+
+/* ---- block tables and slot maps ------------------------------------------
+ * From the lengths of the requests before the step (old_len) and their new
+ * tokens (new_len), with page size s: q_pos (sums of new_len), k_len = old_len
+ * + new_len, and for each new token its request and its slot.  Request r holds
+ * ceil(old_len/s) pages; the ones that it needs beside them, up to
+ * ceil(k_len/s), are taken from free_pages in the requests' order and written
+ * to its row of table (in place; other entries are kept).  used[0] = pages
+ * taken.  Where free_pages or the table's width is too short the entry and the
+ * slots of that page are -1 (validate: SLNR_ERR_INDEX). */
+slnr_status slnr_page_tables(int32_t nreq, const int32_t *new_len, const int32_t *old_len, int32_t *table,
+                             int64_t table_stride, int32_t width, const int32_t *free_pages, int32_t nfree,
+                             int32_t page_size, int32_t ntok, int32_t *q_pos, int32_t *k_len, int32_t *req,
+                             int32_t *slots, int32_t *used, const slnr_opts *opts);
+
+/* ---- new keys and values into the cache -----------------------------------
+ * K[slot_t] = k_t and V[slot_t] = v_t for each new token (a negative slot is
+ * skipped).  Where cache->codes is not NULL, each page whose last slot is
+ * written gets its summary, per head: m = the mean of its keys, scale =
+ * max|m| / 127, codes = m / scale rounded to the nearest whole number (0 if
+ * scale is 0). */
+slnr_status slnr_page_append(const slnr_cache *cache, const slnr_pages *pages, const slnr_rows *k,
+                             const slnr_rows *v, const slnr_opts *opts);
+
+/* ---- pages for each token by a cheap score ---------------------------------
+ * Of the pages up to a token's own, per key head: the first `first`, the last
+ * `last` (its own among them), and of the others those of the highest score,
+ * the lower page where scores are equal, npicked in all (fewer if there are
+ * fewer).  score(page) = (sum_d c_d codes_d) * scales: c is the sum u of the
+ * group's query rows (fp32, in the heads' order) coded as u f rounded to the
+ * nearest whole number, f = 127 (1 / max|u|) in fp32.  The sum is a whole number, so scores do not depend on an order of
+ * summation.  picked[ntok][nheads][npicked] holds pages of the request (columns
+ * of table) in ascending order, -1 behind them.  first >= 0, last >= 1, first +
+ * last <= npicked <= 1024; at most 51000 pages a request. */
+slnr_status slnr_page_select(const slnr_rows *q, int32_t nheads_q, const slnr_cache *cache,
+                             const slnr_pages *pages, int32_t *picked, int32_t npicked, int32_t first,
+                             int32_t last, const slnr_opts *opts);
+
+/* ---- attention over all pages, and over picked ones ------------------------
+ * out[t, h] = sum_j softmax_j(scale q[t, h] . K[j]) V[j] over the keys j that
+ * token t sees (slnr_selected_attention: those in the pages that picked[t,
+ * h div group] lists, which are distinct; negative entries are none), lse[t, h]
+ * = log sum_j exp(scale q . K[j]) (natural; may be NULL).  out has the cache's
+ * type, [ntok][nheads_q][head_dim]; lse is fp32 [ntok][nheads_q]. */
+slnr_status slnr_paged_attention_workspace(const slnr_cache *cache, const slnr_pages *pages, int32_t nheads_q,
+                                           const slnr_opts *opts, size_t *bytes);
+slnr_status slnr_selected_attention_workspace(const slnr_cache *cache, const slnr_pages *pages, int32_t nheads_q,
+                                              int32_t npicked, const slnr_opts *opts, size_t *bytes);
+slnr_status slnr_paged_attention(const slnr_rows *q, int32_t nheads_q, const slnr_cache *cache,
+                                 const slnr_pages *pages, float scale, void *out, float *lse,
+                                 const slnr_opts *opts);
+slnr_status slnr_selected_attention(const slnr_rows *q, int32_t nheads_q, const slnr_cache *cache,
+                                    const slnr_pages *pages, const int32_t *picked, int32_t npicked, float scale,
+                                    void *out, float *lse, const slnr_opts *opts);
+
 /* ---- per-launch timing (instrumentation) --------------------------------
  * With timing enabled, each call on the calling thread records a CUDA event on
  * opts->stream before each of its phases (a named step of one or two kernel

@@ -53,9 +53,28 @@ class slnr_opts(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+class slnr_pages(ctypes.Structure):
+    _fields_ = [("nreq", ctypes.c_int32), ("ntok", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("reserved", ctypes.c_int32), ("table_stride", ctypes.c_int64),
+                ("q_pos", ctypes.c_void_p), ("k_len", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("req", ctypes.c_void_p), ("slots", ctypes.c_void_p)]
+
+
+class slnr_cache(ctypes.Structure):
+    _fields_ = [("npages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("nheads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class slnr_rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("stride_tok", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
+
+
 # name -> (argtypes, restype) of every symbol declared in include/slnr.h
 _P, _I32, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)
 _CSR, _CSF, _OPT = ctypes.POINTER(slnr_csr), ctypes.POINTER(slnr_csf3), ctypes.POINTER(slnr_opts)
+_PG, _CA, _RO = ctypes.POINTER(slnr_pages), ctypes.POINTER(slnr_cache), ctypes.POINTER(slnr_rows)
 SIGNATURES = {
     "slnr_spmm_gemm_workspace": ([_CSR, _I32, _I32, _OPT, _SZ], ctypes.c_int),
     "slnr_sddmm_spmm_workspace": ([_CSR, _I32, _I32, _OPT, _SZ], ctypes.c_int),
@@ -73,6 +92,14 @@ SIGNATURES = {
     "slnr_mttkrp_gemm": ([_CSF, _P, _P, _I32, _P, _I32, _P, _OPT], ctypes.c_int),
     "slnr_spmmh_gemm": ([_CSR, _P, _P, _I32, _P, _I32, _P, _OPT], ctypes.c_int),
     "slnr_sddmm_spmm_noalloc": ([_CSR, _P, _P, _I32, _P, _I32, _P, _P], ctypes.c_int),
+    "slnr_page_tables": ([_I32, _P, _P, _P, ctypes.c_int64, _I32, _P, _I32, _I32, _I32, _P, _P, _P, _P, _P, _OPT],
+                         ctypes.c_int),
+    "slnr_page_append": ([_CA, _PG, _RO, _RO, _OPT], ctypes.c_int),
+    "slnr_page_select": ([_RO, _I32, _CA, _PG, _P, _I32, _I32, _I32, _OPT], ctypes.c_int),
+    "slnr_paged_attention_workspace": ([_CA, _PG, _I32, _OPT, _SZ], ctypes.c_int),
+    "slnr_selected_attention_workspace": ([_CA, _PG, _I32, _I32, _OPT, _SZ], ctypes.c_int),
+    "slnr_paged_attention": ([_RO, _I32, _CA, _PG, ctypes.c_float, _P, _P, _OPT], ctypes.c_int),
+    "slnr_selected_attention": ([_RO, _I32, _CA, _PG, _P, _I32, ctypes.c_float, _P, _P, _OPT], ctypes.c_int),
     "slnr_set_wait_limit": ([ctypes.c_int64], ctypes.c_int),
     "slnr_peak_ffma": ([_P, ctypes.POINTER(ctypes.c_double)], ctypes.c_int),
     "slnr_peak_tf32": ([_P, ctypes.POINTER(ctypes.c_double)], ctypes.c_int),
@@ -521,3 +548,17 @@ def run(op: str, B, dense: dict, **kw):
     if op == "spmmh_gemm":
         return spmmh_gemm(B, dense["C"], dense["D"], dense["E"], **kw)
     raise ValueError(op)
+
+
+# ---- the paged cache (paged.py; imported on first use: it needs torch) ---------------------
+
+_PAGED = ("PageTables", "PagedCache", "page_tables", "page_append", "page_select", "paged_attention",
+          "selected_attention")
+
+
+def __getattr__(name):
+    if name in _PAGED:
+        from . import paged
+        globals().update((n, getattr(paged, n)) for n in _PAGED)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -4,6 +4,7 @@
 #include <cstdio>
 #include <cstring>
 
+#include "call.h"
 #include "launch.h"
 
 using namespace slnr;
@@ -12,14 +13,6 @@ namespace {
 
 thread_local char g_last_error[512] = "";
 thread_local long long g_wait_limit = 0;  // 0: kWaitCycles
-
-slnr_status fail(slnr_status st, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
-  va_end(ap);
-  return st;
-}
 
 // ---------------------------------------------------------------------------
 // per-launch timing (slnr_timing_*): events recorded between launches
@@ -34,6 +27,18 @@ struct Timing {
 };
 thread_local Timing g_timing;
 thread_local int32_t g_launches = 0;  // kernel launches of this thread's current call
+
+}  // namespace
+
+namespace slnr {
+
+slnr_status fail(slnr_status st, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
+  va_end(ap);
+  return st;
+}
 
 void timing_begin() {
   g_timing.n = 0;
@@ -50,18 +55,14 @@ void timing_end(cudaStream_t s) {
   if (g_timing.on && g_timing.n > 0) cudaEventRecord(g_timing.ev[g_timing.n], s);
 }
 
-#define SLNR_CUDA(expr)                                                                   \
-  do {                                                                                    \
-    cudaError_t e_ = (expr);                                                              \
-    if (e_ != cudaSuccess) return fail(SLNR_ERR_CUDA, "%s: %s", #expr, cudaGetErrorString(e_)); \
-  } while (0)
+}  // namespace slnr
+
+namespace {
 
 // Widths the specialised kernels take (powers of two in [4, 256]); any other
 // multiple of 4 up to kWideMax goes to the run-time-width kernels (wide.cu).
 bool pow2_dim(int32_t d) { return d >= 4 && d <= 256 && (d & (d - 1)) == 0; }
 bool all_pow2(int32_t a, int32_t b, int32_t c = 4) { return pow2_dim(a) && pow2_dim(b) && pow2_dim(c); }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // ---------------------------------------------------------------------------
 // workspace layout (identical for the size query and the call)
@@ -233,28 +234,6 @@ slnr_status check_dense(const char* what, const void* p) {
   if (!aligned16(p)) return fail(SLNR_ERR_UNSUPPORTED, "%s must be 16-byte aligned", what);
   return SLNR_OK;
 }
-
-slnr_status check_ws(const slnr_opts* o, size_t need) {
-  if (!o->workspace) return fail(SLNR_ERR_WORKSPACE, "workspace is NULL (needs %zu bytes)", need);
-  if ((reinterpret_cast<uintptr_t>(o->workspace) & 255u) != 0)
-    return fail(SLNR_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (o->workspace_bytes < need)
-    return fail(SLNR_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", o->workspace_bytes, need);
-  return SLNR_OK;
-}
-
-// A kernel launch of the call: timing mark, then the launch, then its status.
-#define SLNR_LAUNCH(name, expr) \
-  do {                          \
-    timing_mark(name, s);       \
-    SLNR_CUDA(expr);            \
-  } while (0)
-
-#define SLNR_CHECK(expr)            \
-  do {                              \
-    slnr_status st_ = (expr);       \
-    if (st_ != SLNR_OK) return st_; \
-  } while (0)
 
 // Zero the header, then (validate mode) run the device check and wait for it.
 // own_header: the call's first kernel sets the only header word that it uses.

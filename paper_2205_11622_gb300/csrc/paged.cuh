@@ -1,0 +1,97 @@
+// What the paged-cache kernels share: their views of the arguments, the
+// division by the page size, and the launchers that the C entry points call.
+#pragma once
+
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "common.cuh"
+#include "divide.h"
+
+namespace slnr {
+
+// The requests of a step (slnr_pages) as kernels take them.
+struct PagesView {
+  int nreq, ntok, width, max_q, max_k;
+  int64_t table_stride;
+  const int32_t *q_pos, *k_len, *table, *req, *slots;
+};
+
+// Rows of a tensor [token, head, column]; strides in values.
+struct RowsView {
+  const void* p;
+  int64_t tok, head;
+};
+
+// The cache (slnr_cache); strides in values.
+struct CacheView {
+  void *k, *v;
+  int64_t ks[3], vs[3];  // page, slot, head
+  int npages, nheads, width;
+  Divisor page;
+  int8_t* codes;
+  float* scales;
+};
+
+#ifdef __CUDACC__
+// Page of a slot.
+__device__ __forceinline__ int page_of(int slot, const CacheView& c) { return c.page.div(slot); }
+#endif
+
+// How the rows of an attention call go to blocks.
+//
+// The rows of a request and key head are its tokens' query rows of that head's
+// group: row x is token x / G, query head g = x % G.  A block takes `tile` of
+// them and at most `chunk` keys; the partial results of a row's `nsplit` chunks
+// are combined in the chunks' order.
+struct AttnPlan {
+  int tile;     // rows a block takes
+  int ntiles;   // bound of the row tiles of all requests
+  int chunk;    // keys of one split, a multiple of kAttnKeys
+  int nsplit;   // splits of the longest request (1: the block writes the result)
+  float* part;  // [ntok * nheads_q][nsplit][width] partial rows, each divided by its own sum
+  float* part_lse;  // [ntok * nheads_q][nsplit] log2 of the partial sums of exponentials
+};
+
+constexpr int kAttnKeys = 64;       // keys of one step of the row kernel
+constexpr int kAttnMaxPicked = 1024;  // pages picked for one row
+
+struct AttnArgs {
+  PagesView p;
+  CacheView c;
+  RowsView q;
+  Divisor group;  // G
+  float scale;
+  void* out;      // [ntok][nheads_q][width], packed
+  float* lse;     // [ntok][nheads_q] or NULL
+  const int32_t* picked;  // selected attention: [ntok][nheads][npicked]
+  int npicked;
+  AttnPlan plan;
+};
+
+// pages.cu
+cudaError_t launch_page_tables(int nreq, const int32_t* new_len, const int32_t* old_len, int32_t* table,
+                               int64_t table_stride, int width, const int32_t* free_pages, int nfree, int page_size,
+                               int ntok, int32_t* q_pos, int32_t* k_len, int32_t* req, int32_t* slots, int32_t* used,
+                               cudaStream_t s);
+cudaError_t launch_page_append(const PagesView& p, const CacheView& c, const RowsView& k, const RowsView& v, int dtype,
+                               cudaStream_t s);
+cudaError_t launch_validate_lengths(int nreq, const int32_t* new_len, const int32_t* old_len, const int32_t* table,
+                                    int64_t table_stride, int width, int nfree, int page_size, int ntok, WsHeader* hdr,
+                                    cudaStream_t s);
+cudaError_t launch_validate_pages(const PagesView& p, int npages, Divisor page, bool slots, const int32_t* picked,
+                                  int npicked, int nheads, WsHeader* hdr, cudaStream_t s);
+
+// page_select.cu
+// Tokens whose scores over `pages` pages one block holds; 0: too many pages.
+int select_tokens(int pages);
+cudaError_t launch_page_select(const PagesView& p, const CacheView& c, const RowsView& q, int dtype, int nheads_q,
+                               int32_t* picked, int npicked, int first, int last, cudaStream_t s);
+
+// paged_attn.cu
+cudaError_t launch_paged_rows(const AttnArgs& a, int dtype, cudaStream_t s);
+cudaError_t launch_paged_combine(const AttnArgs& a, int dtype, cudaStream_t s);
+
+}  // namespace slnr

@@ -1,0 +1,210 @@
+"""Attention over a paged cache against its definition in 64 bits (GPU): all pages and picked ones."""
+import itertools
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import _paged as P  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP16 = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def slnr():
+    import paper_2205_11622_gb300 as m
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    m.build()
+    m.lib()
+    return m
+
+
+# (new tokens, keys): one token; none; fewer keys than tokens (the first tokens see nothing); no keys at all
+EDGES = [(1, 1), (0, 40), (3, 3), (5, 2), (2, 0), (1, 130), (7, 63), (0, 0), (1, 64), (4, 65)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("heads", [(8, 8), (8, 2), (6, 2), (16, 1)])
+@pytest.mark.parametrize("D,page", [(128, 16), (64, 32), (80, 7), (8, 1), (40, 64), (96, 130)])
+def test_edges(slnr, dtype, heads, D, page):
+    b = P.Batch(EDGES, page, *heads, D, dtype, seed=D + page)
+    got = slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), validate=True)
+    b.check(got, b.attention(D ** -0.5))
+
+
+@pytest.mark.parametrize("lens", [[(1, 5000)], [(1, 5000), (1, 77), (1, 2049), (1, 0)], [(2, 3001), (1, 9)],
+                                  [(9, 2500), (1, 1)], [(40, 1500)], [(70, 70), (3, 400), (1, 1)], [(129, 700), (130, 131)],
+                                  [(300, 300)], [(257, 1000), (1, 3000)]])
+@pytest.mark.parametrize("heads,D,page,first", [((4, 1), 128, 16, False), ((8, 4), 64, 48, True), ((3, 3), 128, 64, True)])
+def test_lengths(slnr, lens, heads, D, page, first):
+    """Single tokens over many splits, short chunks, chunks: every row tile, and requests of different kinds together."""
+    b = P.Batch(lens, page, *heads, D, seed=len(lens), heads_first=first)
+    got = slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), validate=True)
+    b.check(got, b.attention(D ** -0.5))
+
+
+@pytest.mark.parametrize("scale", [0.0, 1.0, -0.3, 4.0])
+def test_scales(slnr, scale):
+    """Any finite scale; with a large one a single key takes all the weight."""
+    b = P.Batch([(3, 200), (1, 900)], 16, 4, 2, 64, FP16, seed=5)
+    b.q = (b.q.float() * 0.25).to(FP16)  # keeps the scores' own error (which grows with the scale) below the tolerance
+    got = slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), scale=scale)
+    b.check(got, b.attention(scale))
+
+
+def test_large_scores(slnr):
+    """Scores of some hundreds, rising and falling along the keys: the running maximum rescales what was summed."""
+    for lens in ([(1, 700)], [(200, 700)]):
+        b = P.Batch(lens, 16, 4, 1, 64, BF16, seed=6)
+        ramp = torch.linspace(-30, 30, b.npages).roll(3)[:, None, None, None]
+        b.k = torch.where(torch.isnan(b.k), b.k, ramp.to(BF16).expand_as(b.k))
+        b.q = torch.ones_like(b.q)
+        b.kd = b.k.cuda()
+        got = slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), scale=0.125)
+        b.check(got, b.attention(0.125))
+
+
+def test_lowest_values(slnr):
+    """Keys at the type's lowest finite value: scores of -1e38 and below are finite or -inf, never NaN beside a finite one."""
+    b = P.Batch([(1, 40)], 16, 2, 1, 64, BF16, seed=7)
+    low = torch.finfo(BF16).min
+    at = b.table[0, :3].long()
+    b.k[at] = torch.where(torch.isnan(b.k[at]), b.k[at], torch.zeros_like(b.k[at]))
+    b.k[at[1], 3, 0] = low / 64
+    b.q = torch.full_like(b.q, 0.5)
+    b.kd = b.k.cuda()
+    got = slnr.paged_attention(b.q.cuda(), b.cache(), b.tables())
+    b.check(got, b.attention(64 ** -0.5))
+
+
+def test_inputs_of_other_strides(slnr):
+    """Queries as a slice of a wider projection, a table that is a slice of a wider one, every second page of a cache."""
+    b = P.Batch([(2, 300), (1, 41)], 16, 8, 2, 64, seed=8)
+    wide = torch.full((b.T, 8 + 4, 64 + 8), math.nan, dtype=BF16, device="cuda")
+    wide[:, 2:10, :64] = b.q.cuda()
+    table = torch.full((2, 64), 7, dtype=torch.int32, device="cuda")
+    table[:, 5:5 + b.width] = b.table.cuda()
+    kv = torch.full((2 * b.npages, 16, 2, 2, 64), math.nan, dtype=BF16, device="cuda")
+    kv[::2, :, :, 0], kv[::2, :, :, 1] = b.kd, b.vd
+    cache = slnr.PagedCache(k=kv[::2, :, :, 0], v=kv[::2, :, :, 1])
+    out = torch.empty((b.T, 8, 64), dtype=BF16, device="cuda")
+    lse = torch.empty((b.T, 8), device="cuda")
+    got = slnr.paged_attention(wide[:, 2:10, :64], cache, b.tables(table=table[:, 5:5 + b.width]), out=out, lse=lse)
+    assert got[0] is out and got[1] is lse
+    b.check(got, b.attention(0.125))
+
+
+def test_offsets_past_32_bits(slnr):
+    """Pages 2^27 values apart: the last ones lie past 2^32 values (and 2^33 bytes) into the cache."""
+    b = P.Batch([(1, 600), (70, 90)], 16, 4, 2, 64, seed=9)
+    stride = 1 << 27
+    buf = torch.empty((b.npages - 1) * stride + (1 << 16), dtype=BF16, device="cuda")
+    assert buf.numel() > 1 << 32
+    view = lambda o: buf.as_strided((b.npages, 16, 2, 64), (stride, 128, 64, 1), o)  # noqa: E731
+    k, v = view(0), view(1 << 15)
+    k.copy_(b.kd)
+    v.copy_(b.vd)
+    b.check(slnr.paged_attention(b.q.cuda(), slnr.PagedCache(k=k, v=v), b.tables()), b.attention(0.125))
+
+
+def test_bounds_wider_than_the_batch(slnr):
+    """max_q and max_k are bounds: larger ones change the split of the work, not the result's meaning."""
+    b = P.Batch([(1, 500), (3, 20)], 16, 4, 2, 64, width=200, seed=10)
+    ref = b.attention(0.125)
+    for max_q, max_k in itertools.product((3, 9, 100), (500, 3200)):
+        b.check(slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(max_q=max_q, max_k=max_k)), ref, f"{max_q} {max_k}")
+
+
+@pytest.mark.parametrize("lens", [[(1, 3000)], [(300, 900)]])
+def test_same_call_same_bits(slnr, lens):
+    b = P.Batch(lens, 16, 8, 2, 128, seed=11)
+    args = (b.q.cuda(), b.cache(), b.tables())
+    one, two = slnr.paged_attention(*args), slnr.paged_attention(*args)
+    assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+
+
+def test_other_stream(slnr):
+    """On a stream that is given, and on one that is current; each waits for nothing but what its caller ordered."""
+    b = P.Batch([(1, 3000), (5, 70)], 16, 8, 2, 64, seed=12)
+    ref, cache, tables, q = b.attention(0.125), b.cache(), b.tables(), b.q.cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = slnr.paged_attention(q, cache, tables, stream=side)
+    with torch.cuda.stream(side):
+        also = slnr.paged_attention(q, cache, tables)
+    side.synchronize()
+    b.check(got, ref)
+    b.check(also, ref)
+
+
+def test_graph(slnr):
+    """A captured call, replayed on new inputs in the same tensors."""
+    b = P.Batch([(1, 3000), (1, 70)], 16, 8, 2, 64, seed=13)
+    cache, tables, q = b.cache(), b.tables(), torch.zeros_like(b.q).cuda()
+    slnr.paged_attention(q, cache, tables)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = slnr.paged_attention(q, cache, tables)
+    q.copy_(b.q)
+    graph.replay()
+    torch.cuda.synchronize()
+    b.check(got, b.attention(0.125))
+
+
+def test_nothing_to_do(slnr):
+    b = P.Batch([(0, 10), (0, 0)], 16, 4, 2, 64)
+    out, lse = slnr.paged_attention(b.q.cuda(), b.cache(), b.tables())
+    assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
+    b = P.Batch([], 16, 4, 2, 64)
+    out, lse = slnr.paged_attention(b.q.cuda(), b.cache(), b.tables())
+    assert out.shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("heads", [(8, 8), (8, 2), (6, 2), (40, 1)])
+@pytest.mark.parametrize("D,page,n", [(128, 16, 9), (64, 64, 4), (80, 7, 5), (8, 1, 33)])
+def test_selected(slnr, dtype, heads, D, page, n):
+    b = P.Batch([(1, 700), (0, 5), (3, 3), (5, 2), (9, 400), (2, 0), (1, 1)], page, *heads, D, dtype, seed=D + n)
+    picked = P.picks(b, n, seed=n)
+    got = slnr.selected_attention(b.q.cuda(), b.cache(), b.tables(), picked.cuda(), validate=True)
+    b.check(got, b.attention(D ** -0.5, picked))
+
+
+def test_selected_many_pages(slnr):
+    """More picked pages than one block takes: splits joined, empty ones among them."""
+    b = P.Batch([(1, 5000), (2, 5000)], 16, 8, 2, 128, seed=21)
+    for n in (1, 100, 300):
+        picked = P.picks(b, n, seed=n)
+        picked[0, 0] = -1
+        got = slnr.selected_attention(b.q.cuda(), b.cache(), b.tables(), picked.cuda(), validate=True)
+        b.check(got, b.attention(128 ** -0.5, picked), f"{n} pages")
+
+
+@pytest.mark.parametrize("heads,D,page", [((8, 2), 128, 64), ((4, 4), 64, 16), ((16, 1), 96, 32), ((6, 2), 64, 48)])
+def test_selected_chunk(slnr, heads, D, page):
+    """A chunk of tokens whose picks overlap, beside single tokens."""
+    b = P.Batch([(150, 1200), (1, 300), (60, 60)], page, *heads, D, seed=22)
+    picked = P.picks(b, 6, seed=23)
+    got = slnr.selected_attention(b.q.cuda(), b.cache(), b.tables(), picked.cuda(), validate=True)
+    b.check(got, b.attention(D ** -0.5, picked))
+
+
+def test_selected_pages_past_the_token(slnr):
+    """Picked pages that begin after the token hold nothing that it sees."""
+    b = P.Batch([(4, 64)], 16, 2, 1, 64, seed=24)
+    b.lens, b.k_len = [(4, 64)], torch.tensor([64], dtype=torch.int32)
+    picked = torch.tensor([[[1, 3]], [[3, -1]], [[-1, -1]], [[0, 3]]], dtype=torch.int32)
+    got = slnr.selected_attention(b.q.cuda(), b.cache(), b.tables(), picked.cuda())
+    b.check(got, b.attention(0.125, picked))
+
+
+def test_all_pages_picked_is_paged_attention(slnr):
+    b = P.Batch([(5, 200), (1, 17)], 16, 4, 2, 64, seed=25)
+    picked = torch.arange(b.width, dtype=torch.int32).expand(b.T, 2, b.width).clone()
+    picked[picked > (b.pos // 16)[:, None, None]] = -1
+    b.check(slnr.selected_attention(b.q.cuda(), b.cache(), b.tables(), picked.cuda()), b.attention(0.125))
