@@ -49,13 +49,15 @@ __device__ __forceinline__ int page_of(int slot, const CacheView& c) { return c.
 struct AttnPlan {
   int tile;     // rows a block takes
   int ntiles;   // bound of the row tiles of all requests
-  int chunk;    // keys of one split, a multiple of kAttnKeys
+  int chunk;    // keys of one split, a multiple of kChunkKeys
   int nsplit;   // splits of the longest request (1: the block writes the result)
   float* part;  // [ntok * nheads_q][nsplit][width] partial rows, each divided by its own sum
   float* part_lse;  // [ntok * nheads_q][nsplit] log2 of the partial sums of exponentials
 };
 
 constexpr int kAttnKeys = 64;       // keys of one step of the row kernel
+constexpr int kChunkKeys = 128;     // and of the tensor-core kernel, whose blocks take
+constexpr int kChunkRows = 256;     // that many rows
 constexpr int kAttnMaxPicked = 1024;  // pages picked for one row
 
 struct AttnArgs {
@@ -90,7 +92,10 @@ int select_tokens(int pages);
 cudaError_t launch_page_select(const PagesView& p, const CacheView& c, const RowsView& q, int dtype, int nheads_q,
                                int32_t* picked, int npicked, int first, int last, cudaStream_t s);
 
-// paged_attn.cu
+// paged_chunk.cu (plan.tile == kChunkRows, scale > 0, no picked pages; hdr's flag word is zero)
+cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s);
+
+// paged_attn.cu (any other plan)
 cudaError_t launch_paged_rows(const AttnArgs& a, int dtype, cudaStream_t s);
 cudaError_t launch_paged_combine(const AttnArgs& a, int dtype, cudaStream_t s);
 

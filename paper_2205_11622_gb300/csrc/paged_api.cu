@@ -123,25 +123,27 @@ constexpr int64_t kResident = 304;
 constexpr int64_t kMaxBlocks = 16384;  // splits stop here
 
 // Row tiles and key splits of an attention call: by the bounds alone, never by
-// device data.
+// device data.  Calls with a request of more than 64 rows go to the tensor-core
+// kernel (256 rows a block), the others to the row kernel.
 AttnPlan attn_plan(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, int32_t npicked) {
   AttnPlan a{};
   const int64_t G = nheads_q / c.nheads, rows = npicked > 0 ? G : p.max_q * G;
-  a.tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  a.tile = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || npicked > 0 ? 64 : kChunkRows;
   const int64_t tiles = npicked > 0 ? p.ntok * ceil_div(G, a.tile)
                                     : p.ntok * G / a.tile + (p.nreq < p.ntok ? p.nreq : p.ntok);
   const int64_t keys = npicked > 0 ? (int64_t)npicked * c.page_size : p.max_k;
   const int64_t blocks = tiles * c.nheads;
   int64_t chunk = keys;
   if (blocks > 0) {
-    const int64_t want = ceil_div(2 * kResident, blocks);
-    chunk = ceil_div(keys, want);
-    if (chunk < 128) chunk = 128;
-    if (a.tile == 16 && chunk > 1024) chunk = 1024;
-    const int64_t least = ceil_div(keys * blocks, kMaxBlocks);
+    const bool tc = a.tile == kChunkRows;
+    const int64_t least = tc ? 512 : 128;
+    chunk = ceil_div(keys, ceil_div(tc ? 3 * kResident / 2 : 2 * kResident, blocks));
     if (chunk < least) chunk = least;
+    if (a.tile == 16 && chunk > 1024) chunk = 1024;
+    const int64_t floor = ceil_div(keys * blocks, kMaxBlocks);
+    if (chunk < floor) chunk = floor;
   }
-  chunk = ceil_div(chunk > 0 ? chunk : 1, kAttnKeys) * kAttnKeys;
+  chunk = ceil_div(chunk > 0 ? chunk : 1, kChunkKeys) * kChunkKeys;
   a.ntiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
   a.chunk = (int)chunk;
   a.nsplit = keys > 0 ? (int)ceil_div(keys, chunk) : 1;
@@ -188,7 +190,7 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   if (!aligned16(out)) return fail(SLNR_ERR_UNSUPPORTED, "out must be 16-byte aligned");
   AttnArgs a{view(*pages), view(*cache), view(*q), divisor(nheads_q / cache->nheads), scale, out, lse, picked, npicked,
              attn_plan(*cache, *pages, nheads_q, npicked)};
-  if (a.plan.nsplit > 65535 || a.plan.ntiles == INT32_MAX || (int64_t)pages->max_q * a.group.d >= (int64_t(1) << 31) ||
+  if (a.plan.nsplit > 65535 || a.plan.ntiles == INT32_MAX || (a.plan.tile == kChunkRows && a.plan.ntiles > 65535) || (int64_t)pages->max_q * a.group.d >= (int64_t(1) << 31) ||
       (int64_t)npicked * cache->page_size >= (int64_t(1) << 31))
     return fail(SLNR_ERR_UNSUPPORTED, "too many rows or keys for one call");
   const AttnLayout l = attn_layout(*cache, *pages, nheads_q, a.plan);
@@ -200,9 +202,21 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
     return launch_validate_pages(a.p, a.c.npages, a.c.page, false, picked, npicked, a.c.nheads, hdr, st);
   }));
-  SLNR_LAUNCH("paged_rows", launch_paged_rows(a, cache->dtype, s));
+  const bool tc = a.plan.tile == kChunkRows;
+  if (tc) {
+    SLNR_CUDA(cudaMemsetAsync(ws, 0, sizeof(WsHeader), s));
+    SLNR_LAUNCH("paged_chunk", launch_paged_chunk(a, cache->dtype, (WsHeader*)ws, s));
+  } else {
+    SLNR_LAUNCH("paged_rows", launch_paged_rows(a, cache->dtype, s));
+  }
   if (a.plan.nsplit > 1) SLNR_LAUNCH("paged_combine", launch_paged_combine(a, cache->dtype, s));
   timing_end(s);
+  if (tc && opts->validate) {
+    int flag = 0;
+    SLNR_CUDA(cudaMemcpyAsync(&flag, &((WsHeader*)ws)->error, sizeof(int), cudaMemcpyDeviceToHost, s));
+    SLNR_CUDA(cudaStreamSynchronize(s));
+    if (flag != 0) return fail(SLNR_ERR_TIMEOUT, "a bounded device-side wait gave up (flags 0x%x)", flag);
+  }
   return SLNR_OK;
 }
 

@@ -16,7 +16,7 @@
 // every key is read from shared memory by WM warps only.
 #include "launch.h"
 #include "mma16.cuh"
-#include "paged.cuh"
+#include "paged_tile.cuh"
 
 namespace slnr {
 namespace {
@@ -29,36 +29,6 @@ template <int W>
 constexpr int stage_bytes() { return 2 * kAttnKeys * W * 2; }
 template <int W>
 constexpr size_t smem_bytes() { return (size_t)kStages * stage_bytes<W>(); }
-
-// Row tiles of a request with n rows.
-__device__ __forceinline__ int tiles_of(int rows, int tile) { return rows > 0 ? (rows - 1) / tile + 1 : 0; }
-
-// Request and first row of flat row tile `b`; r = -1 past the last one.  A whole
-// warp looks at 32 requests a step.
-__device__ __forceinline__ void find_tile(const PagesView& p, int group, int tile, int b, int& r, int& x0) {
-  const int lane = threadIdx.x & 31;
-  int before = 0;
-  for (int r0 = 0; r0 < p.nreq; r0 += 32) {
-    int n = 0;
-    if (r0 + lane < p.nreq) n = tiles_of((__ldg(p.q_pos + r0 + lane + 1) - __ldg(p.q_pos + r0 + lane)) * group, tile);
-    int sum = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += y;
-    }
-    const unsigned past = __ballot_sync(0xffffffffu, before + sum > b);
-    if (past) {
-      const int i = __ffs(past) - 1;
-      r = r0 + i;
-      x0 = (b - before - __shfl_sync(0xffffffffu, sum - n, i)) * tile;
-      return;
-    }
-    before += __shfl_sync(0xffffffffu, sum, 31);
-  }
-  r = -1;
-  x0 = 0;
-}
 
 struct Smem {
   int2 window[kAttnMaxPicked > kWindow ? kAttnMaxPicked : kWindow];  // {page of the cache, page of the request}
@@ -319,9 +289,9 @@ k_paged_rows(AttnArgs a) {
         acc[4 * e + 3] += f * z.w;
       }
     }
-    const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
+    const float inv = __fdividef(1.f, sum);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= inv;
+    for (int e = 0; e < 8; ++e) acc[e] = sum == 0.f ? 0.f : acc[e] * inv;  // no key: zeros
     const float lse2 = mx + __log2f(sum);  // no key: -inf
     const int tok = a.group.div(x0 + x), g = x0 + x - tok * G;
     const int64_t at = (q0 + tok) * hq + h * G + g;
@@ -389,7 +359,7 @@ k_paged_combine(AttnArgs a) {
       acc.w += f * x.w;
     }
   }
-  const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
+  const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);  // the parts of a row without keys are zeros
   if (col < a.c.width) {
     uint2 y;
     y.x = Half2<T>::pack(acc.x * inv, acc.y * inv);

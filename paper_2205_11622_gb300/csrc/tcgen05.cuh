@@ -196,5 +196,90 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// ---- 16-bit operands (kind::f16) ---------------------------------------------
+// Instruction descriptor: fp32 accumulator, A and B both fp16 (type 0) or both
+// bf16 (type 1), A K-major, B K-major or, with bmn, MN-major.
+__host__ __device__ constexpr uint32_t idesc_f16(int type, int M, int N, bool bmn) {
+  return (1u << 4) | ((uint32_t)type << 7) | ((uint32_t)type << 10) | ((bmn ? 1u : 0u) << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// Descriptor of an MN-major, 128-byte-swizzled operand: 64 values of MN are a
+// 128-byte row, its 16-byte piece c at piece c ^ (k % 8) for row k; the rows of
+// 8 values of K are a group of 1024 bytes, groups follow one another, and the
+// next 64 values of MN are `block` bytes on.
+__device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t saddr, uint32_t block) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(block >> 4) << 16;
+  d |= (uint64_t)(1024u >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// D[tmem] (+)= A[smem] * B[smem]^T, kind::f16, issued by one thread.
+__device__ __forceinline__ void mma_f16(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// The same with A in tensor memory: lane = row, two consecutive values of K in a column.
+__device__ __forceinline__ void mma_f16_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+#define SLNR_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define SLNR_RW8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
+#define SLNR_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+
+// 32 columns of the thread's lane, not waited for: the registers hold them after tmem_ld_done.
+__device__ __forceinline__ void tmem_ld32_start(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : SLNR_R8(r, 0), SLNR_R8(r, 8), SLNR_R8(r, 16), SLNR_R8(r, 24)
+      : "r"(taddr)
+      : "memory");
+}
+// Waits for the thread's loads; the registers are named so that no use of them moves before.
+__device__ __forceinline__ void tmem_ld_done(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : SLNR_RW8(r, 0), SLNR_RW8(r, 8), SLNR_RW8(r, 16), SLNR_RW8(r, 24)
+               :
+               : "memory");
+}
+// 16 and 32 columns of the thread's lane; done after tmem_st_done.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15};" ::SLNR_W8(r, 0),
+      SLNR_W8(r, 8), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::SLNR_W8(r, 0),
+      SLNR_W8(r, 8), SLNR_W8(r, 16), SLNR_W8(r, 24), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+#undef SLNR_R8
+#undef SLNR_RW8
+#undef SLNR_W8
+
 }  // namespace tc
 }  // namespace slnr
