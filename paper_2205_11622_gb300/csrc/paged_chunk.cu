@@ -12,9 +12,10 @@
 //       its weights are taken against the older maximum, at most 256 each, and
 //       the sum is in the same units, so the quotient is the same;
 //   1 MMA warp:  for each 128 keys and tile: O += P V, then the next S = Q K^T;
-//   3 load warps: Q once, then K and V into a ring of buffers of 128 keys by
-//       asynchronous 16-byte copies, each key's row by its page (any page size
-//       and stride), zeros past the last key.
+//   4 load warps: Q once, then K and V into a ring of buffers of 128 keys by
+//       asynchronous 16-byte copies (any page size and stride), zeros past the
+//       last key.  Each thread finds one key's row by its page, a step ahead,
+//       and all read the rows' offsets from shared memory.
 // While one tile's warps are at its weights, the tensor cores work on the
 // other's.  Keys in 128-byte swizzled rows serve both products: K as the
 // K-major operand of Q K^T, V as the MN-major one of P V.
@@ -29,11 +30,13 @@ namespace slnr {
 namespace {
 
 constexpr int kRows = 128;              // of a tile
-constexpr int kSoftWarps = 8;
-constexpr int kMmaWarp = kSoftWarps;
-constexpr int kLoadWarps = 3;
-constexpr int kLoaders = 32 * kLoadWarps;
-constexpr int kThreads = 32 * (kSoftWarps + 1 + kLoadWarps);
+constexpr int kLoadWarp = 8;            // warps 0-7: softmax
+constexpr int kLoaders = 128;
+constexpr int kMmaWarp = 12;            // 13-15 only complete its warpgroup
+constexpr int kThreads = 512;
+constexpr int kSoftRegs = 200, kOtherRegs = 56;  // of 128 a thread at launch
+static_assert(2 * (kSoftRegs + kOtherRegs) <= 4 * 128, "register shares of the four warpgroups");
+static_assert(kLoaders == kChunkKeys, "a load thread finds one key's row");
 constexpr int kBlock = kRows * 128;     // 128 rows of 64 values, swizzled
 constexpr int kTmemCols = 512;
 constexpr int kColS = 0, kColO = 256;   // S and P of tile t at 128 t, O at kColO + 128 t
@@ -42,16 +45,20 @@ constexpr float kGrow = 8.f;            // growth of a maximum, in powers of two
 template <int W>
 constexpr int tile_bytes() { return kBlock * (W / 64); }
 template <int W>
-constexpr int buffers() { return W == 128 ? 5 : 8; }
+constexpr int buffers() { return W == 128 ? 4 : 8; }
 template <int W>
 constexpr size_t smem_bytes() { return (size_t)(2 + buffers<W>()) * tile_bytes<W>() + 1024; }
-static_assert(smem_bytes<128>() + 512 <= (size_t)227 * 1024, "shared memory of a block");
+template <int W>
+constexpr int lag() { return buffers<W>() - 2; }  // ring steps in flight before one is waited for
 
 struct Barriers {
   uint64_t q_full, s_full[2], p_full[2], o_full, full[8], empty[8], drained;
   uint32_t tmem;
   int failed;
+  int64_t row_k[2][kChunkKeys], row_v[2][kChunkKeys];  // bytes from the head's first row to each key's; -1: zeros
 };
+
+static_assert(smem_bytes<128>() + sizeof(Barriers) <= (size_t)227 * 1024, "shared memory of a block");
 
 // Waits for the phase of that parity; false (and *failed set) after `limit` cycles or once another wait gave up.
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* failed, long long limit) {
@@ -73,6 +80,16 @@ __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volati
 // Byte of 16-byte piece `piece` of a row inside a swizzled tile of 128 rows.
 __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
   return (uint32_t)((piece >> 3) * kBlock + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+}
+
+// Register shares of the calling warpgroup.
+template <int N>
+__device__ __forceinline__ void regs_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
 template <typename T, int W>
@@ -126,231 +143,241 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   const uint32_t tmem = bars.tmem;
   volatile int* failed = &bars.failed;
 
-  if (warp > kMmaWarp) {
-    // ---- loads ----
-    const int lt = tid - 32 * (kMmaWarp + 1), piece = lt % PIECES;
-    const bool col_on = piece * 8 < c.width;
-    for (int x = lt / PIECES; x < 2 * kRows; x += kLoaders / PIECES) {
-      const bool on = x < n && col_on;
-      const int tok = on ? a.group.div(x0 + x) : 0, g = on ? x0 + x - tok * G : 0;
-      copy16(q_tile(x / kRows) + piece_at(x % kRows, piece),
-             (const T*)a.q.p + (int64_t)(q0 + tok) * a.q.tok + (int64_t)(h * G + g) * a.q.head + (on ? piece * 8 : 0), on);
-    }
-    copy_commit();
-    // ring step i: K of keys i / 2 (i even) or V; a step's copies are waited for two steps later
-    const int total = 2 * steps;
-    const int32_t* table = p.table + r * p.table_stride;
-    for (int i = 0; i < total + 2; ++i) {
-      if (i < total) {
-        const int b = i % NB;
-        if (!wait_warp(&bars.empty[b], ((i / NB) & 1) ^ 1, failed, limit)) break;
-        const uint32_t dst = buffer(b);
-        const int ub = u0 + (i >> 1) * kChunkKeys;
-        const char* src = (const char*)((i & 1) ? c.v : c.k);
-        const int64_t* st = (i & 1) ? c.vs : c.ks;
-        const int64_t s0 = st[0] * 2, s1 = st[1] * 2;
-        src += st[2] * 2 * h + (col_on ? piece * 16 : 0);
-        constexpr int STEP = kLoaders / PIECES, BATCH = 8;
-        for (int row0 = lt / PIECES; row0 < kChunkKeys; row0 += STEP * BATCH) {
-          int id[BATCH], off[BATCH];
-#pragma unroll
-          for (int k = 0; k < BATCH; ++k) {
-            const int u = ub + row0 + k * STEP;
-            id[k] = -1;
-            off[k] = 0;
-            if (row0 + k * STEP < kChunkKeys && u < u1) {
-              const int idx = c.page.div(u);
-              off[k] = u - idx * c.page.d;
-              if (idx < p.width) id[k] = __ldg(table + idx);
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < BATCH; ++k) {
-            const int row = row0 + k * STEP;
-            if (row < kChunkKeys) {
-              const bool on = col_on && (unsigned)id[k] < (unsigned)c.npages;
-              copy16(dst + piece_at(row, piece), src + (on ? id[k] * s0 + off[k] * s1 : 0), on);
-            }
-          }
-        }
+  if (warp >= kLoadWarp) {
+    regs_down<kOtherRegs>();
+    if (warp < kMmaWarp) {
+      // ---- loads ----
+      constexpr int ROWS = kLoaders / PIECES;  // rows of a pass: a multiple of 8, so a thread's swizzle is fixed
+      const int lt = tid - 32 * kLoadWarp, piece = lt % PIECES, row0 = lt / PIECES;
+      const bool col_on = piece * 8 < c.width;
+      const uint32_t at = piece_at(row0, piece);
+      for (int x = row0; x < 2 * kRows; x += ROWS) {
+        const bool on = x < n && col_on;
+        const int tok = on ? a.group.div(x0 + x) : 0, g = on ? x0 + x - tok * G : 0;
+        copy16(q_tile(x / kRows) + piece_at(x % kRows, piece),
+               (const T*)a.q.p + (int64_t)(q0 + tok) * a.q.tok + (int64_t)(h * G + g) * a.q.head + (on ? piece * 8 : 0), on);
       }
       copy_commit();
-      if (i >= 1) {
-        copy_wait<2>();
-        tc::fence_proxy_async_smem();
-        if (i == 1) tc::mbar_arrive(&bars.q_full);
-        if (i >= 2) tc::mbar_arrive(&bars.full[(i - 2) % NB]);
-      }
-    }
-    copy_wait<0>();
-  } else if (warp == kMmaWarp) {
-    // ---- products ----
-    const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
-    const uint32_t id_s = tc::idesc_f16(type, kRows, kChunkKeys, false);
-    const int no = (c.width + 15) & ~15;  // columns of O
-    const uint32_t id_o = tc::idesc_f16(type, kRows, no, true);
-    const int ksteps = (c.width + 15) / 16;
-    auto scores = [&](int t, int b) {
-      if (lane == 0) {
-        for (int k = 0; k < ksteps; ++k) {
-          const uint32_t at = (k >> 2) * kBlock + (k & 3) * 32;
-          tc::mma_f16(tmem + kColS + t * 128, tc::desc_k_sw128(q_tile(t) + at), tc::desc_k_sw128(buffer(b) + at), id_s, k > 0);
+      const int32_t* table = p.table + r * p.table_stride;
+      const char* src_k = (const char*)c.k + 2 * (c.ks[2] * h + (col_on ? piece * 8 : 0));
+      const char* src_v = (const char*)c.v + 2 * (c.vs[2] * h + (col_on ? piece * 8 : 0));
+      int id = -1, off = 0;
+      auto find = [&](int j) {  // page and slot of this thread's key of step j
+        const int u = u0 + j * kChunkKeys + lt;
+        id = -1;
+        if (u < u1) {
+          const int idx = c.page.div(u);
+          off = u - idx * c.page.d;
+          if (idx < p.width) id = __ldg(table + idx);
         }
-        tc::mma_commit(&bars.s_full[t]);
+      };
+      find(0);
+      // ring step i: K of keys i / 2 (i even) or V; its copies are waited for `lag` steps later
+      const int total = 2 * steps;
+      constexpr int LAG = lag<W>();
+      bool ok = true;  // where a wait gave up the loop goes on without copies: its warps meet at a barrier
+      for (int i = 0; i < total + LAG; ++i) {
+        // hand over what has landed before waiting for room: the copies of step i - 1 stay in flight
+        if (ok && i >= LAG - 1) {
+          copy_wait<LAG - 1>();
+          tc::fence_proxy_async_smem();
+          tc::mbar_arrive(i == LAG - 1 ? &bars.q_full : &bars.full[(i - LAG) % NB]);
+        }
+        if (i < total) {
+          const int j = i >> 1, b = i % NB;
+          if (!(i & 1)) {
+            const bool on = (unsigned)id < (unsigned)c.npages;
+            bars.row_k[j & 1][lt] = on ? 2 * (id * c.ks[0] + off * c.ks[1]) : -1;
+            bars.row_v[j & 1][lt] = on ? 2 * (id * c.vs[0] + off * c.vs[1]) : -1;
+            find(j + 1);
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+          }
+          ok = ok && wait_warp(&bars.empty[b], ((i / NB) & 1) ^ 1, failed, limit);
+          const uint32_t dst = buffer(b) + at;
+          const char* src = (i & 1) ? src_v : src_k;
+          const int64_t* rows = ((i & 1) ? bars.row_v[j & 1] : bars.row_k[j & 1]) + row0;
+#pragma unroll
+          for (int k = 0; k < kChunkKeys / ROWS; ++k) {
+            const int64_t o = rows[k * ROWS];
+            const bool on = col_on && o >= 0;
+            if (ok) copy16(dst + k * ROWS * 128, src + (on ? o : 0), on);
+          }
+        }
+        copy_commit();
       }
-    };
-    auto output = [&](int t, int b, bool first) {
-      if (lane == 0)
-        for (int k = 0; k < kChunkKeys / 16; ++k)
-          tc::mma_f16_ta(tmem + kColO + t * 128, tmem + kColS + t * 128 + 8 * k,
-                         tc::desc_mn_sw128(buffer(b) + k * 2048, kBlock), id_o, !first || k > 0);
-    };
-    auto release = [&](int b) {
-      if (lane == 0) tc::mma_commit(&bars.empty[b]);
-    };
-    bool ok = steps > 0 && wait_warp(&bars.q_full, 0, failed, limit) && wait_warp(&bars.full[0], 0, failed, limit);
-    if (ok) {
-      tc::tc_fence_after_sync();
-      for (int t = 0; t < tiles; ++t) scores(t, 0);
-      release(0);
-    }
-    for (int j = 0; ok && j < steps; ++j) {
-      const int iv = 2 * j + 1, ik = 2 * j + 2;  // ring steps of V and of the next K
-      ok = wait_warp(&bars.full[iv % NB], (iv / NB) & 1, failed, limit);
-      if (ok && j + 1 < steps) ok = wait_warp(&bars.full[ik % NB], (ik / NB) & 1, failed, limit);
-      for (int t = 0; ok && t < tiles; ++t) {
-        ok = wait_warp(&bars.p_full[t], j & 1, failed, limit);
-        if (!ok) break;
+      copy_wait<0>();
+    } else if (warp == kMmaWarp) {
+      // ---- products ----
+      const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+      const uint32_t id_s = tc::idesc_f16(type, kRows, kChunkKeys, false);
+      const int no = (c.width + 15) & ~15;  // columns of O
+      const uint32_t id_o = tc::idesc_f16(type, kRows, no, true);
+      const int ksteps = (c.width + 15) / 16;
+      auto scores = [&](int t, int b) {
+        if (lane == 0) {
+          for (int k = 0; k < ksteps; ++k) {
+            const uint32_t at = (k >> 2) * kBlock + (k & 3) * 32;
+            tc::mma_f16(tmem + kColS + t * 128, tc::desc_k_sw128(q_tile(t) + at), tc::desc_k_sw128(buffer(b) + at), id_s, k > 0);
+          }
+          tc::mma_commit(&bars.s_full[t]);
+        }
+      };
+      auto output = [&](int t, int b, bool first) {
+        if (lane == 0)
+          for (int k = 0; k < kChunkKeys / 16; ++k)
+            tc::mma_f16_ta(tmem + kColO + t * 128, tmem + kColS + t * 128 + 8 * k,
+                           tc::desc_mn_sw128(buffer(b) + k * 2048, kBlock), id_o, !first || k > 0);
+      };
+      auto release = [&](int b) {
+        if (lane == 0) tc::mma_commit(&bars.empty[b]);
+      };
+      bool ok = steps > 0 && wait_warp(&bars.q_full, 0, failed, limit) && wait_warp(&bars.full[0], 0, failed, limit);
+      if (ok) {
         tc::tc_fence_after_sync();
-        output(t, iv % NB, j == 0);
-        if (t == tiles - 1) release(iv % NB);
-        if (j + 1 < steps) {
-          scores(t, ik % NB);
-          if (t == tiles - 1) release(ik % NB);
-        }
+        for (int t = 0; t < tiles; ++t) scores(t, 0);
+        release(0);
       }
-    }
-    if (ok && lane == 0) tc::mma_commit(&bars.o_full);
-  } else if ((warp >> 2) < tiles) {
-    // ---- softmax: thread = row ----
-    const int t = warp >> 2, x = t * kRows + (warp & 3) * 32 + lane;
-    const bool row_on = x < n;
-    const int tok = row_on ? a.group.div(x0 + x) : 0, g = row_on ? x0 + x - tok * G : 0;
-    const int pos = row_on ? shift + tok : -1;
-    const int pos_min = shift + a.group.div(x0 + t * kRows);  // of the tile's rows
-    const bool tail = n - t * kRows < kRows;                  // rows that are none: their scores are dropped
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t col_s = tmem + lanes + kColS + t * 128, col_o = tmem + lanes + kColO + t * 128;
-    // scores are kept raw and take their factor inside the exponential; one that is not positive goes to them first
-    const bool raw = a.scale > 0.f;
-    const float factor = a.scale * 1.4426950408889634f, sl2 = raw ? factor : 1.f;
-    float m = -INFINITY, l = 0.f;  // maximum of the scores that weights are taken against, sum of weights
-    bool ok = true;
-    for (int j = 0; j < steps; ++j) {
-      ok = wait_warp(&bars.s_full[t], j & 1, failed, limit);
-      if (!ok) break;
-      tc::tc_fence_after_sync();
-      uint32_t s[128];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) tc::tmem_ld32_start(col_s + 32 * k, s + 32 * k);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) tc::tmem_ld_done(s + 32 * k);
-      if (!raw) {
-#pragma unroll
-        for (int k = 0; k < 128; ++k) s[k] = __float_as_uint(__uint_as_float(s[k]) * factor);
-      }
-      const int key0 = u0 + j * kChunkKeys;
-      if (tail || key0 + kChunkKeys - 1 > pos_min) {
-        const int seen = pos - key0;  // keys 0 .. seen of these 128
-#pragma unroll
-        for (int k = 0; k < 128; ++k)
-          if (k > seen) s[k] = 0xff800000u;
-      }
-      float mx[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(s[k]);
-#pragma unroll
-      for (int k = 4; k < 128; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(s[k]));
-      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-      // the first keys that a row sees set m; later m moves only where it has to
-      const bool grow = (top - m) * sl2 > kGrow;  // m = -inf: true for any seen key
-      if (__any_sync(0xffffffffu, grow)) {
-        const float f = grow ? exp2_fast((m - top) * sl2) : 1.f;
-        if (grow) {
-          l *= f;
-          m = top;
-        }
-        if (j > 0) {
-#pragma unroll
-          for (int k = 0; k < W / 16; ++k) {
-            float o[16];
-            uint32_t y[16];
-            tc::tmem_ld16(col_o + 16 * k, o);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(o[e] * f);
-            tc::tmem_st16(col_o + 16 * k, y);
+      for (int j = 0; ok && j < steps; ++j) {
+        const int iv = 2 * j + 1, ik = 2 * j + 2;  // ring steps of V and of the next K
+        ok = wait_warp(&bars.full[iv % NB], (iv / NB) & 1, failed, limit);
+        if (ok && j + 1 < steps) ok = wait_warp(&bars.full[ik % NB], (ik / NB) & 1, failed, limit);
+        for (int t = 0; ok && t < tiles; ++t) {
+          ok = wait_warp(&bars.p_full[t], j & 1, failed, limit);
+          if (!ok) break;
+          tc::tc_fence_after_sync();
+          output(t, iv % NB, j == 0);
+          if (t == tiles - 1) release(iv % NB);
+          if (j + 1 < steps) {
+            scores(t, ik % NB);
+            if (t == tiles - 1) release(ik % NB);
           }
         }
       }
-      const float b = m == -INFINITY ? 0.f : m * sl2;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t w[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float w0 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e]), sl2, -b));
-          const float w1 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e + 1]), sl2, -b));
-          sum[(2 * e) & 3] += w0;
-          sum[(2 * e + 1) & 3] += w1;
-          w[e] = Half2<T>::pack(w0, w1);
-        }
-        tc::tmem_st16(col_s + 16 * k, w);
-      }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      tc::tmem_st_done();
-      tc::tc_fence_before_sync();
-      tc::mbar_arrive(&bars.p_full[t]);
+      if (ok && lane == 0) tc::mma_commit(&bars.o_full);
     }
-    if (ok && steps > 0) ok = wait_warp(&bars.o_full, 0, failed, limit);
-    if (ok) {
-      tc::tc_fence_after_sync();
-      const int splits = end > 0 ? (end - 1) / a.plan.chunk + 1 : 1;
-      const int64_t at = (q0 + tok) * ((int64_t)c.nheads * G) + h * G + g;
-      const int64_t slot = at * a.plan.nsplit + blockIdx.z;
-      const float inv = __fdividef(1.f, l);
-      const float lse2 = l == 0.f ? -INFINITY : m * sl2 + __log2f(l);
+  } else {
+    regs_up<kSoftRegs>();
+    if ((warp >> 2) < tiles) {
+      // ---- softmax: thread = row ----
+      const int t = warp >> 2, x = t * kRows + (warp & 3) * 32 + lane;
+      const bool row_on = x < n;
+      const int tok = row_on ? a.group.div(x0 + x) : 0, g = row_on ? x0 + x - tok * G : 0;
+      const int pos = row_on ? shift + tok : -1;
+      const int pos_min = shift + a.group.div(x0 + t * kRows);  // of the tile's rows
+      const bool tail = n - t * kRows < kRows;                  // rows that are none: their scores are dropped
+      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+      const uint32_t col_s = tmem + lanes + kColS + t * 128, col_o = tmem + lanes + kColO + t * 128;
+      // scores are kept raw and take their factor inside the exponential; one that is not positive goes to them first
+      const bool raw = a.scale > 0.f;
+      const float factor = a.scale * 1.4426950408889634f, sl2 = raw ? factor : 1.f;
+      float m = -INFINITY, l = 0.f;  // maximum of the scores that weights are taken against, sum of weights
+      bool ok = true;
+      for (int j = 0; j < steps; ++j) {
+        ok = wait_warp(&bars.s_full[t], j & 1, failed, limit);
+        if (!ok) break;
+        tc::tc_fence_after_sync();
+        uint32_t s[128];
 #pragma unroll
-      for (int k = 0; k < W / 32; ++k) {
-        float o[32];
+        for (int k = 0; k < 4; ++k) tc::tmem_ld32_start(col_s + 32 * k, s + 32 * k);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) o[e] = 0.f;
-        if (steps > 0) tc::tmem_ld32(col_o + 32 * k, o);
+        for (int k = 0; k < 4; ++k) tc::tmem_ld_done(s + 32 * k);
+        if (!raw) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0.f : o[e] * inv;  // no key: zeros
-        if (!row_on) continue;
-        if (splits == 1) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (32 * k + 8 * e < c.width) {
-              uint4 y;
-              y.x = Half2<T>::pack(o[8 * e], o[8 * e + 1]);
-              y.y = Half2<T>::pack(o[8 * e + 2], o[8 * e + 3]);
-              y.z = Half2<T>::pack(o[8 * e + 4], o[8 * e + 5]);
-              y.w = Half2<T>::pack(o[8 * e + 6], o[8 * e + 7]);
-              *reinterpret_cast<uint4*>((T*)a.out + at * c.width + 32 * k + 8 * e) = y;
-            }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (32 * k + 4 * e < c.width)
-              *reinterpret_cast<float4*>(a.plan.part + slot * c.width + 32 * k + 4 * e) =
-                  make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          for (int k = 0; k < 128; ++k) s[k] = __float_as_uint(__uint_as_float(s[k]) * factor);
         }
+        const int key0 = u0 + j * kChunkKeys;
+        if (tail || key0 + kChunkKeys - 1 > pos_min) {
+          const int seen = pos - key0;  // keys 0 .. seen of these 128
+#pragma unroll
+          for (int k = 0; k < 128; ++k)
+            if (k > seen) s[k] = 0xff800000u;
+        }
+        float mx[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(s[k]);
+#pragma unroll
+        for (int k = 4; k < 128; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(s[k]));
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        // the first keys that a row sees set m; later m moves only where it has to
+        const bool grow = (top - m) * sl2 > kGrow;  // m = -inf: true for any seen key
+        if (__any_sync(0xffffffffu, grow)) {
+          const float f = grow ? exp2_fast((m - top) * sl2) : 1.f;
+          if (grow) {
+            l *= f;
+            m = top;
+          }
+          if (j > 0) {
+#pragma unroll
+            for (int k = 0; k < W / 16; ++k) {
+              float o[16];
+              uint32_t y[16];
+              tc::tmem_ld16(col_o + 16 * k, o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(o[e] * f);
+              tc::tmem_st16(col_o + 16 * k, y);
+            }
+          }
+        }
+        const float b = m == -INFINITY ? 0.f : m * sl2;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float w0 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e]), sl2, -b));
+            const float w1 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e + 1]), sl2, -b));
+            sum[(2 * e) & 3] += w0;
+            sum[(2 * e + 1) & 3] += w1;
+            w[e] = Half2<T>::pack(w0, w1);
+          }
+          tc::tmem_st16(col_s + 16 * k, w);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tc::tmem_st_done();
+        tc::tc_fence_before_sync();
+        tc::mbar_arrive(&bars.p_full[t]);
       }
-      if (row_on) {
-        if (splits != 1) a.plan.part_lse[slot] = lse2;
-        else if (a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
+      if (ok && steps > 0) ok = wait_warp(&bars.o_full, 0, failed, limit);
+      if (ok) {
+        tc::tc_fence_after_sync();
+        const int splits = end > 0 ? (end - 1) / a.plan.chunk + 1 : 1;
+        const int64_t at = (q0 + tok) * ((int64_t)c.nheads * G) + h * G + g;
+        const int64_t slot = at * a.plan.nsplit + blockIdx.z;
+        const float inv = __fdividef(1.f, l);
+        const float lse2 = l == 0.f ? -INFINITY : m * sl2 + __log2f(l);
+#pragma unroll
+        for (int k = 0; k < W / 32; ++k) {
+          float o[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          if (steps > 0) tc::tmem_ld32(col_o + 32 * k, o);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0.f : o[e] * inv;  // no key: zeros
+          if (!row_on) continue;
+          if (splits == 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (32 * k + 8 * e < c.width) {
+                uint4 y;
+                y.x = Half2<T>::pack(o[8 * e], o[8 * e + 1]);
+                y.y = Half2<T>::pack(o[8 * e + 2], o[8 * e + 3]);
+                y.z = Half2<T>::pack(o[8 * e + 4], o[8 * e + 5]);
+                y.w = Half2<T>::pack(o[8 * e + 6], o[8 * e + 7]);
+                *reinterpret_cast<uint4*>((T*)a.out + at * c.width + 32 * k + 8 * e) = y;
+              }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (32 * k + 4 * e < c.width)
+                *reinterpret_cast<float4*>(a.plan.part + slot * c.width + 32 * k + 4 * e) =
+                    make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          }
+        }
+        if (row_on) {
+          if (splits != 1) a.plan.part_lse[slot] = lse2;
+          else if (a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
+        }
       }
     }
   }
