@@ -125,6 +125,8 @@ def build(force: bool = False) -> str:
 def lib():
     """The loaded libslnr.so.  Raises if it has not been built: there is no fallback."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIBRARY):

@@ -180,7 +180,9 @@ cudaError_t launch_page_select(const PagesView& p, const CacheView& c, const Row
   const int ntile = p.max_q <= 1 ? 1 : select_tokens(npages);
   const size_t smem = (size_t)ntile * (kSelMaxWidth + 4 * (size_t)npages);
   auto kernel = dtype == SLNR_FP16 ? k_page_select<__half> : k_page_select<__nv_bfloat16>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelSmem);
+  static OncePerDevice once[2];
+  cudaError_t e = once[dtype == SLNR_FP16](
+      [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelSmem); });
   if (e != cudaSuccess) return e;
   const dim3 grid((unsigned)pieces(p.ntok, ntile), (unsigned)c.nheads);
   kernel<<<(SLNR_COUNTED(grid)), kSelThreads, smem, s>>>(p, c, q, nheads_q / c.nheads, ntile, npages, picked, npicked,

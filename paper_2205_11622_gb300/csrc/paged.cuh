@@ -2,6 +2,7 @@
 // division by the page size, and the launchers that the C entry points call.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -49,8 +50,9 @@ __device__ __forceinline__ int page_of(int slot, const CacheView& c) { return c.
 struct AttnPlan {
   int tile;     // rows a block takes
   int ntiles;   // bound of the row tiles of all requests
-  int chunk;    // keys of one split, a multiple of kChunkKeys
+  int chunk;    // keys of one split, a multiple of the kernel's step
   int nsplit;   // splits of the longest request (1: the block writes the result)
+  bool cluster; // the splits of a row are joined by the blocks of a cluster (row kernel, nsplit in 2 .. 16)
   float* part;  // [ntok * nheads_q][nsplit][width] partial rows, each divided by its own sum
   float* part_lse;  // [ntok * nheads_q][nsplit] log2 of the partial sums of exponentials
 };
@@ -71,6 +73,27 @@ struct AttnArgs {
   const int32_t* picked;  // selected attention: [ntok][nheads][npicked]
   int npicked;
   AttnPlan plan;
+};
+
+// Runs something once a device and keeps its first error: the attributes of a kernel.
+class OncePerDevice {
+ public:
+  template <typename F>
+  cudaError_t operator()(F f) {
+    int d = 0;
+    const cudaError_t e = cudaGetDevice(&d);
+    if (e != cudaSuccess) return e;
+    if (d < 0 || d >= kDevices) return f();
+    const int seen = state_[d].load(std::memory_order_acquire);
+    if (seen != 0) return (cudaError_t)(seen - 1);
+    const cudaError_t r = f();  // by two threads at once: the same attributes twice
+    state_[d].store((int)r + 1, std::memory_order_release);
+    return r;
+  }
+
+ private:
+  static constexpr int kDevices = 64;
+  std::atomic<int> state_[kDevices] = {};
 };
 
 // pages.cu

@@ -11,6 +11,7 @@ using namespace slnr;
 namespace {
 
 constexpr int kMaxWidth = 128;
+constexpr int kMaxKeys = 0x7fff0000;  // steps past a request's last key stay below 2^31
 
 slnr_status check_paged_opts(const slnr_opts* o) {
   if (!o) return fail(SLNR_ERR_NULL, "opts is NULL");
@@ -58,6 +59,7 @@ slnr_status check_cache(const slnr_cache* c, bool keys, bool summary, bool point
 slnr_status check_pages(const slnr_pages* p, const slnr_cache* c, bool pointers, bool req, bool slots) {
   if (!p) return fail(SLNR_ERR_NULL, "pages is NULL");
   if (p->reserved != 0) return fail(SLNR_ERR_UNSUPPORTED, "pages.reserved must be 0");
+  if (p->max_k > kMaxKeys) return fail(SLNR_ERR_UNSUPPORTED, "max_k = %d: at most %d", (int)p->max_k, kMaxKeys);
   if (p->nreq < 0 || p->ntok < 0 || p->max_q < 0 || p->max_k < 0 || p->width < 0 || p->table_stride < p->width)
     return fail(SLNR_ERR_SHAPE, "negative size in pages, or rows of table that overlap");
   if ((int64_t)p->max_k > (int64_t)p->width * c->page_size)
@@ -121,6 +123,7 @@ slnr_status validated(const slnr_opts* o, Launch launch) {
 // Blocks that the GPU holds at once: two of the row kernel's on each of 152 SMs.
 constexpr int64_t kResident = 304;
 constexpr int64_t kMaxBlocks = 16384;  // splits stop here
+constexpr int64_t kMaxCluster = 16;
 
 // Row tiles and key splits of an attention call: by the bounds alone, never by
 // device data.  Calls with a request of more than 64 rows go to the tensor-core
@@ -137,16 +140,30 @@ AttnPlan attn_plan(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, i
   if (blocks > 0) {
     const bool tc = a.tile == kChunkRows;
     const int64_t least = tc ? 512 : 128;
-    chunk = ceil_div(keys, ceil_div(tc ? 3 * kResident / 2 : 2 * kResident, blocks));
+    const int64_t want = tc ? ceil_div(3 * kResident / 2, blocks) : kResident / blocks;
+    chunk = ceil_div(keys, want > 1 ? want : 1);
     if (chunk < least) chunk = least;
-    if (a.tile == 16 && chunk > 1024) chunk = 1024;
+    if (!tc && npicked == 0 && chunk > 2048) chunk = 2048;  // requests of other lengths beside the longest
     const int64_t floor = ceil_div(keys * blocks, kMaxBlocks);
     if (chunk < floor) chunk = floor;
   }
-  chunk = ceil_div(chunk > 0 ? chunk : 1, kChunkKeys) * kChunkKeys;
+  // Where all splits run at once and there are few of them, they are the blocks
+  // of a cluster (a power of two): no second launch.  A larger call would keep
+  // the blocks of short requests waiting for those of long ones.
+  if (a.tile != kChunkRows && chunk < keys) {
+    int64_t n = 2;
+    while (n < kMaxCluster && n * chunk < keys) n *= 2;
+    if (blocks * n <= kResident && keys <= n * (chunk > 512 ? chunk : 512)) {
+      chunk = ceil_div(keys, n);
+      a.cluster = true;
+      a.nsplit = (int)n;
+    }
+  }
+  const int64_t unit = a.tile == kChunkRows ? kChunkKeys : kAttnKeys;
+  chunk = ceil_div(chunk > 0 ? chunk : 1, unit) * unit;
   a.ntiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
   a.chunk = (int)chunk;
-  a.nsplit = keys > 0 ? (int)ceil_div(keys, chunk) : 1;
+  if (!a.cluster) a.nsplit = keys > 0 ? (int)ceil_div(keys, chunk) : 1;
   return a;
 }
 
@@ -156,7 +173,7 @@ struct AttnLayout {
 AttnLayout attn_layout(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, const AttnPlan& a) {
   AttnLayout l;
   l.part = l.lse = l.total = sizeof(WsHeader);
-  if (a.nsplit > 1) {
+  if (a.nsplit > 1 && !a.cluster) {
     const size_t rows = (size_t)p.ntok * nheads_q * a.nsplit;
     l.lse = align256(l.part + rows * c.head_dim * sizeof(float));
     l.total = align256(l.lse + rows * sizeof(float));
@@ -191,7 +208,7 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   AttnArgs a{view(*pages), view(*cache), view(*q), divisor(nheads_q / cache->nheads), scale, out, lse, picked, npicked,
              attn_plan(*cache, *pages, nheads_q, npicked)};
   if (a.plan.nsplit > 65535 || a.plan.ntiles == INT32_MAX || (a.plan.tile == kChunkRows && a.plan.ntiles > 65535) || (int64_t)pages->max_q * a.group.d >= (int64_t(1) << 31) ||
-      (int64_t)npicked * cache->page_size >= (int64_t(1) << 31))
+      (int64_t)npicked * cache->page_size > kMaxKeys)
     return fail(SLNR_ERR_UNSUPPORTED, "too many rows or keys for one call");
   const AttnLayout l = attn_layout(*cache, *pages, nheads_q, a.plan);
   SLNR_CHECK(check_ws(opts, l.total));
@@ -209,7 +226,7 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   } else {
     SLNR_LAUNCH("paged_rows", launch_paged_rows(a, cache->dtype, s));
   }
-  if (a.plan.nsplit > 1) SLNR_LAUNCH("paged_combine", launch_paged_combine(a, cache->dtype, s));
+  if (a.plan.nsplit > 1 && !a.plan.cluster) SLNR_LAUNCH("paged_combine", launch_paged_combine(a, cache->dtype, s));
   timing_end(s);
   if (tc && opts->validate) {
     int flag = 0;

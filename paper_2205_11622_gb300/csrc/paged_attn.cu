@@ -10,8 +10,11 @@
 //
 // A block takes one key head and up to 16 WM rows (the query rows of that
 // head's group, token after token) and streams its keys through shared memory,
-// 64 at a time, by asynchronous 16-byte copies that find each key's page in a
-// window of the block table.  WM warps share the rows; the 4 / WM warps of one
+// 64 at a time, by asynchronous 16-byte copies; each thread finds one key's row
+// of K or V by its page, three steps ahead, and all read the rows' offsets from
+// shared memory.  Few rows are split over their keys: up to 16 splits are the
+// blocks of a cluster, which join their results through each other's shared
+// memory; more go through the workspace and k_paged_combine.  WM warps share the rows; the 4 / WM warps of one
 // row set take a part of each 64 keys and join their sums at the end, so
 // every key is read from shared memory by WM warps only.
 #include "launch.h"
@@ -22,27 +25,72 @@ namespace slnr {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kWindow = 256;  // entries of the block table held in shared memory
 constexpr int kStages = 3;
+constexpr int kOffsets = kStages + 1;  // steps whose rows' offsets are held
 
 template <int W>
 constexpr int stage_bytes() { return 2 * kAttnKeys * W * 2; }
 template <int W>
 constexpr size_t smem_bytes() { return (size_t)kStages * stage_bytes<W>(); }
 
+template <bool SEL>
 struct Smem {
-  int2 window[kAttnMaxPicked > kWindow ? kAttnMaxPicked : kWindow];  // {page of the cache, page of the request}
-  int key_at[kStages][kAttnKeys];                                     // selected: the keys' positions
-  float2 ml[4][16];                                                   // a warp's (maximum, sum) of each row
-  int r, x0, count;
+  int64_t row[kOffsets][2][kAttnKeys];       // bytes from the head's first row of K and V to each key's; -1: zeros
+  int key_at[SEL ? kOffsets : 1][kAttnKeys]; // selected: the keys' positions
+  int2 pick[SEL ? kAttnMaxPicked : 1];       // selected: {page of the cache, page of the request}
+  float2 ml[4][16];                          // a warp's (maximum, sum) of each row
+  float lse[64];                             // of the block's rows, in powers of two
+  int count;
 };
 
-template <typename T, int W, int WM, bool SEL>
+// The other blocks of a cluster.
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t address_in(uint32_t local, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float load_far(uint32_t at) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 load4_far(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(at)
+               : "memory");
+  return v;
+}
+
+// Eight columns of a finished row.
+template <typename T>
+__device__ __forceinline__ void store_row(const AttnArgs& a, int64_t at, int col, const float (&v)[8], float lse2) {
+  if (col < a.c.width) {
+    uint4 y;
+    y.x = Half2<T>::pack(v[0], v[1]);
+    y.y = Half2<T>::pack(v[2], v[3]);
+    y.z = Half2<T>::pack(v[4], v[5]);
+    y.w = Half2<T>::pack(v[6], v[7]);
+    *reinterpret_cast<uint4*>((T*)a.out + at * a.c.width + col) = y;
+  }
+  if (col == 0 && a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
+}
+
+template <typename T, int W, int WM, bool SEL, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads)
 k_paged_rows(AttnArgs a) {
-  constexpr int WK = 4 / WM, KW = kAttnKeys / WK, PIECES = W / 8;
+  constexpr int WK = 4 / WM, KW = kAttnKeys / WK, PIECES = W / 8, ROWS = kThreads / PIECES;
   extern __shared__ __align__(128) unsigned char tiles[];
-  __shared__ Smem sm;
+  __shared__ Smem<SEL> sm;
   const PagesView& p = a.p;
   const CacheView& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wm = warp % WM, wk = warp / WM;
@@ -67,6 +115,7 @@ k_paged_rows(AttnArgs a) {
   const int p_first = shift + a.group.div(x0), p_last = shift + a.group.div(x0 + n - 1);
 
   // its keys: [u0, u1) of the request's keys, or of the picked pages' slots
+  const int32_t* table = p.table + r * p.table_stride;
   int end;
   if (SEL) {
     const int32_t* row = a.picked + ((int64_t)(q0 + x0 / G) * c.nheads + h) * a.npicked;
@@ -76,7 +125,7 @@ k_paged_rows(AttnArgs a) {
     for (int i = tid; i < a.npicked; i += kThreads) {
       const int pg = __ldg(row + i);
       const bool ok = pg >= 0 && pg < p.width && pg <= c.page.div(max(p_last, 0));
-      sm.window[i] = make_int2(ok ? __ldg(p.table + r * p.table_stride + pg) : -1, ok ? pg : -1);
+      sm.pick[i] = make_int2(ok ? __ldg(table + pg) : -1, ok ? pg : -1);
       if (ok) most = i + 1;
     }
     if (most > 0) atomicMax(&sm.count, most);
@@ -86,9 +135,46 @@ k_paged_rows(AttnArgs a) {
     end = max(p_last + 1, 0);
   }
   const int u0 = blockIdx.z * a.plan.chunk;
-  if (!SEL && u0 > 0 && u0 >= end) return;
+  if (!SEL && !CLUSTER && u0 > 0 && u0 >= end) return;
   const int u1 = max(min(end, u0 + a.plan.chunk), u0);
   const int steps = (u1 - u0 + kAttnKeys - 1) / kAttnKeys;
+
+  // Rows' offsets: threads 0-63 find the 64 keys of a step for K, the others for
+  // V.  The block table is read a step before its entry is needed.
+  const int key = tid & (kAttnKeys - 1);
+  int id = -1;
+  auto find = [&](int step) {
+    const int u = u0 + step * kAttnKeys + key;
+    id = -1;
+    if (!SEL && u < u1) {
+      const int i = c.page.div(u);
+      if (i < p.width) id = __ldg(table + i);
+    }
+  };
+  auto place = [&](int step) {
+    const int u = u0 + step * kAttnKeys + key, i = c.page.div(u), off = u - i * c.page.d;
+    bool on = u < u1;
+    if (SEL) {
+      int at = INT32_MAX;
+      id = -1;
+      if (on) {
+        const int2 pk = sm.pick[i];
+        id = pk.x;
+        on = pk.y >= 0 && pk.y * c.page.d + off <= p_last;  // slots past the token hold anything
+        if (on) at = pk.y * c.page.d + off;
+      }
+      if (tid < kAttnKeys) sm.key_at[step % kOffsets][key] = at;
+    }
+    on = on && (unsigned)id < (unsigned)c.npages;
+    const int64_t* st = tid < kAttnKeys ? c.ks : c.vs;
+    sm.row[step % kOffsets][tid / kAttnKeys][key] = on ? 2 * (id * st[0] + off * st[1]) : -1;
+  };
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) {
+    find(s);
+    place(s);
+  }
+  find(kStages);
 
   // query fragments: rows lane / 4 and + 8 of the warp's 16
   uint32_t qf[W / 16][4];
@@ -109,47 +195,21 @@ k_paged_rows(AttnArgs a) {
       }
   }
 
+  // copies: a thread's 16-byte piece of ROWS-th rows, at the same swizzle in all of them
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(tiles);
-  int w0 = 0, w1 = 0;  // dense: entries of the block table in the window
+  const int piece = tid % PIECES, row0 = tid / PIECES;
+  const bool col_on = piece * 8 < c.width;
+  const char* src_k = (const char*)c.k + 2 * (c.ks[2] * h + (col_on ? piece * 8 : 0));
+  const char* src_v = (const char*)c.v + 2 * (c.vs[2] * h + (col_on ? piece * 8 : 0));
   auto load = [&](int step) {
     if (step < steps) {
-      const int ub = u0 + step * kAttnKeys, ue = min(ub + kAttnKeys, u1);
-      if (!SEL) {
-        const int need = c.page.div(ue - 1) + 1;
-        if (need > w1) {  // the same for all threads
-          __syncthreads();
-          w0 = c.page.div(ub);
-          w1 = min(w0 + kWindow, p.width);
-          for (int i = tid; i < w1 - w0; i += kThreads)
-            sm.window[i].x = __ldg(p.table + r * p.table_stride + w0 + i);
-          __syncthreads();
-        }
-      }
-      const uint32_t ks = base + (step % kStages) * stage_bytes<W>(), vs = ks + kAttnKeys * W * 2;
+      const uint32_t dst = base + (step % kStages) * stage_bytes<W>() + tile_offset<W>(row0, piece);
+      const int64_t* rows = sm.row[step % kOffsets][0] + row0;
 #pragma unroll
-      for (int i = 0; i < kAttnKeys * PIECES / kThreads; ++i) {
-        const int row = i * (kThreads / PIECES) + tid / PIECES, piece = tid % PIECES;
-        const int u = ub + row;
-        bool on = u < ue;
-        int idx = 0, off = 0, id = -1;
-        if (on) {
-          idx = c.page.div(u);
-          off = u - idx * c.page.d;
-          const int2 w = sm.window[idx - w0];
-          id = w.x;
-          on = (unsigned)id < (unsigned)c.npages;
-          if (SEL) {
-            on = on && w.y >= 0 && w.y * c.page.d + off <= p_last;  // slots past the token hold anything
-            if (piece == 0) sm.key_at[step % kStages][row] = on ? w.y * c.page.d + off : INT32_MAX;
-          }
-        } else if (SEL && piece == 0) {
-          sm.key_at[step % kStages][row] = INT32_MAX;
-        }
-        on = on && piece * 8 < c.width;
-        const int64_t pg = on ? id : 0;
-        const int o = on ? off : 0, col = on ? piece * 8 : 0;
-        copy16(ks + tile_offset<W>(row, piece), (const T*)c.k + pg * c.ks[0] + o * c.ks[1] + h * c.ks[2] + col, on);
-        copy16(vs + tile_offset<W>(row, piece), (const T*)c.v + pg * c.vs[0] + o * c.vs[1] + h * c.vs[2] + col, on);
+      for (int k = 0; k < kAttnKeys / ROWS; ++k) {
+        const int64_t ok = rows[k * ROWS], ov = rows[kAttnKeys + k * ROWS];
+        copy16(dst + k * ROWS * W * 2, src_k + (ok >= 0 ? ok : 0), col_on && ok >= 0);
+        copy16(dst + (kAttnKeys + k * ROWS) * W * 2, src_v + (ov >= 0 ? ov : 0), col_on && ov >= 0);
       }
     }
     copy_commit();
@@ -160,12 +220,15 @@ k_paged_rows(AttnArgs a) {
   for (int i = 0; i < W / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   const float sl2 = a.scale * 1.4426950408889634f;
 
+  __syncthreads();
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) load(s);
   for (int step = 0; step < steps; ++step) {
     copy_wait<kStages - 2>();
     __syncthreads();
     load(step + kStages - 1);
+    place(step + kStages);
+    find(step + kStages + 1);
     const uint32_t ks = base + (step % kStages) * stage_bytes<W>(), vs = ks + kAttnKeys * W * 2;
     const int kb = wk * KW;  // the warp's keys of the step
     const int ub = u0 + step * kAttnKeys + kb;
@@ -189,19 +252,19 @@ k_paged_rows(AttnArgs a) {
     const bool masked = SEL || ub + KW - 1 > p_first;
 #pragma unroll
     for (int j = 0; j < KW / 8; ++j) {
-      int key[2];
+      int at[2];
       if (SEL) {
-        const int2 k2 = *reinterpret_cast<const int2*>(&sm.key_at[step % kStages][kb + j * 8 + (lane & 3) * 2]);
-        key[0] = k2.x;
-        key[1] = k2.y;
+        const int2 k2 = *reinterpret_cast<const int2*>(&sm.key_at[step % kOffsets][kb + j * 8 + (lane & 3) * 2]);
+        at[0] = k2.x;
+        at[1] = k2.y;
       } else {
-        key[0] = ub + j * 8 + (lane & 3) * 2;
-        key[1] = key[0] + 1;
+        at[0] = ub + j * 8 + (lane & 3) * 2;
+        at[1] = at[0] + 1;
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         s[j][e] *= sl2;
-        if (masked && key[e & 1] > pos[e >> 1]) s[j][e] = -INFINITY;
+        if (masked && at[e & 1] > pos[e >> 1]) s[j][e] = -INFINITY;
       }
     }
     float scale_o[2];
@@ -224,10 +287,12 @@ k_paged_rows(AttnArgs a) {
           l[i] += s[j][2 * i + e];
         }
     }
+    if (__any_sync(0xffffffffu, scale_o[0] != 1.f || scale_o[1] != 1.f)) {
 #pragma unroll
-    for (int i = 0; i < W / 8; ++i)
+      for (int i = 0; i < W / 8; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[i][e] *= scale_o[e >> 1];
+        for (int e = 0; e < 4; ++e) o[i][e] *= scale_o[e >> 1];
+    }
 #pragma unroll
     for (int j = 0; j < KW / 16; ++j) {
       const uint32_t w[4] = {Half2<T>::pack(s[2 * j][0], s[2 * j][1]), Half2<T>::pack(s[2 * j][2], s[2 * j][3]),
@@ -265,8 +330,8 @@ k_paged_rows(AttnArgs a) {
   // a group of PIECES lanes a row, 8 columns a lane
   const int splits = SEL ? a.plan.nsplit : (end > 0 ? (end - 1) / a.plan.chunk + 1 : 1);
   const int64_t hq = (int64_t)c.nheads * G;
-  for (int x = tid / PIECES; x < n; x += kThreads / PIECES) {
-    const int col = (tid % PIECES) * 8;
+  const int col = piece * 8;
+  for (int x = row0; x < n; x += ROWS) {
     float mx = -INFINITY, sum = 0.f, acc[8];
 #pragma unroll
     for (int k = 0; k < WK; ++k) mx = fmaxf(mx, sm.ml[k * WM + x / 16][x % 16].x);
@@ -292,19 +357,16 @@ k_paged_rows(AttnArgs a) {
     const float inv = __fdividef(1.f, sum);
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = sum == 0.f ? 0.f : acc[e] * inv;  // no key: zeros
-    const float lse2 = mx + __log2f(sum);  // no key: -inf
+    const float lse2 = mx + __log2f(sum);                                  // no key: -inf
     const int tok = a.group.div(x0 + x), g = x0 + x - tok * G;
     const int64_t at = (q0 + tok) * hq + h * G + g;
-    if (splits == 1) {
-      if (col < c.width) {
-        uint4 y;
-        y.x = Half2<T>::pack(acc[0], acc[1]);
-        y.y = Half2<T>::pack(acc[2], acc[3]);
-        y.z = Half2<T>::pack(acc[4], acc[5]);
-        y.w = Half2<T>::pack(acc[6], acc[7]);
-        *reinterpret_cast<uint4*>((T*)a.out + at * c.width + col) = y;
-      }
-      if (col == 0 && a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
+    if (CLUSTER) {  // for the other blocks, where the first warp's row was
+      float4* y = reinterpret_cast<float4*>(rows + x * (W + 4) + col);
+      y[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      y[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+      if (col == 0) sm.lse[x] = lse2;
+    } else if (splits == 1) {
+      store_row<T>(a, at, col, acc, lse2);
     } else {
       const int64_t slot = at * a.plan.nsplit + blockIdx.z;
       if (col < c.width) {
@@ -314,6 +376,40 @@ k_paged_rows(AttnArgs a) {
       }
       if (col == 0) a.plan.part_lse[slot] = lse2;
     }
+  }
+  if (CLUSTER) {
+    // the splits of a row are the blocks of the cluster: each joins a share of the rows, in the splits' order
+    cluster_sync();
+    const int size = gridDim.z, rank = (int)cluster_rank();
+    const uint32_t lse_at = (uint32_t)__cvta_generic_to_shared(sm.lse);
+    for (int x = rank + row0 * size; x < n; x += ROWS * size) {
+      float mx = -INFINITY, sum = 0.f, acc[8];
+      for (int k = 0; k < size; ++k) mx = fmaxf(mx, load_far(address_in(lse_at + 4 * x, k)));
+      const float b = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+#pragma unroll 4
+      for (int k = 0; k < size; ++k) {
+        const float f = exp2_fast(load_far(address_in(lse_at + 4 * x, k)) - b);
+        const uint32_t y = address_in(base + (x * (W + 4) + col) * 4, k);
+        const float4 z0 = load4_far(y), z1 = load4_far(y + 16);
+        sum += f;
+        acc[0] += f * z0.x;
+        acc[1] += f * z0.y;
+        acc[2] += f * z0.z;
+        acc[3] += f * z0.w;
+        acc[4] += f * z1.x;
+        acc[5] += f * z1.y;
+        acc[6] += f * z1.z;
+        acc[7] += f * z1.w;
+      }
+      const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] *= inv;
+      const int tok = a.group.div(x0 + x), g = x0 + x - tok * G;
+      store_row<T>(a, (q0 + tok) * hq + h * G + g, col, acc, mx + __log2f(sum));
+    }
+    cluster_sync();  // a block's shared memory stays until the others have read it
   }
 }
 
@@ -369,24 +465,48 @@ k_paged_combine(AttnArgs a) {
   if (lane == 0 && a.lse) a.lse[at] = (m + __log2f(sum)) * 0.6931471805599453f;
 }
 
-template <typename T, int W, int WM, bool SEL>
+template <typename T, int W, int WM, bool SEL, bool CLUSTER>
 cudaError_t launch_rows(const AttnArgs& a, cudaStream_t s) {
-  auto kernel = k_paged_rows<T, W, WM, SEL>;
+  auto kernel = k_paged_rows<T, W, WM, SEL, CLUSTER>;
   static_assert(4 * 16 * (W + 4) * 4 <= (int)smem_bytes<W>(), "the joined rows fit in the stages");
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<W>());
+  static OncePerDevice once;
+  cudaError_t e = once([&] {
+    cudaError_t r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<W>());
+    if (r == cudaSuccess && CLUSTER) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return r;
+  });
   if (e != cudaSuccess) return e;
   const dim3 grid((unsigned)a.plan.ntiles, (unsigned)a.c.nheads, (unsigned)a.plan.nsplit);
+  if (CLUSTER) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = grid.z;
+    cfg.gridDim = SLNR_COUNTED(grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem_bytes<W>();
+    cfg.stream = s;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+  }
   kernel<<<(SLNR_COUNTED(grid)), kThreads, smem_bytes<W>(), s>>>(a);
   return cudaGetLastError();
 }
 
+template <typename T, int W, int WM>
+cudaError_t launch_rows_m(const AttnArgs& a, cudaStream_t s) {
+  if (a.picked) return a.plan.cluster ? launch_rows<T, W, WM, true, true>(a, s) : launch_rows<T, W, WM, true, false>(a, s);
+  return a.plan.cluster ? launch_rows<T, W, WM, false, true>(a, s) : launch_rows<T, W, WM, false, false>(a, s);
+}
+
 template <typename T, int W>
 cudaError_t launch_rows_w(const AttnArgs& a, cudaStream_t s) {
-  const bool sel = a.picked != nullptr;
   switch (a.plan.tile) {
-    case 16: return sel ? launch_rows<T, W, 1, true>(a, s) : launch_rows<T, W, 1, false>(a, s);
-    case 32: return sel ? launch_rows<T, W, 2, true>(a, s) : launch_rows<T, W, 2, false>(a, s);
-    default: return sel ? launch_rows<T, W, 4, true>(a, s) : launch_rows<T, W, 4, false>(a, s);
+    case 16: return launch_rows_m<T, W, 1>(a, s);
+    case 32: return launch_rows_m<T, W, 2>(a, s);
+    default: return launch_rows_m<T, W, 4>(a, s);
   }
 }
 

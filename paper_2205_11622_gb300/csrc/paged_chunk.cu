@@ -402,7 +402,9 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
 template <typename T, int W>
 cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
   auto kernel = k_paged_chunk<T, W>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<W>());
+  static OncePerDevice once;
+  cudaError_t e = once(
+      [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<W>()); });
   if (e != cudaSuccess) return e;
   const dim3 grid((unsigned)a.c.nheads, (unsigned)a.plan.ntiles, (unsigned)a.plan.nsplit);
   kernel<<<(SLNR_COUNTED(grid)), kThreads, smem_bytes<W>(), s>>>(a, hdr, wait_limit_cycles());

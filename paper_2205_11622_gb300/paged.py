@@ -20,13 +20,27 @@ from . import (SlnrError, Workspace, _default_ws, _last_ws, _query, _stream_ptr,
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 
+_byref = ctypes.byref
+# without the objects that the public accessors make, where this torch has these (a call takes some 10 us)
+_device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_stream_now = getattr(torch._C, "_cuda_getCurrentRawStream", lambda _: _stream_ptr(None))
+
+
 def _ints(x, name, shape, device):
     """x's address, after its checks: an int32 CUDA tensor of that shape, contiguous."""
-    if not (isinstance(x, torch.Tensor) and x.dtype == torch.int32 and x.device == device and x.is_contiguous()):
+    if x.dtype != torch.int32 or x.device != device or not x.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor on {device}")
-    if tuple(x.shape) != shape:
+    if x.shape != shape:
         raise ValueError(f"{name} has shape {tuple(x.shape)}, not {shape}")
     return x.data_ptr()
+
+
+def _table(t):
+    """(rows, columns, stride between rows) of a block table, after its checks."""
+    if not t.is_cuda or t.dtype != torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("table must be a 2-D int32 CUDA tensor with packed rows")
+    R, width = t.shape
+    return R, width, t.stride(0) if R > 1 else width
 
 
 @dataclass(frozen=True, eq=False)
@@ -47,17 +61,19 @@ class PageTables:
     _c: slnr_pages = field(init=False, repr=False)
 
     def __post_init__(self):
-        t = self.table
-        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.int32 and t.dim() == 2
-                and (t.shape[1] <= 1 or t.stride(1) == 1)):
-            raise ValueError("table must be a 2-D int32 CUDA tensor with packed rows")
-        R, width = t.shape
-        T = self.req.shape[0]
-        stride = t.stride(0) if R > 1 else width
-        object.__setattr__(self, "_c", slnr_pages(
-            R, T, self.max_q, self.max_k, width, 0, stride, _ints(self.q_pos, "q_pos", (R + 1,), t.device),
-            _ints(self.k_len, "k_len", (R,), t.device), t.data_ptr(), _ints(self.req, "req", (T,), t.device),
-            None if self.slots is None else _ints(self.slots, "slots", (T,), t.device)))
+        R, width, stride = _table(self.table)
+        T, dev = self.req.shape[0], self.table.device
+        self.__dict__["_c"] = slnr_pages(
+            R, T, self.max_q, self.max_k, width, 0, stride, _ints(self.q_pos, "q_pos", (R + 1,), dev),
+            _ints(self.k_len, "k_len", (R,), dev), self.table.data_ptr(), _ints(self.req, "req", (T,), dev),
+            None if self.slots is None else _ints(self.slots, "slots", (T,), dev))
+
+    @classmethod
+    def _of(cls, c, **fields):
+        """Tables whose arrays a call of this module made: nothing to check."""
+        self = object.__new__(cls)
+        self.__dict__.update(fields, _c=c)
+        return self
 
     @property
     def ntok(self) -> int:
@@ -139,39 +155,47 @@ def _empty(shape, dtype, device, stream):
 def _out(out, name, shape, dtype, device, stream):
     if out is None:
         return _empty(shape, dtype, device, stream)
-    if tuple(out.shape) != shape or out.dtype != dtype or out.device != device or not out.is_contiguous():
+    if out.shape != shape or out.dtype != dtype or out.device != device or not out.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}")
     return out
 
 
-def _call(name, args, device, need, validate, workspace, stream, tensors):
-    """Call entry point `name` with `need` bytes of workspace (0: none)."""
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: the tensors are on {device}, the current device is {torch.cuda.current_device()}")
-    s = _stream_ptr(stream)
-    if stream is not None:
+def _scratch(need, index, s, workspace, stream):
+    """A device buffer of `need` bytes: the caller's workspace, or this stream's."""
+    if workspace is None:
+        workspace = _default_ws.get((index, s))
+        if workspace is None:
+            workspace = _default_ws.setdefault((index, s), Workspace(device=f"cuda:{index}"))
+    buf = getattr(workspace, "buf", None)
+    if buf is None or buf.numel() < need:
+        if stream is None:
+            buf = workspace.get(need)
+        else:
+            with torch.cuda.stream(stream):
+                buf = workspace.get(need)
+    _last_ws[0] = buf
+    return buf
+
+
+def _call(name, args, index, need, validate, workspace, stream, tensors):
+    """Call entry point `name` on device `index` with `need` bytes of workspace (0: none)."""
+    if index != _device_now():
+        raise ValueError(f"{name}: the tensors are on cuda:{index}, the current device is {_device_now()}")
+    if stream is None:
+        s = _stream_now(index)
+    else:
+        s = stream.cuda_stream
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
-    buf = None
     if validate and need < 256:
         need = 256
     if need:
-        if workspace is None:
-            workspace = _default_ws.get((device.index, s))
-            if workspace is None:
-                workspace = _default_ws.setdefault((device.index, s), Workspace(device=device))
-        buf = getattr(workspace, "buf", None)
-        if buf is None or buf.numel() < need:
-            if stream is None:
-                buf = workspace.get(need)
-            else:
-                with torch.cuda.stream(stream):
-                    buf = workspace.get(need)
-        _last_ws[0] = buf
-    o = slnr_opts(0, 0, 1 if validate else 0, 0, s, None if buf is None else buf.data_ptr(),
-                  0 if buf is None else buf.numel())
-    status = getattr(lib(), name)(*args, ctypes.byref(o))
+        buf = _scratch(need, index, s, workspace, stream)
+        o = slnr_opts(0, 0, 1 if validate else 0, 0, s, buf.data_ptr(), buf.numel())
+    else:
+        o = slnr_opts(0, 0, 0, 0, s, None, 0)
+    status = getattr(lib(), name)(*args, _byref(o))
     if status != 0:
         raise SlnrError(status, name, last_error())
 
@@ -183,21 +207,20 @@ def page_tables(new_len, old_len, table, free_pages, page_size, ntok, max_q=None
     new_len, old_len [R]: new tokens, and keys already in the cache; free_pages: the pages to take from, in order; ntok
     = sum of new_len.  table [R, width] is written in place.  max_q and max_k go to the PageTables (defaults: ntok, and
     what a row of the table holds)."""
-    dev = table.device
-    if not (table.is_cuda and table.dtype == torch.int32 and table.dim() == 2
-            and (table.shape[1] <= 1 or table.stride(1) == 1)):
-        raise ValueError("table must be a 2-D int32 CUDA tensor with packed rows")
-    R, width = table.shape
+    R, width, stride = _table(table)
+    dev, n = table.device, free_pages.shape[0]
     ints = _empty(2 * R + 2 + 2 * ntok, torch.int32, dev, stream)
-    q_pos, k_len, used = ints[:R + 1], ints[R + 1:2 * R + 1], ints[2 * R + 1:2 * R + 2]
-    req, slots = ints[2 * R + 2:2 * R + 2 + ntok], ints[2 * R + 2 + ntok:]
-    args = (R, _ints(new_len, "new_len", (R,), dev), _ints(old_len, "old_len", (R,), dev), table.data_ptr(),
-            table.stride(0) if R > 1 else width, width, _ints(free_pages, "free_pages", tuple(free_pages.shape[:1]), dev),
-            free_pages.shape[0], page_size, ntok, q_pos.data_ptr(), k_len.data_ptr(), req.data_ptr(), slots.data_ptr(),
-            used.data_ptr())
-    _call("slnr_page_tables", args, dev, 0, validate, workspace, stream, (new_len, old_len, table, free_pages))
-    return PageTables(table, q_pos, k_len, req, slots, ntok if max_q is None else max_q,
-                      width * page_size if max_k is None else max_k), used
+    q_pos, k_len, used, req, slots = ints.split((R + 1, R, 1, ntok, ntok))
+    at = ints.data_ptr()
+    at_k, at_req = at + 4 * (R + 1), at + 4 * (2 * R + 2)
+    at_slots = at_req + 4 * ntok
+    _call("slnr_page_tables",
+          (R, _ints(new_len, "new_len", (R,), dev), _ints(old_len, "old_len", (R,), dev), table.data_ptr(), stride, width,
+           _ints(free_pages, "free_pages", (n,), dev), n, page_size, ntok, at, at_k, at_req, at_slots, at_req - 4),
+          dev.index, 0, validate, workspace, stream, (new_len, old_len, table, free_pages))
+    max_q, max_k = ntok if max_q is None else max_q, width * page_size if max_k is None else max_k
+    c = slnr_pages(R, ntok, max_q, max_k, width, 0, stride, at, at_k, table.data_ptr(), at_req, at_slots)
+    return PageTables._of(c, table=table, q_pos=q_pos, k_len=k_len, req=req, slots=slots, max_q=max_q, max_k=max_k), used
 
 
 def page_append(cache: PagedCache, tables: PageTables, k, v, validate=False, workspace=None, stream=None):
@@ -206,9 +229,9 @@ def page_append(cache: PagedCache, tables: PageTables, k, v, validate=False, wor
     if cache.k is None or tables.slots is None:
         raise ValueError("page_append needs a cache with keys, and tables with slots")
     T, H, dt = tables.ntok, cache._c.nheads, cache.k.dtype
-    args = (ctypes.byref(cache._c), ctypes.byref(tables._c), ctypes.byref(_rows(k, "k", cache, H, T, dt)),
-            ctypes.byref(_rows(v, "v", cache, H, T, dt)))
-    _call("slnr_page_append", args, cache.device, 0, validate, workspace, stream,
+    args = (_byref(cache._c), _byref(tables._c), _byref(_rows(k, "k", cache, H, T, dt)),
+            _byref(_rows(v, "v", cache, H, T, dt)))
+    _call("slnr_page_append", args, cache.device.index, 0, validate, workspace, stream,
           (cache.k, cache.v, cache.codes, cache.scales, tables.slots, tables.req, tables.q_pos, k, v))
 
 
@@ -224,8 +247,8 @@ def page_select(q, cache: PagedCache, tables: PageTables, npicked, first=1, last
         c.dtype = _TYPES[q.dtype]
     rows = _rows(q, "q", cache, None, T, None if cache.k is None else cache.k.dtype)
     out = _out(out, "out", (T, c.nheads, npicked), torch.int32, cache.device, stream)
-    args = (ctypes.byref(rows), q.shape[1], ctypes.byref(c), ctypes.byref(tables._c), out.data_ptr(), npicked, first, last)
-    _call("slnr_page_select", args, cache.device, 0, validate, workspace, stream,
+    args = (_byref(rows), q.shape[1], _byref(c), _byref(tables._c), out.data_ptr(), npicked, first, last)
+    _call("slnr_page_select", args, cache.device.index, 0, validate, workspace, stream,
           (q, cache.codes, cache.scales, tables.table, tables.q_pos, tables.k_len, tables.req, out))
     return out
 
@@ -236,10 +259,10 @@ def _attention_bytes(npages, page_size, heads, width, dtype, nreq, ntok, max_q, 
     c = slnr_cache(npages, page_size, heads, width, dtype)
     p = slnr_pages(nreq, ntok, max_q, max_k, columns, 0, columns)
     o = slnr_opts()
-    args = (ctypes.byref(c), ctypes.byref(p), heads_q)
+    args = (_byref(c), _byref(p), heads_q)
     if npicked:
-        return _query("slnr_selected_attention_workspace", *args, npicked, ctypes.byref(o))
-    return _query("slnr_paged_attention_workspace", *args, ctypes.byref(o))
+        return _query("slnr_selected_attention_workspace", *args, npicked, _byref(o))
+    return _query("slnr_paged_attention_workspace", *args, _byref(o))
 
 
 def _attention(name, q, cache, tables, picked, npicked, scale, out, lse, validate, workspace, stream):
@@ -254,10 +277,10 @@ def _attention(name, q, cache, tables, picked, npicked, scale, out, lse, validat
     out = _out(out, "out", shape, q.dtype, cache.device, stream)
     lse = _out(lse, "lse", shape[:2], torch.float32, cache.device, stream)
     scale = c.head_dim ** -0.5 if scale is None else scale
-    head = (ctypes.byref(rows), heads_q, ctypes.byref(c), ctypes.byref(p))
+    head = (_byref(rows), heads_q, _byref(c), _byref(p))
     tail = (scale, out.data_ptr(), lse.data_ptr())
     mid = (picked.data_ptr(), npicked) if npicked else ()
-    _call(name, (*head, *mid, *tail), cache.device, need, validate, workspace, stream,
+    _call(name, (*head, *mid, *tail), cache.device.index, need, validate, workspace, stream,
           (q, cache.k, cache.v, tables.table, tables.q_pos, tables.k_len, tables.req, picked, out, lse))
     return out, lse
 
