@@ -53,6 +53,12 @@ struct AttnPlan {
   int chunk;    // keys of one split, a multiple of the kernel's step
   int nsplit;   // splits of the longest request (1: the block writes the result)
   bool cluster; // the splits of a row are joined by the blocks of a cluster (row kernel, nsplit in 2 .. 16)
+  // picked pages on the tensor-core kernel: what the tokens of a block's rows
+  // picked together (paged_chunk.cu), for each row tile and key head
+  int32_t* pages;    // [ntiles][nheads][cap] pages of the request, ascending
+  uint32_t* pickers; // [ntiles][nheads][cap][words] bit i: the tile's token i picked the page
+  int32_t* npages;   // [ntiles][nheads]
+  int cap, words;
   float* part;  // [ntok * nheads_q][nsplit][width] partial rows, each divided by its own sum
   float* part_lse;  // [ntok * nheads_q][nsplit] log2 of the partial sums of exponentials
 };
@@ -115,7 +121,9 @@ int select_tokens(int pages);
 cudaError_t launch_page_select(const PagesView& p, const CacheView& c, const RowsView& q, int dtype, int nheads_q,
                                int32_t* picked, int npicked, int first, int last, cudaStream_t s);
 
-// paged_chunk.cu (plan.tile == kChunkRows, scale > 0, no picked pages; hdr's flag word is zero)
+// paged_chunk.cu (plan.tile == kChunkRows; hdr's flag word is zero).  Picked
+// pages: launch_paged_union first; the page size divides 128 or is a multiple of it.
+cudaError_t launch_paged_union(const AttnArgs& a, cudaStream_t s);
 cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s);
 
 // paged_attn.cu (any other plan)

@@ -120,64 +120,98 @@ slnr_status validated(const slnr_opts* o, Launch launch) {
   return SLNR_OK;
 }
 
-// Blocks that the GPU holds at once: two of the row kernel's on each of 152 SMs.
-constexpr int64_t kResident = 304;
+constexpr int64_t kSms = 152;          // of one block of the tensor-core kernel, two of the row kernel's
 constexpr int64_t kMaxBlocks = 16384;  // splits stop here
 constexpr int64_t kMaxCluster = 16;
 
+// Whether picked pages go to the tensor-core kernel: steps of 128 keys are whole
+// pages or parts of one.
+bool whole_steps(int page) { return page >= kChunkKeys ? page % kChunkKeys == 0 : page >= 16 && kChunkKeys % page == 0; }
+
 // Row tiles and key splits of an attention call: by the bounds alone, never by
 // device data.  Calls with a request of more than 64 rows go to the tensor-core
-// kernel (256 rows a block), the others to the row kernel.
+// kernel (256 rows a block), the others to the row kernel; with picked pages its
+// blocks take the rows of one token.
 AttnPlan attn_plan(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, int32_t npicked) {
   AttnPlan a{};
-  const int64_t G = nheads_q / c.nheads, rows = npicked > 0 ? G : p.max_q * G;
-  a.tile = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || npicked > 0 ? 64 : kChunkRows;
-  const int64_t tiles = npicked > 0 ? p.ntok * ceil_div(G, a.tile)
-                                    : p.ntok * G / a.tile + (p.nreq < p.ntok ? p.nreq : p.ntok);
+  const int64_t G = nheads_q / c.nheads, requests = p.nreq < p.ntok ? p.nreq : p.ntok;
+  a.nsplit = 1;
+  if (p.max_q * G > 64 && (npicked == 0 || whole_steps(c.page_size))) {
+    a.tile = kChunkRows;
+    const int64_t tiles = p.ntok * G / a.tile + requests, blocks = tiles * c.nheads;
+    a.ntiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
+    if (npicked > 0) {
+      // the splits of a block's pages are found on the device: up to 4 where the blocks do not fill the GPU
+      const int64_t most = kChunkRows % G == 0 ? kChunkRows / G : (kChunkRows - 1) / G + 2;
+      const int64_t pages = ceil_div(p.max_k > 0 ? p.max_k : 1, c.page_size);
+      a.words = (int)ceil_div(most < kChunkRows ? most : kChunkRows, 32);
+      a.cap = (int)(pages < most * npicked ? pages : most * npicked);
+      while (a.nsplit < 4 && blocks * a.nsplit < kSms) a.nsplit *= 2;
+    } else if (p.max_k > 0) {
+      const int64_t want = ceil_div(3 * kSms, blocks > 0 ? blocks : 1);
+      int64_t chunk = ceil_div(p.max_k, want);
+      if (chunk < 512) chunk = 512;
+      a.chunk = (int)(ceil_div(chunk, kChunkKeys) * kChunkKeys);
+      a.nsplit = (int)ceil_div(p.max_k, a.chunk);
+    } else {
+      a.chunk = kChunkKeys;
+    }
+    return a;
+  }
+  const int64_t rows = npicked > 0 ? G : p.max_q * G;
+  a.tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  const int64_t tiles = npicked > 0 ? p.ntok * ceil_div(G, a.tile) : p.ntok * G / a.tile + requests;
   const int64_t keys = npicked > 0 ? (int64_t)npicked * c.page_size : p.max_k;
   const int64_t blocks = tiles * c.nheads;
   int64_t chunk = keys;
   if (blocks > 0) {
-    const bool tc = a.tile == kChunkRows;
-    const int64_t least = tc ? 512 : 128;
-    const int64_t want = tc ? ceil_div(3 * kResident / 2, blocks) : kResident / blocks;
+    const int64_t want = 2 * kSms / blocks;
     chunk = ceil_div(keys, want > 1 ? want : 1);
+    if (chunk < 128) chunk = 128;
+    if (npicked == 0 && chunk > 2048) chunk = 2048;  // requests of other lengths beside the longest
+    const int64_t least = ceil_div(keys * blocks, kMaxBlocks);
     if (chunk < least) chunk = least;
-    if (!tc && npicked == 0 && chunk > 2048) chunk = 2048;  // requests of other lengths beside the longest
-    const int64_t floor = ceil_div(keys * blocks, kMaxBlocks);
-    if (chunk < floor) chunk = floor;
   }
   // Where all splits run at once and there are few of them, they are the blocks
   // of a cluster (a power of two): no second launch.  A larger call would keep
   // the blocks of short requests waiting for those of long ones.
-  if (a.tile != kChunkRows && chunk < keys) {
+  if (chunk < keys) {
     int64_t n = 2;
     while (n < kMaxCluster && n * chunk < keys) n *= 2;
-    if (blocks * n <= kResident && keys <= n * (chunk > 512 ? chunk : 512)) {
+    if (blocks * n <= 2 * kSms && keys <= n * (chunk > 512 ? chunk : 512)) {
       chunk = ceil_div(keys, n);
       a.cluster = true;
       a.nsplit = (int)n;
     }
   }
-  const int64_t unit = a.tile == kChunkRows ? kChunkKeys : kAttnKeys;
-  chunk = ceil_div(chunk > 0 ? chunk : 1, unit) * unit;
+  chunk = ceil_div(chunk > 0 ? chunk : 1, kAttnKeys) * kAttnKeys;
   a.ntiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
   a.chunk = (int)chunk;
   if (!a.cluster) a.nsplit = keys > 0 ? (int)ceil_div(keys, chunk) : 1;
   return a;
 }
 
+// Workspace of an attention call after the header: partial rows, and the pages
+// that row tiles picked.
 struct AttnLayout {
-  size_t part = 0, lse = 0, total = 0;
+  size_t part, lse, pages, pickers, npages, total;
 };
 AttnLayout attn_layout(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, const AttnPlan& a) {
   AttnLayout l;
-  l.part = l.lse = l.total = sizeof(WsHeader);
-  if (a.nsplit > 1 && !a.cluster) {
-    const size_t rows = (size_t)p.ntok * nheads_q * a.nsplit;
-    l.lse = align256(l.part + rows * c.head_dim * sizeof(float));
-    l.total = align256(l.lse + rows * sizeof(float));
-  }
+  size_t cur = sizeof(WsHeader);
+  const auto take = [&cur](size_t bytes) {
+    const size_t at = align256(cur);
+    cur = at + bytes;
+    return at;
+  };
+  const size_t rows = a.nsplit > 1 && !a.cluster ? (size_t)p.ntok * nheads_q * a.nsplit : 0;
+  const size_t lists = a.cap > 0 ? (size_t)a.ntiles * c.nheads : 0;
+  l.part = take(rows * c.head_dim * sizeof(float));
+  l.lse = take(rows * sizeof(float));
+  l.pages = take(lists * a.cap * sizeof(int32_t));
+  l.pickers = take(lists * a.cap * a.words * sizeof(uint32_t));
+  l.npages = take(lists * sizeof(int32_t));
+  l.total = align256(cur);
   return l;
 }
 
@@ -207,14 +241,17 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   if (!aligned16(out)) return fail(SLNR_ERR_UNSUPPORTED, "out must be 16-byte aligned");
   AttnArgs a{view(*pages), view(*cache), view(*q), divisor(nheads_q / cache->nheads), scale, out, lse, picked, npicked,
              attn_plan(*cache, *pages, nheads_q, npicked)};
-  if (a.plan.nsplit > 65535 || a.plan.ntiles == INT32_MAX || (a.plan.tile == kChunkRows && a.plan.ntiles > 65535) || (int64_t)pages->max_q * a.group.d >= (int64_t(1) << 31) ||
-      (int64_t)npicked * cache->page_size > kMaxKeys)
+  if (a.plan.nsplit > 65535 || a.plan.ntiles == INT32_MAX || (a.plan.tile == kChunkRows && a.plan.ntiles > 65535) ||
+      (int64_t)pages->max_q * a.group.d >= (int64_t(1) << 31) || (int64_t)npicked * cache->page_size > kMaxKeys)
     return fail(SLNR_ERR_UNSUPPORTED, "too many rows or keys for one call");
   const AttnLayout l = attn_layout(*cache, *pages, nheads_q, a.plan);
   SLNR_CHECK(check_ws(opts, l.total));
   char* ws = (char*)opts->workspace;
   a.plan.part = (float*)(ws + l.part);
   a.plan.part_lse = (float*)(ws + l.lse);
+  a.plan.pages = (int32_t*)(ws + l.pages);
+  a.plan.pickers = (uint32_t*)(ws + l.pickers);
+  a.plan.npages = (int32_t*)(ws + l.npages);
   cudaStream_t s = (cudaStream_t)opts->stream;
   SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
     return launch_validate_pages(a.p, a.c.npages, a.c.page, false, picked, npicked, a.c.nheads, hdr, st);
@@ -222,6 +259,7 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   const bool tc = a.plan.tile == kChunkRows;
   if (tc) {
     SLNR_CUDA(cudaMemsetAsync(ws, 0, sizeof(WsHeader), s));
+    if (picked) SLNR_LAUNCH("paged_union", launch_paged_union(a, s));
     SLNR_LAUNCH("paged_chunk", launch_paged_chunk(a, cache->dtype, (WsHeader*)ws, s));
   } else {
     SLNR_LAUNCH("paged_rows", launch_paged_rows(a, cache->dtype, s));

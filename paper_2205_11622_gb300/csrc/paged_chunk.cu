@@ -16,6 +16,11 @@
 //       asynchronous 16-byte copies (any page size and stride), zeros past the
 //       last key.  Each thread finds one key's row by its page, a step ahead,
 //       and all read the rows' offsets from shared memory.
+// Picked pages: a block streams every page that a token of its rows picked, in
+// ascending order (k_paged_union lists them, with the tokens that picked each),
+// and a row's weights are zero in pages that its token did not pick.  A page is
+// read once for all tokens that share it, and never more pages are multiplied
+// than the tokens picked in all.
 // While one tile's warps are at its weights, the tensor cores work on the
 // other's.  Keys in 128-byte swizzled rows serve both products: K as the
 // K-major operand of Q K^T, V as the MN-major one of P V.
@@ -82,6 +87,23 @@ __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
   return (uint32_t)((piece >> 3) * kBlock + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
 }
 
+// Drops the scores of the keys that a row does not see: those past seen[g] of
+// segment g, for `segs` (a power of two) equal segments.
+template <int SEGS>
+__device__ __forceinline__ void mask_equal(uint32_t (&s)[128], const int (&seen)[8]) {
+#pragma unroll
+  for (int k = 0; k < 128; ++k)
+    if (k % (128 / SEGS) > seen[k / (128 / SEGS)]) s[k] = 0xff800000u;
+}
+__device__ __forceinline__ void mask_segments(uint32_t (&s)[128], const int (&seen)[8], int segs) {
+  switch (segs) {
+    case 1: return mask_equal<1>(s, seen);
+    case 2: return mask_equal<2>(s, seen);
+    case 4: return mask_equal<4>(s, seen);
+    default: return mask_equal<8>(s, seen);
+  }
+}
+
 // Register shares of the calling warpgroup.
 template <int N>
 __device__ __forceinline__ void regs_up() {
@@ -92,7 +114,76 @@ __device__ __forceinline__ void regs_down() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-template <typename T, int W>
+// The pages that the tokens of a row tile picked for one head, and who picked
+// each: bits set in shared memory for 1024 pages at a time, then the pages with
+// any written in order.
+constexpr int kUnionThreads = 256;
+constexpr int kUnionPages = 1024;
+constexpr int kMaxWords = 8;  // 256 tokens of one row each
+
+__global__ void __launch_bounds__(kUnionThreads)
+k_paged_union(AttnArgs a) {
+  __shared__ uint32_t s_bits[kUnionPages * kMaxWords];
+  __shared__ int s_count[kUnionThreads / 32 + 1];
+  const PagesView& p = a.p;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.x, words = a.plan.words;
+  int r, x0;
+  find_tile(p, a.group.d, kChunkRows, blockIdx.y, r, x0);
+  const int64_t at = (int64_t)blockIdx.y * gridDim.x + h;
+  if (r < 0) {
+    if (tid == 0) a.plan.npages[at] = 0;
+    return;
+  }
+  const int q0 = __ldg(p.q_pos + r), qn = __ldg(p.q_pos + r + 1) - q0;
+  const int n = min(kChunkRows, qn * a.group.d - x0), shift = __ldg(p.k_len + r) - qn;
+  const int t0 = a.group.div(x0), t1 = a.group.div(x0 + n - 1) + 1;
+  const int last = shift + t1 - 1;
+  const int npages = last < 0 ? 0 : min(a.c.page.div(last) + 1, p.width);
+  int total = 0;
+  for (int w0 = 0; w0 < npages; w0 += kUnionPages) {
+    for (int i = tid; i < kUnionPages * words; i += kUnionThreads) s_bits[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < (t1 - t0) * a.npicked; i += kUnionThreads) {
+      const int t = i / a.npicked, pg = __ldg(a.picked + ((int64_t)(q0 + t0 + t) * a.c.nheads + h) * a.npicked + i % a.npicked);
+      const int pos = shift + t0 + t;
+      if (pg >= w0 && pg < w0 + kUnionPages && pg < npages && pos >= 0 && pg <= a.c.page.div(pos))
+        atomicOr(&s_bits[(pg - w0) * words + (t >> 5)], 1u << (t & 31));
+    }
+    __syncthreads();
+    // each warp lists 128 pages
+    constexpr int SHARE = kUnionPages / (kUnionThreads / 32);
+    uint32_t any[SHARE / 32];
+    int mine = 0;
+#pragma unroll
+    for (int k = 0; k < SHARE / 32; ++k) {
+      const uint32_t* b = s_bits + (warp * SHARE + k * 32 + lane) * words;
+      uint32_t x = 0;
+      for (int w = 0; w < words; ++w) x |= b[w];
+      any[k] = __ballot_sync(0xffffffffu, x != 0);
+      mine += __popc(any[k]);
+    }
+    if (lane == 0) s_count[warp] = mine;
+    __syncthreads();
+    int e = total;
+    for (int w = 0; w < kUnionThreads / 32; ++w) {
+      if (w < warp) e += s_count[w];
+      total += s_count[w];
+    }
+#pragma unroll
+    for (int k = 0; k < SHARE / 32; ++k) {
+      const int slot = e + __popc(any[k] & ((1u << lane) - 1)), local = warp * SHARE + k * 32 + lane;
+      if (((any[k] >> lane) & 1) && slot < a.plan.cap) {
+        a.plan.pages[at * a.plan.cap + slot] = w0 + local;
+        for (int w = 0; w < words; ++w) a.plan.pickers[(at * a.plan.cap + slot) * words + w] = s_bits[local * words + w];
+      }
+      e += __popc(any[k]);
+    }
+    __syncthreads();
+  }
+  if (tid == 0) a.plan.npages[at] = min(total, a.plan.cap);
+}
+
+template <typename T, int W, bool SEL>
 __global__ void __launch_bounds__(kThreads, 1)
 k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   constexpr int PIECES = W / 8, NB = buffers<W>();
@@ -104,15 +195,29 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   const int G = a.group.d, h = blockIdx.x;
 
   int r, x0;
-  find_tile(p, G, kChunkRows, gridDim.y - 1 - blockIdx.y, r, x0);  // the last tiles see the most keys: first
+  const int row_tile = gridDim.y - 1 - blockIdx.y;  // the last tiles see the most keys: first
+  find_tile(p, G, kChunkRows, row_tile, r, x0);
   if (r < 0) return;
   const int q0 = __ldg(p.q_pos + r), qn = __ldg(p.q_pos + r + 1) - q0;
   const int n = min(kChunkRows, qn * G - x0), tiles = n > kRows ? 2 : 1;
   const int shift = __ldg(p.k_len + r) - qn;
-  const int end = max(shift + a.group.div(x0 + n - 1) + 1, 0);
-  const int u0 = blockIdx.z * a.plan.chunk;
-  if (u0 > 0 && u0 >= end) return;
-  const int u1 = max(min(end, u0 + a.plan.chunk), u0);
+  // its keys: [u0, u1) of the request's keys, or of the slots of the listed pages
+  const int last = shift + a.group.div(x0 + n - 1);  // position of the last row's token
+  const int64_t list_at = ((int64_t)row_tile * gridDim.x + h) * a.plan.cap;
+  int u0, u1, splits;
+  if (SEL) {
+    const int end = __ldg(a.plan.npages + (int64_t)row_tile * gridDim.x + h) * c.page.d;
+    splits = a.plan.nsplit;
+    const int share = ((end + kChunkKeys - 1) / kChunkKeys + splits - 1) / splits * kChunkKeys;
+    u0 = min((int)blockIdx.z * share, end);
+    u1 = min(u0 + share, end);
+  } else {
+    const int end = max(last + 1, 0);
+    splits = end > 0 ? (end - 1) / a.plan.chunk + 1 : 1;
+    u0 = blockIdx.z * a.plan.chunk;
+    if (u0 > 0 && u0 >= end) return;
+    u1 = max(min(end, u0 + a.plan.chunk), u0);
+  }
   const int steps = (u1 - u0 + kChunkKeys - 1) / kChunkKeys;
 
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -161,16 +266,23 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const int32_t* table = p.table + r * p.table_stride;
       const char* src_k = (const char*)c.k + 2 * (c.ks[2] * h + (col_on ? piece * 8 : 0));
       const char* src_v = (const char*)c.v + 2 * (c.vs[2] * h + (col_on ? piece * 8 : 0));
-      int id = -1, off = 0;
+      int id = -1, off = 0, next = -1;  // next: the listed page of the key after
+      auto listed = [&](int j) {
+        const int u = u0 + j * kChunkKeys + lt;
+        next = SEL && u < u1 ? __ldg(a.plan.pages + list_at + c.page.div(u)) : -1;
+      };
       auto find = [&](int j) {  // page and slot of this thread's key of step j
         const int u = u0 + j * kChunkKeys + lt;
         id = -1;
         if (u < u1) {
-          const int idx = c.page.div(u);
-          off = u - idx * c.page.d;
-          if (idx < p.width) id = __ldg(table + idx);
+          int i = c.page.div(u);
+          off = u - i * c.page.d;
+          if (SEL) i = next;
+          if (i < p.width && (!SEL || i * c.page.d + off <= last)) id = __ldg(table + i);
         }
+        if (SEL) listed(j + 1);
       };
+      if (SEL) listed(0);
       find(0);
       // ring step i: K of keys i / 2 (i even) or V; its copies are waited for `lag` steps later
       const int total = 2 * steps;
@@ -272,7 +384,24 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const float factor = a.scale * 1.4426950408889634f, sl2 = raw ? factor : 1.f;
       float m = -INFINITY, l = 0.f;  // maximum of the scores that weights are taken against, sum of weights
       bool ok = true;
+      // selected: the row's token in the tile, its page's bit and last slot seen in a listed page
+      const int tl = tok - a.group.div(x0), segs = SEL ? (c.page.d < kChunkKeys ? kChunkKeys / c.page.d : 1) : 0;
+      const uint32_t* pickers = a.plan.pickers + list_at * a.plan.words + (row_on ? tl >> 5 : 0);
       for (int j = 0; j < steps; ++j) {
+        int seen_in[8];  // per segment of the step: keys 0 .. seen_in of it
+        if (SEL) {
+#pragma unroll
+          for (int g2 = 0; g2 < 8; ++g2) {
+            seen_in[g2] = -1;
+            const int u = u0 + j * kChunkKeys + g2 * c.page.d;
+            if (g2 < segs && u < u1 && row_on) {
+              const int e = c.page.div(u);
+              const int pg = __ldg(a.plan.pages + list_at + e);
+              const bool on = (__ldg(pickers + (int64_t)e * a.plan.words) >> (tl & 31)) & 1;
+              if (on) seen_in[g2] = pos - pg * c.page.d - (u - e * c.page.d);
+            }
+          }
+        }
         ok = wait_warp(&bars.s_full[t], j & 1, failed, limit);
         if (!ok) break;
         tc::tc_fence_after_sync();
@@ -286,7 +415,9 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           for (int k = 0; k < 128; ++k) s[k] = __float_as_uint(__uint_as_float(s[k]) * factor);
         }
         const int key0 = u0 + j * kChunkKeys;
-        if (tail || key0 + kChunkKeys - 1 > pos_min) {
+        if (SEL) {
+          mask_segments(s, seen_in, segs);
+        } else if (tail || key0 + kChunkKeys - 1 > pos_min) {
           const int seen = pos - key0;  // keys 0 .. seen of these 128
 #pragma unroll
           for (int k = 0; k < 128; ++k)
@@ -341,7 +472,6 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       if (ok && steps > 0) ok = wait_warp(&bars.o_full, 0, failed, limit);
       if (ok) {
         tc::tc_fence_after_sync();
-        const int splits = end > 0 ? (end - 1) / a.plan.chunk + 1 : 1;
         const int64_t at = (q0 + tok) * ((int64_t)c.nheads * G) + h * G + g;
         const int64_t slot = at * a.plan.nsplit + blockIdx.z;
         const float inv = __fdividef(1.f, l);
@@ -399,9 +529,9 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   if (warp == kMmaWarp) tc::tmem_dealloc(tmem, kTmemCols);
 }
 
-template <typename T, int W>
+template <typename T, int W, bool SEL>
 cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
-  auto kernel = k_paged_chunk<T, W>;
+  auto kernel = k_paged_chunk<T, W, SEL>;
   static OncePerDevice once;
   cudaError_t e = once(
       [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<W>()); });
@@ -411,11 +541,22 @@ cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+template <typename T, bool SEL>
+cudaError_t launch_w(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
+  return a.c.width <= 64 ? launch<T, 64, SEL>(a, hdr, s) : launch<T, 128, SEL>(a, hdr, s);
+}
+
 }  // namespace
 
+cudaError_t launch_paged_union(const AttnArgs& a, cudaStream_t s) {
+  const dim3 grid((unsigned)a.c.nheads, (unsigned)a.plan.ntiles);
+  k_paged_union<<<(SLNR_COUNTED(grid)), kUnionThreads, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
 cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s) {
-  if (a.c.width <= 64) return dtype == SLNR_FP16 ? launch<__half, 64>(a, hdr, s) : launch<__nv_bfloat16, 64>(a, hdr, s);
-  return dtype == SLNR_FP16 ? launch<__half, 128>(a, hdr, s) : launch<__nv_bfloat16, 128>(a, hdr, s);
+  if (a.picked) return dtype == SLNR_FP16 ? launch_w<__half, true>(a, hdr, s) : launch_w<__nv_bfloat16, true>(a, hdr, s);
+  return dtype == SLNR_FP16 ? launch_w<__half, false>(a, hdr, s) : launch_w<__nv_bfloat16, false>(a, hdr, s);
 }
 
 }  // namespace slnr
