@@ -6,6 +6,7 @@
 // is a whole number below 2^24 and the product is rounded once, so the score,
 // and with it the selection, does not depend on the order of summation.
 #include "launch.h"
+#include "mma16.cuh"
 #include "paged.cuh"
 
 namespace slnr {
@@ -23,18 +24,79 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162f
 template <>
 __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
 
-// Whole numbers in the order of the scores; every score's is above 0 (0: not a candidate).
+// Whole numbers in the order of the scores.
 __device__ __forceinline__ uint32_t key_of(float score) {
   const uint32_t b = __float_as_uint(score + 0.f);  // -0 as 0
   return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
 
-// A block takes `ntile` consecutive tokens and one head.  Scores: a thread
-// holds the codes of one page in registers and multiplies them by each token's
-// codes out of shared memory, four products an instruction.  Selection: a warp
-// a token finds the key of the last page to take by halving the keys' range
-// (32 counts over the token's keys in shared memory), then writes the pages in
-// order.
+// The `want` highest of n keys (0 < want < n), the lower index first where keys
+// are equal: v = the least key taken, and how many of the keys equal to v.  A
+// warp halves the range [least, highest] of the keys until as many as wanted lie
+// at or above its middle (some ten steps; 32 at most, where keys are equal).
+struct Cut {
+  uint32_t v;
+  int ties;
+};
+template <typename Count>
+__device__ __forceinline__ Cut find_cut(uint32_t lo, uint32_t hi, int want, Count count) {
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2 + 1;
+    const int c = count(mid);
+    if (c == want) return Cut{mid - 1, 0};  // all keys above mid - 1, none of those equal to it
+    if (c > want) lo = mid;
+    else hi = mid - 1;
+  }
+  return Cut{lo, want - (lo == 0xffffffffu ? 0 : count(lo + 1))};
+}
+// Up to 32 KPL keys: held in registers.
+template <int KPL>
+__device__ __forceinline__ Cut cut_in_registers(const uint32_t* key, int n, int want) {
+  const int lane = threadIdx.x & 31;
+  uint32_t k[KPL], lo = 0xffffffffu, hi = 0;
+#pragma unroll
+  for (int i = 0; i < KPL; ++i) {
+    const bool on = 32 * i + lane < n;
+    k[i] = on ? key[32 * i + lane] : 0;
+    if (on) lo = min(lo, k[i]);
+    hi = max(hi, k[i]);
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  return find_cut(lo, hi, want, [&](uint32_t mid) {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) c += k[i] >= mid;
+    return (int)__reduce_add_sync(0xffffffffu, c);
+  });
+}
+__device__ __forceinline__ Cut cut_in_memory(const uint32_t* key, int n, int want) {
+  const int lane = threadIdx.x & 31;
+  return find_cut(0, 0xffffffffu, want, [&](uint32_t mid) {
+    int c = 0;
+    for (int i = lane; i < n; i += 32) c += key[i] >= mid;
+    return (int)__reduce_add_sync(0xffffffffu, c);
+  });
+}
+
+// Four codes as two pairs of fp16: 1024 + (code + 128) is the fp16 whose low byte
+// is code + 128.  Exact, as whole numbers up to 2048 are.
+__device__ __forceinline__ uint2 halves_of(uint32_t codes) {
+  const uint32_t x = codes ^ 0x80808080u;
+  const __half2 bias = __float2half2_rn(1152.f);
+  uint2 r;
+  r.x = __byte_perm(x, 0x64646464u, 0x4140);
+  r.y = __byte_perm(x, 0x64646464u, 0x4342);
+  *reinterpret_cast<__half2*>(&r.x) = __hsub2(*reinterpret_cast<__half2*>(&r.x), bias);
+  *reinterpret_cast<__half2*>(&r.y) = __hsub2(*reinterpret_cast<__half2*>(&r.y), bias);
+  return r;
+}
+
+// A block takes `ntile` consecutive tokens and one head.  Scores: fp16 matrix
+// products of 16 tokens and 8 pages, exact as all their sums are whole numbers
+// below 2^24; a warp a group of 8 pages, codes straight from memory into the
+// product's registers (the columns of a row in an order of their own, the same
+// for both operands).  Selection: a warp a token, then the pages written in order.
 template <typename T>
 __global__ void __launch_bounds__(kSelThreads)
 k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int npages, int32_t* picked, int npicked,
@@ -84,31 +146,57 @@ k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int np
   }
   __syncthreads();
 
-  // scores of runs of tokens of one request
+  // scores of runs of tokens of one request; lane: columns [quarter, quarter + 4 STEPS) of tokens lane / 4 and + 8,
+  // or of page lane / 4
+  constexpr int STEPS = kSelMaxWidth / 16;
+  const int steps = (c.width + 15) / 16, quarter = (lane & 3) * 4 * steps, row = lane >> 2;
+  uint32_t fa[STEPS][4];
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int w = (lane & 3) * steps + i;
+    const bool on = i < steps && 4 * w < c.width;
+    const uint2 x0 = halves_of(on && row < n ? s_code[row * (kSelMaxWidth / 4) + w] : 0);
+    const uint2 x1 = halves_of(on && row + 8 < n ? s_code[(row + 8) * (kSelMaxWidth / 4) + w] : 0);
+    fa[i][0] = x0.x;
+    fa[i][1] = x1.x;
+    fa[i][2] = x0.y;
+    fa[i][3] = x1.y;
+  }
   for (int i0 = 0; i0 < n;) {
     const int r = s_req[i0];
     int i1 = i0 + 1, most = s_own[i0];
     while (i1 < n && s_req[i1] == r) most = max(most, s_own[i1++]);
-    for (int pg = tid; pg <= most; pg += kSelThreads) {
-      const int id = __ldg(p.table + r * p.table_stride + pg);
+    for (int base = 8 * warp; base <= most; base += 8 * (kSelThreads / 32)) {
+      const int pg = base + row;
+      const int id = pg <= most ? __ldg(p.table + r * p.table_stride + pg) : -1;
       const bool ok = (unsigned)id < (unsigned)c.npages;
       const int64_t at = ok ? (int64_t)id * c.nheads + h : 0;
-      const int2* code = reinterpret_cast<const int2*>(c.codes + at * c.width);
-      int2 x[kSelMaxWidth / 8];
+      const int8_t* code = c.codes + at * c.width + quarter;
+      uint32_t x[STEPS];
+      if (c.width == kSelMaxWidth) {  // two 16-byte loads a lane
+        const uint4 y0 = ok ? __ldg(reinterpret_cast<const uint4*>(code)) : make_uint4(0, 0, 0, 0);
+        const uint4 y1 = ok ? __ldg(reinterpret_cast<const uint4*>(code) + 1) : make_uint4(0, 0, 0, 0);
+        x[0] = y0.x; x[1] = y0.y; x[2] = y0.z; x[3] = y0.w;
+        x[4] = y1.x; x[5] = y1.y; x[6] = y1.z; x[7] = y1.w;
+      } else {
 #pragma unroll
-      for (int w = 0; w < kSelMaxWidth / 8; ++w) x[w] = 2 * w < words && ok ? __ldg(code + w) : make_int2(0, 0);
+        for (int i = 0; i < STEPS; ++i)
+          x[i] = ok && i < steps && quarter + 4 * i < c.width ? __ldg(reinterpret_cast<const uint32_t*>(code) + i) : 0u;
+      }
       const float scale = ok ? __ldg(c.scales + at) : 0.f;
-      for (int i = i0; i < i1; ++i) {
-        const int2* y = reinterpret_cast<const int2*>(s_code + i * (kSelMaxWidth / 4));
-        int dot = 0;
+      float dot[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < kSelMaxWidth / 8; ++w)
-          if (2 * w < words) {
-            const int2 b = y[w];
-            dot = __dp4a(x[w].x, b.x, dot);
-            dot = __dp4a(x[w].y, b.y, dot);
-          }
-        s_key[i * npages + pg] = key_of(__fmul_rn((float)dot, scale));
+      for (int i = 0; i < STEPS; ++i)
+        if (i < steps) {
+          const uint2 b = halves_of(x[i]);
+          Half2<__half>::mma(dot, fa[i], b.x, b.y);
+        }
+      // dot[e]: token lane / 4 + 8 (e / 2), page 2 (lane % 4) + e % 2, whose scale lane 4 (page) holds
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int col = 2 * (lane & 3) + (e & 1), i = row + 8 * (e >> 1);
+        const float f = __shfl_sync(0xffffffffu, scale, 4 * col);
+        if (i >= i0 && i < i1 && base + col <= most) s_key[i * npages + base + col] = key_of(__fmul_rn(dot[e], f));
       }
     }
     i0 = i1;
@@ -121,26 +209,18 @@ k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int np
     const int own = s_own[i];
     // always taken: pages [0, lead) and [tail, own]; between them by score
     const int lead = min(first, own + 1), tail = max(own + 1 - last, lead);
-    int want = min(npicked - lead - (own + 1 - tail), tail - lead);
-    uint32_t v = 0;  // the least key taken
-    int ties = 0;    // of the pages with that key, how many
-    if (want > 0 && want < tail - lead) {
-      uint32_t lo = 1, hi = 0xffffffffu;  // count(key >= lo) >= want
-      while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2 + 1;
-        int cnt = 0;
-        for (int pg = lead + lane; pg < tail; pg += 32) cnt += key[pg] >= mid;
-        cnt = __reduce_add_sync(0xffffffffu, cnt);
-        if (cnt >= want) lo = mid;
-        else hi = mid - 1;
-      }
-      v = lo;
-      int above = 0;
-      for (int pg = lead + lane; pg < tail; pg += 32) above += key[pg] > v;
-      ties = want - __reduce_add_sync(0xffffffffu, above);
-    } else if (want > 0) {
-      ties = want;
+    const int want = min(npicked - lead - (own + 1 - tail), tail - lead);
+    const int among = tail - lead;
+    Cut cut{0, 0};
+    if (want > 0 && want < among) {
+      const uint32_t* k = key + lead;
+      cut = among <= 256    ? cut_in_registers<8>(k, among, want)
+            : among <= 512  ? cut_in_registers<16>(k, among, want)
+            : among <= 1024 ? cut_in_registers<32>(k, among, want)
+                            : cut_in_memory(k, among, want);
     }
+    const uint32_t v = cut.v;
+    int ties = cut.ties;
     const bool all = want > 0 && want == tail - lead, none = want <= 0;
     int at = 0;
     for (int base = 0; base <= own; base += 32) {

@@ -105,11 +105,11 @@ k_page_tables(int nreq, const int32_t* __restrict__ new_len, const int32_t* __re
 // Appending: K and V rows to their slots, and the summary of each page that a
 // token fills.
 //
-// The first blocks copy: a thread takes one 16-byte piece of a row for
+// The last blocks copy: a thread takes one 16-byte piece of a row for
 // kCopyTokens tokens, K and V, so 2 kCopyTokens loads are in flight and the
-// divisions that find the piece are made once.  The others look at 32 tokens a
-// warp, one head each; for a token in a page's last slot the warp sums that
-// head's keys over the page.  Rows of this call are read from the call's own
+// divisions that find the piece are made once.  The others look at 32 tokens
+// and one head each; for a token in a page's last slot the block's warps sum
+// that head's keys over the page.  Rows of this call are read from the call's own
 // input, so no block reads what another writes.  Bound by memory.
 constexpr int kCopyThreads = 256;
 constexpr int kCopyTokens = 4;
@@ -123,9 +123,9 @@ __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 
 template <typename T>
 __global__ void __launch_bounds__(kCopyThreads)
-k_page_append(PagesView p, CacheView c, RowsView kn, RowsView vn, int copy_blocks, Divisor of_token, Divisor of_head) {
-  if ((int)blockIdx.x < copy_blocks) {
-    const int lin = blockIdx.x * kCopyThreads + threadIdx.x;
+k_page_append(PagesView p, CacheView c, RowsView kn, RowsView vn, int sum_blocks, Divisor of_token, Divisor of_head) {
+  if ((int)blockIdx.x >= sum_blocks) {
+    const int lin = (blockIdx.x - sum_blocks) * kCopyThreads + threadIdx.x;
     const int group = of_token.div(lin), piece = lin - group * of_token.d;
     const int h = of_head.div(piece), col = (piece - h * of_head.d) * 8;
     const int t0 = group * kCopyTokens;
@@ -152,11 +152,13 @@ k_page_append(PagesView p, CacheView c, RowsView kn, RowsView vn, int copy_block
       }
     return;
   }
-  const int lane = threadIdx.x & 31;
-  const int64_t w = (int64_t)(blockIdx.x - copy_blocks) * (kCopyThreads / 32) + (threadIdx.x >> 5);
+  // one head of 32 tokens; the block's warps share the keys of each filled page
+  __shared__ float2 s_sum[kCopyThreads / 32][2][32];
+  constexpr int WARPS = kCopyThreads / 32, DEEP = 8;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t w = blockIdx.x;
   const int h = (int)(w % c.nheads);
   const int64_t first = w / c.nheads * 32;
-  if (first >= p.ntok) return;
   int slot = -1;
   if (first + lane < p.ntok) slot = __ldg(p.slots + first + lane);
   bool fills = slot >= 0;
@@ -164,7 +166,7 @@ k_page_append(PagesView p, CacheView c, RowsView kn, RowsView vn, int copy_block
     const int pg = page_of(slot, c);
     fills = pg < c.npages && slot - pg * c.page.d == c.page.d - 1;
   }
-  unsigned todo = __ballot_sync(0xffffffffu, fills);
+  unsigned todo = __ballot_sync(0xffffffffu, fills);  // the same in all warps
   while (todo) {
     const int i = __ffs(todo) - 1;
     todo &= todo - 1;
@@ -174,42 +176,62 @@ k_page_append(PagesView p, CacheView c, RowsView kn, RowsView vn, int copy_block
     const int s = c.page.d, fresh = min(t - __ldg(p.q_pos + r) + 1, s), j0 = s - fresh;
     const T* src_old = (const T*)c.k + pg * c.ks[0] + h * c.ks[2];
     const T* src_new = (const T*)kn.p + (int64_t)(t - (s - 1)) * kn.tok + h * kn.head;
-    // lane: columns 2 lane + 64 e, in pairs
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    // lane: columns 2 lane and 2 lane + 64, in pairs; warp: every eighth key, DEEP of them in flight
     const int col = 2 * lane;
-#pragma unroll 8
-    for (int j = 0; j < s; ++j) {
-      const T* row = j < j0 ? src_old + j * c.ks[1] : src_new + (int64_t)j * kn.tok;
+    float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+    for (int jb = warp; jb < s; jb += WARPS * DEEP) {
+      uint32_t x[DEEP][2];
+#pragma unroll
+      for (int d = 0; d < DEEP; ++d) {
+        const int j = jb + d * WARPS;
+        const T* row = j < j0 ? src_old + j * c.ks[1] : src_new + (int64_t)j * kn.tok;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          x[d][e] = j < s && col + 64 * e < c.width ? *reinterpret_cast<const uint32_t*>(row + col + 64 * e) : 0u;
+      }
+#pragma unroll
+      for (int d = 0; d < DEEP; ++d)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          T y[2];
+          *reinterpret_cast<uint32_t*>(y) = x[d][e];
+          sum[e].x += to_float(y[0]);
+          sum[e].y += to_float(y[1]);
+        }
+    }
+    s_sum[warp][0][lane] = sum[0];
+    s_sum[warp][1][lane] = sum[1];
+    __syncthreads();
+    if (warp == 0) {
+      float most = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        for (int k = 1; k < WARPS; ++k) {
+          const float2 y = s_sum[k][e][lane];
+          sum[e].x += y.x;
+          sum[e].y += y.y;
+        }
+        sum[e].x = __fdiv_rn(sum[e].x, (float)s);
+        sum[e].y = __fdiv_rn(sum[e].y, (float)s);
+        most = fmaxf(most, fmaxf(fabsf(sum[e].x), fabsf(sum[e].y)));
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      const float scale = __fdiv_rn(most, 127.f);
+      int8_t* code = c.codes + ((int64_t)pg * c.nheads + h) * c.width;
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         if (col + 64 * e < c.width) {
-          T x[2];
-          *reinterpret_cast<uint32_t*>(x) = *reinterpret_cast<const uint32_t*>(row + col + 64 * e);
-          sum[2 * e] += to_float(x[0]);
-          sum[2 * e + 1] += to_float(x[1]);
+          char2 x = make_char2(0, 0);
+          if (scale > 0.f) {
+            x.x = (signed char)min(max(__float2int_rn(__fdiv_rn(sum[e].x, scale)), -127), 127);
+            x.y = (signed char)min(max(__float2int_rn(__fdiv_rn(sum[e].y, scale)), -127), 127);
+          }
+          *reinterpret_cast<char2*>(code + col + 64 * e) = x;
         }
+      if (lane == 0) c.scales[(int64_t)pg * c.nheads + h] = scale;
     }
-    float most = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      sum[e] = __fdiv_rn(sum[e], (float)s);
-      most = fmaxf(most, fabsf(sum[e]));
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-    const float scale = __fdiv_rn(most, 127.f);
-    int8_t* code = c.codes + ((int64_t)pg * c.nheads + h) * c.width;
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (col + 64 * e < c.width) {
-        char2 x = make_char2(0, 0);
-        if (scale > 0.f) {
-          x.x = (signed char)min(max(__float2int_rn(__fdiv_rn(sum[2 * e], scale)), -127), 127);
-          x.y = (signed char)min(max(__float2int_rn(__fdiv_rn(sum[2 * e + 1], scale)), -127), 127);
-        }
-        *reinterpret_cast<char2*>(code + col + 64 * e) = x;
-      }
-    if (lane == 0) c.scales[(int64_t)pg * c.nheads + h] = scale;
+    __syncthreads();  // s_sum is read before the next page's sums are written
   }
 }
 
@@ -292,10 +314,10 @@ cudaError_t launch_page_append(const PagesView& p, const CacheView& c, const Row
   if (p.ntok == 0) return cudaSuccess;
   const int per_row = c.width / 8;
   const int64_t copy_blocks = ceil_div(ceil_div(p.ntok, kCopyTokens) * c.nheads * per_row, kCopyThreads);
-  const int64_t sum_blocks = c.codes ? ceil_div(ceil_div(p.ntok, 32) * c.nheads, kCopyThreads / 32) : 0;
+  const int64_t sum_blocks = c.codes ? ceil_div(p.ntok, 32) * c.nheads : 0;
   const unsigned grid = (unsigned)(copy_blocks + sum_blocks);
   auto kernel = dtype == SLNR_FP16 ? k_page_append<__half> : k_page_append<__nv_bfloat16>;
-  kernel<<<SLNR_COUNTED(grid), kCopyThreads, 0, s>>>(p, c, k, v, (int)copy_blocks,
+  kernel<<<SLNR_COUNTED(grid), kCopyThreads, 0, s>>>(p, c, k, v, (int)sum_blocks,
                                                      divisor(c.nheads * per_row), divisor(per_row));
   return cudaGetLastError();
 }

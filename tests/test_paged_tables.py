@@ -173,7 +173,7 @@ def plain_select(b, codes, scales, n, first, last):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("heads,D", [((8, 2), 128), ((4, 4), 64), ((6, 2), 80), ((16, 1), 8)])
+@pytest.mark.parametrize("heads,D", [((8, 2), 128), ((4, 4), 64), ((6, 2), 80), ((16, 1), 8), ((3, 3), 120), ((2, 1), 24)])
 @pytest.mark.parametrize("n,first,last", [(1, 0, 1), (4, 1, 2), (7, 3, 4), (16, 0, 1), (60, 1, 2)])
 def test_select(slnr, dtype, heads, D, n, first, last):
     """Few levels of codes and scales, so that equal scores abound; zero and negative-zero scores; short and empty requests."""
