@@ -308,11 +308,19 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           const uint32_t dst = buffer(b) + at;
           const char* src = (i & 1) ? src_v : src_k;
           const int64_t* rows = ((i & 1) ? bars.row_v[j & 1] : bars.row_k[j & 1]) + row0;
+          if (ok) {
+            constexpr int HALF = kChunkKeys / ROWS / 2;  // offsets are read ahead of the copies that wait for them
 #pragma unroll
-          for (int k = 0; k < kChunkKeys / ROWS; ++k) {
-            const int64_t o = rows[k * ROWS];
-            const bool on = col_on && o >= 0;
-            if (ok) copy16(dst + k * ROWS * 128, src + (on ? o : 0), on);
+            for (int k0 = 0; k0 < 2 * HALF; k0 += HALF) {
+              int64_t o[HALF];
+#pragma unroll
+              for (int k = 0; k < HALF; ++k) o[k] = rows[(k0 + k) * ROWS];
+#pragma unroll
+              for (int k = 0; k < HALF; ++k) {
+                const bool on = col_on && o[k] >= 0;
+                copy16(dst + (k0 + k) * ROWS * 128, src + (on ? o[k] : 0), on);
+              }
+            }
           }
         }
         copy_commit();
@@ -325,23 +333,32 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const int no = (c.width + 15) & ~15;  // columns of O
       const uint32_t id_o = tc::idesc_f16(type, kRows, no, true);
       const int ksteps = (c.width + 15) / 16;
+      // descriptors differ from the first tile's, buffer's and step's by their address, in units of 16 bytes
+      const uint64_t q_desc = tc::desc_k_sw128(q_tile(0)), k_desc = tc::desc_k_sw128(buffer(0));
+      const uint64_t v_desc = tc::desc_mn_sw128(buffer(0), kBlock);
+      constexpr uint64_t TILE = tile_bytes<W>() >> 4;
       auto scores = [&](int t, int b) {
-        if (lane == 0) {
-          for (int k = 0; k < ksteps; ++k) {
-            const uint32_t at = (k >> 2) * kBlock + (k & 3) * 32;
-            tc::mma_f16(tmem + kColS + t * 128, tc::desc_k_sw128(q_tile(t) + at), tc::desc_k_sw128(buffer(b) + at), id_s, k > 0);
+        const uint64_t qd = q_desc + t * TILE, kd = k_desc + b * TILE;
+        if (tc::elect_one()) {
+#pragma unroll
+          for (int k = 0; k < W / 16; ++k) {
+            const uint64_t at = ((k >> 2) * kBlock + (k & 3) * 32) >> 4;
+            if (k < ksteps) tc::mma_f16(tmem + kColS + t * 128, qd + at, kd + at, id_s, k > 0);
           }
           tc::mma_commit(&bars.s_full[t]);
         }
       };
       auto output = [&](int t, int b, bool first) {
-        if (lane == 0)
+        const uint64_t vd = v_desc + b * TILE;
+        const uint32_t o = tmem + kColO + t * 128, w = tmem + kColS + t * 128;
+        if (tc::elect_one()) {
+#pragma unroll
           for (int k = 0; k < kChunkKeys / 16; ++k)
-            tc::mma_f16_ta(tmem + kColO + t * 128, tmem + kColS + t * 128 + 8 * k,
-                           tc::desc_mn_sw128(buffer(b) + k * 2048, kBlock), id_o, !first || k > 0);
+            tc::mma_f16_ta(o, w + 8 * k, vd + k * (2048 >> 4), id_o, !first || k > 0);
+        }
       };
       auto release = [&](int b) {
-        if (lane == 0) tc::mma_commit(&bars.empty[b]);
+        if (tc::elect_one()) tc::mma_commit(&bars.empty[b]);
       };
       bool ok = steps > 0 && wait_warp(&bars.q_full, 0, failed, limit) && wait_warp(&bars.full[0], 0, failed, limit);
       if (ok) {
@@ -365,7 +382,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           }
         }
       }
-      if (ok && lane == 0) tc::mma_commit(&bars.o_full);
+      if (ok && tc::elect_one()) tc::mma_commit(&bars.o_full);
     }
   } else {
     regs_up<kSoftRegs>();
@@ -516,7 +533,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   tc::tc_fence_before_sync();
   __syncthreads();
   if (*failed) {
-    if (warp == kMmaWarp && lane == 0) {  // the products that were issued end before the tensor memory is freed
+    if (warp == kMmaWarp && tc::elect_one()) {  // the products that were issued end before the tensor memory is freed
       tc::mma_commit(&bars.drained);
       const long long t0 = clock64();
       while (!tc::mbar_try_wait(&bars.drained, 0))

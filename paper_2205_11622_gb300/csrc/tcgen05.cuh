@@ -196,6 +196,19 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// True in one lane of a whole warp, the same one each time: the lane that issues
+// a run of MMAs and their commit.  (A run unrolled under `lane == 0` came out
+// with wrong results.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t on;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(on));
+  return on != 0;
+}
+
 // ---- 16-bit operands (kind::f16) ---------------------------------------------
 // Instruction descriptor: fp32 accumulator, A and B both fp16 (type 0) or both
 // bf16 (type 1), A K-major, B K-major or, with bmn, MN-major.
