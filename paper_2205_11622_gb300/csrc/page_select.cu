@@ -126,7 +126,7 @@ k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int np
     if (lane < words) {
       const T* row = (const T*)q.p + (int64_t)t * q.tok + (int64_t)h * group * q.head + 4 * lane;
       for (int g = 0; g < group; ++g, row += q.head) {
-        T x[4];
+        alignas(8) T x[4];
         *reinterpret_cast<uint2*>(x) = __ldg(reinterpret_cast<const uint2*>(row));
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] = __fadd_rn(u[e], as_float(x[e]));

@@ -44,28 +44,36 @@ __device__ __forceinline__ int page_of(int slot, const CacheView& c) { return c.
 // How the rows of an attention call go to blocks.
 //
 // The rows of a request and key head are its tokens' query rows of that head's
-// group: row x is token x / G, query head g = x % G.  A block takes `tile` of
-// them and at most `chunk` keys; the partial results of a row's `nsplit` chunks
-// are combined in the chunks' order.
+// group: row x is token x / G, query head g = x % G.  A block of the row kernel
+// takes `tile` of them and at most `chunk` keys; the partial results of a row's
+// `nsplit` chunks are combined in the chunks' order.
 struct AttnPlan {
   int tile;     // rows a block takes
   int ntiles;   // bound of the row tiles of all requests
   int chunk;    // keys of one split, a multiple of the kernel's step
   int nsplit;   // splits of the longest request (1: the block writes the result)
   bool cluster; // the splits of a row are joined by the blocks of a cluster (row kernel, nsplit in 2 .. 16)
-  // picked pages on the tensor-core kernel: what the tokens of a block's rows
-  // picked together (paged_chunk.cu), for each row tile and key head
-  int32_t* pages;    // [ntiles][nheads][cap] pages of the request, ascending
-  uint32_t* pickers; // [ntiles][nheads][cap][words] bit i: the tile's token i picked the page
-  int32_t* npages;   // [ntiles][nheads]
+  // the tensor-core kernel's items (paged_chunk.cu): row tiles, steps (by their cost)
+  // before each item, the item and step that each block's share begins at
+  int4* tiles;      // [ntiles][2]
+  int64_t* before;  // [ntiles * nheads]
+  int2* shares;     // [kChunkBlocks], then {blocks with a share, items}, {row tiles, 0}
+  // picked pages there: what the tokens of a tile's rows picked together, for each key head and row tile
+  int32_t* pages;    // [nheads][ntiles][cap] pages of the request, ascending
+  uint32_t* pickers; // [nheads][ntiles][cap][words] bit i: the tile's token i picked the page
+  int32_t* npages;   // [nheads][ntiles]
   int cap, words;
-  float* part;  // [ntok * nheads_q][nsplit][width] partial rows, each divided by its own sum
-  float* part_lse;  // [ntok * nheads_q][nsplit] log2 of the partial sums of exponentials
+  // partial rows, each divided by its own sum, and log2 of their sums of exponentials: [ntok * nheads_q][nsplit], or
+  // of the tensor-core kernel [2 kChunkBlocks][kChunkRows]
+  float* part;      // [...][width]
+  float* part_lse;
 };
 
 constexpr int kAttnKeys = 64;       // keys of one step of the row kernel
 constexpr int kChunkKeys = 128;     // and of the tensor-core kernel, whose blocks take
-constexpr int kChunkRows = 256;     // that many rows
+constexpr int kChunkRows = 256;     // that many rows; one block on each of 152 SMs,
+constexpr int kChunkBlocks = 152;   // with a share of
+constexpr int kLeastSteps = 4;      // that much of the steps' cost or more
 constexpr int kAttnMaxPicked = 1024;  // pages picked for one row
 
 struct AttnArgs {
@@ -121,10 +129,11 @@ int select_tokens(int pages);
 cudaError_t launch_page_select(const PagesView& p, const CacheView& c, const RowsView& q, int dtype, int nheads_q,
                                int32_t* picked, int npicked, int first, int last, cudaStream_t s);
 
-// paged_chunk.cu (plan.tile == kChunkRows; hdr's flag word is zero).  Picked
-// pages: launch_paged_union first; the page size divides 128 or is a multiple of it.
-cudaError_t launch_paged_union(const AttnArgs& a, cudaStream_t s);
+// paged_chunk.cu (plan.tile == kChunkRows), in this order; hdr's flag word is
+// zero.  Picked pages: the page size divides 128 or is a multiple of it.
+cudaError_t launch_paged_plan(const AttnArgs& a, cudaStream_t s);
 cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s);
+cudaError_t launch_paged_join(const AttnArgs& a, int dtype, cudaStream_t s);
 
 // paged_attn.cu (any other plan)
 cudaError_t launch_paged_rows(const AttnArgs& a, int dtype, cudaStream_t s);

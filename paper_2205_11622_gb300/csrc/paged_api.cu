@@ -138,23 +138,13 @@ AttnPlan attn_plan(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, i
   a.nsplit = 1;
   if (p.max_q * G > 64 && (npicked == 0 || whole_steps(c.page_size))) {
     a.tile = kChunkRows;
-    const int64_t tiles = p.ntok * G / a.tile + requests, blocks = tiles * c.nheads;
+    const int64_t tiles = p.ntok * G / a.tile + requests;
     a.ntiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
     if (npicked > 0) {
-      // the splits of a block's pages are found on the device: up to 4 where the blocks do not fill the GPU
-      const int64_t most = kChunkRows % G == 0 ? kChunkRows / G : (kChunkRows - 1) / G + 2;
+      const int64_t most = kChunkRows % G == 0 ? kChunkRows / G : (kChunkRows - 1) / G + 2;  // tokens of a tile
       const int64_t pages = ceil_div(p.max_k > 0 ? p.max_k : 1, c.page_size);
       a.words = (int)ceil_div(most < kChunkRows ? most : kChunkRows, 32);
       a.cap = (int)(pages < most * npicked ? pages : most * npicked);
-      while (a.nsplit < 4 && blocks * a.nsplit < kSms) a.nsplit *= 2;
-    } else if (p.max_k > 0) {
-      const int64_t want = ceil_div(3 * kSms, blocks > 0 ? blocks : 1);
-      int64_t chunk = ceil_div(p.max_k, want);
-      if (chunk < 512) chunk = 512;
-      a.chunk = (int)(ceil_div(chunk, kChunkKeys) * kChunkKeys);
-      a.nsplit = (int)ceil_div(p.max_k, a.chunk);
-    } else {
-      a.chunk = kChunkKeys;
     }
     return a;
   }
@@ -194,7 +184,7 @@ AttnPlan attn_plan(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, i
 // Workspace of an attention call after the header: partial rows, and the pages
 // that row tiles picked.
 struct AttnLayout {
-  size_t part, lse, pages, pickers, npages, total;
+  size_t part, lse, tiles, before, shares, pages, pickers, npages, total;
 };
 AttnLayout attn_layout(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, const AttnPlan& a) {
   AttnLayout l;
@@ -204,10 +194,15 @@ AttnLayout attn_layout(const slnr_cache& c, const slnr_pages& p, int32_t nheads_
     cur = at + bytes;
     return at;
   };
-  const size_t rows = a.nsplit > 1 && !a.cluster ? (size_t)p.ntok * nheads_q * a.nsplit : 0;
-  const size_t lists = a.cap > 0 ? (size_t)a.ntiles * c.nheads : 0;
+  const bool tc = a.tile == kChunkRows;
+  const size_t rows = tc ? (size_t)2 * kChunkBlocks * kChunkRows
+                         : a.nsplit > 1 && !a.cluster ? (size_t)p.ntok * nheads_q * a.nsplit : 0;
+  const size_t items = tc ? (size_t)a.ntiles * c.nheads : 0, lists = a.cap > 0 ? items : 0;
   l.part = take(rows * c.head_dim * sizeof(float));
   l.lse = take(rows * sizeof(float));
+  l.tiles = take(tc ? (size_t)a.ntiles * 2 * sizeof(int4) : 0);
+  l.before = take(items * sizeof(int64_t));
+  l.shares = take(tc ? (kChunkBlocks + 2) * sizeof(int2) : 0);
   l.pages = take(lists * a.cap * sizeof(int32_t));
   l.pickers = take(lists * a.cap * a.words * sizeof(uint32_t));
   l.npages = take(lists * sizeof(int32_t));
@@ -249,6 +244,9 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   char* ws = (char*)opts->workspace;
   a.plan.part = (float*)(ws + l.part);
   a.plan.part_lse = (float*)(ws + l.lse);
+  a.plan.tiles = (int4*)(ws + l.tiles);
+  a.plan.before = (int64_t*)(ws + l.before);
+  a.plan.shares = (int2*)(ws + l.shares);
   a.plan.pages = (int32_t*)(ws + l.pages);
   a.plan.pickers = (uint32_t*)(ws + l.pickers);
   a.plan.npages = (int32_t*)(ws + l.npages);
@@ -259,8 +257,9 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   const bool tc = a.plan.tile == kChunkRows;
   if (tc) {
     SLNR_CUDA(cudaMemsetAsync(ws, 0, sizeof(WsHeader), s));
-    if (picked) SLNR_LAUNCH("paged_union", launch_paged_union(a, s));
+    SLNR_LAUNCH("paged_plan", launch_paged_plan(a, s));
     SLNR_LAUNCH("paged_chunk", launch_paged_chunk(a, cache->dtype, (WsHeader*)ws, s));
+    SLNR_LAUNCH("paged_join", launch_paged_join(a, cache->dtype, s));
   } else {
     SLNR_LAUNCH("paged_rows", launch_paged_rows(a, cache->dtype, s));
   }

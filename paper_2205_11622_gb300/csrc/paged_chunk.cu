@@ -1,8 +1,12 @@
 // Attention of chunks of new tokens over a paged cache, on the tcgen05 tensor
 // cores.
 //
-// A block takes 256 rows (two tiles of 128: the query rows of one key head's
-// group, token after token) and streams their keys, 128 at a time.  Tensor
+// An item is 256 rows (two tiles of 128: the query rows of one key head's group,
+// token after token) with all their keys, 128 a step.  One block runs on each
+// SM; the steps of all items, one after another, are cut into as many equal
+// shares, so a block ends one item, takes some whole ones and begins another,
+// and k_paged_join adds up the items that a cut went through.  (A block an item,
+// the last wave of a 4096-token chunk left a fifth of the time unused.)  Tensor
 // memory holds both tiles' scores S (128 x 128 fp32) and outputs O; the weights
 // P, rounded to the cache's type, are written over the scores that they come
 // from and are the A operand of the product with V.
@@ -39,7 +43,7 @@ constexpr int kLoadWarp = 8;            // warps 0-7: softmax
 constexpr int kLoaders = 128;
 constexpr int kMmaWarp = 12;            // 13-15 only complete its warpgroup
 constexpr int kThreads = 512;
-constexpr int kSoftRegs = 200, kOtherRegs = 56;  // of 128 a thread at launch
+constexpr int kSoftRegs = 192, kOtherRegs = 64;  // of 128 a thread at launch
 static_assert(2 * (kSoftRegs + kOtherRegs) <= 4 * 128, "register shares of the four warpgroups");
 static_assert(kLoaders == kChunkKeys, "a load thread finds one key's row");
 constexpr int kBlock = kRows * 128;     // 128 rows of 64 values, swizzled
@@ -53,17 +57,19 @@ template <int W>
 constexpr int buffers() { return W == 128 ? 4 : 8; }
 template <int W>
 constexpr size_t smem_bytes() { return (size_t)(2 + buffers<W>()) * tile_bytes<W>() + 1024; }
-template <int W>
-constexpr int lag() { return buffers<W>() - 2; }  // ring steps in flight before one is waited for
+constexpr int kWarpArrivals = 4;  // a warp arrives once for its lanes
 
-struct Barriers {
-  uint64_t q_full, s_full[2], p_full[2], o_full, full[8], empty[8], drained;
+struct Shared {
+  uint64_t q_full, q_empty, s_full[2], p_full[2], o_full, full[8], empty[8], drained;
   uint32_t tmem;
   int failed;
   int64_t row_k[2][kChunkKeys], row_v[2][kChunkKeys];  // bytes from the head's first row to each key's; -1: zeros
+  int64_t row_q[2 * kRows];                            // the same of the item's query rows
+  float2 other_ml[kRows];          // one tile an item: the second warpgroup's maxima and sums
+  alignas(16) float stage[kLoadWarp][32][20];  // 16 columns of a warp's rows on their way out
 };
 
-static_assert(smem_bytes<128>() + sizeof(Barriers) <= (size_t)227 * 1024, "shared memory of a block");
+static_assert(smem_bytes<128>() + sizeof(Shared) <= (size_t)227 * 1024, "shared memory of a block");
 
 // Waits for the phase of that parity; false (and *failed set) after `limit` cycles or once another wait gave up.
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* failed, long long limit) {
@@ -81,6 +87,19 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
 __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* failed, long long limit) {
   return __all_sync(0xffffffffu, wait(bar, parity, failed, limit));
 }
+
+// One arrival for the warp's lanes, after what each of them did.
+__device__ __forceinline__ void arrive_warp(uint64_t* bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) tc::mbar_arrive(bar);
+}
+// The thread's arrival once its copies so far have landed.  Who waits for them
+// orders its products behind them (fence_proxy_async_smem).
+__device__ __forceinline__ void copy_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(bar)) : "memory");
+}
+// Barrier `id` of n threads.
+__device__ __forceinline__ void meet(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 
 // Byte of 16-byte piece `piece` of a row inside a swizzled tile of 128 rows.
 __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
@@ -129,7 +148,7 @@ k_paged_union(AttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.x, words = a.plan.words;
   int r, x0;
   find_tile(p, a.group.d, kChunkRows, blockIdx.y, r, x0);
-  const int64_t at = (int64_t)blockIdx.y * gridDim.x + h;
+  const int64_t at = (int64_t)h * gridDim.y + blockIdx.y;
   if (r < 0) {
     if (tid == 0) a.plan.npages[at] = 0;
     return;
@@ -183,53 +202,239 @@ k_paged_union(AttnArgs a) {
   if (tid == 0) a.plan.npages[at] = min(total, a.plan.cap);
 }
 
+// What every role of a block knows of the part of an item that it works on.
+struct Item {
+  int h, r, x0, q0, n, tiles;  // key head, request, its first row and token, rows, tiles of 128
+  int shift, last;             // position of the request's first new token, and of the last row's token
+  int u0, u1, steps;           // keys (or slots of the listed pages) of this part
+  int slot;                    // of the partial rows; -1: the whole item
+  int64_t list;                // of the listed pages
+};
+
+// Cost of a step of an item of n rows: one tile takes half as long as two.
+__device__ __forceinline__ int weight_of(int n) { return n > kRows ? 2 : 1; }
+__device__ __forceinline__ int steps_of(int end) { return end > 0 ? (end - 1) / kChunkKeys + 1 : 1; }
+
+// Part [lo, hi) of item i (hi = -1: to its end).
+template <bool SEL>
+__device__ __forceinline__ Item item_of(const AttnArgs& a, int i, int ntiles, int lo, int hi) {
+  Item it;
+  it.h = i / ntiles;
+  const int tile = i - it.h * ntiles;
+  const int4 x = __ldg(a.plan.tiles + 2 * tile), y = __ldg(a.plan.tiles + 2 * tile + 1);
+  it.r = x.x;
+  it.x0 = x.y;
+  it.q0 = x.z;
+  it.n = x.w;
+  it.tiles = it.n > kRows ? 2 : 1;
+  it.shift = y.x;
+  it.last = y.y;
+  const int64_t at = (int64_t)it.h * a.plan.ntiles + tile;
+  it.list = at * a.plan.cap;
+  const int end = SEL ? __ldg(a.plan.npages + at) * a.c.page.d : max(it.last + 1, 0);
+  const int all = steps_of(end);
+  if (hi < 0) hi = all;
+  it.u0 = min(lo * kChunkKeys, end);
+  it.u1 = hi < all ? hi * kChunkKeys : end;
+  it.steps = (it.u1 - it.u0 + kChunkKeys - 1) / kChunkKeys;
+  it.slot = lo == 0 && hi == all ? -1 : 2 * (int)blockIdx.x + (lo == 0);
+  return it;
+}
+
+// Row tiles, and where each block's share of the items' steps begins.  Items go
+// head by head, a head's tiles in order.  One block.
+constexpr int kPlanThreads = 1024;
+
+// Inclusive sum over the block; `total` gets the whole.
+__device__ __forceinline__ int block_sum(int x, int& total, int* s_warp) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) s_warp[warp] = x;
+  __syncthreads();
+  int y = s_warp[lane];
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int z = __shfl_up_sync(0xffffffffu, y, o);
+    if (lane >= o) y += z;
+  }
+  total = __shfl_sync(0xffffffffu, y, 31);
+  const int before = __shfl_sync(0xffffffffu, y, (warp + 31) & 31);
+  return warp > 0 ? x + before : x;
+}
+
+template <bool SEL>
+__global__ void __launch_bounds__(kPlanThreads)
+k_paged_plan(AttnArgs a) {
+  __shared__ int s_first[kPlanThreads], s_warp[32];
+  const PagesView& p = a.p;
+  const int tid = threadIdx.x, G = a.group.d;
+  int ntiles = 0;
+  for (int r0 = 0; r0 < p.nreq; r0 += kPlanThreads) {
+    const int r = r0 + tid;
+    const int rows = r < p.nreq ? (__ldg(p.q_pos + r + 1) - __ldg(p.q_pos + r)) * G : 0;
+    int total;
+    const int mine = tiles_of(rows, kChunkRows), sum = block_sum(mine, total, s_warp);
+    s_first[tid] = sum - mine;
+    __syncthreads();
+    for (int t = tid; t < total && ntiles + t < a.plan.ntiles; t += kPlanThreads) {
+      int i = 0;  // the last request whose first tile is at or before t: the ones after it that start there are empty
+#pragma unroll
+      for (int w = kPlanThreads / 2; w > 0; w >>= 1)
+        if (s_first[i + w] <= t) i += w;
+      const int q0 = __ldg(p.q_pos + r0 + i), qn = __ldg(p.q_pos + r0 + i + 1) - q0;
+      const int x0 = (t - s_first[i]) * kChunkRows, n = min(kChunkRows, qn * G - x0);
+      const int shift = __ldg(p.k_len + r0 + i) - qn;
+      a.plan.tiles[2 * (ntiles + t)] = make_int4(r0 + i, x0, q0, n);
+      a.plan.tiles[2 * (ntiles + t) + 1] = make_int4(shift, shift + a.group.div(x0 + n - 1), 0, 0);
+    }
+    ntiles += total;
+    __syncthreads();
+  }
+  ntiles = min(ntiles, a.plan.ntiles);
+  // steps before each item, by their cost
+  const int items = ntiles * a.c.nheads;
+  int64_t steps = 0;
+  for (int i0 = 0; i0 < items; i0 += kPlanThreads) {
+    const int i = i0 + tid;
+    int mine = 0, total;
+    if (i < items) {
+      const int h = i / ntiles, tile = i - h * ntiles;
+      mine = weight_of(a.plan.tiles[2 * tile].w) *
+             steps_of(SEL ? a.plan.npages[(int64_t)h * a.plan.ntiles + tile] * a.c.page.d
+                          : max(a.plan.tiles[2 * tile + 1].y + 1, 0));
+    }
+    const int sum = block_sum(mine, total, s_warp);
+    if (i < items) a.plan.before[i] = steps + sum - mine;
+    steps += total;
+  }
+  __syncthreads();
+  const int64_t most = steps / kLeastSteps > 1 ? steps / kLeastSteps : 1;
+  const int n = (int)(most < kChunkBlocks ? most : kChunkBlocks);  // blocks with a share
+  // share c begins at step c steps / n
+  for (int i = tid; i < items; i += kPlanThreads) {
+    const int64_t lo = a.plan.before[i], hi = i + 1 < items ? a.plan.before[i + 1] : steps;
+    const int w = weight_of(a.plan.tiles[2 * (i % ntiles)].w);
+    for (int64_t c = (lo * n + steps - 1) / steps; c < n && c * steps / n < hi; ++c)
+      a.plan.shares[c] = make_int2(i, (int)(c * steps / n - lo) / w);
+  }
+  if (tid == 0) {
+    a.plan.shares[kChunkBlocks] = make_int2(items > 0 ? n : 0, items);
+    a.plan.shares[kChunkBlocks + 1] = make_int2(ntiles, 0);
+  }
+}
+
+// 16 columns of the second warpgroup's rows, where its rows are staged otherwise.
+__device__ __forceinline__ float (&other_rows(Shared& sh))[16][kRows] {
+  static_assert(sizeof(float) * 16 * kRows <= sizeof(sh.stage) / 2, "the second warpgroup's half");
+  return *reinterpret_cast<float(*)[16][kRows]>(&sh.stage[kLoadWarp / 2]);
+}
+
+// The rows of a warp out of tensor memory, times inv (0: no key), with f_other
+// times the other warpgroup's where an item has one tile: 16 columns at a time
+// a thread a row, and through shared memory to whole 32-byte sectors a few lanes
+// a row.  m: maximum in powers of two, l: sum.
+template <typename T, int W>
+__device__ __forceinline__ void write_rows(const AttnArgs& a, const Item& it, Shared& sh, uint32_t col_o, int warp,
+                                           int lane, bool ok, bool mine, float inv, float f_other, float m, float l) {
+  const bool pair = it.tiles == 1;
+  const int G = a.group.d, x0 = (pair ? 0 : (warp >> 2) * kRows) + (warp & 3) * 32;  // the warp's first row
+  const int row = (warp & 3) * 32 + lane;
+  const int64_t hq = (int64_t)a.c.nheads * G;
+  auto place = [&](int x) {  // of the item's row x in out and lse, or in the parts
+    if (it.slot >= 0) return (int64_t)it.slot * kChunkRows + x;
+    const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
+    return (it.q0 + tok) * hq + it.h * G + g;
+  };
+  float(&stage)[32][20] = sh.stage[warp];
+  for (int col0 = 0; col0 < W; col0 += 16) {
+    float o[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = 0.f;
+    if (ok && mine) tc::tmem_ld16(col_o + col0, o);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = inv == 0.f ? 0.f : o[e] * inv;
+    if (pair) {
+      const float(&other)[16][kRows] = other_rows(sh);
+      meet(2, 2 * kRows);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e] = f_other == 0.f ? o[e] : fmaf(other[e][row], f_other, o[e]);
+      meet(2, 2 * kRows);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<float4*>(&stage[lane][4 * e]) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+    __syncwarp();
+    if (it.slot >= 0) {  // 4 lanes a row
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int q = 8 * i + (lane >> 2), col = 4 * (lane & 3);
+        if (ok && x0 + q < it.n && col0 + col < a.c.width)
+          *reinterpret_cast<float4*>(a.plan.part + place(x0 + q) * a.c.width + col0 + col) =
+              *reinterpret_cast<const float4*>(&stage[q][col]);
+      }
+    } else {  // 2 lanes a row
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int q = 16 * i + (lane >> 1), col = 8 * (lane & 1);
+        if (ok && x0 + q < it.n && col0 + col < a.c.width) {
+          const float4 y0 = *reinterpret_cast<const float4*>(&stage[q][col]);
+          const float4 y1 = *reinterpret_cast<const float4*>(&stage[q][col + 4]);
+          uint4 z;
+          z.x = Half2<T>::pack(y0.x, y0.y);
+          z.y = Half2<T>::pack(y0.z, y0.w);
+          z.z = Half2<T>::pack(y1.x, y1.y);
+          z.w = Half2<T>::pack(y1.z, y1.w);
+          *reinterpret_cast<uint4*>((T*)a.out + place(x0 + q) * a.c.width + col0 + col) = z;
+        }
+      }
+    }
+  }
+  if (ok && x0 + lane < it.n) {
+    const float lse2 = l == 0.f ? -INFINITY : m + __log2f(l);
+    if (it.slot >= 0) a.plan.part_lse[place(x0 + lane)] = lse2;
+    else if (a.lse) a.lse[place(x0 + lane)] = lse2 * 0.6931471805599453f;
+  }
+}
+
+// Calls f(item) for the parts of items that are this block's.
+template <bool SEL, typename F>
+__device__ __forceinline__ void each_item(const AttnArgs& a, F f) {
+  const int c = blockIdx.x, n = __ldg(a.plan.shares + kChunkBlocks).x, items = __ldg(a.plan.shares + kChunkBlocks).y;
+  const int ntiles = __ldg(a.plan.shares + kChunkBlocks + 1).x;
+  if (c >= n) return;
+  const int2 from = __ldg(a.plan.shares + c), to = c + 1 < n ? __ldg(a.plan.shares + c + 1) : make_int2(items, 0);
+  for (int i = from.x; i < to.x || (i == to.x && to.y > 0); ++i)
+    f(item_of<SEL>(a, i, ntiles, i == from.x ? from.y : 0, i == to.x ? to.y : -1));
+}
+
 template <typename T, int W, bool SEL>
 __global__ void __launch_bounds__(kThreads, 1)
 k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   constexpr int PIECES = W / 8, NB = buffers<W>();
   extern __shared__ unsigned char smem_raw[];
-  __shared__ Barriers bars;
+  __shared__ Shared bars;
   const PagesView& p = a.p;
   const CacheView& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int G = a.group.d, h = blockIdx.x;
-
-  int r, x0;
-  const int row_tile = gridDim.y - 1 - blockIdx.y;  // the last tiles see the most keys: first
-  find_tile(p, G, kChunkRows, row_tile, r, x0);
-  if (r < 0) return;
-  const int q0 = __ldg(p.q_pos + r), qn = __ldg(p.q_pos + r + 1) - q0;
-  const int n = min(kChunkRows, qn * G - x0), tiles = n > kRows ? 2 : 1;
-  const int shift = __ldg(p.k_len + r) - qn;
-  // its keys: [u0, u1) of the request's keys, or of the slots of the listed pages
-  const int last = shift + a.group.div(x0 + n - 1);  // position of the last row's token
-  const int64_t list_at = ((int64_t)row_tile * gridDim.x + h) * a.plan.cap;
-  int u0, u1, splits;
-  if (SEL) {
-    const int end = __ldg(a.plan.npages + (int64_t)row_tile * gridDim.x + h) * c.page.d;
-    splits = a.plan.nsplit;
-    const int share = ((end + kChunkKeys - 1) / kChunkKeys + splits - 1) / splits * kChunkKeys;
-    u0 = min((int)blockIdx.z * share, end);
-    u1 = min(u0 + share, end);
-  } else {
-    const int end = max(last + 1, 0);
-    splits = end > 0 ? (end - 1) / a.plan.chunk + 1 : 1;
-    u0 = blockIdx.z * a.plan.chunk;
-    if (u0 > 0 && u0 >= end) return;
-    u1 = max(min(end, u0 + a.plan.chunk), u0);
-  }
-  const int steps = (u1 - u0 + kChunkKeys - 1) / kChunkKeys;
+  const int G = a.group.d;
 
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
   auto q_tile = [&](int t) { return base + t * tile_bytes<W>(); };
   auto buffer = [&](int b) { return base + (2 + b) * tile_bytes<W>(); };
   if (tid == 0) {
     tc::mbar_init(&bars.q_full, kLoaders);
+    tc::mbar_init(&bars.q_empty, 1);
     tc::mbar_init(&bars.o_full, 1);
     tc::mbar_init(&bars.drained, 1);
     for (int t = 0; t < 2; ++t) {
       tc::mbar_init(&bars.s_full[t], 1);
-      tc::mbar_init(&bars.p_full[t], kRows);
+      tc::mbar_init(&bars.p_full[t], kWarpArrivals);
     }
     for (int b = 0; b < NB; ++b) {
       tc::mbar_init(&bars.full[b], kLoaders);
@@ -248,6 +453,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   const uint32_t tmem = bars.tmem;
   volatile int* failed = &bars.failed;
 
+  // Counters run on from item to item: ring steps, steps of each tile, items with keys.
   if (warp >= kLoadWarp) {
     regs_down<kOtherRegs>();
     if (warp < kMmaWarp) {
@@ -256,76 +462,77 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const int lt = tid - 32 * kLoadWarp, piece = lt % PIECES, row0 = lt / PIECES;
       const bool col_on = piece * 8 < c.width;
       const uint32_t at = piece_at(row0, piece);
-      for (int x = row0; x < 2 * kRows; x += ROWS) {
-        const bool on = x < n && col_on;
-        const int tok = on ? a.group.div(x0 + x) : 0, g = on ? x0 + x - tok * G : 0;
-        copy16(q_tile(x / kRows) + piece_at(x % kRows, piece),
-               (const T*)a.q.p + (int64_t)(q0 + tok) * a.q.tok + (int64_t)(h * G + g) * a.q.head + (on ? piece * 8 : 0), on);
-      }
-      copy_commit();
-      const int32_t* table = p.table + r * p.table_stride;
-      const char* src_k = (const char*)c.k + 2 * (c.ks[2] * h + (col_on ? piece * 8 : 0));
-      const char* src_v = (const char*)c.v + 2 * (c.vs[2] * h + (col_on ? piece * 8 : 0));
-      int id = -1, off = 0, next = -1;  // next: the listed page of the key after
-      auto listed = [&](int j) {
-        const int u = u0 + j * kChunkKeys + lt;
-        next = SEL && u < u1 ? __ldg(a.plan.pages + list_at + c.page.div(u)) : -1;
-      };
-      auto find = [&](int j) {  // page and slot of this thread's key of step j
-        const int u = u0 + j * kChunkKeys + lt;
-        id = -1;
-        if (u < u1) {
-          int i = c.page.div(u);
-          off = u - i * c.page.d;
-          if (SEL) i = next;
-          if (i < p.width && (!SEL || i * c.page.d + off <= last)) id = __ldg(table + i);
+      int ring = 0, count = 0;
+      bool ok = true;  // where a wait gave up the loops go on without copies: their warps meet at barriers
+      each_item<SEL>(a, [&](const Item& it) {
+        if (it.steps == 0) return;
+        const int32_t* table = p.table + it.r * p.table_stride;
+        const char* src_k = (const char*)c.k + 2 * (c.ks[2] * it.h + (col_on ? piece * 8 : 0));
+        const char* src_v = (const char*)c.v + 2 * (c.vs[2] * it.h + (col_on ? piece * 8 : 0));
+        int id = -1, off = 0, next = -1;  // next: the listed page of the key after
+        auto listed = [&](int j) {
+          const int u = it.u0 + j * kChunkKeys + lt;
+          next = SEL && u < it.u1 ? __ldg(a.plan.pages + it.list + c.page.div(u)) : -1;
+        };
+        auto find = [&](int j) {  // page and slot of this thread's key of step j
+          const int u = it.u0 + j * kChunkKeys + lt;
+          id = -1;
+          if (u < it.u1) {
+            int i = c.page.div(u);
+            off = u - i * c.page.d;
+            if (SEL) i = next;
+            if (i < p.width && (!SEL || i * c.page.d + off <= it.last)) id = __ldg(table + i);
+          }
+          if (SEL) listed(j + 1);
+        };
+        if (SEL) listed(0);
+        find(0);
+        for (int x = lt; x < it.tiles * kRows; x += kLoaders) {
+          const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
+          bars.row_q[x] = x < it.n ? 2 * ((it.q0 + tok) * a.q.tok + (it.h * G + g) * a.q.head) : -1;
         }
-        if (SEL) listed(j + 1);
-      };
-      if (SEL) listed(0);
-      find(0);
-      // ring step i: K of keys i / 2 (i even) or V; its copies are waited for `lag` steps later
-      const int total = 2 * steps;
-      constexpr int LAG = lag<W>();
-      bool ok = true;  // where a wait gave up the loop goes on without copies: its warps meet at a barrier
-      for (int i = 0; i < total + LAG; ++i) {
-        // hand over what has landed before waiting for room: the copies of step i - 1 stay in flight
-        if (ok && i >= LAG - 1) {
-          copy_wait<LAG - 1>();
-          tc::fence_proxy_async_smem();
-          tc::mbar_arrive(i == LAG - 1 ? &bars.q_full : &bars.full[(i - LAG) % NB]);
-        }
-        if (i < total) {
-          const int j = i >> 1, b = i % NB;
-          if (!(i & 1)) {
+        meet(1, kLoaders);
+        ok = ok && wait_warp(&bars.q_empty, (count & 1) ^ 1, failed, limit);
+        constexpr int BATCH = kChunkKeys / ROWS / 2;  // offsets are read ahead of the copies that wait for them
+        auto copy_rows = [&](uint32_t dst, const char* src, const int64_t* rows) {
+#pragma unroll
+          for (int k0 = 0; k0 < 2 * BATCH; k0 += BATCH) {
+            int64_t o[BATCH];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) o[k] = rows[row0 + (k0 + k) * ROWS];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+              const bool on = col_on && o[k] >= 0;
+              copy16(dst + at + (k0 + k) * ROWS * 128, src + (on ? o[k] : 0), on);
+            }
+          }
+        };
+        if (ok)
+          for (int t = 0; t < it.tiles; ++t)
+            copy_rows(q_tile(t), (const char*)a.q.p + (col_on ? piece * 16 : 0), bars.row_q + t * kRows);
+        if (ok) copy_arrive(&bars.q_full);
+        const int total = 2 * it.steps;
+        for (int i = 0; i < total; ++i) {
+          const bool value = i & 1;  // K0 V0 K1 V1 ...
+          const int j = i >> 1, b = (ring + i) % NB;
+          if (!value) {
             const bool on = (unsigned)id < (unsigned)c.npages;
             bars.row_k[j & 1][lt] = on ? 2 * (id * c.ks[0] + off * c.ks[1]) : -1;
             bars.row_v[j & 1][lt] = on ? 2 * (id * c.vs[0] + off * c.vs[1]) : -1;
             find(j + 1);
-            asm volatile("bar.sync 1, 128;" ::: "memory");
+            meet(1, kLoaders);
           }
-          ok = ok && wait_warp(&bars.empty[b], ((i / NB) & 1) ^ 1, failed, limit);
-          const uint32_t dst = buffer(b) + at;
-          const char* src = (i & 1) ? src_v : src_k;
-          const int64_t* rows = ((i & 1) ? bars.row_v[j & 1] : bars.row_k[j & 1]) + row0;
+          ok = ok && wait_warp(&bars.empty[b], (((ring + i) / NB) & 1) ^ 1, failed, limit);
           if (ok) {
-            constexpr int HALF = kChunkKeys / ROWS / 2;  // offsets are read ahead of the copies that wait for them
-#pragma unroll
-            for (int k0 = 0; k0 < 2 * HALF; k0 += HALF) {
-              int64_t o[HALF];
-#pragma unroll
-              for (int k = 0; k < HALF; ++k) o[k] = rows[(k0 + k) * ROWS];
-#pragma unroll
-              for (int k = 0; k < HALF; ++k) {
-                const bool on = col_on && o[k] >= 0;
-                copy16(dst + (k0 + k) * ROWS * 128, src + (on ? o[k] : 0), on);
-              }
-            }
+            copy_rows(buffer(b), value ? src_v : src_k, value ? bars.row_v[j & 1] : bars.row_k[j & 1]);
+            copy_arrive(&bars.full[b]);
           }
         }
-        copy_commit();
-      }
-      copy_wait<0>();
+        meet(1, kLoaders);  // the offsets are read before the next item's are written
+        ring += total;
+        ++count;
+      });
+      asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp == kMmaWarp) {
       // ---- products ----
       const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
@@ -337,89 +544,156 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const uint64_t q_desc = tc::desc_k_sw128(q_tile(0)), k_desc = tc::desc_k_sw128(buffer(0));
       const uint64_t v_desc = tc::desc_mn_sw128(buffer(0), kBlock);
       constexpr uint64_t TILE = tile_bytes<W>() >> 4;
-      auto scores = [&](int t, int b) {
-        const uint64_t qd = q_desc + t * TILE, kd = k_desc + b * TILE;
-        if (tc::elect_one()) {
+      // S of tile t from query tile q and the K in buffer b
+      auto scores = [&](int t, int q, int b) {
+        const uint64_t qd = q_desc + q * TILE, kd = k_desc + b * TILE;
 #pragma unroll
-          for (int k = 0; k < W / 16; ++k) {
-            const uint64_t at = ((k >> 2) * kBlock + (k & 3) * 32) >> 4;
-            if (k < ksteps) tc::mma_f16(tmem + kColS + t * 128, qd + at, kd + at, id_s, k > 0);
-          }
-          tc::mma_commit(&bars.s_full[t]);
+        for (int k = 0; k < W / 16; ++k) {
+          const uint64_t at = ((k >> 2) * kBlock + (k & 3) * 32) >> 4;
+          if (k < ksteps) tc::mma_f16(tmem + kColS + t * 128, qd + at, kd + at, id_s, k > 0);
         }
+        tc::mma_commit(&bars.s_full[t]);
       };
+      // O of tile t (+)= P V of buffer b
       auto output = [&](int t, int b, bool first) {
         const uint64_t vd = v_desc + b * TILE;
         const uint32_t o = tmem + kColO + t * 128, w = tmem + kColS + t * 128;
-        if (tc::elect_one()) {
 #pragma unroll
-          for (int k = 0; k < kChunkKeys / 16; ++k)
-            tc::mma_f16_ta(o, w + 8 * k, vd + k * (2048 >> 4), id_o, !first || k > 0);
-        }
+        for (int k = 0; k < kChunkKeys / 16; ++k)
+          tc::mma_f16_ta(o, w + 8 * k, vd + k * (2048 >> 4), id_o, !first || k > 0);
       };
-      auto release = [&](int b) {
-        if (tc::elect_one()) tc::mma_commit(&bars.empty[b]);
-      };
-      bool ok = steps > 0 && wait_warp(&bars.q_full, 0, failed, limit) && wait_warp(&bars.full[0], 0, failed, limit);
-      if (ok) {
+      int ring = 0, count = 0, done[2] = {0, 0};
+      bool ok = true;
+      auto landed = [&](int i) { return wait_warp(&bars.full[i % NB], (i / NB) & 1, failed, limit); };
+      each_item<SEL>(a, [&](const Item& it) {
+        if (it.steps == 0 || !ok) return;
+        // The queue of issued products is short: what lies between one tile's and
+        // the next one's is kept to a wait, so that it does not run dry.
+        ok = wait_warp(&bars.q_full, count & 1, failed, limit) && landed(ring);
+        if (!ok) return;
+        tc::fence_proxy_async_smem();
         tc::tc_fence_after_sync();
-        for (int t = 0; t < tiles; ++t) scores(t, 0);
-        release(0);
-      }
-      for (int j = 0; ok && j < steps; ++j) {
-        const int iv = 2 * j + 1, ik = 2 * j + 2;  // ring steps of V and of the next K
-        ok = wait_warp(&bars.full[iv % NB], (iv / NB) & 1, failed, limit);
-        if (ok && j + 1 < steps) ok = wait_warp(&bars.full[ik % NB], (ik / NB) & 1, failed, limit);
-        for (int t = 0; ok && t < tiles; ++t) {
-          ok = wait_warp(&bars.p_full[t], j & 1, failed, limit);
-          if (!ok) break;
-          tc::tc_fence_after_sync();
-          output(t, iv % NB, j == 0);
-          if (t == tiles - 1) release(iv % NB);
-          if (j + 1 < steps) {
-            scores(t, ik % NB);
-            if (t == tiles - 1) release(ik % NB);
+        if (it.tiles == 2) {  // two tiles take every step each
+          if (tc::elect_one()) {
+            scores(0, 0, ring % NB);
+            scores(1, 1, ring % NB);
+            tc::mma_commit(&bars.empty[ring % NB]);
+            if (it.steps == 1) tc::mma_commit(&bars.q_empty);
           }
+          for (int j = 0; ok && j < it.steps; ++j) {
+            const int iv = ring + 2 * j + 1, ik = iv + 1, bv = iv % NB, bk = ik % NB;
+            const bool more = j + 1 < it.steps;
+            ok = landed(iv) && (!more || landed(ik));
+            tc::fence_proxy_async_smem();
+            ok = ok && wait_warp(&bars.p_full[0], (done[0] + j) & 1, failed, limit);
+            if (!ok) break;
+            tc::tc_fence_after_sync();
+            if (tc::elect_one()) {
+              output(0, bv, j == 0);
+              if (more) scores(0, 0, bk);
+            }
+            ok = wait_warp(&bars.p_full[1], (done[1] + j) & 1, failed, limit);
+            if (!ok) break;
+            tc::tc_fence_after_sync();
+            if (tc::elect_one()) {
+              output(1, bv, j == 0);
+              tc::mma_commit(&bars.empty[bv]);
+              if (more) {
+                scores(1, 1, bk);
+                tc::mma_commit(&bars.empty[bk]);
+                if (j + 2 == it.steps) tc::mma_commit(&bars.q_empty);
+              }
+            }
+          }
+          done[0] += it.steps;
+          done[1] += it.steps;
+        } else {  // one tile takes the even steps on the first's S and O and the odd ones on the second's: its weights
+                  // and its products overlap too
+          if (tc::elect_one()) {
+            scores(0, 0, ring % NB);
+            tc::mma_commit(&bars.empty[ring % NB]);
+            if (it.steps == 1) tc::mma_commit(&bars.q_empty);
+          }
+          if (it.steps > 1) {
+            const int bk = (ring + 2) % NB;
+            ok = landed(ring + 2);
+            if (ok) {
+              tc::fence_proxy_async_smem();
+              tc::tc_fence_after_sync();
+              if (tc::elect_one()) {
+                scores(1, 0, bk);
+                tc::mma_commit(&bars.empty[bk]);
+                if (it.steps == 2) tc::mma_commit(&bars.q_empty);
+              }
+            }
+          }
+          for (int j = 0; ok && j < it.steps; ++j) {
+            const int t = j & 1, iv = ring + 2 * j + 1, ik = iv + 3, bv = iv % NB, bk = ik % NB;
+            const bool more = j + 2 < it.steps;
+            ok = landed(iv) && (!more || landed(ik));
+            tc::fence_proxy_async_smem();
+            ok = ok && wait_warp(&bars.p_full[t], (done[t] + j / 2) & 1, failed, limit);
+            if (!ok) break;
+            tc::tc_fence_after_sync();
+            if (tc::elect_one()) {
+              output(t, bv, j < 2);
+              tc::mma_commit(&bars.empty[bv]);
+              if (more) {
+                scores(t, 0, bk);
+                tc::mma_commit(&bars.empty[bk]);
+                if (j + 3 == it.steps) tc::mma_commit(&bars.q_empty);
+              }
+            }
+          }
+          done[0] += (it.steps + 1) / 2;
+          done[1] += it.steps / 2;
         }
-      }
-      if (ok && tc::elect_one()) tc::mma_commit(&bars.o_full);
+        if (ok && tc::elect_one()) tc::mma_commit(&bars.o_full);
+        ring += 2 * it.steps;
+        ++count;
+      });
     }
   } else {
     regs_up<kSoftRegs>();
-    if ((warp >> 2) < tiles) {
-      // ---- softmax: thread = row ----
-      const int t = warp >> 2, x = t * kRows + (warp & 3) * 32 + lane;
-      const bool row_on = x < n;
-      const int tok = row_on ? a.group.div(x0 + x) : 0, g = row_on ? x0 + x - tok * G : 0;
-      const int pos = row_on ? shift + tok : -1;
-      const int pos_min = shift + a.group.div(x0 + t * kRows);  // of the tile's rows
-      const bool tail = n - t * kRows < kRows;                  // rows that are none: their scores are dropped
-      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-      const uint32_t col_s = tmem + lanes + kColS + t * 128, col_o = tmem + lanes + kColO + t * 128;
-      // scores are kept raw and take their factor inside the exponential; one that is not positive goes to them first
-      const bool raw = a.scale > 0.f;
-      const float factor = a.scale * 1.4426950408889634f, sl2 = raw ? factor : 1.f;
+    // ---- softmax: thread = row ----
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t col_s = tmem + lanes + kColS + t * 128, col_o = tmem + lanes + kColO + t * 128;
+    // scores are kept raw and take their factor inside the exponential; one that is not positive goes to them first
+    const bool raw = a.scale > 0.f;
+    const float factor = a.scale * 1.4426950408889634f, sl2 = raw ? factor : 1.f;
+    int done = 0, count = 0;
+    bool ok = true;  // where a wait gave up the items go on without work: the two warpgroups meet at barriers
+    each_item<SEL>(a, [&](const Item& it) {
+      const bool pair = it.tiles == 1;  // this warpgroup's steps are every second one of the same rows
+      const int x = pair ? row : t * kRows + row;
+      const bool row_on = x < it.n;
+      const int tok = row_on ? a.group.div(it.x0 + x) : 0, g = row_on ? it.x0 + x - tok * G : 0;
+      const int pos = row_on ? it.shift + tok : -1;
+      const int pos_min = it.shift + a.group.div(it.x0 + x - row);  // of the tile's rows
+      const bool tail = it.n - (x - row) < kRows;                   // rows that are none: their scores are dropped
       float m = -INFINITY, l = 0.f;  // maximum of the scores that weights are taken against, sum of weights
-      bool ok = true;
       // selected: the row's token in the tile, its page's bit and last slot seen in a listed page
-      const int tl = tok - a.group.div(x0), segs = SEL ? (c.page.d < kChunkKeys ? kChunkKeys / c.page.d : 1) : 0;
-      const uint32_t* pickers = a.plan.pickers + list_at * a.plan.words + (row_on ? tl >> 5 : 0);
-      for (int j = 0; j < steps; ++j) {
+      const int tl = tok - a.group.div(it.x0), segs = SEL ? (c.page.d < kChunkKeys ? kChunkKeys / c.page.d : 1) : 0;
+      const uint32_t* pickers = a.plan.pickers + it.list * a.plan.words + (row_on ? tl >> 5 : 0);
+      const int stride = pair ? 2 : 1, first = pair ? t : 0;
+      for (int j = first; ok && j < it.steps; j += stride) {
         int seen_in[8];  // per segment of the step: keys 0 .. seen_in of it
         if (SEL) {
 #pragma unroll
           for (int g2 = 0; g2 < 8; ++g2) {
             seen_in[g2] = -1;
-            const int u = u0 + j * kChunkKeys + g2 * c.page.d;
-            if (g2 < segs && u < u1 && row_on) {
+            const int u = it.u0 + j * kChunkKeys + g2 * c.page.d;
+            if (g2 < segs && u < it.u1 && row_on) {
               const int e = c.page.div(u);
-              const int pg = __ldg(a.plan.pages + list_at + e);
+              const int pg = __ldg(a.plan.pages + it.list + e);
               const bool on = (__ldg(pickers + (int64_t)e * a.plan.words) >> (tl & 31)) & 1;
               if (on) seen_in[g2] = pos - pg * c.page.d - (u - e * c.page.d);
             }
           }
         }
-        ok = wait_warp(&bars.s_full[t], j & 1, failed, limit);
+        ok = wait_warp(&bars.s_full[t], done & 1, failed, limit);
+        ++done;
         if (!ok) break;
         tc::tc_fence_after_sync();
         uint32_t s[128];
@@ -431,7 +705,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
 #pragma unroll
           for (int k = 0; k < 128; ++k) s[k] = __float_as_uint(__uint_as_float(s[k]) * factor);
         }
-        const int key0 = u0 + j * kChunkKeys;
+        const int key0 = it.u0 + j * kChunkKeys;
         if (SEL) {
           mask_segments(s, seen_in, segs);
         } else if (tail || key0 + kChunkKeys - 1 > pos_min) {
@@ -454,7 +728,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
             l *= f;
             m = top;
           }
-          if (j > 0) {
+          if (j > first) {
 #pragma unroll
             for (int k = 0; k < W / 16; ++k) {
               float o[16];
@@ -481,52 +755,48 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           }
           tc::tmem_st16(col_s + 16 * k, w);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         tc::tmem_st_done();
         tc::tc_fence_before_sync();
-        tc::mbar_arrive(&bars.p_full[t]);
+        arrive_warp(&bars.p_full[t]);
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
-      if (ok && steps > 0) ok = wait_warp(&bars.o_full, 0, failed, limit);
-      if (ok) {
-        tc::tc_fence_after_sync();
-        const int64_t at = (q0 + tok) * ((int64_t)c.nheads * G) + h * G + g;
-        const int64_t slot = at * a.plan.nsplit + blockIdx.z;
-        const float inv = __fdividef(1.f, l);
-        const float lse2 = l == 0.f ? -INFINITY : m * sl2 + __log2f(l);
+      const bool keys = it.steps > 0;
+      if (ok && keys) ok = wait_warp(&bars.o_full, count & 1, failed, limit);
+      count += keys;
+      tc::tc_fence_after_sync();
+      m = m == -INFINITY ? m : m * sl2;  // in powers of two from here on
+      float f_other = 0.f;
+      const bool mine = it.steps > first;  // this warpgroup's O holds something
+      if (pair) {
+        if (t == 1) bars.other_ml[row] = make_float2(m, l);
+        meet(2, 2 * kRows);
+        if (t == 0) {
+          const float2 ml = bars.other_ml[row];
+          const float top = fmaxf(m, ml.x), b = top == -INFINITY ? 0.f : top;
+          const float f = exp2_fast(m - b);
+          f_other = exp2_fast(ml.x - b);
+          l = l * f + ml.y * f_other;
+          f_other = l == 0.f ? 0.f : f_other * __fdividef(1.f, l);
+          m = top;
+          const float inv = l == 0.f ? 0.f : f * __fdividef(1.f, l);
+          write_rows<T, W>(a, it, bars, col_o, warp, lane, ok, mine, inv, f_other, m, l);
+        } else {
+          float(&other)[16][kRows] = other_rows(bars);
+          for (int col0 = 0; col0 < W; col0 += 16) {
+            float o[16];
 #pragma unroll
-        for (int k = 0; k < W / 32; ++k) {
-          float o[32];
+            for (int e = 0; e < 16; ++e) o[e] = 0.f;
+            if (ok && mine) tc::tmem_ld16(col_o + col0, o);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
-          if (steps > 0) tc::tmem_ld32(col_o + 32 * k, o);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0.f : o[e] * inv;  // no key: zeros
-          if (!row_on) continue;
-          if (splits == 1) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (32 * k + 8 * e < c.width) {
-                uint4 y;
-                y.x = Half2<T>::pack(o[8 * e], o[8 * e + 1]);
-                y.y = Half2<T>::pack(o[8 * e + 2], o[8 * e + 3]);
-                y.z = Half2<T>::pack(o[8 * e + 4], o[8 * e + 5]);
-                y.w = Half2<T>::pack(o[8 * e + 6], o[8 * e + 7]);
-                *reinterpret_cast<uint4*>((T*)a.out + at * c.width + 32 * k + 8 * e) = y;
-              }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (32 * k + 4 * e < c.width)
-                *reinterpret_cast<float4*>(a.plan.part + slot * c.width + 32 * k + 4 * e) =
-                    make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            for (int e = 0; e < 16; ++e) other[e][row] = o[e];
+            meet(2, 2 * kRows);
+            meet(2, 2 * kRows);
           }
         }
-        if (row_on) {
-          if (splits != 1) a.plan.part_lse[slot] = lse2;
-          else if (a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
-        }
+      } else {
+        write_rows<T, W>(a, it, bars, col_o, warp, lane, ok, mine, l == 0.f ? 0.f : __fdividef(1.f, l), 0.f, m, l);
       }
-    }
+    });
   }
 
   __syncwarp();
@@ -546,6 +816,60 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   if (warp == kMmaWarp) tc::tmem_dealloc(tmem, kTmemCols);
 }
 
+// Items that cuts went through: o = sum 2^(lse - m) o_part / sum 2^(lse - m) over
+// their parts, in the keys' order.  Block x: the item that share x + 1 begins
+// inside of, if no share before does; block y: 4 of its rows, one a warp.
+constexpr int kJoinRows = 4;
+
+template <typename T, bool SEL>
+__global__ void __launch_bounds__(128)
+k_paged_join(AttnArgs a) {
+  const int n = __ldg(a.plan.shares + kChunkBlocks).x, ntiles = __ldg(a.plan.shares + kChunkBlocks + 1).x;
+  const int c0 = blockIdx.x + 1;
+  if (c0 >= n) return;
+  const int2 cut = __ldg(a.plan.shares + c0), before = __ldg(a.plan.shares + c0 - 1);
+  if (cut.y == 0 || (before.x == cut.x && before.y > 0)) return;
+  int c1 = c0 + 1;  // shares c0 .. c1 - 1 begin inside of the item
+  while (c1 < n && __ldg(a.plan.shares + c1).x == cut.x) ++c1;
+  const Item it = item_of<SEL>(a, cut.x, ntiles, 0, -1);
+  const int lane = threadIdx.x & 31, G = a.group.d, col = 4 * lane;
+  for (int x = blockIdx.y * kJoinRows + (threadIdx.x >> 5); x < min(it.n, ((int)blockIdx.y + 1) * kJoinRows); x += 4) {
+    // the part that begins the item, then one a share
+    auto part = [&](int k) { return (int64_t)(2 * (c0 - 1 + k) + (k == 0)) * kChunkRows + x; };
+    const int parts = c1 - c0 + 1;
+    float m = -INFINITY;
+    for (int k = lane; k < parts; k += 32) m = fmaxf(m, a.plan.part_lse[part(k)]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float b = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) {
+      const int64_t at = part(k);
+      const float f = exp2_fast(a.plan.part_lse[at] - b);
+      sum += f;
+      if (col < a.c.width) {
+        const float4 y = *reinterpret_cast<const float4*>(a.plan.part + at * a.c.width + col);
+        acc.x += f * y.x;
+        acc.y += f * y.y;
+        acc.z += f * y.z;
+        acc.w += f * y.w;
+      }
+    }
+    const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);  // the parts of a row without keys are zeros
+    const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
+    const int64_t at = (it.q0 + tok) * ((int64_t)a.c.nheads * G) + it.h * G + g;
+    if (col < a.c.width) {
+      uint2 y;
+      y.x = Half2<T>::pack(acc.x * inv, acc.y * inv);
+      y.y = Half2<T>::pack(acc.z * inv, acc.w * inv);
+      *reinterpret_cast<uint2*>((T*)a.out + at * a.c.width + col) = y;
+    }
+    if (lane == 0 && a.lse) a.lse[at] = (m + __log2f(sum)) * 0.6931471805599453f;
+  }
+}
+
 template <typename T, int W, bool SEL>
 cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
   auto kernel = k_paged_chunk<T, W, SEL>;
@@ -553,8 +877,7 @@ cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
   cudaError_t e = once(
       [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<W>()); });
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)a.c.nheads, (unsigned)a.plan.ntiles, (unsigned)a.plan.nsplit);
-  kernel<<<(SLNR_COUNTED(grid)), kThreads, smem_bytes<W>(), s>>>(a, hdr, wait_limit_cycles());
+  kernel<<<SLNR_COUNTED(kChunkBlocks), kThreads, smem_bytes<W>(), s>>>(a, hdr, wait_limit_cycles());
   return cudaGetLastError();
 }
 
@@ -565,15 +888,28 @@ cudaError_t launch_w(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_paged_union(const AttnArgs& a, cudaStream_t s) {
-  const dim3 grid((unsigned)a.c.nheads, (unsigned)a.plan.ntiles);
-  k_paged_union<<<(SLNR_COUNTED(grid)), kUnionThreads, 0, s>>>(a);
+cudaError_t launch_paged_plan(const AttnArgs& a, cudaStream_t s) {
+  if (a.picked) {
+    const dim3 grid((unsigned)a.c.nheads, (unsigned)a.plan.ntiles);
+    k_paged_union<<<(SLNR_COUNTED(grid)), kUnionThreads, 0, s>>>(a);
+    k_paged_plan<true><<<SLNR_COUNTED(1), kPlanThreads, 0, s>>>(a);
+  } else {
+    k_paged_plan<false><<<SLNR_COUNTED(1), kPlanThreads, 0, s>>>(a);
+  }
   return cudaGetLastError();
 }
 
 cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s) {
   if (a.picked) return dtype == SLNR_FP16 ? launch_w<__half, true>(a, hdr, s) : launch_w<__nv_bfloat16, true>(a, hdr, s);
   return dtype == SLNR_FP16 ? launch_w<__half, false>(a, hdr, s) : launch_w<__nv_bfloat16, false>(a, hdr, s);
+}
+
+cudaError_t launch_paged_join(const AttnArgs& a, int dtype, cudaStream_t s) {
+  const dim3 grid(kChunkBlocks - 1, kChunkRows / kJoinRows);
+  auto kernel = dtype == SLNR_FP16 ? (a.picked ? k_paged_join<__half, true> : k_paged_join<__half, false>)
+                                   : (a.picked ? k_paged_join<__nv_bfloat16, true> : k_paged_join<__nv_bfloat16, false>);
+  kernel<<<(SLNR_COUNTED(grid)), 128, 0, s>>>(a);
+  return cudaGetLastError();
 }
 
 }  // namespace slnr

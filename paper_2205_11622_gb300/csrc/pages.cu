@@ -193,7 +193,7 @@ k_page_append(PagesView p, CacheView c, RowsView kn, RowsView vn, int sum_blocks
       for (int d = 0; d < DEEP; ++d)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          T y[2];
+          alignas(4) T y[2];
           *reinterpret_cast<uint32_t*>(y) = x[d][e];
           sum[e].x += to_float(y[0]);
           sum[e].y += to_float(y[1]);
