@@ -53,8 +53,8 @@ struct AttnPlan {
   int chunk;    // keys of one split, a multiple of the kernel's step
   int nsplit;   // splits of the longest request (1: the block writes the result)
   bool cluster; // the splits of a row are joined by the blocks of a cluster (row kernel, nsplit in 2 .. 16)
-  // the tensor-core kernel's items (paged_chunk.cu): row tiles, steps (by their cost)
-  // before each item, the item and step that each block's share begins at
+  // the tensor-core kernel's items (paged_chunk.cu): row tiles, cost of the items
+  // before each, the item and step that each block's share begins at
   int4* tiles;      // [ntiles][2]
   int64_t* before;  // [ntiles * nheads]
   int2* shares;     // [kChunkBlocks], then {blocks with a share, items}, {row tiles, 0}
@@ -73,7 +73,7 @@ constexpr int kAttnKeys = 64;       // keys of one step of the row kernel
 constexpr int kChunkKeys = 128;     // and of the tensor-core kernel, whose blocks take
 constexpr int kChunkRows = 256;     // that many rows; one block on each of 152 SMs,
 constexpr int kChunkBlocks = 152;   // with a share of
-constexpr int kLeastSteps = 4;      // that much of the steps' cost or more
+constexpr int kLeastCost = 8;       // that much of their cost or more
 constexpr int kAttnMaxPicked = 1024;  // pages picked for one row
 
 struct AttnArgs {

@@ -211,8 +211,11 @@ struct Item {
   int64_t list;                // of the listed pages
 };
 
-// Cost of a step of an item of n rows: one tile takes half as long as two.
+// Cost of a step of an item of n rows: one tile takes half as long as two.  Of an
+// item itself (its queries, the last product, its rows out): 10k cycles, where a
+// step of two tiles takes 3k.
 __device__ __forceinline__ int weight_of(int n) { return n > kRows ? 2 : 1; }
+constexpr int kItemCost = 6;
 __device__ __forceinline__ int steps_of(int end) { return end > 0 ? (end - 1) / kChunkKeys + 1 : 1; }
 
 // Part [lo, hi) of item i (hi = -1: to its end).
@@ -296,31 +299,31 @@ k_paged_plan(AttnArgs a) {
     __syncthreads();
   }
   ntiles = min(ntiles, a.plan.ntiles);
-  // steps before each item, by their cost
+  // cost of the items before each
   const int items = ntiles * a.c.nheads;
-  int64_t steps = 0;
+  int64_t cost = 0;
   for (int i0 = 0; i0 < items; i0 += kPlanThreads) {
     const int i = i0 + tid;
     int mine = 0, total;
     if (i < items) {
       const int h = i / ntiles, tile = i - h * ntiles;
-      mine = weight_of(a.plan.tiles[2 * tile].w) *
+      mine = kItemCost + weight_of(a.plan.tiles[2 * tile].w) *
              steps_of(SEL ? a.plan.npages[(int64_t)h * a.plan.ntiles + tile] * a.c.page.d
                           : max(a.plan.tiles[2 * tile + 1].y + 1, 0));
     }
     const int sum = block_sum(mine, total, s_warp);
-    if (i < items) a.plan.before[i] = steps + sum - mine;
-    steps += total;
+    if (i < items) a.plan.before[i] = cost + sum - mine;
+    cost += total;
   }
   __syncthreads();
-  const int64_t most = steps / kLeastSteps > 1 ? steps / kLeastSteps : 1;
+  const int64_t most = cost / kLeastCost > 1 ? cost / kLeastCost : 1;
   const int n = (int)(most < kChunkBlocks ? most : kChunkBlocks);  // blocks with a share
-  // share c begins at step c steps / n
+  // share c begins at cost c cost / n
   for (int i = tid; i < items; i += kPlanThreads) {
-    const int64_t lo = a.plan.before[i], hi = i + 1 < items ? a.plan.before[i + 1] : steps;
+    const int64_t lo = a.plan.before[i], hi = i + 1 < items ? a.plan.before[i + 1] : cost;
     const int w = weight_of(a.plan.tiles[2 * (i % ntiles)].w);
-    for (int64_t c = (lo * n + steps - 1) / steps; c < n && c * steps / n < hi; ++c)
-      a.plan.shares[c] = make_int2(i, (int)(c * steps / n - lo) / w);
+    for (int64_t c = (lo * n + cost - 1) / cost; c < n && c * cost / n < hi; ++c)
+      a.plan.shares[c] = make_int2(i, max((int)(c * cost / n - lo) - kItemCost, 0) / w);
   }
   if (tid == 0) {
     a.plan.shares[kChunkBlocks] = make_int2(items > 0 ? n : 0, items);
@@ -334,71 +337,90 @@ __device__ __forceinline__ float (&other_rows(Shared& sh))[16][kRows] {
   return *reinterpret_cast<float(*)[16][kRows]>(&sh.stage[kLoadWarp / 2]);
 }
 
-// The rows of a warp out of tensor memory, times inv (0: no key), with f_other
-// times the other warpgroup's where an item has one tile: 16 columns at a time
-// a thread a row, and through shared memory to whole 32-byte sectors a few lanes
-// a row.  m: maximum in powers of two, l: sum.
+// A row of O out of tensor memory (zeros where !on).
+template <int W>
+__device__ __forceinline__ void read_row(uint32_t col_o, bool on, uint32_t (&o)[W]) {
+  if (on) {
+#pragma unroll
+    for (int k = 0; k < W / 32; ++k) tc::tmem_ld32_start(col_o + 32 * k, o + 32 * k);
+#pragma unroll
+    for (int k = 0; k < W / 32; ++k) tc::tmem_ld_done(o + 32 * k);
+  } else {
+#pragma unroll
+    for (int k = 0; k < W; ++k) o[k] = 0;
+  }
+}
+
+// The rows of a warp, times inv (0: no key), with f_other times the other
+// warpgroup's where an item has one tile: a thread a row, and through shared
+// memory, 16 columns at a time, to whole 32-byte sectors a few lanes a row.
+// m: maximum in powers of two, l: sum.
 template <typename T, int W>
-__device__ __forceinline__ void write_rows(const AttnArgs& a, const Item& it, Shared& sh, uint32_t col_o, int warp,
-                                           int lane, bool ok, bool mine, float inv, float f_other, float m, float l) {
-  const bool pair = it.tiles == 1;
+__device__ __forceinline__ void write_rows(const AttnArgs& a, const Item& it, Shared& sh, uint32_t (&o)[W], int warp,
+                                           int lane, bool ok, float inv, float f_other, float m, float l) {
+  const bool pair = it.tiles == 1, whole = it.slot < 0;
   const int G = a.group.d, x0 = (pair ? 0 : (warp >> 2) * kRows) + (warp & 3) * 32;  // the warp's first row
   const int row = (warp & 3) * 32 + lane;
   const int64_t hq = (int64_t)a.c.nheads * G;
-  auto place = [&](int x) {  // of the item's row x in out and lse, or in the parts
-    if (it.slot >= 0) return (int64_t)it.slot * kChunkRows + x;
+  auto place = [&](int x) {  // of the item's row x in out and lse, or in the parts; -1: none
+    if (!ok || x >= it.n) return (int64_t)-1;
+    if (!whole) return (int64_t)it.slot * kChunkRows + x;
     const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
     return (it.q0 + tok) * hq + it.h * G + g;
   };
+  // whole items: 2 lanes a row, 8 columns each; parts: 4 lanes a row, 4 columns each
+  const int per = whole ? 2 : 4, q0 = lane / per, col = lane % per * (whole ? 8 : 4);
+  char* to[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t at = i < per ? place(x0 + q0 + i * (32 / per)) : -1;
+    to[i] = at < 0 ? nullptr
+            : whole ? (char*)((T*)a.out + at * a.c.width + col) : (char*)(a.plan.part + at * a.c.width + col);
+  }
   float(&stage)[32][20] = sh.stage[warp];
-  for (int col0 = 0; col0 < W; col0 += 16) {
-    float o[16];
+  const float(&other)[16][kRows] = other_rows(sh);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) o[e] = 0.f;
-    if (ok && mine) tc::tmem_ld16(col_o + col0, o);
+  for (int k = 0; k < W; k += 16) {
+    float v[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) o[e] = inv == 0.f ? 0.f : o[e] * inv;
+    for (int e = 0; e < 16; ++e) v[e] = inv == 0.f ? 0.f : __uint_as_float(o[k + e]) * inv;
     if (pair) {
-      const float(&other)[16][kRows] = other_rows(sh);
       meet(2, 2 * kRows);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[e] = f_other == 0.f ? o[e] : fmaf(other[e][row], f_other, o[e]);
+      for (int e = 0; e < 16; ++e) v[e] = f_other == 0.f ? v[e] : fmaf(other[e][row], f_other, v[e]);
       meet(2, 2 * kRows);
     }
     __syncwarp();
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      *reinterpret_cast<float4*>(&stage[lane][4 * e]) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<float4*>(&stage[lane][e]) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
     __syncwarp();
-    if (it.slot >= 0) {  // 4 lanes a row
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int q = 8 * i + (lane >> 2), col = 4 * (lane & 3);
-        if (ok && x0 + q < it.n && col0 + col < a.c.width)
-          *reinterpret_cast<float4*>(a.plan.part + place(x0 + q) * a.c.width + col0 + col) =
-              *reinterpret_cast<const float4*>(&stage[q][col]);
-      }
-    } else {  // 2 lanes a row
+    const bool on = k + col < a.c.width;
+    if (whole) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int q = 16 * i + (lane >> 1), col = 8 * (lane & 1);
-        if (ok && x0 + q < it.n && col0 + col < a.c.width) {
-          const float4 y0 = *reinterpret_cast<const float4*>(&stage[q][col]);
-          const float4 y1 = *reinterpret_cast<const float4*>(&stage[q][col + 4]);
-          uint4 z;
-          z.x = Half2<T>::pack(y0.x, y0.y);
-          z.y = Half2<T>::pack(y0.z, y0.w);
-          z.z = Half2<T>::pack(y1.x, y1.y);
-          z.w = Half2<T>::pack(y1.z, y1.w);
-          *reinterpret_cast<uint4*>((T*)a.out + place(x0 + q) * a.c.width + col0 + col) = z;
-        }
+        const float4 y0 = *reinterpret_cast<const float4*>(&stage[q0 + 16 * i][col]);
+        const float4 y1 = *reinterpret_cast<const float4*>(&stage[q0 + 16 * i][col + 4]);
+        uint4 z;
+        z.x = Half2<T>::pack(y0.x, y0.y);
+        z.y = Half2<T>::pack(y0.z, y0.w);
+        z.z = Half2<T>::pack(y1.x, y1.y);
+        z.w = Half2<T>::pack(y1.z, y1.w);
+        if (on && to[i]) *reinterpret_cast<uint4*>((T*)to[i] + k) = z;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 y = *reinterpret_cast<const float4*>(&stage[q0 + 8 * i][col]);
+        if (on && to[i]) *reinterpret_cast<float4*>((float*)to[i] + k) = y;
       }
     }
   }
-  if (ok && x0 + lane < it.n) {
+  const int64_t at = place(x0 + lane);
+  if (at >= 0) {
     const float lse2 = l == 0.f ? -INFINITY : m + __log2f(l);
-    if (it.slot >= 0) a.plan.part_lse[place(x0 + lane)] = lse2;
-    else if (a.lse) a.lse[place(x0 + lane)] = lse2 * 0.6931471805599453f;
+    if (!whole) a.plan.part_lse[at] = lse2;
+    else if (a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
   }
 }
 
@@ -766,7 +788,8 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       tc::tc_fence_after_sync();
       m = m == -INFINITY ? m : m * sl2;  // in powers of two from here on
       float f_other = 0.f;
-      const bool mine = it.steps > first;  // this warpgroup's O holds something
+      uint32_t o[W];
+      read_row<W>(col_o, ok && it.steps > first, o);  // this warpgroup's O holds something from its first step on
       if (pair) {
         if (t == 1) bars.other_ml[row] = make_float2(m, l);
         meet(2, 2 * kRows);
@@ -779,22 +802,19 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           f_other = l == 0.f ? 0.f : f_other * __fdividef(1.f, l);
           m = top;
           const float inv = l == 0.f ? 0.f : f * __fdividef(1.f, l);
-          write_rows<T, W>(a, it, bars, col_o, warp, lane, ok, mine, inv, f_other, m, l);
+          write_rows<T, W>(a, it, bars, o, warp, lane, ok, inv, f_other, m, l);
         } else {
           float(&other)[16][kRows] = other_rows(bars);
-          for (int col0 = 0; col0 < W; col0 += 16) {
-            float o[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = 0.f;
-            if (ok && mine) tc::tmem_ld16(col_o + col0, o);
+          for (int k = 0; k < W; k += 16) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) other[e][row] = o[e];
+            for (int e = 0; e < 16; ++e) other[e][row] = __uint_as_float(o[k + e]);
             meet(2, 2 * kRows);
             meet(2, 2 * kRows);
           }
         }
       } else {
-        write_rows<T, W>(a, it, bars, col_o, warp, lane, ok, mine, l == 0.f ? 0.f : __fdividef(1.f, l), 0.f, m, l);
+        write_rows<T, W>(a, it, bars, o, warp, lane, ok, l == 0.f ? 0.f : __fdividef(1.f, l), 0.f, m, l);
       }
     });
   }
