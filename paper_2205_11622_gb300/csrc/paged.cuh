@@ -89,6 +89,29 @@ struct AttnArgs {
   AttnPlan plan;
 };
 
+// Launches that follow one another in a call: the next grid may start once every
+// block of the one before has called let_next_start (or ended), and waits in
+// wait_for_previous until that one is done and its writes can be read.
+#ifdef __CUDACC__
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t launch_next(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+#endif
+
 // Runs something once a device and keeps its first error: the attributes of a kernel.
 class OncePerDevice {
  public:
@@ -129,9 +152,9 @@ int select_tokens(int pages);
 cudaError_t launch_page_select(const PagesView& p, const CacheView& c, const RowsView& q, int dtype, int nheads_q,
                                int32_t* picked, int npicked, int first, int last, cudaStream_t s);
 
-// paged_chunk.cu (plan.tile == kChunkRows), in this order; hdr's flag word is
-// zero.  Picked pages: the page size divides 128 or is a multiple of it.
-cudaError_t launch_paged_plan(const AttnArgs& a, cudaStream_t s);
+// paged_chunk.cu (plan.tile == kChunkRows), in this order; the first zeroes hdr's
+// flag word.  Picked pages: the page size divides 128 or is a multiple of it.
+cudaError_t launch_paged_plan(const AttnArgs& a, WsHeader* hdr, cudaStream_t s);
 cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s);
 cudaError_t launch_paged_join(const AttnArgs& a, int dtype, cudaStream_t s);
 

@@ -256,8 +256,7 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   }));
   const bool tc = a.plan.tile == kChunkRows;
   if (tc) {
-    SLNR_CUDA(cudaMemsetAsync(ws, 0, sizeof(WsHeader), s));
-    SLNR_LAUNCH("paged_plan", launch_paged_plan(a, s));
+    SLNR_LAUNCH("paged_plan", launch_paged_plan(a, (WsHeader*)ws, s));
     SLNR_LAUNCH("paged_chunk", launch_paged_chunk(a, cache->dtype, (WsHeader*)ws, s));
     SLNR_LAUNCH("paged_join", launch_paged_join(a, cache->dtype, s));
   } else {

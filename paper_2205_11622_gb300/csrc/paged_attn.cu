@@ -96,6 +96,7 @@ k_paged_rows(AttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wm = warp % WM, wk = warp / WM;
   const int G = a.group.d, h = blockIdx.y, tile = 16 * WM;
 
+  if (!CLUSTER) let_next_start();  // k_paged_combine
   // the block's rows: [x0, x0 + n) of request r and head h
   int r, x0, q0, qn;
   if (SEL) {
@@ -418,6 +419,7 @@ k_paged_rows(AttnArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(128)
 k_paged_combine(AttnArgs a) {
+  wait_for_previous();
   const PagesView& p = a.p;
   const int lane = threadIdx.x & 31, G = a.group.d;
   const int64_t hq = (int64_t)a.c.nheads * G, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
@@ -525,8 +527,7 @@ cudaError_t launch_paged_combine(const AttnArgs& a, int dtype, cudaStream_t s) {
   const int64_t rows = (int64_t)a.p.ntok * a.c.nheads * a.group.d;
   const unsigned grid = (unsigned)ceil_div(rows, 4);
   auto kernel = dtype == SLNR_FP16 ? k_paged_combine<__half> : k_paged_combine<__nv_bfloat16>;
-  kernel<<<SLNR_COUNTED(grid), 128, 0, s>>>(a);
-  return cudaGetLastError();
+  return launch_next(kernel, SLNR_COUNTED(dim3(grid)), dim3(128), 0, s, a);
 }
 
 }  // namespace slnr

@@ -58,6 +58,8 @@ constexpr int buffers() { return W == 128 ? 4 : 8; }
 template <int W>
 constexpr size_t smem_bytes() { return (size_t)(2 + buffers<W>()) * tile_bytes<W>() + 1024; }
 constexpr int kWarpArrivals = 4;  // a warp arrives once for its lanes
+constexpr int kSegments = 8;      // pages of a step, at most
+constexpr int kMaxWords = 8;      // of the bits of 256 tokens of one row each
 
 struct Shared {
   uint64_t q_full, q_empty, s_full[2], p_full[2], o_full, full[8], empty[8], drained;
@@ -65,6 +67,7 @@ struct Shared {
   int failed;
   int64_t row_k[2][kChunkKeys], row_v[2][kChunkKeys];  // bytes from the head's first row to each key's; -1: zeros
   int64_t row_q[2 * kRows];                            // the same of the item's query rows
+  uint32_t listed[8][kSegments * (1 + kMaxWords)];  // selected: a step's pages, then who picked each
   float2 other_ml[kRows];          // one tile an item: the second warpgroup's maxima and sums
   alignas(16) float stage[kLoadWarp][32][20];  // 16 columns of a warp's rows on their way out
 };
@@ -138,7 +141,6 @@ __device__ __forceinline__ void regs_down() {
 // any written in order.
 constexpr int kUnionThreads = 256;
 constexpr int kUnionPages = 1024;
-constexpr int kMaxWords = 8;  // 256 tokens of one row each
 
 __global__ void __launch_bounds__(kUnionThreads)
 k_paged_union(AttnArgs a) {
@@ -146,6 +148,7 @@ k_paged_union(AttnArgs a) {
   __shared__ int s_count[kUnionThreads / 32 + 1];
   const PagesView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.x, words = a.plan.words;
+  let_next_start();
   int r, x0;
   find_tile(p, a.group.d, kChunkRows, blockIdx.y, r, x0);
   const int64_t at = (int64_t)h * gridDim.y + blockIdx.y;
@@ -272,10 +275,13 @@ __device__ __forceinline__ int block_sum(int x, int& total, int* s_warp) {
 
 template <bool SEL>
 __global__ void __launch_bounds__(kPlanThreads)
-k_paged_plan(AttnArgs a) {
+k_paged_plan(AttnArgs a, WsHeader* hdr) {
   __shared__ int s_first[kPlanThreads], s_warp[32];
   const PagesView& p = a.p;
   const int tid = threadIdx.x, G = a.group.d;
+  let_next_start();
+  wait_for_previous();
+  if (tid == 0) hdr->error = 0;
   int ntiles = 0;
   for (int r0 = 0; r0 < p.nreq; r0 += kPlanThreads) {
     const int r = r0 + tid;
@@ -474,6 +480,8 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   tc::tc_fence_after_sync();
   const uint32_t tmem = bars.tmem;
   volatile int* failed = &bars.failed;
+  let_next_start();
+  wait_for_previous();
 
   // Counters run on from item to item: ring steps, steps of each tile, items with keys.
   if (warp >= kLoadWarp) {
@@ -491,6 +499,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         const int32_t* table = p.table + it.r * p.table_stride;
         const char* src_k = (const char*)c.k + 2 * (c.ks[2] * it.h + (col_on ? piece * 8 : 0));
         const char* src_v = (const char*)c.v + 2 * (c.vs[2] * it.h + (col_on ? piece * 8 : 0));
+        const int segs = SEL ? (c.page.d < kChunkKeys ? kChunkKeys / c.page.d : 1) : 0;
         int id = -1, off = 0, next = -1;  // next: the listed page of the key after
         auto listed = [&](int j) {
           const int u = it.u0 + j * kChunkKeys + lt;
@@ -545,6 +554,14 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
             meet(1, kLoaders);
           }
           ok = ok && wait_warp(&bars.empty[b], (((ring + i) / NB) & 1) ^ 1, failed, limit);
+          if (SEL && ok && !value && lt < segs * (1 + a.plan.words)) {  // with K: the step's pages and their pickers
+            const int g = lt < segs ? lt : (lt - segs) / a.plan.words, u = it.u0 + j * kChunkKeys + g * c.page.d;
+            const bool on = u < it.u1;
+            const int64_t e = it.list + (on ? c.page.div(u) : 0);
+            copy4(tc::smem_u32(&bars.listed[(ring / 2 + j) % NB][lt]),
+                  lt < segs ? (const void*)(a.plan.pages + e)
+                            : (const void*)(a.plan.pickers + e * a.plan.words + (lt - segs) % a.plan.words), on);
+          }
           if (ok) {
             copy_rows(buffer(b), value ? src_v : src_k, value ? bars.row_v[j & 1] : bars.row_k[j & 1]);
             copy_arrive(&bars.full[b]);
@@ -684,7 +701,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
     // scores are kept raw and take their factor inside the exponential; one that is not positive goes to them first
     const bool raw = a.scale > 0.f;
     const float factor = a.scale * 1.4426950408889634f, sl2 = raw ? factor : 1.f;
-    int done = 0, count = 0;
+    int done = 0, count = 0, ring = 0;
     bool ok = true;  // where a wait gave up the items go on without work: the two warpgroups meet at barriers
     each_item<SEL>(a, [&](const Item& it) {
       const bool pair = it.tiles == 1;  // this warpgroup's steps are every second one of the same rows
@@ -695,25 +712,10 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const int pos_min = it.shift + a.group.div(it.x0 + x - row);  // of the tile's rows
       const bool tail = it.n - (x - row) < kRows;                   // rows that are none: their scores are dropped
       float m = -INFINITY, l = 0.f;  // maximum of the scores that weights are taken against, sum of weights
-      // selected: the row's token in the tile, its page's bit and last slot seen in a listed page
+      // selected: the row's token in the tile
       const int tl = tok - a.group.div(it.x0), segs = SEL ? (c.page.d < kChunkKeys ? kChunkKeys / c.page.d : 1) : 0;
-      const uint32_t* pickers = a.plan.pickers + it.list * a.plan.words + (row_on ? tl >> 5 : 0);
       const int stride = pair ? 2 : 1, first = pair ? t : 0;
       for (int j = first; ok && j < it.steps; j += stride) {
-        int seen_in[8];  // per segment of the step: keys 0 .. seen_in of it
-        if (SEL) {
-#pragma unroll
-          for (int g2 = 0; g2 < 8; ++g2) {
-            seen_in[g2] = -1;
-            const int u = it.u0 + j * kChunkKeys + g2 * c.page.d;
-            if (g2 < segs && u < it.u1 && row_on) {
-              const int e = c.page.div(u);
-              const int pg = __ldg(a.plan.pages + it.list + e);
-              const bool on = (__ldg(pickers + (int64_t)e * a.plan.words) >> (tl & 31)) & 1;
-              if (on) seen_in[g2] = pos - pg * c.page.d - (u - e * c.page.d);
-            }
-          }
-        }
         ok = wait_warp(&bars.s_full[t], done & 1, failed, limit);
         ++done;
         if (!ok) break;
@@ -729,6 +731,15 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         }
         const int key0 = it.u0 + j * kChunkKeys;
         if (SEL) {
+          int seen_in[kSegments];  // per page: its slots 0 .. seen_in
+          const uint32_t* listed = bars.listed[(ring / 2 + j) % NB];
+#pragma unroll
+          for (int g2 = 0; g2 < kSegments; ++g2) {
+            seen_in[g2] = -1;
+            const int u = key0 + g2 * c.page.d;
+            if (g2 < segs && u < it.u1 && row_on && (listed[segs + g2 * a.plan.words + (tl >> 5)] >> (tl & 31)) & 1)
+              seen_in[g2] = pos - (int)listed[g2] * c.page.d - (u - c.page.div(u) * c.page.d);
+          }
           mask_segments(s, seen_in, segs);
         } else if (tail || key0 + kChunkKeys - 1 > pos_min) {
           const int seen = pos - key0;  // keys 0 .. seen of these 128
@@ -783,6 +794,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
       const bool keys = it.steps > 0;
+      ring += 2 * it.steps;
       if (ok && keys) ok = wait_warp(&bars.o_full, count & 1, failed, limit);
       count += keys;
       tc::tc_fence_after_sync();
@@ -844,6 +856,7 @@ constexpr int kJoinRows = 4;
 template <typename T, bool SEL>
 __global__ void __launch_bounds__(128)
 k_paged_join(AttnArgs a) {
+  wait_for_previous();
   const int n = __ldg(a.plan.shares + kChunkBlocks).x, ntiles = __ldg(a.plan.shares + kChunkBlocks + 1).x;
   const int c0 = blockIdx.x + 1;
   if (c0 >= n) return;
@@ -897,8 +910,8 @@ cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
   cudaError_t e = once(
       [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<W>()); });
   if (e != cudaSuccess) return e;
-  kernel<<<SLNR_COUNTED(kChunkBlocks), kThreads, smem_bytes<W>(), s>>>(a, hdr, wait_limit_cycles());
-  return cudaGetLastError();
+  return launch_next(kernel, SLNR_COUNTED(dim3(kChunkBlocks)), dim3(kThreads), smem_bytes<W>(), s, a, hdr,
+                     wait_limit_cycles());
 }
 
 template <typename T, bool SEL>
@@ -908,15 +921,16 @@ cudaError_t launch_w(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_paged_plan(const AttnArgs& a, cudaStream_t s) {
-  if (a.picked) {
-    const dim3 grid((unsigned)a.c.nheads, (unsigned)a.plan.ntiles);
-    k_paged_union<<<(SLNR_COUNTED(grid)), kUnionThreads, 0, s>>>(a);
-    k_paged_plan<true><<<SLNR_COUNTED(1), kPlanThreads, 0, s>>>(a);
-  } else {
-    k_paged_plan<false><<<SLNR_COUNTED(1), kPlanThreads, 0, s>>>(a);
+cudaError_t launch_paged_plan(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
+  if (!a.picked) {
+    k_paged_plan<false><<<SLNR_COUNTED(1), kPlanThreads, 0, s>>>(a, hdr);
+    return cudaGetLastError();
   }
-  return cudaGetLastError();
+  const dim3 grid((unsigned)a.c.nheads, (unsigned)a.plan.ntiles);
+  k_paged_union<<<(SLNR_COUNTED(grid)), kUnionThreads, 0, s>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  return launch_next(k_paged_plan<true>, SLNR_COUNTED(dim3(1)), dim3(kPlanThreads), 0, s, a, hdr);
 }
 
 cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s) {
@@ -928,8 +942,7 @@ cudaError_t launch_paged_join(const AttnArgs& a, int dtype, cudaStream_t s) {
   const dim3 grid(kChunkBlocks - 1, kChunkRows / kJoinRows);
   auto kernel = dtype == SLNR_FP16 ? (a.picked ? k_paged_join<__half, true> : k_paged_join<__half, false>)
                                    : (a.picked ? k_paged_join<__nv_bfloat16, true> : k_paged_join<__nv_bfloat16, false>);
-  kernel<<<(SLNR_COUNTED(grid)), 128, 0, s>>>(a);
-  return cudaGetLastError();
+  return launch_next(kernel, SLNR_COUNTED(grid), dim3(128), 0, s, a);
 }
 
 }  // namespace slnr
