@@ -59,6 +59,7 @@ template <int W>
 constexpr size_t smem_bytes() { return (size_t)(2 + buffers<W>()) * tile_bytes<W>() + 1024; }
 constexpr int kWarpArrivals = 4;  // a warp arrives once for its lanes
 constexpr int kSegments = 8;      // pages of a step, at most
+constexpr int kGroups = 8;        // of 16 keys of a step
 constexpr int kMaxWords = 8;      // of the bits of 256 tokens of one row each
 
 struct Shared {
@@ -107,23 +108,6 @@ __device__ __forceinline__ void meet(int id, int n) { asm volatile("bar.sync %0,
 // Byte of 16-byte piece `piece` of a row inside a swizzled tile of 128 rows.
 __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
   return (uint32_t)((piece >> 3) * kBlock + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
-}
-
-// Drops the scores of the keys that a row does not see: those past seen[g] of
-// segment g, for `segs` (a power of two) equal segments.
-template <int SEGS>
-__device__ __forceinline__ void mask_equal(uint32_t (&s)[128], const int (&seen)[8]) {
-#pragma unroll
-  for (int k = 0; k < 128; ++k)
-    if (k % (128 / SEGS) > seen[k / (128 / SEGS)]) s[k] = 0xff800000u;
-}
-__device__ __forceinline__ void mask_segments(uint32_t (&s)[128], const int (&seen)[8], int segs) {
-  switch (segs) {
-    case 1: return mask_equal<1>(s, seen);
-    case 2: return mask_equal<2>(s, seen);
-    case 4: return mask_equal<4>(s, seen);
-    default: return mask_equal<8>(s, seen);
-  }
 }
 
 // Register shares of the calling warpgroup.
@@ -713,7 +697,8 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const bool tail = it.n - (x - row) < kRows;                   // rows that are none: their scores are dropped
       float m = -INFINITY, l = 0.f;  // maximum of the scores that weights are taken against, sum of weights
       // selected: the row's token in the tile
-      const int tl = tok - a.group.div(it.x0), segs = SEL ? (c.page.d < kChunkKeys ? kChunkKeys / c.page.d : 1) : 0;
+      const int tl = tok - a.group.div(it.x0), page_shift = c.page.d < kChunkKeys ? 31 - __clz(c.page.d) : 7;
+      const int segs = kChunkKeys >> page_shift, per_page = kGroups / segs, own_page = c.page.div(max(pos, 0));
       const int stride = pair ? 2 : 1, first = pair ? t : 0;
       for (int j = first; ok && j < it.steps; j += stride) {
         ok = wait_warp(&bars.s_full[t], done & 1, failed, limit);
@@ -730,29 +715,43 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           for (int k = 0; k < 128; ++k) s[k] = __float_as_uint(__uint_as_float(s[k]) * factor);
         }
         const int key0 = it.u0 + j * kChunkKeys;
+        // selected: bit g: the row's token picked the page of keys 16 g .. 16 g + 15.  Groups that it did not pick are
+        // left out of the maximum and get weights of 2^-inf; the slots past the token in its own page are dropped.
+        uint32_t picked = 0;
         if (SEL) {
-          int seen_in[kSegments];  // per page: its slots 0 .. seen_in
           const uint32_t* listed = bars.listed[(ring / 2 + j) % NB];
-#pragma unroll
-          for (int g2 = 0; g2 < kSegments; ++g2) {
-            seen_in[g2] = -1;
-            const int u = key0 + g2 * c.page.d;
-            if (g2 < segs && u < it.u1 && row_on && (listed[segs + g2 * a.plan.words + (tl >> 5)] >> (tl & 31)) & 1)
-              seen_in[g2] = pos - (int)listed[g2] * c.page.d - (u - c.page.div(u) * c.page.d);
+          bool own = false;
+          for (int i = 0; i < segs; ++i) {
+            const bool on = row_on && key0 + (i << page_shift) < it.u1 &&
+                            ((listed[segs + i * a.plan.words + (tl >> 5)] >> (tl & 31)) & 1);
+            if (on) picked |= ((1u << per_page) - 1) << (i * per_page);
+            own = own || (on && (int)listed[i] == own_page);
           }
-          mask_segments(s, seen_in, segs);
+          if (__any_sync(0xffffffffu, own)) {
+            const int off = key0 - c.page.div(key0) * c.page.d;  // of a page of more than 128 slots
+#pragma unroll
+            for (int g2 = 0; g2 < kGroups; ++g2) {
+              const int i = (16 * g2) >> page_shift;
+              const int last = pos - (int)listed[i] * c.page.d - off - (16 * g2 - (i << page_shift));
+#pragma unroll
+              for (int k = 0; k < 16; ++k)
+                if (k > last) s[16 * g2 + k] = 0xff800000u;
+            }
+          }
         } else if (tail || key0 + kChunkKeys - 1 > pos_min) {
-          const int seen = pos - key0;  // keys 0 .. seen of these 128
+          const int last = pos - key0;  // keys 0 .. last of these 128
 #pragma unroll
           for (int k = 0; k < 128; ++k)
-            if (k > seen) s[k] = 0xff800000u;
+            if (k > last) s[k] = 0xff800000u;
         }
-        float mx[4];
+        float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(s[k]);
+        for (int g2 = 0; g2 < kGroups; ++g2) {
+          float mx = __uint_as_float(s[16 * g2]);
 #pragma unroll
-        for (int k = 4; k < 128; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(s[k]));
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          for (int k = 1; k < 16; ++k) mx = fmaxf(mx, __uint_as_float(s[16 * g2 + k]));
+          if (!SEL || ((picked >> g2) & 1)) top = fmaxf(top, mx);
+        }
         // the first keys that a row sees set m; later m moves only where it has to
         const bool grow = (top - m) * sl2 > kGrow;  // m = -inf: true for any seen key
         if (__any_sync(0xffffffffu, grow)) {
@@ -780,8 +779,9 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           uint32_t w[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float w0 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e]), sl2, -b));
-            const float w1 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e + 1]), sl2, -b));
+            const float off = SEL && !((picked >> (2 * k + e / 8)) & 1) ? -INFINITY : -b;
+            const float w0 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e]), sl2, off));
+            const float w1 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e + 1]), sl2, off));
             sum[(2 * e) & 3] += w0;
             sum[(2 * e + 1) & 3] += w1;
             w[e] = Half2<T>::pack(w0, w1);
