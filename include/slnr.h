@@ -343,7 +343,8 @@ slnr_status slnr_page_tables(int32_t nreq, const int32_t *new_len, const int32_t
 
 /* ---- new keys and values into the cache -----------------------------------
  * K[slot_t] = k_t and V[slot_t] = v_t for each new token (a negative slot is
- * skipped).  Where cache->codes is not NULL, each page whose last slot is
+ * skipped; validate: SLNR_ERR_INDEX).  Slots are those of slnr_page_tables: a
+ * request's new tokens lie behind its older keys, k_len[r] of them in all.  Where cache->codes is not NULL, each page whose last slot is
  * written gets its summary, per head: m = the mean of its keys, scale =
  * max|m| / 127, codes = m / scale rounded to the nearest whole number (0 if
  * scale is 0). */

@@ -24,6 +24,10 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162f
 template <>
 __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
 
+// Keys of a token's row in shared memory: 8 mod 32, so that the rows that a product's lanes write fall on different
+// banks, and whole groups of 8 pages.
+__host__ __device__ __forceinline__ int key_pitch(int npages) { return (npages + 23) / 32 * 32 + 8; }
+
 // Whole numbers in the order of the scores.
 __device__ __forceinline__ uint32_t key_of(float score) {
   const uint32_t b = __float_as_uint(score + 0.f);  // -0 as 0
@@ -103,11 +107,11 @@ k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int np
               int first, int last) {
   extern __shared__ __align__(16) unsigned char smem[];
   int* s_code = reinterpret_cast<int*>(smem);                             // [ntile][width / 4]
-  uint32_t* s_key = reinterpret_cast<uint32_t*>(smem) + ntile * (kSelMaxWidth / 4);  // [ntile][npages]
+  uint32_t* s_key = reinterpret_cast<uint32_t*>(smem) + ntile * (kSelMaxWidth / 4);  // [ntile][pitch]
   __shared__ int s_req[kSelMaxTokens], s_own[kSelMaxTokens];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int h = blockIdx.y, t0 = blockIdx.x * ntile, n = min(ntile, p.ntok - t0);
-  const int words = c.width / 4;
+  const int words = c.width / 4, pitch = key_pitch(npages);
 
   // codes of the tokens' queries: a warp a token, 4 columns a lane
   for (int i = warp; i < n; i += kSelThreads / 32) {
@@ -192,11 +196,14 @@ k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int np
           Half2<__half>::mma(dot, fa[i], b.x, b.y);
         }
       // dot[e]: token lane / 4 + 8 (e / 2), page 2 (lane % 4) + e % 2, whose scale lane 4 (page) holds
+      const int col = 2 * (lane & 3);
+      const float f0 = __shfl_sync(0xffffffffu, scale, 4 * col), f1 = __shfl_sync(0xffffffffu, scale, 4 * col + 4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int col = 2 * (lane & 3) + (e & 1), i = row + 8 * (e >> 1);
-        const float f = __shfl_sync(0xffffffffu, scale, 4 * col);
-        if (i >= i0 && i < i1 && base + col <= most) s_key[i * npages + base + col] = key_of(__fmul_rn(dot[e], f));
+      for (int e = 0; e < 4; e += 2) {
+        const int i = row + 4 * e;
+        if (i >= i0 && i < i1)
+          *reinterpret_cast<uint2*>(s_key + i * pitch + base + col) =
+              make_uint2(key_of(__fmul_rn(dot[e], f0)), key_of(__fmul_rn(dot[e + 1], f1)));
       }
     }
     i0 = i1;
@@ -204,7 +211,7 @@ k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int np
   __syncthreads();
 
   for (int i = warp; i < n; i += kSelThreads / 32) {
-    uint32_t* key = s_key + i * npages;
+    const uint32_t* key = s_key + i * pitch;
     int32_t* out = picked + ((int64_t)(t0 + i) * c.nheads + h) * npicked;
     const int own = s_own[i];
     // always taken: pages [0, lead) and [tail, own]; between them by score
@@ -225,16 +232,15 @@ k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int np
     int at = 0;
     for (int base = 0; base <= own; base += 32) {
       const int pg = base + lane;
-      bool take = pg <= own && (pg < lead || pg >= tail);
-      bool tie = false;
-      if (pg >= lead && pg < tail && !none) {
-        const uint32_t x = key[pg];
-        take = all || x > v;
-        tie = !all && x == v;
+      const bool scored = pg >= lead && pg < tail;
+      const uint32_t x = scored ? key[pg] : 0;
+      bool take = pg <= own && (scored ? !none && (all || x > v) : true);
+      if (ties > 0) {
+        const bool tie = scored && !none && !all && x == v;
+        const unsigned tied = __ballot_sync(0xffffffffu, tie);
+        if (tie && __popc(tied & ((1u << lane) - 1)) < ties) take = true;
+        ties = max(ties - __popc(tied), 0);
       }
-      const unsigned tied = __ballot_sync(0xffffffffu, tie);
-      if (tie && __popc(tied & ((1u << lane) - 1)) < ties) take = true;
-      ties = max(ties - __popc(tied), 0);
       const unsigned m = __ballot_sync(0xffffffffu, take);
       const int where = at + __popc(m & ((1u << lane) - 1));
       if (take && where < npicked) out[where] = pg;
@@ -248,7 +254,7 @@ k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int np
 
 int select_tokens(int pages) {
   for (int n = kSelMaxTokens; n > 0; n /= 2)
-    if ((int64_t)n * (kSelMaxWidth + 4 * (int64_t)pages) <= kSelSmem) return n;
+    if ((int64_t)n * (kSelMaxWidth + 4 * (int64_t)key_pitch(pages)) <= kSelSmem) return n;
   return 0;
 }
 
@@ -258,7 +264,7 @@ cudaError_t launch_page_select(const PagesView& p, const CacheView& c, const Row
   const int npages = p.max_k > 0 ? (p.max_k - 1) / c.page.d + 1 : 1;
   // one token a block where requests have one: more blocks, and no two tokens share a page's codes
   const int ntile = p.max_q <= 1 ? 1 : select_tokens(npages);
-  const size_t smem = (size_t)ntile * (kSelMaxWidth + 4 * (size_t)npages);
+  const size_t smem = (size_t)ntile * (kSelMaxWidth + 4 * (size_t)key_pitch(npages));
   auto kernel = dtype == SLNR_FP16 ? k_page_select<__half> : k_page_select<__nv_bfloat16>;
   static OncePerDevice once[2];
   cudaError_t e = once[dtype == SLNR_FP16](

@@ -310,8 +310,6 @@ slnr_status slnr_page_append(const slnr_cache* cache, const slnr_pages* pages, c
   SLNR_CHECK(check_rows("k", k, pages->ntok > 0));
   SLNR_CHECK(check_rows("v", v, pages->ntok > 0));
   if (pages->ntok == 0) return SLNR_OK;
-  if (((int64_t)pages->ntok / 4 + 1) * cache->nheads * (cache->head_dim / 8) >= (int64_t(1) << 31) - 256)
-    return fail(SLNR_ERR_UNSUPPORTED, "too many rows for one call");
   cudaStream_t s = (cudaStream_t)opts->stream;
   const PagesView p = view(*pages);
   const CacheView c = view(*cache);

@@ -105,134 +105,157 @@ k_page_tables(int nreq, const int32_t* __restrict__ new_len, const int32_t* __re
 // Appending: K and V rows to their slots, and the summary of each page that a
 // token fills.
 //
-// The last blocks copy: a thread takes one 16-byte piece of a row for
-// kCopyTokens tokens, K and V, so 2 kCopyTokens loads are in flight and the
-// divisions that find the piece are made once.  The others look at 32 tokens
-// and one head each; for a token in a page's last slot the block's warps sum
-// that head's keys over the page.  Rows of this call are read from the call's own
-// input, so no block reads what another writes.  Bound by memory.
-constexpr int kCopyThreads = 256;
-constexpr int kCopyTokens = 4;
+// A block takes the new tokens that go to one page of one request (found from
+// the lengths alone) and one key head: a thread a 16-byte piece of every
+// ROWS-th row, K and V, kDeep rows in flight.  If the last of them fills the
+// page, the block sums the keys while it has them, with the older ones out of
+// the cache: no key is read twice, and no block reads what another writes.
+// Bound by memory.
+constexpr int kAppendThreads = 256;
+constexpr int kDeep = 4;
 
 template <typename T>
-__device__ __forceinline__ float to_float(T x);
+__device__ __forceinline__ float2 to_float2(uint32_t x);
 template <>
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float2 to_float2<__nv_bfloat16>(uint32_t x) {
+  return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+}
 template <>
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+__device__ __forceinline__ float2 to_float2<__half>(uint32_t x) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&x));
+}
+
+// Pages that the new tokens of a request go to.
+__device__ __forceinline__ int pages_touched(int old, int n, Divisor page) {
+  return n > 0 ? page.div(max(old, 0) + n - 1) - page.div(max(old, 0)) + 1 : 0;
+}
 
 template <typename T>
-__global__ void __launch_bounds__(kCopyThreads)
-k_page_append(PagesView p, CacheView c, RowsView kn, RowsView vn, int sum_blocks, Divisor of_token, Divisor of_head) {
-  if ((int)blockIdx.x >= sum_blocks) {
-    const int lin = (blockIdx.x - sum_blocks) * kCopyThreads + threadIdx.x;
-    const int group = of_token.div(lin), piece = lin - group * of_token.d;
-    const int h = of_head.div(piece), col = (piece - h * of_head.d) * 8;
-    const int t0 = group * kCopyTokens;
-    if (t0 >= p.ntok) return;
-    int slot[kCopyTokens];
-    uint4 a[kCopyTokens], b[kCopyTokens];
-#pragma unroll
-    for (int i = 0; i < kCopyTokens; ++i) {
-      slot[i] = inside(t0, i, p.ntok) ? __ldg(p.slots + t0 + i) : -1;
-      if (slot[i] >= 0 && page_of(slot[i], c) >= c.npages) slot[i] = -1;
+__global__ void __launch_bounds__(kAppendThreads)
+k_page_append(PagesView p, CacheView c, RowsView kn, RowsView vn, Divisor pieces) {
+  __shared__ float s_sum[kAppendThreads][9];  // a thread's 8 columns
+  const int tid = threadIdx.x, lane = tid & 31, h = blockIdx.y;
+  // request and page of flat page blockIdx.x: 32 requests a step, in every warp
+  int r = -1, nth = 0, before = 0;
+  for (int r0 = 0; r0 < p.nreq; r0 += 32) {
+    int n = 0;
+    if (r0 + lane < p.nreq) {
+      const int q = __ldg(p.q_pos + r0 + lane + 1) - __ldg(p.q_pos + r0 + lane);
+      n = pages_touched(__ldg(p.k_len + r0 + lane) - q, q, c.page);
     }
+    int sum = n;
 #pragma unroll
-    for (int i = 0; i < kCopyTokens; ++i)
-      if (slot[i] >= 0) {
-        a[i] = __ldg(reinterpret_cast<const uint4*>((const T*)kn.p + (int64_t)(t0 + i) * kn.tok + h * kn.head + col));
-        b[i] = __ldg(reinterpret_cast<const uint4*>((const T*)vn.p + (int64_t)(t0 + i) * vn.tok + h * vn.head + col));
-      }
-#pragma unroll
-    for (int i = 0; i < kCopyTokens; ++i)
-      if (slot[i] >= 0) {
-        const int pg = page_of(slot[i], c), off = slot[i] - pg * c.page.d;
-        *reinterpret_cast<uint4*>((T*)c.k + pg * c.ks[0] + off * c.ks[1] + h * c.ks[2] + col) = a[i];
-        *reinterpret_cast<uint4*>((T*)c.v + pg * c.vs[0] + off * c.vs[1] + h * c.vs[2] + col) = b[i];
-      }
-    return;
-  }
-  // one head of 32 tokens; the block's warps share the keys of each filled page
-  __shared__ float2 s_sum[kCopyThreads / 32][2][32];
-  constexpr int WARPS = kCopyThreads / 32, DEEP = 8;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t w = blockIdx.x;
-  const int h = (int)(w % c.nheads);
-  const int64_t first = w / c.nheads * 32;
-  int slot = -1;
-  if (first + lane < p.ntok) slot = __ldg(p.slots + first + lane);
-  bool fills = slot >= 0;
-  if (fills) {
-    const int pg = page_of(slot, c);
-    fills = pg < c.npages && slot - pg * c.page.d == c.page.d - 1;
-  }
-  unsigned todo = __ballot_sync(0xffffffffu, fills);  // the same in all warps
-  while (todo) {
-    const int i = __ffs(todo) - 1;
-    todo &= todo - 1;
-    const int pg = page_of(__shfl_sync(0xffffffffu, slot, i), c);
-    const int t = (int)first + i, r = __ldg(p.req + t);
-    // slot j of the page: a token of this call from j0 on, an older key before
-    const int s = c.page.d, fresh = min(t - __ldg(p.q_pos + r) + 1, s), j0 = s - fresh;
-    const T* src_old = (const T*)c.k + pg * c.ks[0] + h * c.ks[2];
-    const T* src_new = (const T*)kn.p + (int64_t)(t - (s - 1)) * kn.tok + h * kn.head;
-    // lane: columns 2 lane and 2 lane + 64, in pairs; warp: every eighth key, DEEP of them in flight
-    const int col = 2 * lane;
-    float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
-    for (int jb = warp; jb < s; jb += WARPS * DEEP) {
-      uint32_t x[DEEP][2];
-#pragma unroll
-      for (int d = 0; d < DEEP; ++d) {
-        const int j = jb + d * WARPS;
-        const T* row = j < j0 ? src_old + j * c.ks[1] : src_new + (int64_t)j * kn.tok;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          x[d][e] = j < s && col + 64 * e < c.width ? *reinterpret_cast<const uint32_t*>(row + col + 64 * e) : 0u;
-      }
-#pragma unroll
-      for (int d = 0; d < DEEP; ++d)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          alignas(4) T y[2];
-          *reinterpret_cast<uint32_t*>(y) = x[d][e];
-          sum[e].x += to_float(y[0]);
-          sum[e].y += to_float(y[1]);
-        }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
     }
-    s_sum[warp][0][lane] = sum[0];
-    s_sum[warp][1][lane] = sum[1];
-    __syncthreads();
-    if (warp == 0) {
-      float most = 0.f;
+    const unsigned past = __ballot_sync(0xffffffffu, before + sum > (int)blockIdx.x);
+    if (past) {
+      const int i = __ffs(past) - 1;
+      r = r0 + i;
+      nth = blockIdx.x - before - __shfl_sync(0xffffffffu, sum - n, i);
+      break;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (r < 0) return;
+  const int s = c.page.d, q0 = __ldg(p.q_pos + r), qn = __ldg(p.q_pos + r + 1) - q0;
+  const int old = max(__ldg(p.k_len + r) - qn, 0);
+  // tokens [t0, t1) at positions from `at` on, slots [at % s, ..) of their page
+  const int page0 = c.page.div(old) + nth, at = max(old, page0 * s);
+  const int t0 = q0 + at - old, t1 = q0 + min(qn, (page0 + 1) * s - old);
+  const int col = tid % pieces.d, row0 = tid / pieces.d, rows = kAppendThreads / pieces.d;
+  const bool on = row0 < rows;  // pieces that do not divide the block leave some threads out
+  const int last = __ldg(p.slots + t1 - 1);
+  const int last_page = last >= 0 ? page_of(last, c) : 0;
+  const bool fills = c.codes && last >= 0 && last_page < c.npages && last - last_page * s == s - 1;
+  float sum[8];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        for (int k = 1; k < WARPS; ++k) {
-          const float2 y = s_sum[k][e][lane];
-          sum[e].x += y.x;
-          sum[e].y += y.y;
+  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+  auto add = [&](const uint4& x) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 y = to_float2<T>(w[e]);
+      sum[2 * e] += y.x;
+      sum[2 * e + 1] += y.y;
+    }
+  };
+  const T* src_k = (const T*)kn.p + (int64_t)h * kn.head + col * 8;
+  const T* src_v = (const T*)vn.p + (int64_t)h * vn.head + col * 8;
+  T* dst_k = (T*)c.k + h * c.ks[2] + col * 8;
+  T* dst_v = (T*)c.v + h * c.vs[2] + col * 8;
+  if (on) {
+    for (int t = t0 + row0; t < t1; t += rows * kDeep) {
+      uint4 x[kDeep], y[kDeep];
+      int slot[kDeep];
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) {
+        const int u = t + d * rows;
+        slot[d] = u < t1 ? __ldg(p.slots + u) : -1;
+        x[d] = y[d] = make_uint4(0, 0, 0, 0);
+        if (u < t1) {
+          x[d] = __ldg(reinterpret_cast<const uint4*>(src_k + u * kn.tok));
+          y[d] = __ldg(reinterpret_cast<const uint4*>(src_v + u * vn.tok));
         }
-        sum[e].x = __fdiv_rn(sum[e].x, (float)s);
-        sum[e].y = __fdiv_rn(sum[e].y, (float)s);
-        most = fmaxf(most, fmaxf(fabsf(sum[e].x), fabsf(sum[e].y)));
       }
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-      const float scale = __fdiv_rn(most, 127.f);
-      int8_t* code = c.codes + ((int64_t)pg * c.nheads + h) * c.width;
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (col + 64 * e < c.width) {
-          char2 x = make_char2(0, 0);
-          if (scale > 0.f) {
-            x.x = (signed char)min(max(__float2int_rn(__fdiv_rn(sum[e].x, scale)), -127), 127);
-            x.y = (signed char)min(max(__float2int_rn(__fdiv_rn(sum[e].y, scale)), -127), 127);
-          }
-          *reinterpret_cast<char2*>(code + col + 64 * e) = x;
+      for (int d = 0; d < kDeep; ++d) {
+        if (fills) add(x[d]);
+        const int pg = slot[d] >= 0 ? page_of(slot[d], c) : c.npages, off = slot[d] - pg * s;
+        if (pg < c.npages) {
+          *reinterpret_cast<uint4*>(dst_k + pg * c.ks[0] + off * c.ks[1]) = x[d];
+          *reinterpret_cast<uint4*>(dst_v + pg * c.vs[0] + off * c.vs[1]) = y[d];
         }
-      if (lane == 0) c.scales[(int64_t)pg * c.nheads + h] = scale;
+      }
     }
-    __syncthreads();  // s_sum is read before the next page's sums are written
   }
+  if (!fills) return;
+  if (on) {  // the page's older keys
+    for (int j = row0; j < s - (t1 - t0); j += rows * kDeep) {
+      uint4 x[kDeep];
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) {
+        x[d] = make_uint4(0, 0, 0, 0);
+        if (j + d * rows < s - (t1 - t0))
+          x[d] = *reinterpret_cast<const uint4*>(dst_k + last_page * c.ks[0] + (j + d * rows) * c.ks[1]);
+      }
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) add(x[d]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s_sum[tid][e] = sum[e];
+  __syncthreads();
+  // warp 0: columns 4 lane .. 4 lane + 3, in the threads' order
+  if (tid >= 32) return;
+  float m[4] = {0.f, 0.f, 0.f, 0.f}, most = 0.f;
+  const bool mine = 4 * lane < c.width;
+  if (mine) {
+    for (int i = 0; i < rows; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] += s_sum[i * pieces.d + lane / 2][4 * (lane & 1) + e];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    m[e] = __fdiv_rn(m[e], (float)s);
+    most = fmaxf(most, fabsf(m[e]));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  const float scale = __fdiv_rn(most, 127.f);
+  const int64_t to = (int64_t)last_page * c.nheads + h;
+  if (mine) {
+    char4 code = make_char4(0, 0, 0, 0);
+    if (scale > 0.f) {
+      code.x = (signed char)min(max(__float2int_rn(__fdiv_rn(m[0], scale)), -127), 127);
+      code.y = (signed char)min(max(__float2int_rn(__fdiv_rn(m[1], scale)), -127), 127);
+      code.z = (signed char)min(max(__float2int_rn(__fdiv_rn(m[2], scale)), -127), 127);
+      code.w = (signed char)min(max(__float2int_rn(__fdiv_rn(m[3], scale)), -127), 127);
+    }
+    *reinterpret_cast<char4*>(c.codes + to * c.width + 4 * lane) = code;
+  }
+  if (lane == 0) c.scales[to] = scale;
 }
 
 // ---------------------------------------------------------------------------
@@ -270,7 +293,7 @@ __global__ void k_validate_pages(PagesView p, int npages, Divisor page, bool slo
   if (id == 0 && (p.q_pos[0] != 0 || p.q_pos[p.nreq] != p.ntok)) bad |= kErrPos;
   for (int64_t r = id; r < p.nreq; r += step) {
     const long long n = (long long)p.q_pos[r + 1] - p.q_pos[r], k = p.k_len[r];
-    if (n < 0 || n > p.max_q || k < 0 || k > p.max_k || k > (long long)p.width * page.d) bad |= kErrPos;
+    if (n < 0 || n > p.max_q || k < (slots ? n : 0) || k > p.max_k || k > (long long)p.width * page.d) bad |= kErrPos;
     else
       for (int i = 0; i < clamped_div_up((int)k, page); ++i)
         if ((unsigned)p.table[r * p.table_stride + i] >= (unsigned)npages) bad |= kErrCrdRange;
@@ -312,13 +335,11 @@ cudaError_t launch_page_tables(int nreq, const int32_t* new_len, const int32_t* 
 cudaError_t launch_page_append(const PagesView& p, const CacheView& c, const RowsView& k, const RowsView& v, int dtype,
                                cudaStream_t s) {
   if (p.ntok == 0) return cudaSuccess;
-  const int per_row = c.width / 8;
-  const int64_t copy_blocks = ceil_div(ceil_div(p.ntok, kCopyTokens) * c.nheads * per_row, kCopyThreads);
-  const int64_t sum_blocks = c.codes ? ceil_div(p.ntok, 32) * c.nheads : 0;
-  const unsigned grid = (unsigned)(copy_blocks + sum_blocks);
+  const int64_t pages = p.ntok / c.page.d + 2 * (int64_t)(p.nreq < p.ntok ? p.nreq : p.ntok);
+  if (pages >= (int64_t(1) << 31)) return cudaErrorInvalidConfiguration;
+  const dim3 grid((unsigned)pages, (unsigned)c.nheads);
   auto kernel = dtype == SLNR_FP16 ? k_page_append<__half> : k_page_append<__nv_bfloat16>;
-  kernel<<<SLNR_COUNTED(grid), kCopyThreads, 0, s>>>(p, c, k, v, (int)sum_blocks,
-                                                     divisor(c.nheads * per_row), divisor(per_row));
+  kernel<<<(SLNR_COUNTED(grid)), kAppendThreads, 0, s>>>(p, c, k, v, divisor(c.width / 8));
   return cudaGetLastError();
 }
 
