@@ -53,26 +53,70 @@ __device__ __forceinline__ Cut find_cut(uint32_t lo, uint32_t hi, int want, Coun
   }
   return Cut{lo, want - (lo == 0xffffffffu ? 0 : count(lo + 1))};
 }
-// Up to 32 KPL keys: held in registers.
-template <int KPL>
-__device__ __forceinline__ Cut cut_in_registers(const uint32_t* key, int n, int want) {
+// The same where the lanes' own maxima leave few of the keys: the want-th highest maximum is at or below the cut, so what
+// lies below it is out.  The others (a few more than want) go to `found` in their
+// order, and the cut is found among them alone.  Writes the indexes of the keys
+// taken, in order, plus `base`, to out; false (nothing written) where more than
+// kFound are left or more than a warp are wanted.
+constexpr int kFound = 128;
+__device__ __forceinline__ bool take_few(const uint32_t* key, int n, int want, int base, uint2* found, int32_t* out) {
   const int lane = threadIdx.x & 31;
-  uint32_t k[KPL], lo = 0xffffffffu, hi = 0;
-#pragma unroll
-  for (int i = 0; i < KPL; ++i) {
-    const bool on = 32 * i + lane < n;
-    k[i] = on ? key[32 * i + lane] : 0;
-    if (on) lo = min(lo, k[i]);
-    hi = max(hi, k[i]);
+  const unsigned below = (1u << lane) - 1;
+  if (want > 32) return false;
+  uint32_t most = 0;
+#pragma unroll 8
+  for (int i = lane; i < n; i += 32) most = max(most, key[i]);
+  const uint32_t top = __reduce_max_sync(0xffffffffu, most);
+  uint32_t lo = __reduce_min_sync(0xffffffffu, most), hi = top;
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2 + 1;
+    const int c = __popc(__ballot_sync(0xffffffffu, most >= mid));
+    if (c >= want) lo = mid;
+    else hi = mid - 1;
+    if (c == want) break;
   }
-  lo = __reduce_min_sync(0xffffffffu, lo);
-  hi = __reduce_max_sync(0xffffffffu, hi);
-  return find_cut(lo, hi, want, [&](uint32_t mid) {
-    int c = 0;
+  int total = 0;
+#pragma unroll 8
+  for (int i = 0; i < n; i += 32) {
+    const uint32_t k = i + lane < n ? key[i + lane] : 0;
+    const bool in = i + lane < n && k >= lo;
+    const unsigned m = __ballot_sync(0xffffffffu, in);
+    const int at = total + __popc(m & below);
+    if (in && at < kFound) found[at] = make_uint2(k, i + lane);
+    total += __popc(m);
+  }
+  if (total > kFound || total < want) return false;  // fewer: keys of 0, as a score of NaN can have
+  __syncwarp();
+  uint2 f[kFound / 32];
 #pragma unroll
-    for (int i = 0; i < KPL; ++i) c += k[i] >= mid;
-    return (int)__reduce_add_sync(0xffffffffu, c);
-  });
+  for (int i = 0; i < kFound / 32; ++i) f[i] = 32 * i + lane < total ? found[32 * i + lane] : make_uint2(0, 0);
+  __syncwarp();
+  Cut cut{lo, want};
+  if (total > want) {
+    cut = find_cut(lo, top, want, [&](uint32_t mid) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < kFound / 32; ++i)
+        if (32 * i < total) c += __popc(__ballot_sync(0xffffffffu, f[i].x >= mid && 32 * i + lane < total));
+      return c;
+    });
+  } else {
+    cut = Cut{lo - 1, 0};  // all of them (lo > 0: see above)
+    if (lo == 0) return false;
+  }
+  int at = 0;
+#pragma unroll
+  for (int i = 0; i < kFound / 32; ++i) {
+    if (32 * i >= total) break;
+    const bool on = 32 * i + lane < total, tie = on && f[i].x == cut.v;
+    const unsigned tied = __ballot_sync(0xffffffffu, tie);
+    const bool take = on && (f[i].x > cut.v || (tie && __popc(tied & below) < cut.ties));
+    cut.ties = max(cut.ties - __popc(tied), 0);
+    const unsigned m = __ballot_sync(0xffffffffu, take);
+    if (take) out[at + __popc(m & below)] = base + (int)f[i].y;
+    at += __popc(m);
+  }
+  return true;
 }
 __device__ __forceinline__ Cut cut_in_memory(const uint32_t* key, int n, int want) {
   const int lane = threadIdx.x & 31;
@@ -102,13 +146,14 @@ __device__ __forceinline__ uint2 halves_of(uint32_t codes) {
 // product's registers (the columns of a row in an order of their own, the same
 // for both operands).  Selection: a warp a token, then the pages written in order.
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads)
+__global__ void __launch_bounds__(kSelThreads, 4)
 k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int npages, int32_t* picked, int npicked,
               int first, int last) {
   extern __shared__ __align__(16) unsigned char smem[];
   int* s_code = reinterpret_cast<int*>(smem);                             // [ntile][width / 4]
   uint32_t* s_key = reinterpret_cast<uint32_t*>(smem) + ntile * (kSelMaxWidth / 4);  // [ntile][pitch]
   __shared__ int s_req[kSelMaxTokens], s_own[kSelMaxTokens];
+  __shared__ uint2 s_found[kSelThreads / 32][kFound];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int h = blockIdx.y, t0 = blockIdx.x * ntile, n = min(ntile, p.ntok - t0);
   const int words = c.width / 4, pitch = key_pitch(npages);
@@ -221,10 +266,16 @@ k_page_select(PagesView p, CacheView c, RowsView q, int group, int ntile, int np
     Cut cut{0, 0};
     if (want > 0 && want < among) {
       const uint32_t* k = key + lead;
-      cut = among <= 256    ? cut_in_registers<8>(k, among, want)
-            : among <= 512  ? cut_in_registers<16>(k, among, want)
-            : among <= 1024 ? cut_in_registers<32>(k, among, want)
-                            : cut_in_memory(k, among, want);
+      uint2* found = s_found[warp];
+      const bool done = take_few(k, among, want, lead, found, out + lead);
+      if (done) {
+        for (int w = lane; w < npicked; w += 32) {
+          if (w < lead) out[w] = w;
+          if (w >= lead + want) out[w] = w - lead - want <= own - tail ? tail + w - lead - want : -1;
+        }
+        continue;
+      }
+      cut = cut_in_memory(k, among, want);
     }
     const uint32_t v = cut.v;
     int ties = cut.ties;
