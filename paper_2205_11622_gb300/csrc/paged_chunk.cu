@@ -850,8 +850,8 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
 
 // Items that cuts went through: o = sum 2^(lse - m) o_part / sum 2^(lse - m) over
 // their parts, in the keys' order.  Block x: the item that share x + 1 begins
-// inside of, if no share before does; block y: 4 of its rows, one a warp.
-constexpr int kJoinRows = 4;
+// inside of, if no share before does; block y: 16 of its rows, 4 a warp at once.
+constexpr int kJoinRows = 16;
 
 template <typename T, bool SEL>
 __global__ void __launch_bounds__(128)
@@ -866,40 +866,54 @@ k_paged_join(AttnArgs a) {
   while (c1 < n && __ldg(a.plan.shares + c1).x == cut.x) ++c1;
   const Item it = item_of<SEL>(a, cut.x, ntiles, 0, -1);
   const int lane = threadIdx.x & 31, G = a.group.d, col = 4 * lane;
-  for (int x = blockIdx.y * kJoinRows + (threadIdx.x >> 5); x < min(it.n, ((int)blockIdx.y + 1) * kJoinRows); x += 4) {
-    // the part that begins the item, then one a share
-    auto part = [&](int k) { return (int64_t)(2 * (c0 - 1 + k) + (k == 0)) * kChunkRows + x; };
-    const int parts = c1 - c0 + 1;
-    float m = -INFINITY;
-    for (int k = lane; k < parts; k += 32) m = fmaxf(m, a.plan.part_lse[part(k)]);
+  constexpr int ROWS = kJoinRows / 4;
+  const int x0 = blockIdx.y * kJoinRows + (threadIdx.x >> 5) * ROWS, parts = c1 - c0 + 1;
+  if (x0 >= it.n) return;
+  // row x of part k: the one that begins the item, then one a share
+  auto part = [&](int k, int i) {
+    return (int64_t)(2 * (c0 - 1 + k) + (k == 0)) * kChunkRows + min(x0 + i, it.n - 1);
+  };
+  float m[ROWS], sum[ROWS];
+  float4 acc[ROWS];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float b = m == -INFINITY ? 0.f : m;
-    float sum = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int k = 0; k < parts; ++k) {
-      const int64_t at = part(k);
-      const float f = exp2_fast(a.plan.part_lse[at] - b);
-      sum += f;
+  for (int i = 0; i < ROWS; ++i) {
+    m[i] = -INFINITY;
+    sum[i] = 0.f;
+    acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+#pragma unroll 2
+  for (int k = 0; k < parts; ++k)
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) m[i] = fmaxf(m[i], a.plan.part_lse[part(k, i)]);
+#pragma unroll 2
+  for (int k = 0; k < parts; ++k)
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int64_t at = part(k, i);
+      const float f = exp2_fast(a.plan.part_lse[at] - (m[i] == -INFINITY ? 0.f : m[i]));
+      sum[i] += f;
       if (col < a.c.width) {
         const float4 y = *reinterpret_cast<const float4*>(a.plan.part + at * a.c.width + col);
-        acc.x += f * y.x;
-        acc.y += f * y.y;
-        acc.z += f * y.z;
-        acc.w += f * y.w;
+        acc[i].x += f * y.x;
+        acc[i].y += f * y.y;
+        acc[i].z += f * y.z;
+        acc[i].w += f * y.w;
       }
     }
-    const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);  // the parts of a row without keys are zeros
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const int x = x0 + i;
+    if (x >= it.n) break;
+    const float inv = sum[i] == 0.f ? 0.f : __fdividef(1.f, sum[i]);  // the parts of a row without keys are zeros
     const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
     const int64_t at = (it.q0 + tok) * ((int64_t)a.c.nheads * G) + it.h * G + g;
     if (col < a.c.width) {
       uint2 y;
-      y.x = Half2<T>::pack(acc.x * inv, acc.y * inv);
-      y.y = Half2<T>::pack(acc.z * inv, acc.w * inv);
+      y.x = Half2<T>::pack(acc[i].x * inv, acc[i].y * inv);
+      y.y = Half2<T>::pack(acc[i].z * inv, acc[i].w * inv);
       *reinterpret_cast<uint2*>((T*)a.out + at * a.c.width + col) = y;
     }
-    if (lane == 0 && a.lse) a.lse[at] = (m + __log2f(sum)) * 0.6931471805599453f;
+    if (lane == 0 && a.lse) a.lse[at] = (m[i] + __log2f(sum[i])) * 0.6931471805599453f;
   }
 }
 
