@@ -69,8 +69,9 @@ struct Shared {
   int64_t row_k[2][kChunkKeys], row_v[2][kChunkKeys];  // bytes from the head's first row to each key's; -1: zeros
   int64_t row_q[2 * kRows];                            // the same of the item's query rows
   uint32_t listed[8][kSegments * (1 + kMaxWords)];  // selected: a step's pages, then who picked each
-  float2 other_ml[kRows];          // one tile an item: the second warpgroup's maxima and sums
-  alignas(16) float stage[kLoadWarp][32][20];  // 16 columns of a warp's rows on their way out
+  // one tile an item: 16 columns of the second warpgroup's O, its maxima and sums
+  float other[16][kRows];
+  float2 other_ml[kRows];
 };
 
 static_assert(smem_bytes<128>() + sizeof(Shared) <= (size_t)227 * 1024, "shared memory of a block");
@@ -321,12 +322,6 @@ k_paged_plan(AttnArgs a, WsHeader* hdr) {
   }
 }
 
-// 16 columns of the second warpgroup's rows, where its rows are staged otherwise.
-__device__ __forceinline__ float (&other_rows(Shared& sh))[16][kRows] {
-  static_assert(sizeof(float) * 16 * kRows <= sizeof(sh.stage) / 2, "the second warpgroup's half");
-  return *reinterpret_cast<float(*)[16][kRows]>(&sh.stage[kLoadWarp / 2]);
-}
-
 // A row of O out of tensor memory (zeros where !on).
 template <int W>
 __device__ __forceinline__ void read_row(uint32_t col_o, bool on, uint32_t (&o)[W]) {
@@ -341,34 +336,31 @@ __device__ __forceinline__ void read_row(uint32_t col_o, bool on, uint32_t (&o)[
   }
 }
 
-// The rows of a warp, times inv (0: no key), with f_other times the other
-// warpgroup's where an item has one tile: a thread a row, and through shared
-// memory, 16 columns at a time, to whole 32-byte sectors a few lanes a row.
+// 32 bytes of a row: one store where they are aligned.
+__device__ __forceinline__ void store32(void* to, const uint32_t (&v)[8], bool aligned) {
+  if (aligned) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<uint4*>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
+}
+
+// A thread's row of the item, times inv (0: no key), with f_other times the other
+// warpgroup's where an item has one tile.  Whole 32-byte sectors a thread: as
+// fast as the memory system takes them, without shared memory in between.
 // m: maximum in powers of two, l: sum.
 template <typename T, int W>
-__device__ __forceinline__ void write_rows(const AttnArgs& a, const Item& it, Shared& sh, uint32_t (&o)[W], int warp,
-                                           int lane, bool ok, float inv, float f_other, float m, float l) {
-  const bool pair = it.tiles == 1, whole = it.slot < 0;
-  const int G = a.group.d, x0 = (pair ? 0 : (warp >> 2) * kRows) + (warp & 3) * 32;  // the warp's first row
-  const int row = (warp & 3) * 32 + lane;
-  const int64_t hq = (int64_t)a.c.nheads * G;
-  auto place = [&](int x) {  // of the item's row x in out and lse, or in the parts; -1: none
-    if (!ok || x >= it.n) return (int64_t)-1;
-    if (!whole) return (int64_t)it.slot * kChunkRows + x;
-    const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
-    return (it.q0 + tok) * hq + it.h * G + g;
-  };
-  // whole items: 2 lanes a row, 8 columns each; parts: 4 lanes a row, 4 columns each
-  const int per = whole ? 2 : 4, q0 = lane / per, col = lane % per * (whole ? 8 : 4);
-  char* to[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t at = i < per ? place(x0 + q0 + i * (32 / per)) : -1;
-    to[i] = at < 0 ? nullptr
-            : whole ? (char*)((T*)a.out + at * a.c.width + col) : (char*)(a.plan.part + at * a.c.width + col);
-  }
-  float(&stage)[32][20] = sh.stage[warp];
-  const float(&other)[16][kRows] = other_rows(sh);
+__device__ __forceinline__ void write_row(const AttnArgs& a, const Item& it, Shared& sh, uint32_t (&o)[W], int x, int row,
+                                          bool ok, float inv, float f_other, float m, float l) {
+  const bool pair = it.tiles == 1, whole = it.slot < 0, on = ok && x < it.n;
+  const int G = a.group.d, tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
+  const int64_t at = whole ? (it.q0 + tok) * ((int64_t)a.c.nheads * G) + it.h * G + g : (int64_t)it.slot * kChunkRows + x;
+  T* out = (T*)a.out + at * a.c.width;
+  float* part = a.plan.part + at * a.c.width;
+  const bool aligned = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && a.c.width % 16 == 0;
 #pragma unroll
   for (int k = 0; k < W; k += 16) {
     float v[16];
@@ -377,37 +369,27 @@ __device__ __forceinline__ void write_rows(const AttnArgs& a, const Item& it, Sh
     if (pair) {
       meet(2, 2 * kRows);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = f_other == 0.f ? v[e] : fmaf(other[e][row], f_other, v[e]);
+      for (int e = 0; e < 16; ++e) v[e] = f_other == 0.f ? v[e] : fmaf(sh.other[e][row], f_other, v[e]);
       meet(2, 2 * kRows);
     }
-    __syncwarp();
+    if (on && k < a.c.width) {
+      uint32_t z[8];
+      if (whole) {
 #pragma unroll
-    for (int e = 0; e < 16; e += 4)
-      *reinterpret_cast<float4*>(&stage[lane][e]) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-    __syncwarp();
-    const bool on = k + col < a.c.width;
-    if (whole) {
+        for (int e = 0; e < 8; ++e) z[e] = Half2<T>::pack(v[2 * e], v[2 * e + 1]);
+        if (k + 8 < a.c.width) store32(out + k, z, aligned);
+        else *reinterpret_cast<uint4*>(out + k) = make_uint4(z[0], z[1], z[2], z[3]);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float4 y0 = *reinterpret_cast<const float4*>(&stage[q0 + 16 * i][col]);
-        const float4 y1 = *reinterpret_cast<const float4*>(&stage[q0 + 16 * i][col + 4]);
-        uint4 z;
-        z.x = Half2<T>::pack(y0.x, y0.y);
-        z.y = Half2<T>::pack(y0.z, y0.w);
-        z.z = Half2<T>::pack(y1.x, y1.y);
-        z.w = Half2<T>::pack(y1.z, y1.w);
-        if (on && to[i]) *reinterpret_cast<uint4*>((T*)to[i] + k) = z;
-      }
-    } else {
+        for (int half = 0; half < 2; ++half) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 y = *reinterpret_cast<const float4*>(&stage[q0 + 8 * i][col]);
-        if (on && to[i]) *reinterpret_cast<float4*>((float*)to[i] + k) = y;
+          for (int e = 0; e < 8; ++e) z[e] = __float_as_uint(v[8 * half + e]);
+          if (k + 8 * half < a.c.width) store32(part + k + 8 * half, z, true);
+        }
       }
     }
   }
-  const int64_t at = place(x0 + lane);
-  if (at >= 0) {
+  if (on) {
     const float lse2 = l == 0.f ? -INFINITY : m + __log2f(l);
     if (!whole) a.plan.part_lse[at] = lse2;
     else if (a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
@@ -814,19 +796,18 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           f_other = l == 0.f ? 0.f : f_other * __fdividef(1.f, l);
           m = top;
           const float inv = l == 0.f ? 0.f : f * __fdividef(1.f, l);
-          write_rows<T, W>(a, it, bars, o, warp, lane, ok, inv, f_other, m, l);
+          write_row<T, W>(a, it, bars, o, x, row, ok, inv, f_other, m, l);
         } else {
-          float(&other)[16][kRows] = other_rows(bars);
 #pragma unroll
           for (int k = 0; k < W; k += 16) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) other[e][row] = __uint_as_float(o[k + e]);
+            for (int e = 0; e < 16; ++e) bars.other[e][row] = __uint_as_float(o[k + e]);
             meet(2, 2 * kRows);
             meet(2, 2 * kRows);
           }
         }
       } else {
-        write_rows<T, W>(a, it, bars, o, warp, lane, ok, l == 0.f ? 0.f : __fdividef(1.f, l), 0.f, m, l);
+        write_row<T, W>(a, it, bars, o, x, row, ok, l == 0.f ? 0.f : __fdividef(1.f, l), 0.f, m, l);
       }
     });
   }
