@@ -76,11 +76,26 @@ struct Shared {
 
 static_assert(smem_bytes<128>() + sizeof(Shared) <= (size_t)227 * 1024, "shared memory of a block");
 
+// One poll that does not sleep.
+__device__ __forceinline__ bool test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(tc::smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+constexpr long long kShortLimit = 1 << 20;  // cycles; a try_wait may sleep for longer than a limit below that
+
 // Waits for the phase of that parity; false (and *failed set) after `limit` cycles or once another wait gave up.
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* failed, long long limit) {
-  if (tc::mbar_try_wait(bar, parity)) return true;
+  const bool sleeps = limit >= kShortLimit;
+  if (sleeps ? tc::mbar_try_wait(bar, parity) : test(bar, parity)) return true;
   const long long t0 = clock64();
-  while (!tc::mbar_try_wait(bar, parity)) {
+  while (!(sleeps ? tc::mbar_try_wait(bar, parity) : test(bar, parity))) {
     if (*failed) return false;
     if (clock64() - t0 > limit) {
       *failed = 1;

@@ -208,3 +208,170 @@ def test_all_pages_picked_is_paged_attention(slnr):
     picked = torch.arange(b.width, dtype=torch.int32).expand(b.T, 2, b.width).clone()
     picked[picked > (b.pos // 16)[:, None, None]] = -1
     b.check(slnr.selected_attention(b.q.cuda(), b.cache(), b.tables(), picked.cuda()), b.attention(0.125))
+
+
+def test_many_requests(slnr):
+    """More requests, row tiles and items than one step of the plan takes; a chunk among single tokens."""
+    lens = [(1, 1 + r % 19) for r in range(1300)] + [(0, 4)] * 40 + [(70, 90)] + [(1, 300)] * 3
+    b = P.Batch(lens, 16, 2, 2, 16, seed=26)
+    b.check(slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), validate=True), b.attention(0.25))
+
+
+@pytest.mark.parametrize("page", [16, 128, 256])
+def test_selected_chunk_many_pages(slnr, page):
+    """Pages far into a long request: the list of picked pages is made in several windows."""
+    b = P.Batch([(20, 20000 if page == 16 else 9000), (3, 500)], page, 4, 1, 16, seed=27)
+    picked = P.picks(b, 5, seed=28)
+    got = slnr.selected_attention(b.q.cuda(), b.cache(), b.tables(), picked.cuda(), validate=True)
+    b.check(got, b.attention(0.25, picked))
+
+
+def test_selected_chunk_nothing_picked(slnr):
+    """Row tiles whose tokens picked no page at all, beside others."""
+    b = P.Batch([(64, 200), (64, 64)], 64, 4, 1, 64, seed=29)
+    picked = torch.full((b.T, 1, 3), -1, dtype=torch.int32)
+    picked[70:, 0, 1] = 0
+    got = slnr.selected_attention(b.q.cuda(), b.cache(), b.tables(), picked.cuda(), validate=True)
+    b.check(got, b.attention(0.125, picked))
+
+
+def test_chunk_with_fewer_keys_than_tokens(slnr):
+    """The first tokens of a chunk see nothing; a chunk without any key."""
+    b = P.Batch([(200, 150), (90, 0), (80, 80)], 16, 4, 2, 64, seed=30)
+    b.check(slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), validate=True), b.attention(0.125))
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2])
+def test_chunk_scales(slnr, scale):
+    b = P.Batch([(70, 400)], 16, 2, 1, 64, FP16, seed=31)
+    b.q = (b.q.float() * 0.25).to(FP16)
+    b.check(slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), scale=scale), b.attention(scale))
+
+
+def test_out_of_any_alignment(slnr):
+    """An output on a 16-byte boundary that is none of 32, and widths whose rows are not whole sectors."""
+    for D in (64, 40, 8):
+        b = P.Batch([(90, 300)], 16, 2, 1, D, seed=D)
+        room = torch.zeros(b.T * 2 * D + 8, dtype=BF16, device="cuda")
+        out = room[8:].view(b.T, 2, D)
+        got = slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), out=out)
+        b.check(got, b.attention(D ** -0.5))
+        assert (room[:8] == 0).all()
+
+
+@pytest.mark.parametrize("selected", [False, True])
+def test_chunk_graph_and_stream(slnr, selected):
+    """The launches of a chunk, which wait for one another on the device, captured and replayed on another stream."""
+    b = P.Batch([(100, 700), (1, 90)], 64, 4, 2, 64, seed=32)
+    picked = P.picks(b, 4, seed=33)
+    cache, tables, q, pd = b.cache(), b.tables(), torch.zeros_like(b.q).cuda(), picked.cuda()
+    call = (lambda: slnr.selected_attention(q, cache, tables, pd)) if selected else \
+        (lambda: slnr.paged_attention(q, cache, tables))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = call()
+        q.copy_(b.q)
+        for _ in range(3):
+            graph.replay()
+    side.synchronize()
+    b.check(got, b.attention(0.125, picked if selected else None))
+
+
+@pytest.mark.parametrize("selected", [False, True])
+def test_calls_after_one_another_share_a_workspace(slnr, selected):
+    """Calls of different sizes back to back on one workspace: none sees what another left there."""
+    batches = [P.Batch(lens, 64, 4, 2, 64, seed=40 + i) for i, lens in
+               enumerate([[(100, 700)], [(1, 3000)], [(300, 310), (2, 50)], [(70, 2000)], [(1, 5)], [(90, 90)]])]
+    ws = slnr.Workspace()
+    picked = [P.picks(b, 4, seed=50 + i) for i, b in enumerate(batches)]
+    on_gpu = [(b.q.cuda(), b.cache(), b.tables(), p.cuda()) for b, p in zip(batches, picked)]
+    torch.cuda.synchronize()
+    got = [slnr.selected_attention(q, c, t, p, workspace=ws) if selected else slnr.paged_attention(q, c, t, workspace=ws)
+           for _ in range(2) for q, c, t, p in on_gpu]
+    for i, b in enumerate(batches):
+        ref = b.attention(0.125, picked[i] if selected else None)
+        b.check(got[i], ref, f"call {i}")
+        b.check(got[i + len(batches)], ref, f"call {i} again")
+
+
+def test_short_wait_limit_reports_timeout(slnr):
+    """The tensor-core kernel's bounded waits: with a limit far below a step's time a validated call returns
+    SLNR_ERR_TIMEOUT, and the next call with the default limit is right."""
+    import ctypes
+    b = P.Batch([(200, 1500)], 16, 4, 1, 64, seed=34)
+    args, ref = (b.q.cuda(), b.cache(), b.tables()), b.attention(0.125)
+    lib = slnr.lib()
+    assert lib.slnr_set_wait_limit(ctypes.c_int64(100)) == 0
+    try:
+        with pytest.raises(slnr.SlnrError) as e:
+            slnr.paged_attention(*args, validate=True)
+        assert e.value.status == 7, str(e.value)
+        assert slnr.device_flags() & 16
+    finally:
+        assert lib.slnr_set_wait_limit(ctypes.c_int64(0)) == 0
+    b.check(slnr.paged_attention(*args, validate=True), ref)
+    assert slnr.device_flags() == 0
+
+
+def test_malformed_tables_are_reported(slnr):
+    """Validate mode: a page outside the cache, too many keys, positions that do not add up, picked pages out of order."""
+    b = P.Batch([(2, 100), (1, 30)], 16, 2, 1, 64, seed=35)
+    q, cache = b.q.cuda(), b.cache()
+
+    def refused(picked=None, **kw):
+        with pytest.raises(slnr.SlnrError) as e:
+            if picked is None:
+                slnr.paged_attention(q, cache, b.tables(**kw), validate=True)
+            else:
+                slnr.selected_attention(q, cache, b.tables(**kw), picked, validate=True)
+        assert e.value.status == 3, str(e.value)
+
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    for bad in (-1, b.npages):
+        table = b.table.clone()
+        table[1, 1] = bad
+        refused(table=table.cuda())
+    refused(k_len=i32([100, 113]))
+    refused(k_len=i32([100, -1]))
+    refused(q_pos=i32([0, 1, 2]))
+    refused(q_pos=i32([1, 2, 3]))
+    refused(q_pos=i32([0, 4, 3]))
+    refused(req=i32([0, 1, 1]))
+    refused(max_q=1)
+    refused(picked=i32([[[3, 2]], [[0, 1]], [[0, 1]]]))
+    refused(picked=i32([[[1, 1]], [[0, 1]], [[0, 1]]]))
+    refused(picked=i32([[[0, 99]], [[0, 1]], [[0, 1]]]))
+
+
+def test_wrapper_refusals(slnr):
+    b = P.Batch([(2, 40)], 16, 4, 2, 64, seed=36)
+    q, cache, tables = b.q.cuda(), b.cache(), b.tables()
+    for bad in (b.q, q.half(), q.float(), q[:1], q[:, :, :32], q.transpose(1, 2), q[:, :3]):
+        with pytest.raises((ValueError, slnr.SlnrError)):
+            slnr.paged_attention(bad, cache, tables)
+    with pytest.raises(ValueError):
+        slnr.paged_attention(q, cache, tables, out=torch.empty_like(q).half())
+    with pytest.raises(ValueError):
+        slnr.paged_attention(q, cache, tables, lse=torch.empty((2, 4), device="cuda", dtype=torch.float64))
+    with pytest.raises(ValueError):
+        slnr.selected_attention(q, cache, tables, torch.zeros((2, 2, 3), device="cuda", dtype=torch.int64))
+    with pytest.raises(ValueError):
+        slnr.selected_attention(q, cache, tables, torch.zeros((2, 2, 0), device="cuda", dtype=torch.int32))
+    with pytest.raises(ValueError):
+        slnr.page_select(q, cache, tables, 4)  # no summaries
+    with pytest.raises(ValueError):
+        slnr.page_append(cache, tables, b.k[0], b.v[0])  # no slots
+    with pytest.raises(ValueError):
+        b.tables(q_pos=b.q_pos.long().cuda())
+    with pytest.raises(ValueError):
+        b.tables(table=b.table.cuda().t())
+    with pytest.raises(slnr.SlnrError) as e:
+        slnr.paged_attention(q, cache, b.tables(max_k=49))
+    assert e.value.status == 2
+    with pytest.raises(ValueError):
+        slnr.PagedCache(k=b.kd, v=b.vd.transpose(1, 3))

@@ -195,3 +195,50 @@ def test_select_all_codes(slnr):
     cache = slnr.PagedCache(codes=codes.cuda(), scales=scales.cuda(), page_size=4)
     got = slnr.page_select(b.q.cuda(), cache, b.tables(), 31, validate=True)
     assert torch.equal(got.cpu(), plain_select(b, codes, scales, 31, 1, 2))
+
+
+def test_select_long_requests(slnr):
+    """So many pages that a block holds two tokens' scores, and one's."""
+    for n in (20000, 40000):
+        b = P.Batch([(5, n), (1, 700)], 1, 2, 1, 8, seed=4)
+        codes = torch.randint(-127, 128, (b.npages, 1, 8), generator=b.g).to(torch.int8)
+        scales = torch.rand((b.npages, 1), generator=b.g)
+        cache = slnr.PagedCache(codes=codes.cuda(), scales=scales.cuda(), page_size=1)
+        got = slnr.page_select(b.q.cuda(), cache, b.tables(), 20, validate=True)
+        assert torch.equal(got.cpu(), plain_select(b, codes, scales, 20, 1, 2))
+
+
+def test_select_scores_that_are_not_finite(slnr):
+    """Scales of NaN and infinity: no page twice, the forced ones there, nothing outside."""
+    b = P.Batch([(3, 900)], 16, 2, 1, 64, seed=5)
+    codes = torch.randint(-9, 10, (b.npages, 1, 64), generator=b.g).to(torch.int8)
+    scales = torch.rand((b.npages, 1), generator=b.g)
+    scales[::3], scales[1::7] = math.nan, math.inf
+    got = slnr.page_select(b.q.cuda(), b.cache(codes=codes.cuda(), scales=scales.cuda()), b.tables(), 9).cpu()
+    for t in range(3):
+        own = int(b.pos[t]) // 16
+        pages = [p for p in got[t, 0].tolist() if p >= 0]
+        assert pages == sorted(set(pages)) and pages[0] == 0 and pages[-2:] == [own - 1, own]
+
+
+def test_append_refuses_more_tokens_than_keys(slnr):
+    b = P.Batch([(3, 3)], 4, 1, 1, 8)
+    ones = torch.ones((3, 1, 8), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(slnr.SlnrError) as e:
+        slnr.page_append(b.cache(), b.tables(slots=i32([0, 1, 2]), k_len=i32([2])), ones, ones, validate=True)
+    assert e.value.status == 3
+
+
+def test_tables_on_another_stream_and_in_a_wider_table(slnr):
+    """A table that is a slice of a wider one, on a stream of its own."""
+    wide = torch.full((2, 30), 77, dtype=torch.int32, device="cuda")
+    wide[:, 4:10] = -1
+    new, old, free = i32([20, 3]), i32([0, 0]), i32([5, 3, 8, 1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    t, used = slnr.page_tables(new, old, wide[:, 4:10], free, 16, 23, stream=side)
+    side.synchronize()
+    assert wide[0].tolist() == [77] * 4 + [5, 3] + [-1] * 4 + [77] * 20
+    assert wide[1].tolist() == [77] * 4 + [8] + [-1] * 5 + [77] * 20
+    assert t.slots.tolist() == [5 * 16 + i for i in range(16)] + [48 + i for i in range(4)] + [128, 129, 130]
+    assert used.tolist() == [3]
