@@ -281,9 +281,10 @@ slnr_status slnr_spmm_gemm_original(const slnr_csr *B, const float *C, int32_t K
  *    request include its new tokens, so new token i of n lies at position
  *    k_len[r] - n + i and sees the keys up to that position.  A token at a
  *    negative position sees none: its output is zero, its lse -inf.
- *  - Slots past a request's last key, and pages not in use, are not read.
- *    A key or value that is not finite makes the rows that see it, and the
- *    rows of the same block that do not see it yet, not finite.
+ *  - Slots past a request's last key, and pages not in use, may hold anything.
+ *    A key or value that is not finite makes the rows that see it not finite,
+ *    and can do so to rows of the same request that do not see it (a token
+ *    before it in the same call, a token that did not pick its page).
  *  - q_pos, k_len, tables, req and slots are trusted without opts->validate; a page
  *    outside the cache is then not read or written, what its keys add to a
  *    result is not defined.
@@ -368,7 +369,7 @@ slnr_status slnr_page_select(const slnr_rows *q, int32_t nheads_q, const slnr_ca
 /* ---- attention over all pages, and over picked ones ------------------------
  * out[t, h] = sum_j softmax_j(scale q[t, h] . K[j]) V[j] over the keys j that
  * token t sees (slnr_selected_attention: those in the pages that picked[t,
- * h div group] lists, which are distinct; negative entries are none), lse[t, h]
+ * h div group] lists, ascending; negative entries, anywhere, are none), lse[t, h]
  * = log sum_j exp(scale q . K[j]) (natural; may be NULL).  out has the cache's
  * type, [ntok][nheads_q][head_dim]; lse is fp32 [ntok][nheads_q]. */
 slnr_status slnr_paged_attention_workspace(const slnr_cache *cache, const slnr_pages *pages, int32_t nheads_q,

@@ -150,7 +150,7 @@ AttnPlan attn_plan(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, i
   }
   const int64_t rows = npicked > 0 ? G : p.max_q * G;
   a.tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-  const int64_t tiles = npicked > 0 ? p.ntok * ceil_div(G, a.tile) : p.ntok * G / a.tile + requests;
+  const int64_t tiles = npicked > 0 ? p.ntok * ceil_div(G, a.tile) : p.nreq;
   const int64_t keys = npicked > 0 ? (int64_t)npicked * c.page_size : p.max_k;
   const int64_t blocks = tiles * c.nheads;
   int64_t chunk = keys;

@@ -8,8 +8,8 @@
 // to the cache's type for the product with V (their sum is not): the error of
 // one rounding of the output.
 //
-// A block takes one key head and up to 16 WM rows (the query rows of that
-// head's group, token after token) and streams its keys through shared memory,
+// A block takes one key head and a request's rows (the query rows of that head's
+// group, token after token; 16 WM at most), or with picked pages a token's, and streams its keys through shared memory,
 // 64 at a time, by asynchronous 16-byte copies; each thread finds one key's row
 // of K or V by its page, three steps ahead, and all read the rows' offsets from
 // shared memory.  Few rows are split over their keys: up to 16 splits are the
@@ -106,11 +106,12 @@ k_paged_rows(AttnArgs a) {
     q0 = __ldg(p.q_pos + r);
     x0 = (t - q0) * G + (blockIdx.x - t * per) * tile;
   } else {
-    find_tile(p, G, tile, blockIdx.x, r, x0);
-    if (r < 0) return;
+    r = blockIdx.x;  // its rows fit a tile
+    x0 = 0;
     q0 = __ldg(p.q_pos + r);
   }
   qn = __ldg(p.q_pos + r + 1) - q0;
+  if (!SEL && qn == 0) return;
   const int n = SEL ? min(tile, G - x0 % G) : min(tile, qn * G - x0);
   const int shift = __ldg(p.k_len + r) - qn;  // position of the request's first new token
   const int p_first = shift + a.group.div(x0), p_last = shift + a.group.div(x0 + n - 1);
@@ -430,8 +431,7 @@ k_paged_combine(AttnArgs a) {
   int splits = a.plan.nsplit;
   if (!a.picked) {
     const int q0 = __ldg(p.q_pos + r), qn = __ldg(p.q_pos + r + 1) - q0;
-    const int x = (t - q0) * G + g, last = min((x / a.plan.tile + 1) * a.plan.tile, qn * G) - 1;
-    const int end = __ldg(p.k_len + r) - qn + last / G + 1;
+    const int end = __ldg(p.k_len + r) - qn + (min(a.plan.tile, qn * G) - 1) / G + 1;
     splits = end > 0 ? (end - 1) / a.plan.chunk + 1 : 1;
   }
   if (splits == 1) return;

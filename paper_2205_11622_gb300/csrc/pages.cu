@@ -1,7 +1,7 @@
 // Block tables, slot maps and the cache's writes: the parts of a step over a
 // paged cache that come before its attention.
 #include "launch.h"
-#include "paged.cuh"
+#include "paged_tile.cuh"
 
 namespace slnr {
 namespace {
@@ -135,31 +135,19 @@ __global__ void __launch_bounds__(kAppendThreads)
 k_page_append(PagesView p, CacheView c, RowsView kn, RowsView vn, Divisor pieces) {
   __shared__ float s_sum[kAppendThreads][9];  // a thread's 8 columns
   const int tid = threadIdx.x, lane = tid & 31, h = blockIdx.y;
-  // request and page of flat page blockIdx.x: 32 requests a step, in every warp
-  int r = -1, nth = 0, before = 0;
-  for (int r0 = 0; r0 < p.nreq; r0 += 32) {
-    int n = 0;
-    if (r0 + lane < p.nreq) {
-      const int q = __ldg(p.q_pos + r0 + lane + 1) - __ldg(p.q_pos + r0 + lane);
-      n = pages_touched(__ldg(p.k_len + r0 + lane) - q, q, c.page);
-    }
-    int sum = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += y;
-    }
-    const unsigned past = __ballot_sync(0xffffffffu, before + sum > (int)blockIdx.x);
-    if (past) {
-      const int i = __ffs(past) - 1;
-      r = r0 + i;
-      nth = blockIdx.x - before - __shfl_sync(0xffffffffu, sum - n, i);
-      break;
-    }
-    before += __shfl_sync(0xffffffffu, sum, 31);
-  }
+  // request and which of its pages: at most one new token each, or parts counted request after request
+  int r = blockIdx.x, nth = 0;
+  if (p.max_q > 1)
+    find_part(
+        p.nreq, blockIdx.x,
+        [&](int i) {
+          const int q = __ldg(p.q_pos + i + 1) - __ldg(p.q_pos + i);
+          return pages_touched(__ldg(p.k_len + i) - q, q, c.page);
+        },
+        r, nth);
   if (r < 0) return;
   const int s = c.page.d, q0 = __ldg(p.q_pos + r), qn = __ldg(p.q_pos + r + 1) - q0;
+  if (qn <= 0) return;
   const int old = max(__ldg(p.k_len + r) - qn, 0);
   // tokens [t0, t1) at positions from `at` on, slots [at % s, ..) of their page
   const int page0 = c.page.div(old) + nth, at = max(old, page0 * s);
@@ -335,7 +323,7 @@ cudaError_t launch_page_tables(int nreq, const int32_t* new_len, const int32_t* 
 cudaError_t launch_page_append(const PagesView& p, const CacheView& c, const RowsView& k, const RowsView& v, int dtype,
                                cudaStream_t s) {
   if (p.ntok == 0) return cudaSuccess;
-  const int64_t pages = p.ntok / c.page.d + 2 * (int64_t)(p.nreq < p.ntok ? p.nreq : p.ntok);
+  const int64_t pages = p.max_q > 1 ? p.ntok / c.page.d + 2 * (int64_t)(p.nreq < p.ntok ? p.nreq : p.ntok) : p.nreq;
   if (pages >= (int64_t(1) << 31)) return cudaErrorInvalidConfiguration;
   const dim3 grid((unsigned)pages, (unsigned)c.nheads);
   auto kernel = dtype == SLNR_FP16 ? k_page_append<__half> : k_page_append<__nv_bfloat16>;

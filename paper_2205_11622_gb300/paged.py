@@ -144,17 +144,18 @@ def _rows(x, name, cache, heads, ntok, dtype=None):
     return slnr_rows(x.data_ptr(), x.stride(0) if ntok > 1 else 0, x.stride(1) if x.shape[1] > 1 else 0)
 
 
-def _empty(shape, dtype, device, stream):
-    """An output: of the stream that it is written on, so that its memory is not given to others before."""
+def _empty(like, shape, dtype, stream):
+    """An output beside `like`: of the stream that it is written on, so that its memory is not given to others before."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape) if like.dtype == dtype else like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _out(out, name, shape, dtype, device, stream):
+def _out(out, name, like, shape, dtype, stream):
     if out is None:
-        return _empty(shape, dtype, device, stream)
+        return _empty(like, shape, dtype, stream)
+    device = like.device
     if out.shape != shape or out.dtype != dtype or out.device != device or not out.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}")
     return out
@@ -209,8 +210,8 @@ def page_tables(new_len, old_len, table, free_pages, page_size, ntok, max_q=None
     what a row of the table holds)."""
     R, width, stride = _table(table)
     dev, n = table.device, free_pages.shape[0]
-    ints = _empty(2 * R + 2 + 2 * ntok, torch.int32, dev, stream)
-    q_pos, k_len, used, req, slots = ints.split((R + 1, R, 1, ntok, ntok))
+    ints = _empty(table, 2 * R + 2 + 2 * ntok, torch.int32, stream)
+    q_pos, k_len, used, req, slots = ints.split_with_sizes((R + 1, R, 1, ntok, ntok))
     at = ints.data_ptr()
     at_k, at_req = at + 4 * (R + 1), at + 4 * (2 * R + 2)
     at_slots = at_req + 4 * ntok
@@ -246,7 +247,7 @@ def page_select(q, cache: PagedCache, tables: PageTables, npicked, first=1, last
         c = slnr_cache.from_buffer_copy(c)
         c.dtype = _TYPES[q.dtype]
     rows = _rows(q, "q", cache, None, T, None if cache.k is None else cache.k.dtype)
-    out = _out(out, "out", (T, c.nheads, npicked), torch.int32, cache.device, stream)
+    out = _out(out, "out", tables.req, (T, c.nheads, npicked), torch.int32, stream)
     args = (_byref(rows), q.shape[1], _byref(c), _byref(tables._c), out.data_ptr(), npicked, first, last)
     _call("slnr_page_select", args, cache.device.index, 0, validate, workspace, stream,
           (q, cache.codes, cache.scales, tables.table, tables.q_pos, tables.k_len, tables.req, out))
@@ -274,8 +275,8 @@ def _attention(name, q, cache, tables, picked, npicked, scale, out, lse, validat
     shape = (T, heads_q, c.head_dim)
     need = _attention_bytes(c.npages, c.page_size, c.nheads, c.head_dim, c.dtype, p.nreq, T, p.max_q, p.max_k, p.width,
                             heads_q, npicked)
-    out = _out(out, "out", shape, q.dtype, cache.device, stream)
-    lse = _out(lse, "lse", shape[:2], torch.float32, cache.device, stream)
+    out = _out(out, "out", q, shape, q.dtype, stream)
+    lse = _out(lse, "lse", q, shape[:2], torch.float32, stream)
     scale = c.head_dim ** -0.5 if scale is None else scale
     head = (_byref(rows), heads_q, _byref(c), _byref(p))
     tail = (scale, out.data_ptr(), lse.data_ptr())

@@ -375,3 +375,31 @@ def test_wrapper_refusals(slnr):
     assert e.value.status == 2
     with pytest.raises(ValueError):
         slnr.PagedCache(k=b.kd, v=b.vd.transpose(1, 3))
+
+
+def test_no_room_for_keys(slnr):
+    """A table without columns: no request has a key."""
+    b = P.Batch([(3, 0), (1, 0)], 16, 4, 2, 64, seed=37)
+    for q in (1, 100):
+        t = b.tables(table=torch.empty((2, 0), dtype=torch.int32, device="cuda"), max_q=max(3, q), max_k=0)
+        out, lse = slnr.paged_attention(b.q.cuda(), b.cache(), t)
+        assert (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("lens", [[(1, 700), (2, 5)], [(100, 300)]])
+def test_without_lse(slnr, lens):
+    """The C entry point with no place for lse."""
+    import ctypes
+    from paper_2205_11622_gb300 import slnr_opts, slnr_rows
+    b = P.Batch(lens, 16, 4, 2, 64, seed=38)
+    cache, tables, q, lib, r = b.cache(), b.tables(), b.q.cuda(), slnr.lib(), ctypes.byref
+    out, ref = torch.zeros_like(q), b.attention(0.125)
+    o, need = slnr_opts(), ctypes.c_size_t()
+    assert lib.slnr_paged_attention_workspace(r(cache._c), r(tables._c), 4, r(o), r(need)) == 0
+    ws = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+    o.workspace, o.workspace_bytes, o.stream = ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream
+    rows = slnr_rows(q.data_ptr(), q.stride(0), q.stride(1))
+    assert lib.slnr_paged_attention(r(rows), 4, r(cache._c), r(tables._c), 0.125, out.data_ptr(), None, r(o)) == 0
+    b.check((out, ref[1].float()), ref)
+    o.workspace_bytes = need.value - 256
+    assert lib.slnr_paged_attention(r(rows), 4, r(cache._c), r(tables._c), 0.125, out.data_ptr(), None, r(o)) == 4
