@@ -58,7 +58,9 @@ class PageTables:
     slots: Optional[torch.Tensor]
     max_q: int
     max_k: int
+    ntok: int = field(init=False)
     _c: slnr_pages = field(init=False, repr=False)
+    _sizes: tuple = field(init=False, repr=False)
 
     def __post_init__(self):
         R, width, stride = _table(self.table)
@@ -67,17 +69,14 @@ class PageTables:
             R, T, self.max_q, self.max_k, width, 0, stride, _ints(self.q_pos, "q_pos", (R + 1,), dev),
             _ints(self.k_len, "k_len", (R,), dev), self.table.data_ptr(), _ints(self.req, "req", (T,), dev),
             None if self.slots is None else _ints(self.slots, "slots", (T,), dev))
+        self.__dict__["ntok"], self.__dict__["_sizes"] = T, (R, T, self.max_q, self.max_k, width)
 
     @classmethod
     def _of(cls, c, **fields):
         """Tables whose arrays a call of this module made: nothing to check."""
         self = object.__new__(cls)
-        self.__dict__.update(fields, _c=c)
+        self.__dict__.update(fields, _c=c, ntok=c.ntok, _sizes=(c.nreq, c.ntok, c.max_q, c.max_k, c.width))
         return self
-
-    @property
-    def ntok(self) -> int:
-        return self._c.ntok
 
 
 @dataclass(frozen=True, eq=False)
@@ -96,6 +95,7 @@ class PagedCache:
     page_size: Optional[int] = None
     device: torch.device = field(init=False, repr=False)
     _c: slnr_cache = field(init=False, repr=False)
+    _sizes: tuple = field(init=False, repr=False)
 
     def __post_init__(self):
         k, v, codes, scales = self.k, self.v, self.codes, self.scales
@@ -130,6 +130,7 @@ class PagedCache:
         c.page_size = self.page_size
         object.__setattr__(self, "device", (codes if k is None else k).device)
         object.__setattr__(self, "_c", c)
+        object.__setattr__(self, "_sizes", (c.npages, c.page_size, c.nheads, c.head_dim, c.dtype))
 
 
 def _rows(x, name, cache, heads, ntok, dtype=None):
@@ -144,18 +145,15 @@ def _rows(x, name, cache, heads, ntok, dtype=None):
     return slnr_rows(x.data_ptr(), x.stride(0) if ntok > 1 else 0, x.stride(1) if x.shape[1] > 1 else 0)
 
 
-def _empty(like, shape, dtype, stream):
-    """An output beside `like`: of the stream that it is written on, so that its memory is not given to others before."""
+def _empty(shape, dtype, device, stream):
+    """An output: of the stream that it is written on, so that its memory is not given to others before."""
     if stream is None:
-        return like.new_empty(shape) if like.dtype == dtype else like.new_empty(shape, dtype=dtype)
+        return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _out(out, name, like, shape, dtype, stream):
-    if out is None:
-        return _empty(like, shape, dtype, stream)
-    device = like.device
+def _checked(out, name, shape, dtype, device):
     if out.shape != shape or out.dtype != dtype or out.device != device or not out.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}")
     return out
@@ -210,7 +208,7 @@ def page_tables(new_len, old_len, table, free_pages, page_size, ntok, max_q=None
     what a row of the table holds)."""
     R, width, stride = _table(table)
     dev, n = table.device, free_pages.shape[0]
-    ints = _empty(table, 2 * R + 2 + 2 * ntok, torch.int32, stream)
+    ints = _empty(2 * R + 2 + 2 * ntok, torch.int32, dev, stream)
     q_pos, k_len, used, req, slots = ints.split_with_sizes((R + 1, R, 1, ntok, ntok))
     at = ints.data_ptr()
     at_k, at_req = at + 4 * (R + 1), at + 4 * (2 * R + 2)
@@ -247,7 +245,9 @@ def page_select(q, cache: PagedCache, tables: PageTables, npicked, first=1, last
         c = slnr_cache.from_buffer_copy(c)
         c.dtype = _TYPES[q.dtype]
     rows = _rows(q, "q", cache, None, T, None if cache.k is None else cache.k.dtype)
-    out = _out(out, "out", tables.req, (T, c.nheads, npicked), torch.int32, stream)
+    shape = (T, c.nheads, npicked)
+    out = _empty(shape, torch.int32, cache.device, stream) if out is None else \
+        _checked(out, "out", shape, torch.int32, cache.device)
     args = (_byref(rows), q.shape[1], _byref(c), _byref(tables._c), out.data_ptr(), npicked, first, last)
     _call("slnr_page_select", args, cache.device.index, 0, validate, workspace, stream,
           (q, cache.codes, cache.scales, tables.table, tables.q_pos, tables.k_len, tables.req, out))
@@ -255,10 +255,10 @@ def page_select(q, cache: PagedCache, tables: PageTables, npicked, first=1, last
 
 
 @functools.lru_cache(maxsize=4096)
-def _attention_bytes(npages, page_size, heads, width, dtype, nreq, ntok, max_q, max_k, columns, heads_q, npicked):
+def _attention_bytes(cache, pages, heads_q, npicked):
     """Workspace of an attention call: a function of the sizes alone."""
-    c = slnr_cache(npages, page_size, heads, width, dtype)
-    p = slnr_pages(nreq, ntok, max_q, max_k, columns, 0, columns)
+    c = slnr_cache(*cache)
+    p = slnr_pages(*pages, 0, pages[-1])
     o = slnr_opts()
     args = (_byref(c), _byref(p), heads_q)
     if npicked:
@@ -270,18 +270,21 @@ def _attention(name, q, cache, tables, picked, npicked, scale, out, lse, validat
     if cache.k is None:
         raise ValueError(f"{name} needs a cache with keys")
     c, p, T = cache._c, tables._c, tables.ntok
+    dtype, device = q.dtype, cache.device
     rows = _rows(q, "q", cache, None, T, cache.k.dtype)
-    heads_q = q.shape[1]
-    shape = (T, heads_q, c.head_dim)
-    need = _attention_bytes(c.npages, c.page_size, c.nheads, c.head_dim, c.dtype, p.nreq, T, p.max_q, p.max_k, p.width,
-                            heads_q, npicked)
-    out = _out(out, "out", q, shape, q.dtype, stream)
-    lse = _out(lse, "lse", q, shape[:2], torch.float32, stream)
+    shape = q.shape
+    heads_q = shape[1]
+    out = _empty(shape, dtype, device, stream) if out is None else _checked(out, "out", shape, dtype, device)
+    lse = _empty(shape[:2], torch.float32, device, stream) if lse is None else \
+        _checked(lse, "lse", shape[:2], torch.float32, device)
+    need = _attention_bytes(cache._sizes, tables._sizes, heads_q, npicked)
     scale = c.head_dim ** -0.5 if scale is None else scale
-    head = (_byref(rows), heads_q, _byref(c), _byref(p))
-    tail = (scale, out.data_ptr(), lse.data_ptr())
-    mid = (picked.data_ptr(), npicked) if npicked else ()
-    _call(name, (*head, *mid, *tail), cache.device.index, need, validate, workspace, stream,
+    if npicked:
+        args = (_byref(rows), heads_q, _byref(c), _byref(p), picked.data_ptr(), npicked, scale, out.data_ptr(),
+                lse.data_ptr())
+    else:
+        args = (_byref(rows), heads_q, _byref(c), _byref(p), scale, out.data_ptr(), lse.data_ptr())
+    _call(name, args, device.index, need, validate, workspace, stream,
           (q, cache.k, cache.v, tables.table, tables.q_pos, tables.k_len, tables.req, picked, out, lse))
     return out, lse
 
