@@ -28,6 +28,17 @@
 // While one tile's warps are at its weights, the tensor cores work on the
 // other's.  Keys in 128-byte swizzled rows serve both products: K as the
 // K-major operand of Q K^T, V as the MN-major one of P V.
+//
+// Measured (32 query and 8 key heads of 128, bf16): 4096 tokens over 16384 keys
+// 0.64 ms of kernel time, 1.5 PFLOP/s over the visible pairs; a step 3.4k
+// cycles, of which the products are 2.05k (both tiles, measured alone), and the
+// rest is the way from a product's end to the next one's start (barriers,
+// scores out of tensor memory, 16k exponentials a tile, weights back), of which
+// the other tile's products hide 1k.  Handing over half of the weights early
+// changed nothing.  With copies that their threads waited for 0.72 ms, with one
+// block an item 0.79, with a table lookup in each copying thread 3.3.
+// 2048 tokens over 16 picked pages of 64 each: 0.13 ms; the row kernel, which
+// reads every page once for every token, 1.29.
 #include <type_traits>
 
 #include "launch.h"
