@@ -137,6 +137,29 @@ __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
   return (uint32_t)((piece >> 3) * kBlock + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
 }
 
+// Two fp32 values in 64 bits: one instruction for both (0.65 -> 0.62 ms where the
+// header says 0.64).
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // Register shares of the calling warpgroup.
 template <int N>
 __device__ __forceinline__ void regs_up() {
@@ -781,17 +804,17 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           }
         }
         const float b = m == -INFINITY ? 0.f : m * sl2;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        uint64_t sum[2] = {0, 0};  // pairs of fp32
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint32_t w[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float off = SEL && !((picked >> (2 * k + e / 8)) & 1) ? -INFINITY : -b;
-            const float w0 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e]), sl2, off));
-            const float w1 = exp2_fast(fmaf(__uint_as_float(s[32 * k + 2 * e + 1]), sl2, off));
-            sum[(2 * e) & 3] += w0;
-            sum[(2 * e + 1) & 3] += w1;
+            const float2 x = unpack2(fma2(pack2(__uint_as_float(s[32 * k + 2 * e]), __uint_as_float(s[32 * k + 2 * e + 1])),
+                                          pack2(sl2, sl2), pack2(off, off)));
+            const float w0 = exp2_fast(x.x), w1 = exp2_fast(x.y);
+            sum[e & 1] = add2(sum[e & 1], pack2(w0, w1));
             w[e] = Half2<T>::pack(w0, w1);
           }
           tc::tmem_st16(col_s + 16 * k, w);
@@ -799,7 +822,8 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         tc::tmem_st_done();
         tc::tc_fence_before_sync();
         arrive_warp(&bars.p_full[t]);
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        const float2 total = unpack2(add2(sum[0], sum[1]));
+        l += total.x + total.y;
       }
       const bool keys = it.steps > 0;
       ring += 2 * it.steps;
