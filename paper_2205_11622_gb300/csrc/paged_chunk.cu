@@ -30,15 +30,18 @@
 // K-major operand of Q K^T, V as the MN-major one of P V.
 //
 // Measured (32 query and 8 key heads of 128, bf16): 4096 tokens over 16384 keys
-// 0.64 ms of kernel time, 1.5 PFLOP/s over the visible pairs; a step 3.4k
-// cycles, of which the products are 2.05k (both tiles, measured alone), and the
-// rest is the way from a product's end to the next one's start (barriers,
-// scores out of tensor memory, 16k exponentials a tile, weights back), of which
-// the other tile's products hide 1k.  Handing over half of the weights early
-// changed nothing.  With copies that their threads waited for 0.72 ms, with one
-// block an item 0.79, with a table lookup in each copying thread 3.3.
-// 2048 tokens over 16 picked pages of 64 each: 0.13 ms; the row kernel, which
-// reads every page once for every token, 1.29.
+// 0.62 ms of kernel time, 1.56 PFLOP/s over the visible pairs, bound by the way
+// from one of a tile's products to its next: a step takes 3.3k cycles, of which
+// a tile's own products are 1.03k and hide as much of the other tile's way.  The
+// rest is its weights (scores out of tensor memory 340, maximum 400, 128
+// exponentials a thread 1060, back 150), 290 from a product's end to the warps
+// that wait for it and 170 from theirs to the product.  What did not shorten it:
+// handing over the first half of the weights early; exponentials by polynomials
+// on the other pipes (a quarter of them 0.68 ms, half 0.83); more registers.
+// Copies that their threads wait for take 0.72 ms, a block an item 0.79, a table
+// lookup in each copying thread 3.3.  2048 tokens over 16 picked pages of 64
+// each: 0.13 ms; the row kernel, which reads every page once for every token,
+// 1.29.
 #include <type_traits>
 
 #include "launch.h"
@@ -137,8 +140,8 @@ __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
   return (uint32_t)((piece >> 3) * kBlock + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
 }
 
-// Two fp32 values in 64 bits: one instruction for both (0.65 -> 0.62 ms where the
-// header says 0.64).
+// Two fp32 values in 64 bits: one instruction for both (0.62 ms where single ones
+// took 0.65).
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
   uint64_t r;
   asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
