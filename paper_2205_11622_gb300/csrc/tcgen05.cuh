@@ -273,19 +273,12 @@ __device__ __forceinline__ void tmem_ld_done(uint32_t* r) {
                :
                : "memory");
 }
-// 16 and 32 columns of the thread's lane; done after tmem_st_done.
+// 16 columns of the thread's lane; done after tmem_st_done.
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
       "%15};" ::SLNR_W8(r, 0),
       SLNR_W8(r, 8), "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
-      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::SLNR_W8(r, 0),
-      SLNR_W8(r, 8), SLNR_W8(r, 16), SLNR_W8(r, 24), "r"(taddr)
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
