@@ -135,14 +135,15 @@ class PagedCache:
 
 def _rows(x, name, cache, heads, ntok, dtype=None):
     """slnr_rows of x [tokens, heads, width]: any strides that are multiples of 8 values, packed last axis."""
-    c = cache._c
-    if x.dim() != 3 or x.shape[0] != ntok or x.shape[2] != c.head_dim or (heads is not None and x.shape[1] != heads):
-        raise ValueError(f"{name} has shape {tuple(x.shape)}, not ({ntok}, {heads or 'heads'}, {c.head_dim})")
-    if x.device != cache.device or x.dtype not in _TYPES or (dtype is not None and x.dtype != dtype):
+    shape, strides, dt = x.shape, x.stride(), x.dtype
+    width = cache._c.head_dim
+    if len(shape) != 3 or shape[0] != ntok or shape[2] != width or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name} has shape {tuple(shape)}, not ({ntok}, {heads or 'heads'}, {width})")
+    if x.device != cache.device or dt not in _TYPES or (dtype is not None and dt != dtype):
         raise ValueError(f"{name} must be {dtype or 'a bf16 or fp16 tensor'} on {cache.device}")
-    if x.stride(2) != 1 and x.shape[2] > 1:
+    if strides[2] != 1 and width > 1:
         raise ValueError(f"the last axis of {name} must be packed")
-    return slnr_rows(x.data_ptr(), x.stride(0) if ntok > 1 else 0, x.stride(1) if x.shape[1] > 1 else 0)
+    return slnr_rows(x.data_ptr(), strides[0] if ntok > 1 else 0, strides[1] if shape[1] > 1 else 0)
 
 
 def _empty(shape, dtype, device, stream):
