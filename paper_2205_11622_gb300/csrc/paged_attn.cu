@@ -422,16 +422,21 @@ k_paged_rows(AttnArgs a) {
   }
 }
 
-// Rows of several splits: o = sum_s 2^(lse_s - m) o_s / sum_s 2^(lse_s - m), in
-// the splits' order.  A warp a row.
+// Rows of several splits: o = sum_s 2^(lse_s - m) o_s / sum_s 2^(lse_s - m).  A
+// block a row, every fourth split a warp: a long cache of few heads has hundreds
+// of splits, whose loads would follow one another in one warp: 32768 keys of one
+// key head of 128 and 16 query heads, 256 splits, 65 us a call with a warp a row,
+// 23 so.  Each warp adds its splits in their order, the warps' sums are added in
+// theirs.
 template <typename T>
 __global__ void __launch_bounds__(128)
 k_paged_combine(AttnArgs a) {
+  __shared__ float4 sums[4][32];
+  __shared__ float weights[4];
   wait_for_previous();
   const PagesView& p = a.p;
-  const int lane = threadIdx.x & 31, G = a.group.d;
-  const int64_t hq = (int64_t)a.c.nheads * G, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (at >= p.ntok * hq) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.group.d;
+  const int64_t hq = (int64_t)a.c.nheads * G, at = blockIdx.x;
   const int t = (int)(at / hq), g = (int)(at % hq) % G;
   const int r = __ldg(p.req + t);
   if (r < 0) return;
@@ -453,7 +458,7 @@ k_paged_combine(AttnArgs a) {
   float sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
+  for (int s = warp; s < splits; s += 4) {
     const float f = exp2_fast(lse[s] - b);
     sum += f;
     if (col < a.c.width) {
@@ -463,6 +468,19 @@ k_paged_combine(AttnArgs a) {
       acc.z += f * x.z;
       acc.w += f * x.w;
     }
+  }
+  sums[warp][lane] = acc;
+  if (lane == 0) weights[warp] = sum;
+  __syncthreads();
+  if (warp > 0) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+    const float4 x = sums[w][lane];
+    sum += weights[w];
+    acc.x += x.x;
+    acc.y += x.y;
+    acc.z += x.z;
+    acc.w += x.w;
   }
   const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);  // the parts of a row without keys are zeros
   if (col < a.c.width) {
@@ -531,8 +549,7 @@ cudaError_t launch_paged_rows(const AttnArgs& a, int dtype, cudaStream_t s) {
 }
 
 cudaError_t launch_paged_combine(const AttnArgs& a, int dtype, cudaStream_t s) {
-  const int64_t rows = (int64_t)a.p.ntok * a.c.nheads * a.group.d;
-  const unsigned grid = (unsigned)ceil_div(rows, 4);
+  const unsigned grid = (unsigned)((int64_t)a.p.ntok * a.c.nheads * a.group.d);
   auto kernel = dtype == SLNR_FP16 ? k_paged_combine<__half> : k_paged_combine<__nv_bfloat16>;
   return launch_next(kernel, SLNR_COUNTED(dim3(grid)), dim3(128), 0, s, a);
 }
