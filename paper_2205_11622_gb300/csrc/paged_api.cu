@@ -123,6 +123,7 @@ slnr_status validated(const slnr_opts* o, Launch launch) {
 constexpr int64_t kSms = 152;          // of one block of the tensor-core kernel, two of the row kernel's
 constexpr int64_t kMaxBlocks = 16384;  // splits stop here
 constexpr int64_t kMaxCluster = 16;
+constexpr int64_t kManyKeys = 1 << 19;
 
 // Whether picked pages go to the tensor-core kernel: steps of 128 keys are whole
 // pages or parts of one.
@@ -131,12 +132,18 @@ bool whole_steps(int page) { return page >= kChunkKeys ? page % kChunkKeys == 0 
 // Row tiles and key splits of an attention call: by the bounds alone, never by
 // device data.  Calls with a request of more than 64 rows go to the tensor-core
 // kernel (256 rows a block), the others to the row kernel; with picked pages its
-// blocks take the rows of one token.
+// blocks take the rows of one token.  From 33 to 64 rows the tensor-core kernel
+// also takes calls of many keys over all requests and key heads (us, key heads of
+// 128, 64 rows, row kernel and tensor-core kernel): 64 requests of 4096 keys, 8
+// heads, 408 and 294; 8 of 8192, 108 and 95; 32 of 1024, 58 and 57; but 1 of 32768
+// 57 and 69, 1 of 4096 28 and 32, where its longer way through a step shows.  With
+// 32 rows it has no such call (276 and 288).
 AttnPlan attn_plan(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, int32_t npicked) {
   AttnPlan a{};
   const int64_t G = nheads_q / c.nheads, requests = p.nreq < p.ntok ? p.nreq : p.ntok;
   a.nsplit = 1;
-  if (p.max_q * G > 64 && (npicked == 0 || whole_steps(c.page_size))) {
+  const bool many = p.max_q * G > 32 && npicked == 0 && (int64_t)p.nreq * c.nheads * p.max_k >= kManyKeys;
+  if ((p.max_q * G > 64 || many) && (npicked == 0 || whole_steps(c.page_size))) {
     a.tile = kChunkRows;
     const int64_t tiles = p.ntok * G / a.tile + requests;
     a.ntiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);

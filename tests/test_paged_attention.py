@@ -119,6 +119,17 @@ def test_bounds_wider_than_the_batch(slnr):
         b.check(slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(max_q=max_q, max_k=max_k)), ref, f"{max_q} {max_k}")
 
 
+@pytest.mark.parametrize("lens,heads", [([(9, 500), (1, 20)], (8, 2)), ([(33, 70), (0, 3), (40, 12), (64, 1030)], (2, 2)),
+                                        ([(5, 4000), (7, 3)], (8, 1))])
+@pytest.mark.parametrize("D", [64, 128])
+def test_short_chunks_of_many_keys(slnr, lens, heads, D):
+    """33 to 64 rows a request: the bound on the keys decides which kernel takes them."""
+    b = P.Batch(lens, 16, *heads, D, width=(1 << 19) // 16 // heads[1] // len(lens) + 1, seed=D + len(lens))
+    ref = b.attention(D ** -0.5)
+    for max_k in (4000, 16 * b.width - 16, 16 * b.width):
+        b.check(slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(max_k=max_k)), ref, f"{max_k}")
+
+
 @pytest.mark.parametrize("lens", [[(1, 3000)], [(300, 900)]])
 def test_same_call_same_bits(slnr, lens):
     b = P.Batch(lens, 16, 8, 2, 128, seed=11)
