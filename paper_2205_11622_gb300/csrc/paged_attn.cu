@@ -9,8 +9,8 @@
 // one rounding of the output.
 //
 // A block takes one key head and a request's rows (the query rows of that head's
-// group, token after token; 16 WM at most), or with picked pages a token's, and streams its keys through shared memory,
-// 64 at a time, by asynchronous 16-byte copies; each thread finds one key's row
+// group, token after token; 16 WM at most), or with picked pages a token's, and
+// streams its keys through shared memory, 64 at a time, by asynchronous 16-byte copies; each thread finds one key's row
 // of K or V by its page, three steps ahead, and all read the rows' offsets from
 // shared memory.  Few rows are split over their keys: up to 16 splits are the
 // blocks of a cluster, which join their results through each other's shared
