@@ -197,6 +197,20 @@ def test_select_all_codes(slnr):
     assert torch.equal(got.cpu(), plain_select(b, codes, scales, 31, 1, 2))
 
 
+@pytest.mark.parametrize("lens", [[(1, 9000), (1, 5000), (1, 30), (0, 7)], [(1, 2800), (1, 400)] * 30, [(35, 9000), (2, 600)]])
+@pytest.mark.parametrize("n", [19, 20, 60, 99, 100, 300])
+@pytest.mark.parametrize("levels", [2, 127])
+def test_select_many(slnr, lens, n, levels):
+    """Single tokens of few and of many requests, and chunks, over hundreds of pages; few and many taken, with and without
+    equal scores."""
+    b = P.Batch(lens, 4, 8, 4, 128, seed=n)
+    codes = torch.randint(-levels, levels + 1, (b.npages, 4, 128), generator=b.g).to(torch.int8)
+    scales = torch.randint(0, levels + 1, (b.npages, 4), generator=b.g).float()
+    cache = slnr.PagedCache(codes=codes.cuda(), scales=scales.cuda(), page_size=4)
+    got = slnr.page_select(b.q.cuda(), cache, b.tables(), n, validate=True)
+    assert torch.equal(got.cpu(), plain_select(b, codes, scales, n, 1, 2))
+
+
 def test_select_long_requests(slnr):
     """So many pages that a block holds two tokens' scores, and one's."""
     for n in (20000, 40000):
