@@ -309,11 +309,15 @@ class DeviceCSF3:
 
 
 class Workspace:
-    """Caller-owned device scratch for the library, grown on demand (one per stream)."""
+    """Caller-owned device scratch for the library, grown on demand (one per stream).
+
+    A buffer that a captured call was given is kept as long as the workspace, as the graph writes it on every replay;
+    the workspace has to outlive the graph."""
 
     def __init__(self, device="cuda"):
         self.device = device
         self.buf = None
+        self._captured = []
 
     def get(self, nbytes: int):
         torch = _torch()
@@ -321,6 +325,11 @@ class Workspace:
         if self.buf is None or self.buf.numel() < nbytes:
             self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return self.buf
+
+    def captured(self):
+        """Keep the present buffer for good: a graph holds its address."""
+        if not any(b is self.buf for b in self._captured):
+            self._captured.append(self.buf)
 
 
 _default_ws = {}
@@ -337,6 +346,42 @@ def device_flags(workspace=None) -> int:
     if buf is None:
         return 0
     return int(buf[12:16].view(_torch().int32).item())
+
+
+def _capturing(stream) -> bool:
+    """Whether the call's stream (None: the current one) is being captured in a graph."""
+    cuda = _torch().cuda
+    if stream is None:
+        return cuda.is_current_stream_capturing()
+    with cuda.stream(stream):
+        return cuda.is_current_stream_capturing()
+
+
+def _workspace_of(workspace, dev, s, capturing):
+    """The workspace of a call on stream s of device dev: the caller's, or the stream's own.  A graph holds the addresses
+    that its calls were given, and a later call may replace the stream's buffer by a larger one; so a captured call
+    without a workspace has one of its own, whose memory is the graph's."""
+    if workspace is None:
+        if capturing:
+            return Workspace(device=f"cuda:{dev}")
+        workspace = _default_ws.get((dev, s))
+        if workspace is None:
+            workspace = _default_ws.setdefault((dev, s), Workspace(device=f"cuda:{dev}"))
+    return workspace
+
+
+def _buffer(workspace, need, stream, capturing, grow):
+    """(buffer of `need` bytes of the workspace, None), or what grow(workspace, need) returns, on the call's stream."""
+    buf, short = getattr(workspace, "buf", None), None
+    if buf is None or buf.numel() < need:
+        if stream is None:
+            buf, short = grow(workspace, need)
+        else:  # of the stream that uses it, so that it is not given to others before that has ended
+            with _torch().cuda.stream(stream):
+                buf, short = grow(workspace, need)
+    if capturing and isinstance(workspace, Workspace):
+        workspace.captured()
+    return buf, short
 
 
 _VARIANTS = {"fused": FUSED, "unfused": UNFUSED, FUSED: FUSED, UNFUSED: UNFUSED}
@@ -384,18 +429,13 @@ def _run(name, B, args, sizes, variant, allow_tf32, validate, workspace, stream)
     """Call entry point `name` with the structure B, `args` and the options."""
     L = _lib if _lib is not None else lib()
     s = _stream_ptr(stream)
-    if workspace is None:
-        dev = _torch().cuda.current_device()
-        workspace = _default_ws.get((dev, s))
-        if workspace is None:
-            workspace = _default_ws.setdefault((dev, s), Workspace(device=f"cuda:{dev}"))
+    capturing = _capturing(stream)
+    workspace = _workspace_of(workspace, _torch().cuda.current_device(), s, capturing)
     v = _VARIANTS.get(variant)
     v = int(variant) if v is None else v
     tf32 = 1 if allow_tf32 else 0
     shape = (B.nrows, B.ncols, B.nnz) if isinstance(B, slnr_csr) else (*B.dim, B.nnz, B.nslices, B.nfibers)
-    need, buf, short = _ws_bytes(name, shape, sizes, v, tf32), getattr(workspace, "buf", None), None
-    if buf is None or buf.numel() < need:
-        buf, short = _room(workspace, need)
+    buf, short = _buffer(workspace, _ws_bytes(name, shape, sizes, v, tf32), stream, capturing, _room)
     o = slnr_opts(v, tf32, 1 if validate else 0, 0, s, buf.data_ptr(), buf.numel())
     _last_ws[0] = buf
     status = getattr(L, name)(ctypes.byref(B), *args, ctypes.byref(o))

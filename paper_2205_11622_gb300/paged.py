@@ -14,8 +14,8 @@ from typing import Optional
 
 import torch
 
-from . import (SlnrError, Workspace, _default_ws, _last_ws, _query, _stream_ptr, last_error, lib, slnr_cache, slnr_opts,
-               slnr_pages, slnr_rows)
+from . import (SlnrError, _buffer, _capturing, _last_ws, _query, _stream_ptr, _workspace_of, last_error, lib, slnr_cache,
+               slnr_opts, slnr_pages, slnr_rows)
 
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
@@ -162,17 +162,9 @@ def _checked(out, name, shape, dtype, device):
 
 def _scratch(need, index, s, workspace, stream):
     """A device buffer of `need` bytes: the caller's workspace, or this stream's."""
-    if workspace is None:
-        workspace = _default_ws.get((index, s))
-        if workspace is None:
-            workspace = _default_ws.setdefault((index, s), Workspace(device=f"cuda:{index}"))
-    buf = getattr(workspace, "buf", None)
-    if buf is None or buf.numel() < need:
-        if stream is None:
-            buf = workspace.get(need)
-        else:
-            with torch.cuda.stream(stream):
-                buf = workspace.get(need)
+    capturing = _capturing(stream)
+    workspace = _workspace_of(workspace, index, s, capturing)
+    buf, _ = _buffer(workspace, need, stream, capturing, lambda w, n: (w.get(n), None))
     _last_ws[0] = buf
     return buf
 
