@@ -311,12 +311,14 @@ class DeviceCSF3:
 class Workspace:
     """Caller-owned device scratch for the library, grown on demand (one per stream).
 
+    The launches of a call that uses it are made under its lock: threads that share a stream may share a workspace.
     A buffer that a captured call was given is kept as long as the workspace, as the graph writes it on every replay;
     the workspace has to outlive the graph."""
 
     def __init__(self, device="cuda"):
         self.device = device
         self.buf = None
+        self.lock = threading.Lock()
         self._captured = []
 
     def get(self, nbytes: int):
@@ -332,6 +334,7 @@ class Workspace:
             self._captured.append(self.buf)
 
 
+_lock_of_others = threading.Lock()  # of callers' workspaces that have none
 _default_ws = {}
 _last_ws = [None]
 
@@ -435,10 +438,13 @@ def _run(name, B, args, sizes, variant, allow_tf32, validate, workspace, stream)
     v = int(variant) if v is None else v
     tf32 = 1 if allow_tf32 else 0
     shape = (B.nrows, B.ncols, B.nnz) if isinstance(B, slnr_csr) else (*B.dim, B.nnz, B.nslices, B.nfibers)
-    buf, short = _buffer(workspace, _ws_bytes(name, shape, sizes, v, tf32), stream, capturing, _room)
-    o = slnr_opts(v, tf32, 1 if validate else 0, 0, s, buf.data_ptr(), buf.numel())
-    _last_ws[0] = buf
-    status = getattr(L, name)(ctypes.byref(B), *args, ctypes.byref(o))
+    need = _ws_bytes(name, shape, sizes, v, tf32)
+    # a call's launches follow one another on the stream: no other thread's come between them
+    with getattr(workspace, "lock", _lock_of_others):
+        buf, short = _buffer(workspace, need, stream, capturing, _room)
+        o = slnr_opts(v, tf32, 1 if validate else 0, 0, s, buf.data_ptr(), buf.numel())
+        _last_ws[0] = buf
+        status = getattr(L, name)(ctypes.byref(B), *args, ctypes.byref(o))
     if status != 0:
         raise short if short is not None and STATUS[status] == "SLNR_ERR_WORKSPACE" else \
             SlnrError(status, name, last_error())

@@ -14,8 +14,8 @@ from typing import Optional
 
 import torch
 
-from . import (SlnrError, _buffer, _capturing, _last_ws, _query, _stream_ptr, _workspace_of, last_error, lib, slnr_cache,
-               slnr_opts, slnr_pages, slnr_rows)
+from . import (SlnrError, _buffer, _capturing, _last_ws, _lock_of_others, _query, _stream_ptr, _workspace_of, last_error,
+               lib, slnr_cache, slnr_opts, slnr_pages, slnr_rows)
 
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
@@ -160,15 +160,6 @@ def _checked(out, name, shape, dtype, device):
     return out
 
 
-def _scratch(need, index, s, workspace, stream):
-    """A device buffer of `need` bytes: the caller's workspace, or this stream's."""
-    capturing = _capturing(stream)
-    workspace = _workspace_of(workspace, index, s, capturing)
-    buf, _ = _buffer(workspace, need, stream, capturing, lambda w, n: (w.get(n), None))
-    _last_ws[0] = buf
-    return buf
-
-
 def _call(name, args, index, need, validate, workspace, stream, tensors):
     """Call entry point `name` on device `index` with `need` bytes of workspace (0: none)."""
     if index != _device_now():
@@ -183,11 +174,16 @@ def _call(name, args, index, need, validate, workspace, stream, tensors):
     if validate and need < 256:
         need = 256
     if need:
-        buf = _scratch(need, index, s, workspace, stream)
-        o = slnr_opts(0, 0, 1 if validate else 0, 0, s, buf.data_ptr(), buf.numel())
+        capturing = _capturing(stream)
+        workspace = _workspace_of(workspace, index, s, capturing)
+        # a call's launches follow one another on the stream: no other thread's come between them
+        with getattr(workspace, "lock", _lock_of_others):
+            buf, _ = _buffer(workspace, need, stream, capturing, lambda w, n: (w.get(n), None))
+            _last_ws[0] = buf
+            status = getattr(lib(), name)(*args, _byref(slnr_opts(0, 0, 1 if validate else 0, 0, s, buf.data_ptr(),
+                                                                  buf.numel())))
     else:
-        o = slnr_opts(0, 0, 0, 0, s, None, 0)
-    status = getattr(lib(), name)(*args, _byref(o))
+        status = getattr(lib(), name)(*args, _byref(slnr_opts(0, 0, 0, 0, s, None, 0)))
     if status != 0:
         raise SlnrError(status, name, last_error())
 

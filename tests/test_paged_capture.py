@@ -1,4 +1,4 @@
-"""Captured calls of attention over a paged cache, beside calls that the same stream makes later (GPU)."""
+"""Captured calls of attention over a paged cache beside calls that the same stream makes later, and threads that share one (GPU)."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -68,3 +68,29 @@ def test_graphs_of_one_stream_replayed_on_two(slnr):
     torch.cuda.synchronize()
     for b, (_, got, _) in zip(batches, made):
         b.check(got, b.attention(0.125))
+
+
+def test_threads_that_share_a_stream(slnr):
+    """Calls of several launches from several threads, all on the current stream and its workspace."""
+    import threading
+    batches = [P.Batch(lens, 16, 4, 2, 64, seed=70 + i) for i, lens in
+               enumerate([[(100, 700)], [(1, 9000)], [(300, 310), (2, 50)], [(90, 2000)]])]
+    on_gpu = [(b.q.cuda(), b.cache(), b.tables()) for b in batches]
+    torch.cuda.synchronize()
+    got = [[] for _ in batches]
+
+    def work(i):
+        for _ in range(20):
+            got[i].append(slnr.paged_attention(*on_gpu[i]))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(batches))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for b, results in zip(batches, got):
+        ref = b.attention(0.125)
+        assert len(results) == 20
+        for r in results:
+            b.check(r, ref)

@@ -1,4 +1,6 @@
 """Which device buffer a call is given: by the bookkeeping alone, with the library and the GPU faked (no GPU needed)."""
+import threading
+import time
 import weakref
 
 import pytest
@@ -107,3 +109,48 @@ def test_an_uncaptured_workspace_frees_what_it_outgrew(machine, call):
     old = weakref.ref(ws.buf)
     call(50000, ws)
     assert old() is None
+
+
+class Bare:
+    """A caller's workspace with get() alone."""
+
+    def __init__(self):
+        self.held = []
+
+    def get(self, need):
+        self.held.append(torch.empty(need, dtype=torch.uint8))
+        return self.held[-1]
+
+
+@pytest.mark.parametrize("workspace", [None, slnr.Workspace, Bare])
+def test_threads_of_a_stream_do_not_share_a_buffer_at_once(machine, call, workspace):
+    """A call is several launches that hand their results on in the workspace: those of two threads that use one stream
+    (all threads do, by default) may not mix."""
+    ws = workspace() if workspace else None
+    inside, mixed, calls = [], [], []
+
+    def entry(*args):
+        inside.append(1)
+        time.sleep(0.002)  # as a foreign call without the interpreter's lock
+        if len(inside) > 1:
+            mixed.append(len(inside))
+        calls.append(args[-1]._obj.workspace)
+        inside.pop()
+        return 0
+
+    machine.slnr_paged_attention = machine.slnr_spmm_gemm = entry
+    threads = [threading.Thread(target=lambda i=i: [call(1000 + 500 * i + k, ws) for k in range(5)]) for i in range(6)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(calls) == 30 and not mixed
+
+
+def test_a_refused_call_leaves_the_workspace_usable(machine, call):
+    machine.slnr_paged_attention = machine.slnr_spmm_gemm = lambda *args: 2
+    machine.slnr_last_error = lambda: b"refused"
+    for _ in range(2):
+        with pytest.raises(slnr.SlnrError) as e:
+            call(1000)
+        assert e.value.status == 2
