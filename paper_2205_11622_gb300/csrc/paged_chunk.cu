@@ -242,7 +242,11 @@ k_paged_union(AttnArgs a) {
   if (tid == 0) a.plan.npages[at] = min(total, a.plan.cap);
 }
 
-// What every role of a block knows of the part of an item that it works on.
+// What every role of a block knows of the part of an item that it works on.  What
+// is read of AttnPlan here and below was written by a kernel that may still run
+// when this one starts, so by plain loads behind wait_for_previous: read-only ones
+// (__ldg) are for data that no kernel writes meanwhile, and may be moved ahead of
+// the wait.
 struct Item {
   int h, r, x0, q0, n, tiles;  // key head, request, its first row and token, rows, tiles of 128
   int shift, last;             // position of the request's first new token, and of the last row's token
@@ -264,7 +268,7 @@ __device__ __forceinline__ Item item_of(const AttnArgs& a, int i, int ntiles, in
   Item it;
   it.h = i / ntiles;
   const int tile = i - it.h * ntiles;
-  const int4 x = __ldg(a.plan.tiles + 2 * tile), y = __ldg(a.plan.tiles + 2 * tile + 1);
+  const int4 x = a.plan.tiles[2 * tile], y = a.plan.tiles[2 * tile + 1];
   it.r = x.x;
   it.x0 = x.y;
   it.q0 = x.z;
@@ -274,7 +278,7 @@ __device__ __forceinline__ Item item_of(const AttnArgs& a, int i, int ntiles, in
   it.last = y.y;
   const int64_t at = (int64_t)it.h * a.plan.ntiles + tile;
   it.list = at * a.plan.cap;
-  const int end = SEL ? __ldg(a.plan.npages + at) * a.c.page.d : max(it.last + 1, 0);
+  const int end = SEL ? a.plan.npages[at] * a.c.page.d : max(it.last + 1, 0);
   const int all = steps_of(end);
   if (hi < 0) hi = all;
   it.u0 = min(lo * kChunkKeys, end);
@@ -451,10 +455,10 @@ __device__ __forceinline__ void write_row(const AttnArgs& a, const Item& it, Sha
 // Calls f(item) for the parts of items that are this block's.
 template <bool SEL, typename F>
 __device__ __forceinline__ void each_item(const AttnArgs& a, F f) {
-  const int c = blockIdx.x, n = __ldg(a.plan.shares + kChunkBlocks).x, items = __ldg(a.plan.shares + kChunkBlocks).y;
-  const int ntiles = __ldg(a.plan.shares + kChunkBlocks + 1).x;
+  const int c = blockIdx.x, n = a.plan.shares[kChunkBlocks].x, items = a.plan.shares[kChunkBlocks].y;
+  const int ntiles = a.plan.shares[kChunkBlocks + 1].x;
   if (c >= n) return;
-  const int2 from = __ldg(a.plan.shares + c), to = c + 1 < n ? __ldg(a.plan.shares + c + 1) : make_int2(items, 0);
+  const int2 from = a.plan.shares[c], to = c + 1 < n ? a.plan.shares[c + 1] : make_int2(items, 0);
   for (int i = from.x; i < to.x || (i == to.x && to.y > 0); ++i)
     f(item_of<SEL>(a, i, ntiles, i == from.x ? from.y : 0, i == to.x ? to.y : -1));
 }
@@ -521,7 +525,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         int id = -1, off = 0, next = -1;  // next: the listed page of the key after
         auto listed = [&](int j) {
           const int u = it.u0 + j * kChunkKeys + lt;
-          next = SEL && u < it.u1 ? __ldg(a.plan.pages + it.list + c.page.div(u)) : -1;
+          next = SEL && u < it.u1 ? a.plan.pages[it.list + c.page.div(u)] : -1;
         };
         auto find = [&](int j) {  // page and slot of this thread's key of step j
           const int u = it.u0 + j * kChunkKeys + lt;
@@ -891,13 +895,13 @@ template <typename T, bool SEL>
 __global__ void __launch_bounds__(128)
 k_paged_join(AttnArgs a) {
   wait_for_previous();
-  const int n = __ldg(a.plan.shares + kChunkBlocks).x, ntiles = __ldg(a.plan.shares + kChunkBlocks + 1).x;
+  const int n = a.plan.shares[kChunkBlocks].x, ntiles = a.plan.shares[kChunkBlocks + 1].x;
   const int c0 = blockIdx.x + 1;
   if (c0 >= n) return;
-  const int2 cut = __ldg(a.plan.shares + c0), before = __ldg(a.plan.shares + c0 - 1);
+  const int2 cut = a.plan.shares[c0], before = a.plan.shares[c0 - 1];
   if (cut.y == 0 || (before.x == cut.x && before.y > 0)) return;
   int c1 = c0 + 1;  // shares c0 .. c1 - 1 begin inside of the item
-  while (c1 < n && __ldg(a.plan.shares + c1).x == cut.x) ++c1;
+  while (c1 < n && a.plan.shares[c1].x == cut.x) ++c1;
   const Item it = item_of<SEL>(a, cut.x, ntiles, 0, -1);
   const int lane = threadIdx.x & 31, G = a.group.d, col = 4 * lane;
   constexpr int ROWS = kJoinRows / 4;

@@ -1,0 +1,20 @@
+"""What the sources of the paged-cache kernels have to keep to, where no run can show it (no GPU needed)."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2205_11622_gb300", "csrc")
+
+
+def code(name):
+    with open(os.path.join(CSRC, name)) as f:
+        return re.sub(r"//[^\n]*", "", f.read())
+
+
+def test_no_read_only_load_of_what_an_earlier_launch_of_the_call_writes():
+    """Kernels of a call start before the one ahead of them has ended and read the plan that it writes.  A read-only
+    (non-coherent) load wants data that nothing writes while the kernel runs, and may be moved ahead of the wait."""
+    for name in ("paged_chunk.cu", "paged_attn.cu", "paged_tile.cuh", "paged.cuh"):
+        text = code(name)
+        assert not re.search(r"__ldg\s*\(\s*(\([^()]*\)\s*)?&?a\.plan\b", text), name
+        assert "ld.global.nc" not in text, name
+        assert not re.search(r"const\s+\w+\s*\*\s*__restrict__[^;]*a\.plan", text), name
