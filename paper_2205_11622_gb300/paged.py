@@ -133,6 +133,11 @@ class PagedCache:
         object.__setattr__(self, "_sizes", (c.npages, c.page_size, c.nheads, c.head_dim, c.dtype))
 
 
+def _same_device(cache, tables, name):
+    if tables.table.device != cache.device:
+        raise ValueError(f"{name}: the tables are on {tables.table.device}, the cache is on {cache.device}")
+
+
 def _rows(x, name, cache, heads, ntok, dtype=None):
     """slnr_rows of x [tokens, heads, width]: any strides that are multiples of 8 values, packed last axis."""
     shape, strides, dt = x.shape, x.stride(), x.dtype
@@ -216,6 +221,7 @@ def page_append(cache: PagedCache, tables: PageTables, k, v, validate=False, wor
     (slnr_page_append); the cache's tensors are written in place."""
     if cache.k is None or tables.slots is None:
         raise ValueError("page_append needs a cache with keys, and tables with slots")
+    _same_device(cache, tables, "page_append")
     T, H, dt = tables.ntok, cache._c.nheads, cache.k.dtype
     args = (_byref(cache._c), _byref(tables._c), _byref(_rows(k, "k", cache, H, T, dt)),
             _byref(_rows(v, "v", cache, H, T, dt)))
@@ -229,6 +235,7 @@ def page_select(q, cache: PagedCache, tables: PageTables, npicked, first=1, last
     -1 behind.  The first `first` pages and the last `last` are always among them."""
     if cache.codes is None:
         raise ValueError("page_select needs a cache with summaries")
+    _same_device(cache, tables, "page_select")
     c, T = cache._c, tables.ntok
     if cache.k is None and q.dtype in _TYPES:
         c = slnr_cache.from_buffer_copy(c)
@@ -258,6 +265,7 @@ def _attention_bytes(cache, pages, heads_q, npicked):
 def _attention(name, q, cache, tables, picked, npicked, scale, out, lse, validate, workspace, stream):
     if cache.k is None:
         raise ValueError(f"{name} needs a cache with keys")
+    _same_device(cache, tables, name)
     c, p, T = cache._c, tables._c, tables.ntok
     dtype, device = q.dtype, cache.device
     rows = _rows(q, "q", cache, None, T, cache.k.dtype)
