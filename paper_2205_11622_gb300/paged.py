@@ -71,6 +71,10 @@ class PageTables:
             None if self.slots is None else _ints(self.slots, "slots", (T,), dev))
         self.__dict__["ntok"], self.__dict__["_sizes"] = T, (R, T, self.max_q, self.max_k, width)
 
+    def _tensors(self):
+        """What a call that takes the tables may read: held on the stream that it is given."""
+        return self.table, self.q_pos, self.k_len, self.req, self.slots
+
     @classmethod
     def _of(cls, c, **fields):
         """Tables whose arrays a call of this module made: nothing to check."""
@@ -226,7 +230,7 @@ def page_append(cache: PagedCache, tables: PageTables, k, v, validate=False, wor
     args = (_byref(cache._c), _byref(tables._c), _byref(_rows(k, "k", cache, H, T, dt)),
             _byref(_rows(v, "v", cache, H, T, dt)))
     _call("slnr_page_append", args, cache.device.index, 0, validate, workspace, stream,
-          (cache.k, cache.v, cache.codes, cache.scales, tables.slots, tables.req, tables.q_pos, k, v))
+          (cache.k, cache.v, cache.codes, cache.scales, k, v, *tables._tensors()))
 
 
 def page_select(q, cache: PagedCache, tables: PageTables, npicked, first=1, last=2, out=None, validate=False,
@@ -246,7 +250,7 @@ def page_select(q, cache: PagedCache, tables: PageTables, npicked, first=1, last
         _checked(out, "out", shape, torch.int32, cache.device)
     args = (_byref(rows), q.shape[1], _byref(c), _byref(tables._c), out.data_ptr(), npicked, first, last)
     _call("slnr_page_select", args, cache.device.index, 0, validate, workspace, stream,
-          (q, cache.codes, cache.scales, tables.table, tables.q_pos, tables.k_len, tables.req, out))
+          (q, cache.codes, cache.scales, out, *tables._tensors()))
     return out
 
 
@@ -282,7 +286,7 @@ def _attention(name, q, cache, tables, picked, npicked, scale, out, lse, validat
     else:
         args = (_byref(rows), heads_q, _byref(c), _byref(p), scale, out.data_ptr(), lse.data_ptr())
     _call(name, args, device.index, need, validate, workspace, stream,
-          (q, cache.k, cache.v, tables.table, tables.q_pos, tables.k_len, tables.req, picked, out, lse))
+          (q, cache.k, cache.v, picked, out, lse, *tables._tensors()))
     return out, lse
 
 

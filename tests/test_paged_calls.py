@@ -79,3 +79,15 @@ def test_tables_of_another_device(calls, entry):
     with pytest.raises(ValueError, match="tables are on cuda:1"):
         off[entry]()
     assert launched == [entry]
+
+
+@pytest.mark.parametrize("entry", ENTRIES)
+def test_tables_are_held_on_the_stream_of_the_call(calls, entry):
+    """Every tensor of the tables that a call may read is recorded on the stream that it is given: a caller may drop the
+    tables while the call is pending there, and each may be an allocation of its own."""
+    stream = SimpleNamespace(cuda_stream=0x20)
+    launched, tables, on = calls(HERE, stream)
+    on[entry]()
+    assert launched == [entry]
+    for name in FIELDS:
+        assert getattr(tables, name).recorded == [stream], name
