@@ -271,7 +271,8 @@ slnr_status slnr_spmm_gemm_original(const slnr_csr *B, const float *C, int32_t K
  * Conventions beside those at the top of this file:
  *  - Keys, values and queries are bf16 or fp16 (slnr_dtype), one type for a
  *    call; products, sums, maxima and weights' sums are fp32, the weights are
- *    rounded to that type before their product with the values.
+ *    rounded to that type before their product with the values: each by a share
+ *    of itself, in fp16 those of at least 2^-26 of a row's largest.
  *  - head_dim is a multiple of 8 in [8, 128]; query heads are a multiple of
  *    key heads, consecutive query heads share one.
  *  - Strides are in values, multiples of 8, the last axis is packed; base

@@ -46,7 +46,7 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr)
                : "memory");
 }
 
-// The two 16-bit types: product, packing of two fp32 values (rounded to nearest), and back.
+// The two 16-bit types: product, packing of two fp32 values (rounded to nearest).
 template <typename T>
 struct Half2;
 template <>

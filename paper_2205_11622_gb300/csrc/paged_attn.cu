@@ -6,7 +6,9 @@
 // over the keys j that the row sees.  One pass over the keys: m, the sum and o
 // are held in fp32 registers and rescaled when m grows.  The weights are rounded
 // to the cache's type for the product with V (their sum is not): the error of
-// one rounding of the output.
+// one rounding of the output.  fp16 rounds by a share of a weight down to 2^-14
+// only and to nothing below 2^-25, so there m - 14 takes m's place: weights of up
+// to 2^14, and what is lost of n small ones is n 2^-39 of the largest at most.
 //
 // A block takes one key head and a request's rows (the query rows of that head's
 // group, token after token; 16 WM at most), or with picked pages a token's, and
@@ -40,12 +42,21 @@ constexpr int stage_bytes() { return 2 * kAttnKeys * W * 2; }
 template <int W>
 constexpr size_t smem_bytes() { return (size_t)kStages * stage_bytes<W>(); }
 
+// What weights are taken against, from their scores' maximum (in powers of two): no
+// weight is above 2^14 in fp16, however large the maximum (rounded up).
+template <typename T>
+__device__ __forceinline__ float reference(float m);
+template <>
+__device__ __forceinline__ float reference<__nv_bfloat16>(float m) { return m; }
+template <>
+__device__ __forceinline__ float reference<__half>(float m) { return __fsub_ru(m, 14.f); }
+
 template <bool SEL>
 struct Smem {
   int64_t row[kOffsets][2][kAttnKeys];       // bytes from the head's first row of K and V to each key's; -1: zeros
   int key_at[SEL ? kOffsets : 1][kAttnKeys]; // selected: the keys' positions
   int2 pick[SEL ? kAttnMaxPicked : 1];       // selected: {page of the cache, page of the request}
-  float2 ml[4][16];                          // a warp's (maximum, sum) of each row
+  float2 ml[4][16];                          // a warp's (reference, sum) of each row
   float lse[64];                             // of the block's rows, in powers of two
   int count;
 };
@@ -284,8 +295,8 @@ k_paged_rows(AttnArgs a) {
       for (int j = 0; j < KW / 8; ++j) mx = fmaxf(mx, fmaxf(s[j][2 * i], s[j][2 * i + 1]));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      const float b = mx == -INFINITY ? 0.f : mx;  // no key seen yet: every weight is 2^-inf
-      scale_o[i] = exp2_fast(m[i] - b);
+      const float b = mx == -INFINITY ? 0.f : reference<T>(mx);  // no key seen yet: every weight is 2^-inf
+      scale_o[i] = exp2_fast(reference<T>(m[i]) - b);
       m[i] = mx;
       l[i] *= scale_o[i];
 #pragma unroll
@@ -328,7 +339,7 @@ k_paged_rows(AttnArgs a) {
     l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
     l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
     const int row = lane / 4 + 8 * i;
-    if ((lane & 3) == 0) sm.ml[warp][row] = make_float2(m[i], l[i]);
+    if ((lane & 3) == 0) sm.ml[warp][row] = make_float2(reference<T>(m[i]), l[i]);
 #pragma unroll
     for (int j = 0; j < W / 8; ++j)
       *reinterpret_cast<float2*>(rows + (warp * 16 + row) * (W + 4) + j * 8 + (lane & 3) * 2) =

@@ -14,7 +14,11 @@
 //       maximum, weights and their sum, weights back.  O is rescaled only where
 //       a row's maximum grew by more than 2^8 since the last time: until then
 //       its weights are taken against the older maximum, at most 256 each, and
-//       the sum is in the same units, so the quotient is the same;
+//       the sum is in the same units, so the quotient is the same (a published
+//       way to keep most steps free of it).  In fp16, which rounds by a share of
+//       a weight down to 2^-14 only and to nothing below 2^-25, they are taken
+//       against 2^-12 of the maximum, and it may grow by 2^3: at most 2^15 each,
+//       and what is lost of n small ones is n 2^-37 of the largest at most;
 //   1 MMA warp:  for each 128 keys and tile: O += P V, then the next S = Q K^T;
 //   4 load warps: Q once, then K and V into a ring of buffers of 128 keys by
 //       asynchronous 16-byte copies (any page size and stride), zeros past the
@@ -63,7 +67,12 @@ static_assert(kLoaders == kChunkKeys, "a load thread finds one key's row");
 constexpr int kBlock = kRows * 128;     // 128 rows of 64 values, swizzled
 constexpr int kTmemCols = 512;
 constexpr int kColS = 0, kColO = 256;   // S and P of tile t at 128 t, O at kColO + 128 t
-constexpr float kGrow = 8.f;            // growth of a maximum, in powers of two, that O is rescaled for
+// In powers of two: how far below the maximum weights are taken against, and the
+// growth of a maximum that O is rescaled for.
+template <typename T>
+constexpr float kBelow = std::is_same<T, __half>::value ? 12.f : 0.f;
+template <typename T>
+constexpr float kGrow = std::is_same<T, __half>::value ? 3.f : 8.f;
 
 template <int W>
 constexpr int tile_bytes() { return kBlock * (W / 64); }
@@ -407,7 +416,7 @@ __device__ __forceinline__ void store32(void* to, const uint32_t (&v)[8], bool a
 // A thread's row of the item, times inv (0: no key), with f_other times the other
 // warpgroup's where an item has one tile.  Whole 32-byte sectors a thread: as
 // fast as the memory system takes them, without shared memory in between.
-// m: maximum in powers of two, l: sum.
+// m: what weights were taken against, in powers of two, l: their sum.
 template <typename T, int W>
 __device__ __forceinline__ void write_row(const AttnArgs& a, const Item& it, Shared& sh, uint32_t (&o)[W], int x, int row,
                                           bool ok, float inv, float f_other, float m, float l) {
@@ -733,7 +742,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const int pos = row_on ? it.shift + tok : -1;
       const int pos_min = it.shift + a.group.div(it.x0 + x - row);  // of the tile's rows
       const bool tail = it.n - (x - row) < kRows;                   // rows that are none: their scores are dropped
-      float m = -INFINITY, l = 0.f;  // maximum of the scores that weights are taken against, sum of weights
+      float m = -INFINITY, l = 0.f;  // what weights are taken against (in powers of two), sum of weights
       // selected: the row's token in the tile
       const int tl = tok - a.group.div(it.x0), page_shift = c.page.d < kChunkKeys ? 31 - __clz(c.page.d) : 7;
       const int segs = kChunkKeys >> page_shift, per_page = kGroups / segs, own_page = c.page.div(max(pos, 0));
@@ -790,14 +799,14 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           for (int k = 1; k < 16; ++k) mx = fmaxf(mx, __uint_as_float(s[16 * g2 + k]));
           if (!SEL || ((picked >> g2) & 1)) top = fmaxf(top, mx);
         }
-        // the first keys that a row sees set m; later m moves only where it has to
-        const bool grow = (top - m) * sl2 > kGrow;  // m = -inf: true for any seen key
+        // the first keys that a row sees set m; later m moves only where it has to.  Rounded up: no weight of the highest
+        // score is above 2^kBelow, however large that is
+        const bool grow = fmaf(top, sl2, -m) > kBelow<T> + kGrow<T>;  // m = -inf: true for any seen key
         if (__any_sync(0xffffffffu, grow)) {
-          const float f = grow ? exp2_fast((m - top) * sl2) : 1.f;
-          if (grow) {
-            l *= f;
-            m = top;
-          }
+          const float to = grow ? __fmaf_ru(top, sl2, -kBelow<T>) : m;
+          const float f = grow ? exp2_fast(m - to) : 1.f;
+          if (grow) l *= f;
+          m = to;
           if (j > first) {
 #pragma unroll
             for (int k = 0; k < W / 16; ++k) {
@@ -810,7 +819,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
             }
           }
         }
-        const float b = m == -INFINITY ? 0.f : m * sl2;
+        const float b = m == -INFINITY ? 0.f : m;
         uint64_t sum[2] = {0, 0};  // pairs of fp32
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -837,7 +846,6 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       if (ok && keys) ok = wait_warp(&bars.o_full, count & 1, failed, limit);
       count += keys;
       tc::tc_fence_after_sync();
-      m = m == -INFINITY ? m : m * sl2;  // in powers of two from here on
       float f_other = 0.f;
       uint32_t o[W];
       read_row<W>(col_o, ok && it.steps > first, o);  // this warpgroup's O holds something from its first step on
