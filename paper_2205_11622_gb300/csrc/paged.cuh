@@ -158,8 +158,8 @@ cudaError_t launch_paged_plan(const AttnArgs& a, WsHeader* hdr, cudaStream_t s);
 cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s);
 cudaError_t launch_paged_join(const AttnArgs& a, int dtype, cudaStream_t s);
 
-// paged_attn.cu (any other plan)
-cudaError_t launch_paged_rows(const AttnArgs& a, int dtype, cudaStream_t s);
+// paged_attn.cu (any other plan); the first zeroes hdr's flag word
+cudaError_t launch_paged_rows(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s);
 cudaError_t launch_paged_combine(const AttnArgs& a, int dtype, cudaStream_t s);
 
 }  // namespace slnr

@@ -267,7 +267,7 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
     SLNR_LAUNCH("paged_chunk", launch_paged_chunk(a, cache->dtype, (WsHeader*)ws, s));
     SLNR_LAUNCH("paged_join", launch_paged_join(a, cache->dtype, s));
   } else {
-    SLNR_LAUNCH("paged_rows", launch_paged_rows(a, cache->dtype, s));
+    SLNR_LAUNCH("paged_rows", launch_paged_rows(a, cache->dtype, (WsHeader*)ws, s));
   }
   if (a.plan.nsplit > 1 && !a.plan.cluster) SLNR_LAUNCH("paged_combine", launch_paged_combine(a, cache->dtype, s));
   timing_end(s);

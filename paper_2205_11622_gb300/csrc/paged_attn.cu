@@ -105,7 +105,7 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, int64_t at, int col
 
 template <typename T, int W, int WM, bool SEL, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads)
-k_paged_rows(AttnArgs a) {
+k_paged_rows(AttnArgs a, WsHeader* hdr) {
   constexpr int WK = 4 / WM, KW = kAttnKeys / WK, PIECES = W / 8, ROWS = kThreads / PIECES;
   extern __shared__ __align__(128) unsigned char tiles[];
   __shared__ Smem<SEL> sm;
@@ -115,6 +115,7 @@ k_paged_rows(AttnArgs a) {
   const int G = a.group.d, h = blockIdx.y, tile = 16 * WM;
 
   if (!CLUSTER) let_next_start();  // k_paged_combine
+  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && tid == 0) hdr->error = 0;  // no wait here can give up
   // the block's rows: [x0, x0 + n) of request r and head h
   int r, x0, q0, qn;
   if (SEL) {
@@ -504,7 +505,7 @@ k_paged_combine(AttnArgs a) {
 }
 
 template <typename T, int W, int WM, bool SEL, bool CLUSTER>
-cudaError_t launch_rows(const AttnArgs& a, cudaStream_t s) {
+cudaError_t launch_rows(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
   auto kernel = k_paged_rows<T, W, WM, SEL, CLUSTER>;
   static_assert(4 * 16 * (W + 4) * 4 <= (int)smem_bytes<W>(), "the joined rows fit in the stages");
   static OncePerDevice once;
@@ -527,36 +528,37 @@ cudaError_t launch_rows(const AttnArgs& a, cudaStream_t s) {
     cfg.stream = s;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a);
+    return cudaLaunchKernelEx(&cfg, kernel, a, hdr);
   }
-  kernel<<<(SLNR_COUNTED(grid)), kThreads, smem_bytes<W>(), s>>>(a);
+  kernel<<<(SLNR_COUNTED(grid)), kThreads, smem_bytes<W>(), s>>>(a, hdr);
   return cudaGetLastError();
 }
 
 template <typename T, int W, int WM>
-cudaError_t launch_rows_m(const AttnArgs& a, cudaStream_t s) {
-  if (a.picked) return a.plan.cluster ? launch_rows<T, W, WM, true, true>(a, s) : launch_rows<T, W, WM, true, false>(a, s);
-  return a.plan.cluster ? launch_rows<T, W, WM, false, true>(a, s) : launch_rows<T, W, WM, false, false>(a, s);
+cudaError_t launch_rows_m(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
+  if (a.picked)
+    return a.plan.cluster ? launch_rows<T, W, WM, true, true>(a, hdr, s) : launch_rows<T, W, WM, true, false>(a, hdr, s);
+  return a.plan.cluster ? launch_rows<T, W, WM, false, true>(a, hdr, s) : launch_rows<T, W, WM, false, false>(a, hdr, s);
 }
 
 template <typename T, int W>
-cudaError_t launch_rows_w(const AttnArgs& a, cudaStream_t s) {
+cudaError_t launch_rows_w(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
   switch (a.plan.tile) {
-    case 16: return launch_rows_m<T, W, 1>(a, s);
-    case 32: return launch_rows_m<T, W, 2>(a, s);
-    default: return launch_rows_m<T, W, 4>(a, s);
+    case 16: return launch_rows_m<T, W, 1>(a, hdr, s);
+    case 32: return launch_rows_m<T, W, 2>(a, hdr, s);
+    default: return launch_rows_m<T, W, 4>(a, hdr, s);
   }
 }
 
 template <typename T>
-cudaError_t launch_rows_t(const AttnArgs& a, cudaStream_t s) {
-  return a.c.width <= 64 ? launch_rows_w<T, 64>(a, s) : launch_rows_w<T, 128>(a, s);
+cudaError_t launch_rows_t(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
+  return a.c.width <= 64 ? launch_rows_w<T, 64>(a, hdr, s) : launch_rows_w<T, 128>(a, hdr, s);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_rows(const AttnArgs& a, int dtype, cudaStream_t s) {
-  return dtype == SLNR_FP16 ? launch_rows_t<__half>(a, s) : launch_rows_t<__nv_bfloat16>(a, s);
+cudaError_t launch_paged_rows(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s) {
+  return dtype == SLNR_FP16 ? launch_rows_t<__half>(a, hdr, s) : launch_rows_t<__nv_bfloat16>(a, hdr, s);
 }
 
 cudaError_t launch_paged_combine(const AttnArgs& a, int dtype, cudaStream_t s) {

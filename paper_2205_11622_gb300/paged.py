@@ -229,7 +229,7 @@ def page_append(cache: PagedCache, tables: PageTables, k, v, validate=False, wor
     T, H, dt = tables.ntok, cache._c.nheads, cache.k.dtype
     args = (_byref(cache._c), _byref(tables._c), _byref(_rows(k, "k", cache, H, T, dt)),
             _byref(_rows(v, "v", cache, H, T, dt)))
-    _call("slnr_page_append", args, cache.device.index, 0, validate, workspace, stream,
+    _call("slnr_page_append", args, cache.device.index, 0, validate and T > 0, workspace, stream,
           (cache.k, cache.v, cache.codes, cache.scales, k, v, *tables._tensors()))
 
 
@@ -249,7 +249,7 @@ def page_select(q, cache: PagedCache, tables: PageTables, npicked, first=1, last
     out = _empty(shape, torch.int32, cache.device, stream) if out is None else \
         _checked(out, "out", shape, torch.int32, cache.device)
     args = (_byref(rows), q.shape[1], _byref(c), _byref(tables._c), out.data_ptr(), npicked, first, last)
-    _call("slnr_page_select", args, cache.device.index, 0, validate, workspace, stream,
+    _call("slnr_page_select", args, cache.device.index, 0, validate and T > 0, workspace, stream,
           (q, cache.codes, cache.scales, out, *tables._tensors()))
     return out
 
@@ -278,14 +278,15 @@ def _attention(name, q, cache, tables, picked, npicked, scale, out, lse, validat
     out = _empty(shape, dtype, device, stream) if out is None else _checked(out, "out", shape, dtype, device)
     lse = _empty(shape[:2], torch.float32, device, stream) if lse is None else \
         _checked(lse, "lse", shape[:2], torch.float32, device)
-    need = _attention_bytes(cache._sizes, tables._sizes, heads_q, npicked)
+    # without tokens nothing is launched, and no flag word is written
+    need = _attention_bytes(cache._sizes, tables._sizes, heads_q, npicked) if T else 0
     scale = c.head_dim ** -0.5 if scale is None else scale
     if npicked:
         args = (_byref(rows), heads_q, _byref(c), _byref(p), picked.data_ptr(), npicked, scale, out.data_ptr(),
                 lse.data_ptr())
     else:
         args = (_byref(rows), heads_q, _byref(c), _byref(p), scale, out.data_ptr(), lse.data_ptr())
-    _call(name, args, device.index, need, validate, workspace, stream,
+    _call(name, args, device.index, need, validate and T > 0, workspace, stream,
           (q, cache.k, cache.v, picked, out, lse, *tables._tensors()))
     return out, lse
 
