@@ -63,10 +63,11 @@ struct AttnPlan {
   uint32_t* pickers; // [nheads][ntiles][cap][words] bit i: the tile's token i picked the page
   int32_t* npages;   // [nheads][ntiles]
   int cap, words;
-  // partial rows, each divided by its own sum, and log2 of their sums of exponentials: [ntok * nheads_q][nsplit], or
-  // of the tensor-core kernel [2 kChunkBlocks][kChunkRows]
+  // partial rows, each divided by its own sum, and {what their weights were taken against (a power of two), that sum}:
+  // [ntok * nheads_q][nsplit], or of the tensor-core kernel [2 kChunkBlocks][kChunkRows].  One number for the two, the
+  // logarithm of the sum, would lose the sum beside large scores.
   float* part;      // [...][width]
-  float* part_lse;
+  float2* part_ml;
 };
 
 constexpr int kAttnKeys = 64;       // keys of one step of the row kernel

@@ -191,7 +191,7 @@ AttnPlan attn_plan(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, i
 // Workspace of an attention call after the header: partial rows, and the pages
 // that row tiles picked.
 struct AttnLayout {
-  size_t part, lse, tiles, before, shares, pages, pickers, npages, total;
+  size_t part, ml, tiles, before, shares, pages, pickers, npages, total;
 };
 AttnLayout attn_layout(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, const AttnPlan& a) {
   AttnLayout l;
@@ -206,7 +206,7 @@ AttnLayout attn_layout(const slnr_cache& c, const slnr_pages& p, int32_t nheads_
                          : a.nsplit > 1 && !a.cluster ? (size_t)p.ntok * nheads_q * a.nsplit : 0;
   const size_t items = tc ? (size_t)a.ntiles * c.nheads : 0, lists = a.cap > 0 ? items : 0;
   l.part = take(rows * c.head_dim * sizeof(float));
-  l.lse = take(rows * sizeof(float));
+  l.ml = take(rows * sizeof(float2));
   l.tiles = take(tc ? (size_t)a.ntiles * 2 * sizeof(int4) : 0);
   l.before = take(items * sizeof(int64_t));
   l.shares = take(tc ? (kChunkBlocks + 2) * sizeof(int2) : 0);
@@ -250,7 +250,7 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   SLNR_CHECK(check_ws(opts, l.total));
   char* ws = (char*)opts->workspace;
   a.plan.part = (float*)(ws + l.part);
-  a.plan.part_lse = (float*)(ws + l.lse);
+  a.plan.part_ml = (float2*)(ws + l.ml);
   a.plan.tiles = (int4*)(ws + l.tiles);
   a.plan.before = (int64_t*)(ws + l.before);
   a.plan.shares = (int2*)(ws + l.shares);

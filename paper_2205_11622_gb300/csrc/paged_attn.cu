@@ -57,7 +57,7 @@ struct Smem {
   int key_at[SEL ? kOffsets : 1][kAttnKeys]; // selected: the keys' positions
   int2 pick[SEL ? kAttnMaxPicked : 1];       // selected: {page of the cache, page of the request}
   float2 ml[4][16];                          // a warp's (reference, sum) of each row
-  float lse[64];                             // of the block's rows, in powers of two
+  float2 joined[64];                         // the same of the block's rows
   int count;
 };
 
@@ -75,9 +75,9 @@ __device__ __forceinline__ uint32_t address_in(uint32_t local, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
   return r;
 }
-__device__ __forceinline__ float load_far(uint32_t at) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+__device__ __forceinline__ float2 load2_far(uint32_t at) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
   return v;
 }
 __device__ __forceinline__ float4 load4_far(uint32_t at) {
@@ -284,7 +284,7 @@ k_paged_rows(AttnArgs a, WsHeader* hdr) {
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        s[j][e] *= sl2;
+        s[j][e] = __fmul_rn(s[j][e], sl2);  // one value here and below, so that no weight passes its reference
         if (masked && at[e & 1] > pos[e >> 1]) s[j][e] = -INFINITY;
       }
     }
@@ -304,7 +304,7 @@ k_paged_rows(AttnArgs a, WsHeader* hdr) {
       for (int j = 0; j < KW / 8; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          s[j][2 * i + e] = exp2_fast(s[j][2 * i + e] - b);
+          s[j][2 * i + e] = exp2_fast(__fsub_rn(s[j][2 * i + e], b));
           l[i] += s[j][2 * i + e];
         }
     }
@@ -378,16 +378,15 @@ k_paged_rows(AttnArgs a, WsHeader* hdr) {
     const float inv = __fdividef(1.f, sum);
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = sum == 0.f ? 0.f : acc[e] * inv;  // no key: zeros
-    const float lse2 = mx + __log2f(sum);                                  // no key: -inf
     const int tok = a.group.div(x0 + x), g = x0 + x - tok * G;
     const int64_t at = (q0 + tok) * hq + h * G + g;
     if (CLUSTER) {  // for the other blocks, where the first warp's row was
       float4* y = reinterpret_cast<float4*>(rows + x * (W + 4) + col);
       y[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
       y[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-      if (col == 0) sm.lse[x] = lse2;
+      if (col == 0) sm.joined[x] = make_float2(mx, sum);
     } else if (splits == 1) {
-      store_row<T>(a, at, col, acc, lse2);
+      store_row<T>(a, at, col, acc, mx + __log2f(sum));  // no key: -inf
     } else {
       const int64_t slot = at * a.plan.nsplit + blockIdx.z;
       if (col < c.width) {
@@ -395,23 +394,24 @@ k_paged_rows(AttnArgs a, WsHeader* hdr) {
         y[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
         y[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
       }
-      if (col == 0) a.plan.part_lse[slot] = lse2;
+      if (col == 0) a.plan.part_ml[slot] = make_float2(mx, sum);
     }
   }
   if (CLUSTER) {
     // the splits of a row are the blocks of the cluster: each joins a share of the rows, in the splits' order
     cluster_sync();
     const int size = gridDim.z, rank = (int)cluster_rank();
-    const uint32_t lse_at = (uint32_t)__cvta_generic_to_shared(sm.lse);
+    const uint32_t ml_at = (uint32_t)__cvta_generic_to_shared(sm.joined);
     for (int x = rank + row0 * size; x < n; x += ROWS * size) {
       float mx = -INFINITY, sum = 0.f, acc[8];
-      for (int k = 0; k < size; ++k) mx = fmaxf(mx, load_far(address_in(lse_at + 4 * x, k)));
+      for (int k = 0; k < size; ++k) mx = fmaxf(mx, load2_far(address_in(ml_at + 8 * x, k)).x);
       const float b = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] = 0.f;
 #pragma unroll 4
       for (int k = 0; k < size; ++k) {
-        const float f = exp2_fast(load_far(address_in(lse_at + 4 * x, k)) - b);
+        const float2 ml = load2_far(address_in(ml_at + 8 * x, k));
+        const float f = exp2_fast(ml.x - b) * ml.y;
         const uint32_t y = address_in(base + (x * (W + 4) + col) * 4, k);
         const float4 z0 = load4_far(y), z1 = load4_far(y + 16);
         sum += f;
@@ -434,7 +434,7 @@ k_paged_rows(AttnArgs a, WsHeader* hdr) {
   }
 }
 
-// Rows of several splits: o = sum_s 2^(lse_s - m) o_s / sum_s 2^(lse_s - m).  A
+// Rows of several splits: o = sum_s 2^(m_s - m) l_s o_s / sum_s 2^(m_s - m) l_s.  A
 // block a row, every fourth split a warp: a long cache of few heads has hundreds
 // of splits, whose loads would follow one another in one warp: 32768 keys of one
 // key head of 128 and 16 query heads, 256 splits, 65 us a call with a warp a row,
@@ -459,9 +459,9 @@ k_paged_combine(AttnArgs a) {
     splits = end > 0 ? (end - 1) / a.plan.chunk + 1 : 1;
   }
   if (splits == 1) return;
-  const float* lse = a.plan.part_lse + at * a.plan.nsplit;
+  const float2* ml = a.plan.part_ml + at * a.plan.nsplit;
   float m = -INFINITY;
-  for (int s = lane; s < splits; s += 32) m = fmaxf(m, lse[s]);
+  for (int s = lane; s < splits; s += 32) m = fmaxf(m, ml[s].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   const float b = m == -INFINITY ? 0.f : m;
@@ -471,7 +471,7 @@ k_paged_combine(AttnArgs a) {
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
   for (int s = warp; s < splits; s += 4) {
-    const float f = exp2_fast(lse[s] - b);
+    const float f = exp2_fast(ml[s].x - b) * ml[s].y;
     sum += f;
     if (col < a.c.width) {
       const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)s * a.c.width);

@@ -73,6 +73,7 @@ template <typename T>
 constexpr float kBelow = std::is_same<T, __half>::value ? 12.f : 0.f;
 template <typename T>
 constexpr float kGrow = std::is_same<T, __half>::value ? 3.f : 8.f;
+constexpr float kCoarse = 1 << 22;
 
 template <int W>
 constexpr int tile_bytes() { return kBlock * (W / 64); }
@@ -455,9 +456,8 @@ __device__ __forceinline__ void write_row(const AttnArgs& a, const Item& it, Sha
     }
   }
   if (on) {
-    const float lse2 = l == 0.f ? -INFINITY : m + __log2f(l);
-    if (!whole) a.plan.part_lse[at] = lse2;
-    else if (a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
+    if (!whole) a.plan.part_ml[at] = make_float2(l == 0.f ? -INFINITY : m, l);
+    else if (a.lse) a.lse[at] = (l == 0.f ? -INFINITY : m + __log2f(l)) * 0.6931471805599453f;
   }
 }
 
@@ -730,8 +730,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t col_s = tmem + lanes + kColS + t * 128, col_o = tmem + lanes + kColO + t * 128;
     // scores are kept raw and take their factor inside the exponential; one that is not positive goes to them first
-    const bool raw = a.scale > 0.f;
-    const float factor = a.scale * 1.4426950408889634f, sl2 = raw ? factor : 1.f;
+    const float factor = a.scale * 1.4426950408889634f;
     int done = 0, count = 0, ring = 0;
     bool ok = true;  // where a wait gave up the items go on without work: the two warpgroups meet at barriers
     each_item<SEL>(a, [&](const Item& it) {
@@ -742,6 +741,8 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const int pos = row_on ? it.shift + tok : -1;
       const int pos_min = it.shift + a.group.div(it.x0 + x - row);  // of the tile's rows
       const bool tail = it.n - (x - row) < kRows;                   // rows that are none: their scores are dropped
+      bool raw = a.scale > 0.f;
+      float sl2 = raw ? factor : 1.f;
       float m = -INFINITY, l = 0.f;  // what weights are taken against (in powers of two), sum of weights
       // selected: the row's token in the tile
       const int tl = tok - a.group.div(it.x0), page_shift = c.page.d < kChunkKeys ? 31 - __clz(c.page.d) : 7;
@@ -803,6 +804,15 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         // score is above 2^kBelow, however large that is
         const bool grow = fmaf(top, sl2, -m) > kBelow<T> + kGrow<T>;  // m = -inf: true for any seen key
         if (__any_sync(0xffffffffu, grow)) {
+          // Beside scores past 2^22 m is too coarse for their exact products with sl2: from here on both are rounded
+          // alike.
+          if (__any_sync(0xffffffffu, raw && grow && fabsf(top) * sl2 >= kCoarse)) {
+#pragma unroll
+            for (int k = 0; k < 128; ++k) s[k] = __float_as_uint(__uint_as_float(s[k]) * factor);
+            top *= factor;
+            raw = false;
+            sl2 = 1.f;
+          }
           const float to = grow ? __fmaf_ru(top, sl2, -kBelow<T>) : m;
           const float f = grow ? exp2_fast(m - to) : 1.f;
           if (grow) l *= f;
@@ -894,8 +904,8 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   if (warp == kMmaWarp) tc::tmem_dealloc(tmem, kTmemCols);
 }
 
-// Items that cuts went through: o = sum 2^(lse - m) o_part / sum 2^(lse - m) over
-// their parts, in the keys' order.  Block x: the item that share x + 1 begins
+// Items that cuts went through: o = sum 2^(m_part - m) l_part o_part / sum 2^(m_part - m) l_part
+// over their parts, in the keys' order.  Block x: the item that share x + 1 begins
 // inside of, if no share before does; block y: 16 of its rows, 4 a warp at once.
 constexpr int kJoinRows = 16;
 
@@ -930,13 +940,14 @@ k_paged_join(AttnArgs a) {
 #pragma unroll 2
   for (int k = 0; k < parts; ++k)
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) m[i] = fmaxf(m[i], a.plan.part_lse[part(k, i)]);
+    for (int i = 0; i < ROWS; ++i) m[i] = fmaxf(m[i], a.plan.part_ml[part(k, i)].x);
 #pragma unroll 2
   for (int k = 0; k < parts; ++k)
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       const int64_t at = part(k, i);
-      const float f = exp2_fast(a.plan.part_lse[at] - (m[i] == -INFINITY ? 0.f : m[i]));
+      const float2 ml = a.plan.part_ml[at];
+      const float f = exp2_fast(ml.x - (m[i] == -INFINITY ? 0.f : m[i])) * ml.y;
       sum[i] += f;
       if (col < a.c.width) {
         const float4 y = *reinterpret_cast<const float4*>(a.plan.part + at * a.c.width + col);
