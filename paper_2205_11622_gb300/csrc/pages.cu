@@ -15,6 +15,8 @@ namespace {
 // table's entry, and no thread needs another's.  Every block scans the lengths
 // of all requests (1024 at a time, a few hundred bytes to a few KB out of L2)
 // and writes the tokens of its own range: one launch, nothing to wait for.
+// Lengths that no cache holds (sums past 2^31) give slots of -1 where they are
+// looked up, and no access outside the arrays.
 // Bound by the latency of its dependent reads: 64 requests of one token 4 us,
 // 512 requests of 284k tokens 6 us.
 constexpr int kTablesThreads = 1024;
@@ -36,7 +38,8 @@ k_page_tables(int nreq, const int32_t* __restrict__ new_len, const int32_t* __re
     const int r = r0 + tid;
     const bool on = r < nreq;
     const int n = on ? max(new_len[r], 0) : 0, old = on ? max(old_len[r], 0) : 0;
-    const int take = clamped_div_up(old + n, page) - clamped_div_up(old, page);
+    const int end = n > INT32_MAX - old ? INT32_MAX : old + n;
+    const int take = clamped_div_up(end, page) - clamped_div_up(old, page);
     // inclusive sums of new tokens and taken pages over the block
     int a = n, b = take;
 #pragma unroll
@@ -65,7 +68,7 @@ k_page_tables(int nreq, const int32_t* __restrict__ new_len, const int32_t* __re
     s_old[tid] = old;
     if (blockIdx.x == 0 && on) {
       q_pos[r] = tok_base + a - n;
-      k_len[r] = old + n;
+      k_len[r] = end;
     }
     __syncthreads();
     const int lo = max(t0, tok_base), hi = min(t1, tok_end);
@@ -75,15 +78,18 @@ k_page_tables(int nreq, const int32_t* __restrict__ new_len, const int32_t* __re
 #pragma unroll
       for (int w = kTablesThreads / 2; w > 0; w >>= 1)
         if (s_tok[i + w] <= t) i += w;
-      const int o = s_old[i], p = o + (t - s_tok[i]);
-      const int held = clamped_div_up(o, page), n_page = page.div(p), off = p - n_page * page.d;
-      int id = -1;
-      if (n_page < held) {
-        if (n_page < width) id = table[(r0 + i) * table_stride + n_page];
-      } else {
-        const int f = s_pg[i] + (n_page - held);
-        if (f < nfree && n_page < width) id = free_pages[f];
-        if (off == 0 && n_page < width) table[(r0 + i) * table_stride + n_page] = id;
+      const int o = s_old[i], p = (int)((unsigned)o + (unsigned)t - (unsigned)s_tok[i]);
+      int id = -1, off = 0;
+      if (p >= o && r0 + i < nreq) {
+        const int held = clamped_div_up(o, page), n_page = page.div(p);
+        off = p - n_page * page.d;
+        if (n_page < held) {
+          if (n_page < width) id = table[(r0 + i) * table_stride + n_page];
+        } else {
+          const int f = (int)((unsigned)s_pg[i] + (unsigned)(n_page - held));
+          if ((unsigned)f < (unsigned)nfree && n_page < width) id = free_pages[f];
+          if (off == 0 && n_page < width) table[(r0 + i) * table_stride + n_page] = id;
+        }
       }
       req[t] = r0 + i;
       slots[t] = id < 0 ? -1 : id * page.d + off;
