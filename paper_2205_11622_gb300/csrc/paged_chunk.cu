@@ -303,24 +303,25 @@ __device__ __forceinline__ Item item_of(const AttnArgs& a, int i, int ntiles, in
 constexpr int kPlanThreads = 1024;
 
 // Inclusive sum over the block; `total` gets the whole.
-__device__ __forceinline__ int block_sum(int x, int& total, int* s_warp) {
+template <typename N>
+__device__ __forceinline__ N block_sum(N x, N& total, N* s_warp) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    const N y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
   __syncthreads();
   if (lane == 31) s_warp[warp] = x;
   __syncthreads();
-  int y = s_warp[lane];
+  N y = s_warp[lane];
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int z = __shfl_up_sync(0xffffffffu, y, o);
+    const N z = __shfl_up_sync(0xffffffffu, y, o);
     if (lane >= o) y += z;
   }
   total = __shfl_sync(0xffffffffu, y, 31);
-  const int before = __shfl_sync(0xffffffffu, y, (warp + 31) & 31);
+  const N before = __shfl_sync(0xffffffffu, y, (warp + 31) & 31);
   return warp > 0 ? x + before : x;
 }
 
@@ -328,6 +329,7 @@ template <bool SEL>
 __global__ void __launch_bounds__(kPlanThreads)
 k_paged_plan(AttnArgs a, WsHeader* hdr) {
   __shared__ int s_first[kPlanThreads], s_warp[32];
+  __shared__ long long s_cost[32];
   const PagesView& p = a.p;
   const int tid = threadIdx.x, G = a.group.d;
   let_next_start();
@@ -356,19 +358,19 @@ k_paged_plan(AttnArgs a, WsHeader* hdr) {
     __syncthreads();
   }
   ntiles = min(ntiles, a.plan.ntiles);
-  // cost of the items before each
+  // cost of the items before each: in 64 bits, as those of 1024 items of 2^27 keys pass 2^31
   const int items = ntiles * a.c.nheads;
   int64_t cost = 0;
   for (int i0 = 0; i0 < items; i0 += kPlanThreads) {
     const int i = i0 + tid;
-    int mine = 0, total;
+    long long mine = 0, total;
     if (i < items) {
       const int h = i / ntiles, tile = i - h * ntiles;
       mine = kItemCost + weight_of(a.plan.tiles[2 * tile].w) *
              steps_of(SEL ? a.plan.npages[(int64_t)h * a.plan.ntiles + tile] * a.c.page.d
                           : max(a.plan.tiles[2 * tile + 1].y + 1, 0));
     }
-    const int sum = block_sum(mine, total, s_warp);
+    const long long sum = block_sum(mine, total, s_cost);
     if (i < items) a.plan.before[i] = cost + sum - mine;
     cost += total;
   }

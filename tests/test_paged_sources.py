@@ -18,3 +18,16 @@ def test_no_read_only_load_of_what_an_earlier_launch_of_the_call_writes():
         assert not re.search(r"__ldg\s*\(\s*(\([^()]*\)\s*)?&?a\.plan\b", text), name
         assert "ld.global.nc" not in text, name
         assert not re.search(r"const\s+\w+\s*\*\s*__restrict__[^;]*a\.plan", text), name
+
+
+def test_costs_of_items_are_summed_in_64_bits():
+    """An item's cost is a few units and one or two for each 128 keys.  The sum of a step of 1024 items passes the largest
+    int where they have 2^27 keys each, and a wrapped sum would be an index of the shares; such a call takes ten seconds of
+    a GPU, so no run shows it."""
+    plan = code("paged_chunk.cu")
+    plan = plan[plan.index("k_paged_plan(AttnArgs a"):plan.index("read_row")]
+    cost = plan[plan.index("kItemCost") - 200:]
+    assert 1024 * (6 + 2 * (2 ** 27 // 128)) > 2 ** 31
+    assert re.search(r"(int64_t|long long) mine = 0, total;", cost)
+    assert re.search(r"(int64_t|long long) sum = block_sum\(mine, total, \w+\)", cost)
+    assert re.search(r"__shared__ (int64_t|long long) s_cost\[32\]", plan)
