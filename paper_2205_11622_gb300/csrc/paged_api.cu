@@ -11,7 +11,7 @@ using namespace slnr;
 namespace {
 
 constexpr int kMaxWidth = 128;
-constexpr int kMaxKeys = 0x7fff0000;  // steps past a request's last key stay below 2^31
+constexpr int kMaxKeys = 0x7fff0000;  // whole pages of a request, and steps past its last key, stay below 2^31
 
 slnr_status check_paged_opts(const slnr_opts* o) {
   if (!o) return fail(SLNR_ERR_NULL, "opts is NULL");
@@ -59,7 +59,8 @@ slnr_status check_cache(const slnr_cache* c, bool keys, bool summary, bool point
 slnr_status check_pages(const slnr_pages* p, const slnr_cache* c, bool pointers, bool req, bool slots) {
   if (!p) return fail(SLNR_ERR_NULL, "pages is NULL");
   if (p->reserved != 0) return fail(SLNR_ERR_UNSUPPORTED, "pages.reserved must be 0");
-  if (p->max_k > kMaxKeys) return fail(SLNR_ERR_UNSUPPORTED, "max_k = %d: at most %d", (int)p->max_k, kMaxKeys);
+  if (p->max_k > 0 && ceil_div(p->max_k, c->page_size) * c->page_size > kMaxKeys)
+    return fail(SLNR_ERR_UNSUPPORTED, "max_k = %d: at most %d in whole pages", (int)p->max_k, kMaxKeys);
   if (p->nreq < 0 || p->ntok < 0 || p->max_q < 0 || p->max_k < 0 || p->width < 0 || p->table_stride < p->width)
     return fail(SLNR_ERR_SHAPE, "negative size in pages, or rows of table that overlap");
   if ((int64_t)p->max_k > (int64_t)p->width * c->page_size)
