@@ -244,7 +244,11 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   if (!aligned16(out)) return fail(SLNR_ERR_UNSUPPORTED, "out must be 16-byte aligned");
   AttnArgs a{view(*pages), view(*cache), view(*q), divisor(nheads_q / cache->nheads), scale, out, lse, picked, npicked,
              attn_plan(*cache, *pages, nheads_q, npicked)};
-  if (a.plan.nsplit > 65535 || a.plan.ntiles == INT32_MAX || (a.plan.tile == kChunkRows && a.plan.ntiles > 65535) ||
+  // Blocks of a launch and rows of a request are counted in ints: row tiles (times key heads on the tensor cores, where
+  // they are items), splits (a grid's third axis).  Rows with splits to join are few: see attn_plan.
+  const bool tc = a.plan.tile == kChunkRows;
+  if (a.plan.nsplit > 65535 || a.plan.ntiles == INT32_MAX ||
+      (tc && (int64_t)a.plan.ntiles * cache->nheads > kMaxKeys) ||
       (int64_t)pages->max_q * a.group.d >= (int64_t(1) << 31) || (int64_t)npicked * cache->page_size > kMaxKeys)
     return fail(SLNR_ERR_UNSUPPORTED, "too many rows or keys for one call");
   const AttnLayout l = attn_layout(*cache, *pages, nheads_q, a.plan);
@@ -262,7 +266,6 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
     return launch_validate_pages(a.p, a.c.npages, a.c.page, false, picked, npicked, a.c.nheads, hdr, st);
   }));
-  const bool tc = a.plan.tile == kChunkRows;
   if (tc) {
     SLNR_LAUNCH("paged_plan", launch_paged_plan(a, (WsHeader*)ws, s));
     SLNR_LAUNCH("paged_chunk", launch_paged_chunk(a, cache->dtype, (WsHeader*)ws, s));

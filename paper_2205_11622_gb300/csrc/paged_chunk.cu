@@ -194,11 +194,11 @@ k_paged_union(AttnArgs a) {
   __shared__ uint32_t s_bits[kUnionPages * kMaxWords];
   __shared__ int s_count[kUnionThreads / 32 + 1];
   const PagesView& p = a.p;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.x, words = a.plan.words;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, words = a.plan.words;
   let_next_start();
   int r, x0;
-  find_tile(p, a.group.d, kChunkRows, blockIdx.y, r, x0);
-  const int64_t at = (int64_t)h * gridDim.y + blockIdx.y;
+  find_tile(p, a.group.d, kChunkRows, blockIdx.x, r, x0);
+  const int64_t at = (int64_t)h * gridDim.x + blockIdx.x;
   if (r < 0) {
     if (tid == 0) a.plan.npages[at] = 0;
     return;
@@ -999,7 +999,7 @@ cudaError_t launch_paged_plan(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) 
     k_paged_plan<false><<<SLNR_COUNTED(1), kPlanThreads, 0, s>>>(a, hdr);
     return cudaGetLastError();
   }
-  const dim3 grid((unsigned)a.c.nheads, (unsigned)a.plan.ntiles);
+  const dim3 grid((unsigned)a.plan.ntiles, (unsigned)a.c.nheads);
   k_paged_union<<<(SLNR_COUNTED(grid)), kUnionThreads, 0, s>>>(a);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
