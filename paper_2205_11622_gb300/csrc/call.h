@@ -31,10 +31,15 @@ inline slnr_status check_ws(const slnr_opts* o, size_t need) {
 
 }  // namespace slnr
 
+// A failure is reported by the call that met it: the runtime's copy, which the next
+// launch would return again, is taken out.
 #define SLNR_CUDA(expr)                                                                   \
   do {                                                                                    \
     cudaError_t e_ = (expr);                                                              \
-    if (e_ != cudaSuccess) return ::slnr::fail(SLNR_ERR_CUDA, "%s: %s", #expr, cudaGetErrorString(e_)); \
+    if (e_ != cudaSuccess) {                                                              \
+      (void)cudaGetLastError();                                                           \
+      return ::slnr::fail(SLNR_ERR_CUDA, "%s: %s", #expr, cudaGetErrorString(e_));        \
+    }                                                                                     \
   } while (0)
 
 // A kernel launch of the call: timing mark, then the launch, then its status.

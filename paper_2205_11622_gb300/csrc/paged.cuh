@@ -2,7 +2,6 @@
 // division by the page size, and the launchers that the C entry points call.
 #pragma once
 
-#include <atomic>
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -10,6 +9,7 @@
 
 #include "common.cuh"
 #include "divide.h"
+#include "once.h"
 
 namespace slnr {
 
@@ -112,27 +112,6 @@ cudaError_t launch_next(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 #endif
-
-// Runs something once a device and keeps its first error: the attributes of a kernel.
-class OncePerDevice {
- public:
-  template <typename F>
-  cudaError_t operator()(F f) {
-    int d = 0;
-    const cudaError_t e = cudaGetDevice(&d);
-    if (e != cudaSuccess) return e;
-    if (d < 0 || d >= kDevices) return f();
-    const int seen = state_[d].load(std::memory_order_acquire);
-    if (seen != 0) return (cudaError_t)(seen - 1);
-    const cudaError_t r = f();  // by two threads at once: the same attributes twice
-    state_[d].store((int)r + 1, std::memory_order_release);
-    return r;
-  }
-
- private:
-  static constexpr int kDevices = 64;
-  std::atomic<int> state_[kDevices] = {};
-};
 
 // pages.cu
 cudaError_t launch_page_tables(int nreq, const int32_t* new_len, const int32_t* old_len, int32_t* table,
