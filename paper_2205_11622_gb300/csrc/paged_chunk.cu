@@ -652,6 +652,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
             tc::mma_commit(&bars.empty[ring % NB]);
             if (it.steps == 1) tc::mma_commit(&bars.q_empty);
           }
+          __syncwarp();
           for (int j = 0; ok && j < it.steps; ++j) {
             const int iv = ring + 2 * j + 1, ik = iv + 1, bv = iv % NB, bk = ik % NB;
             const bool more = j + 1 < it.steps;
@@ -664,6 +665,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
               output(0, bv, j == 0);
               if (more) scores(0, 0, bk);
             }
+            __syncwarp();
             ok = wait_warp(&bars.p_full[1], (done[1] + j) & 1, failed, limit);
             if (!ok) break;
             tc::tc_fence_after_sync();
@@ -676,6 +678,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
                 if (j + 2 == it.steps) tc::mma_commit(&bars.q_empty);
               }
             }
+            __syncwarp();
           }
           done[0] += it.steps;
           done[1] += it.steps;
@@ -686,6 +689,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
             tc::mma_commit(&bars.empty[ring % NB]);
             if (it.steps == 1) tc::mma_commit(&bars.q_empty);
           }
+          __syncwarp();
           if (it.steps > 1) {
             const int bk = (ring + 2) % NB;
             ok = landed(ring + 2);
@@ -697,6 +701,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
                 tc::mma_commit(&bars.empty[bk]);
                 if (it.steps == 2) tc::mma_commit(&bars.q_empty);
               }
+              __syncwarp();
             }
           }
           for (int j = 0; ok && j < it.steps; ++j) {
@@ -716,11 +721,13 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
                 if (j + 3 == it.steps) tc::mma_commit(&bars.q_empty);
               }
             }
+            __syncwarp();
           }
           done[0] += (it.steps + 1) / 2;
           done[1] += it.steps / 2;
         }
         if (ok && tc::elect_one()) tc::mma_commit(&bars.o_full);
+        __syncwarp();
         ring += 2 * it.steps;
         ++count;
       });

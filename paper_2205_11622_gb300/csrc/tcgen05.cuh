@@ -197,8 +197,13 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
 }
 
 // True in one lane of a whole warp, the same one each time: the lane that issues
-// a run of MMAs and their commit.  (A run unrolled under `lane == 0` came out
-// with wrong results.)
+// a run of MMAs and their commit.  The other lanes wait behind the run
+// (__syncwarp), as they do where one lane runs a whole loop of waits and products
+// (tc_gemm.cu, tc_premul.cu): in no kernel here does a warp go on past a run that
+// one of its lanes still issues.  An unrolled run under `lane == 0`, past which the
+// other lanes went on to their next wait, came out with wrong results.  By the
+// instructions' definition it issues the same products from one thread in the same
+// order, so the source does not show why; that form is not used.
 __device__ __forceinline__ bool elect_one() {
   uint32_t on;
   asm volatile(

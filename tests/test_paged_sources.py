@@ -31,3 +31,13 @@ def test_costs_of_items_are_summed_in_64_bits():
     assert re.search(r"(int64_t|long long) mine = 0, total;", cost)
     assert re.search(r"(int64_t|long long) sum = block_sum\(mine, total, \w+\)", cost)
     assert re.search(r"__shared__ (int64_t|long long) s_cost\[32\]", plan)
+
+
+def test_no_lane_runs_on_beside_a_run_of_products():
+    """The warp's other lanes wait behind each run that an elected lane issues."""
+    text = code("paged_chunk.cu")
+    text = text[text.index("const uint32_t id_s ="):text.index("regs_up<kSoftRegs>();")]
+    runs = list(re.finditer(r"^( *)if \((ok && )?tc::elect_one\(\)\) ?(\{.*?^\1\}|[^\n]*;)\n\s*(\S[^\n]*)", text, re.M | re.S))
+    assert len(runs) == text.count("elect_one") == 7
+    for run in runs:
+        assert run.group(4).startswith("__syncwarp();"), run.group(0)
