@@ -289,6 +289,8 @@ slnr_status slnr_spmm_gemm_original(const slnr_csr *B, const float *C, int32_t K
  *  - q_pos, k_len, tables, req and slots are trusted without opts->validate; a page
  *    outside the cache is then not read or written, what its keys add to a
  *    result is not defined.
+ *  - Where a bounded device-side wait gave up (slnr_set_wait_limit), the rows
+ *    that it concerns are NaN; validate mode returns SLNR_ERR_TIMEOUT.
  *  - opts->variant and allow_tf32 have no effect.  slnr_page_tables,
  *    slnr_page_append and slnr_page_select need a workspace (256 bytes) in
  *    validate mode only.

@@ -422,8 +422,8 @@ __device__ __forceinline__ void store32(void* to, const uint32_t (&v)[8], bool a
 // m: what weights were taken against, in powers of two, l: their sum.
 template <typename T, int W>
 __device__ __forceinline__ void write_row(const AttnArgs& a, const Item& it, Shared& sh, uint32_t (&o)[W], int x, int row,
-                                          bool ok, float inv, float f_other, float m, float l) {
-  const bool pair = it.tiles == 1, whole = it.slot < 0, on = ok && x < it.n;
+                                          float inv, float f_other, float m, float l) {
+  const bool pair = it.tiles == 1, whole = it.slot < 0, on = x < it.n;
   const int G = a.group.d, tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
   const int64_t at = whole ? (it.q0 + tok) * ((int64_t)a.c.nheads * G) + it.h * G + g : (int64_t)it.slot * kChunkRows + x;
   T* out = (T*)a.out + at * a.c.width;
@@ -741,7 +741,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
     // scores are kept raw and take their factor inside the exponential; one that is not positive goes to them first
     const float factor = a.scale * 1.4426950408889634f;
     int done = 0, count = 0, ring = 0;
-    bool ok = true;  // where a wait gave up the items go on without work: the two warpgroups meet at barriers
+    bool ok = true;  // where a wait gave up the items go on without work, and their rows are NaN
     each_item<SEL>(a, [&](const Item& it) {
       const bool pair = it.tiles == 1;  // this warpgroup's steps are every second one of the same rows
       const int x = pair ? row : t * kRows + row;
@@ -865,6 +865,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       if (ok && keys) ok = wait_warp(&bars.o_full, count & 1, failed, limit);
       count += keys;
       tc::tc_fence_after_sync();
+      if (!ok) m = l = __int_as_float(0x7fffffff);  // NaN, not what the output's memory held: no wait gives up unseen
       float f_other = 0.f;
       uint32_t o[W];
       read_row<W>(col_o, ok && it.steps > first, o);  // this warpgroup's O holds something from its first step on
@@ -880,7 +881,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           f_other = l == 0.f ? 0.f : f_other * __fdividef(1.f, l);
           m = top;
           const float inv = l == 0.f ? 0.f : f * __fdividef(1.f, l);
-          write_row<T, W>(a, it, bars, o, x, row, ok, inv, f_other, m, l);
+          write_row<T, W>(a, it, bars, o, x, row, inv, f_other, m, l);
         } else {
 #pragma unroll
           for (int k = 0; k < W; k += 16) {
@@ -891,7 +892,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           }
         }
       } else {
-        write_row<T, W>(a, it, bars, o, x, row, ok, l == 0.f ? 0.f : __fdividef(1.f, l), 0.f, m, l);
+        write_row<T, W>(a, it, bars, o, x, row, l == 0.f ? 0.f : __fdividef(1.f, l), 0.f, m, l);
       }
     });
   }
