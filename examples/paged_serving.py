@@ -27,7 +27,7 @@ class Layer:
             k=torch.zeros(shape, dtype=dtype, device=device), v=torch.zeros(shape, dtype=dtype, device=device),
             codes=torch.zeros((npages, heads, width), dtype=torch.int8, device=device),
             scales=torch.zeros((npages, heads), device=device))
-        self.page_size, self.max_keys = page_size, max_keys
+        self.page_size = page_size
         self.table = torch.full((requests, -(-max_keys // page_size)), -1, dtype=torch.int32, device=device)
         self.free = torch.arange(npages, dtype=torch.int32, device=device)
         self.lens = [0] * requests
@@ -37,8 +37,12 @@ class Layer:
         """Attention of `new` tokens of each request (packed in q, k, v): over all pages, or `picked` of each token."""
         i32 = dict(dtype=torch.int32, device=self.device)
         taken = sum(-(-(o + n) // self.page_size) - -(-o // self.page_size) for o, n in zip(self.lens, new))
+        # The bounds on new tokens and keys lay out the work: near the truth, and whole pages, so that the sizes of a call
+        # change once a page.  A step that is captured for replay takes the most keys it will ever have.
+        most = max(o + n for o, n in zip(self.lens, new))
         tables, _ = slnr.page_tables(torch.tensor(new, **i32), torch.tensor(self.lens, **i32), self.table, self.free,
-                                     self.page_size, sum(new), max_q=max(new), max_k=self.max_keys)
+                                     self.page_size, sum(new), max_q=max(new),
+                                     max_k=-(-most // self.page_size) * self.page_size)
         self.free = self.free[taken:]
         self.lens = [o + n for o, n in zip(self.lens, new)]
         slnr.page_append(self.cache, tables, k, v)

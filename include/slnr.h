@@ -302,7 +302,8 @@ typedef struct slnr_pages {
   int32_t nreq;         /* requests */
   int32_t ntok;         /* new tokens in all == q_pos[nreq] */
   int32_t max_q;        /* no request has more new tokens */
-  int32_t max_k;        /* no request has more keys; <= width * page size */
+  int32_t max_k;        /* no request has more keys; <= width * page size, below 2^31 - 2^16 in whole pages.  The work is
+                           laid out by these two: bounds near the truth are faster, results do not depend on them */
   int32_t width;        /* columns of table */
   int32_t reserved;     /* must be 0 */
   int64_t table_stride; /* from one row of table to the next */
@@ -339,7 +340,9 @@ typedef struct slnr_rows {
  * ceil(k_len/s), are taken from free_pages in the requests' order and written
  * to its row of table (in place; other entries are kept).  used[0] = pages
  * taken.  Where free_pages or the table's width is too short the entry and the
- * slots of that page are -1 (validate: SLNR_ERR_INDEX). */
+ * slots of that page are -1 (validate: SLNR_ERR_INDEX).  Lengths that pass 2^31
+ * in a request or in all give slots of -1 or of free pages, and touch nothing
+ * outside the arrays; negative ones are none. */
 slnr_status slnr_page_tables(int32_t nreq, const int32_t *new_len, const int32_t *old_len, int32_t *table,
                              int64_t table_stride, int32_t width, const int32_t *free_pages, int32_t nfree,
                              int32_t page_size, int32_t ntok, int32_t *q_pos, int32_t *k_len, int32_t *req,
@@ -348,10 +351,10 @@ slnr_status slnr_page_tables(int32_t nreq, const int32_t *new_len, const int32_t
 /* ---- new keys and values into the cache -----------------------------------
  * K[slot_t] = k_t and V[slot_t] = v_t for each new token (a negative slot is
  * skipped; validate: SLNR_ERR_INDEX).  Slots are those of slnr_page_tables: a
- * request's new tokens lie behind its older keys, k_len[r] of them in all.  Where cache->codes is not NULL, each page whose last slot is
- * written gets its summary, per head: m = the mean of its keys, scale =
- * max|m| / 127, codes = m / scale rounded to the nearest whole number (0 if
- * scale is 0). */
+ * request's new tokens lie behind its older keys, k_len[r] of them in all.
+ * Where cache->codes is not NULL, each page whose last slot is written gets its
+ * summary, per head: m = the mean of its keys, scale = max|m| / 127, codes = m /
+ * scale rounded to the nearest whole number (0 if scale is 0). */
 slnr_status slnr_page_append(const slnr_cache *cache, const slnr_pages *pages, const slnr_rows *k,
                              const slnr_rows *v, const slnr_opts *opts);
 
@@ -372,7 +375,7 @@ slnr_status slnr_page_select(const slnr_rows *q, int32_t nheads_q, const slnr_ca
 /* ---- attention over all pages, and over picked ones ------------------------
  * out[t, h] = sum_j softmax_j(scale q[t, h] . K[j]) V[j] over the keys j that
  * token t sees (slnr_selected_attention: those in the pages that picked[t,
- * h div group] lists, ascending; negative entries, anywhere, are none), lse[t, h]
+ * h div group] lists, ascending, none twice; negative entries, anywhere, are none), lse[t, h]
  * = log sum_j exp(scale q . K[j]) (natural; may be NULL).  out has the cache's
  * type, [ntok][nheads_q][head_dim]; lse is fp32 [ntok][nheads_q]. */
 slnr_status slnr_paged_attention_workspace(const slnr_cache *cache, const slnr_pages *pages, int32_t nheads_q,

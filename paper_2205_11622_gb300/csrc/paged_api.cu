@@ -138,7 +138,10 @@ bool whole_steps(int page) { return page >= kChunkKeys ? page % kChunkKeys == 0 
 // 128, 64 rows, row kernel and tensor-core kernel): 64 requests of 4096 keys, 8
 // heads, 408 and 294; 8 of 8192, 108 and 95; 32 of 1024, 58 and 57; but 1 of 32768
 // 57 and 69, 1 of 4096 28 and 32, where its longer way through a step shows.  With
-// 32 rows it has no such call (276 and 288).
+// 32 rows it has no such call (276 and 288).  A call whose bounds are wider than its
+// requests is taken by the bounds: single tokens with max_q = 64 as chunks, 658 us
+// where max_q = 1 takes 421, and few keys with a wide max_k in few splits, one
+// request of 4095 keys 17 us with max_k = 4095, 33 with 32768.
 AttnPlan attn_plan(const slnr_cache& c, const slnr_pages& p, int32_t nheads_q, int32_t npicked) {
   AttnPlan a{};
   const int64_t G = nheads_q / c.nheads, requests = p.nreq < p.ntok ? p.nreq : p.ntok;

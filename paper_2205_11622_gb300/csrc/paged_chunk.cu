@@ -34,18 +34,19 @@
 // K-major operand of Q K^T, V as the MN-major one of P V.
 //
 // Measured (32 query and 8 key heads of 128, bf16): 4096 tokens over 16384 keys
-// 0.62 ms of kernel time, 1.56 PFLOP/s over the visible pairs, bound by the way
+// 0.63 ms of kernel time, 1.53 PFLOP/s over the visible pairs (fp16, whose maxima are
+// followed more closely, 0.66), bound by the way
 // from one of a tile's products to its next: a step takes 3.3k cycles, of which
 // a tile's own products are 1.03k and hide as much of the other tile's way.  The
 // rest is its weights (scores out of tensor memory 340, maximum 400, 128
 // exponentials a thread 1060, back 150), 290 from a product's end to the warps
 // that wait for it and 170 from theirs to the product.  What did not shorten it:
 // handing over the first half of the weights early; exponentials by polynomials
-// on the other pipes (a quarter of them 0.68 ms, half 0.83); more registers.
-// Copies that their threads wait for take 0.72 ms, a block an item 0.79, a table
-// lookup in each copying thread 3.3.  2048 tokens over 16 picked pages of 64
-// each: 0.13 ms; the row kernel, which reads every page once for every token,
-// 1.29.
+// on the other pipes (a quarter of them 0.68 ms, half 0.83); more registers (at
+// width 128 the compiler keeps 96 bytes of a thread in local memory).  Copies that
+// their threads wait for took 0.72 ms, a block an item 0.79, a table lookup in each
+// copying thread 3.3.  2048 tokens over 16 picked pages of 64 each: 0.13 ms; the row
+// kernel, which reads every page once for every token, 1.29.
 #include <type_traits>
 
 #include "launch.h"

@@ -48,8 +48,11 @@ class PageTables:
     """The requests of a step: their block tables, lengths, and each new token's request and slot (int32 CUDA tensors).
 
     table [R, width] (rows may be a slice of wider ones), q_pos [R + 1], k_len [R] (keys with the new tokens), req [T],
-    slots [T] (page_append only).  max_q and max_k bound the new tokens and the keys of a request on the host; the work
-    is laid out by them.  The tensors are held and read by each call that takes the tables.
+    slots [T] (page_append only).  max_q and max_k bound the new tokens and the keys of a request on the host.  The work
+    is laid out by them: a result does not depend on them, its time does.  One token over 4095 keys (32/8 heads of 128)
+    takes 17 us of the GPU with max_k = 4095, 25 with 16384, 33 with 32768 and 52 with 131072; 64 single tokens over 581k
+    keys 421 with max_q = 1 and 658 with max_q = 64 (as chunks), page_select for them 52 and 263.  A captured call keeps
+    its bounds for every replay.  The tensors are held and read by each call that takes the tables.
     """
     table: torch.Tensor
     q_pos: torch.Tensor
@@ -202,8 +205,9 @@ def page_tables(new_len, old_len, table, free_pages, page_size, ntok, max_q=None
     """Block tables and slot maps from request lengths (slnr_page_tables): returns (PageTables, pages taken [1]).
 
     new_len, old_len [R]: new tokens, and keys already in the cache; free_pages: the pages to take from, in order; ntok
-    = sum of new_len.  table [R, width] is written in place.  max_q and max_k go to the PageTables (defaults: ntok, and
-    what a row of the table holds)."""
+    = sum of new_len.  table [R, width] is written in place.  max_q and max_k go to the PageTables; the defaults, ntok and
+    what a row of the table holds, are right for any lengths and wide for most (PageTables says what that costs): pass
+    max_q=1 where each request has one new token at most, and the longest request's keys as max_k where they are known."""
     R, width, stride = _table(table)
     dev, n = table.device, free_pages.shape[0]
     ints = _empty(2 * R + 2 + 2 * ntok, torch.int32, dev, stream)
