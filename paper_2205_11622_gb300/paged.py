@@ -14,8 +14,8 @@ from typing import Optional
 
 import torch
 
-from . import (SlnrError, _buffer, _capturing, _last_ws, _lock_of_others, _query, _stream_ptr, _workspace_of, last_error,
-               lib, slnr_cache, slnr_opts, slnr_pages, slnr_rows)
+from . import (SlnrError, _buffer, _capturing, _default_ws, _last_ws, _lock_of_others, _new_workspace, _query, _stream_ptr,
+               last_error, lib, slnr_cache, slnr_opts, slnr_pages, slnr_rows)
 
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
@@ -186,14 +186,17 @@ def _call(name, args, index, need, validate, workspace, stream, tensors):
     if validate and need < 256:
         need = 256
     if need:
-        capturing = _capturing(stream)
-        workspace = _workspace_of(workspace, index, s, capturing)
+        capturing = torch.cuda.is_current_stream_capturing() if stream is None else _capturing(s)
+        if workspace is None:
+            workspace = (None if capturing else _default_ws.get((index, s))) or _new_workspace(index, s, capturing)
         # a call's launches follow one another on the stream: no other thread's come between them
         with getattr(workspace, "lock", _lock_of_others):
-            buf, _ = _buffer(workspace, need, stream, capturing, lambda w, n: (w.get(n), None))
+            buf = getattr(workspace, "buf", None)
+            if capturing or buf is None or buf.numel() < need:
+                buf, _ = _buffer(workspace, need, stream, capturing, lambda w, n: (w.get(n), None))
             _last_ws[0] = buf
-            status = getattr(lib(), name)(*args, _byref(slnr_opts(0, 0, 1 if validate else 0, 0, s, buf.data_ptr(),
-                                                                  buf.numel())))
+            o = slnr_opts(0, 0, 1 if validate else 0, 0, s, buf.data_ptr(), buf.numel())
+            status = getattr(lib(), name)(*args, _byref(o))
     else:
         status = getattr(lib(), name)(*args, _byref(slnr_opts(0, 0, 0, 0, s, None, 0)))
     if status != 0:

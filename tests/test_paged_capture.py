@@ -94,3 +94,32 @@ def test_threads_that_share_a_stream(slnr):
         assert len(results) == 20
         for r in results:
             b.check(r, ref)
+
+
+@pytest.mark.parametrize("lens", [[(1, 9000)], [(90, 700)]])
+def test_a_captured_stream_that_is_given(slnr, lens):
+    """The call's stream joins the capture of another that is current; a larger call on it later."""
+    b, larger = P.Batch(lens, 16, 4, 2, 64, seed=66), P.Batch([(1, 9000)] * 40 + [(300, 900)], 16, 4, 2, 64, seed=67)
+    main, side, q, ref = torch.cuda.Stream(), torch.cuda.Stream(), torch.zeros_like(b.q).cuda(), b.attention(0.125)
+    cache, tables = b.cache(), b.tables()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    args = (larger.q.cuda(), larger.cache(), larger.tables())
+    torch.cuda.synchronize()
+    slnr.paged_attention(q, cache, tables, out=out, lse=lse, stream=side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=main):
+        side.wait_stream(main)
+        slnr.paged_attention(q, cache, tables, out=out, lse=lse, stream=side)
+        main.wait_stream(side)
+    slnr.paged_attention(*args, stream=side)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        others = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for n in [1 << k for k in range(9, 27)] * 2]
+    torch.cuda.synchronize()
+    q.copy_(b.q)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    b.check((out, lse), ref)
+    assert all((x == 7).all() for x in others)

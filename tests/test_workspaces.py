@@ -1,7 +1,9 @@
 """Which device buffer a call is given: by the bookkeeping alone, with the library and the GPU faked (no GPU needed)."""
+import contextlib
 import threading
 import time
 import weakref
+from types import SimpleNamespace
 
 import pytest
 
@@ -154,3 +156,34 @@ def test_a_refused_call_leaves_the_workspace_usable(machine, call):
         with pytest.raises(slnr.SlnrError) as e:
             call(1000)
         assert e.value.status == 2
+
+
+def test_a_captured_stream_that_is_given(machine, monkeypatch):
+    """The stream of the call counts, not the current one: captured there, or captured here."""
+    side = SimpleNamespace(cuda_stream=0x20)
+    made, states = [], {0x20: 0}
+
+    def state_of(s, out):
+        out._obj.value = states[s]
+        return 0
+
+    machine.cudaStreamIsCapturing = state_of
+    monkeypatch.setattr(slnr, "_stream_ptr", lambda stream: stream.cuda_stream)
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: made.append(s) or contextlib.nullcontext())
+    run = lambda: slnr._run("slnr_spmm_gemm", slnr.slnr_csr(4, 4, 4, None, None, None), (), (1000,), "fused", True, False,  # noqa: E731
+                            None, side)
+    run()
+    run()
+    assert machine.given[0] == machine.given[1] and made == [side]  # its memory is that stream's; made once
+    states[0x20] = 1
+    run()
+    assert machine.given[2][0] != machine.given[0][0] and made == [side, side]
+    paged._call("slnr_paged_attention", (), 0, 1000, False, None, side, ())
+    assert machine.given[3][0] != machine.given[0][0]
+    states[0x20], machine.capturing = 0, True
+    run()
+    paged._call("slnr_paged_attention", (), 0, 1000, False, None, side, ())
+    assert machine.given[0] == machine.given[4] == machine.given[5]
+    states[0x20] = 2  # a capture that something made void
+    run()
+    assert machine.given[6][0] != machine.given[0][0]
