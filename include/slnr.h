@@ -389,6 +389,109 @@ slnr_status slnr_selected_attention(const slnr_rows *q, int32_t nheads_q, const 
                                     const slnr_pages *pages, const int32_t *picked, int32_t npicked, float scale,
                                     void *out, float *lse, const slnr_opts *opts);
 
+/* ======================================================================
+ * A cache held in 4 bits
+ *
+ * slnr_page_append4 codes new keys and values as it writes them,
+ * slnr_paged_attention4 reads the codes, slnr_page_values4 gives the values
+ * that pages stand for.  Per head, blocks of 16 consecutive columns of a key
+ * (or value) x share a scale s, the smallest number with 7.5 s >= max|x| of
+ * those that have 4 significant bits and are multiples of 2^-17, at most 9216;
+ * x is held as c s, c = x / s rounded to the nearest whole number, halves away
+ * from zero, in [-7, 7].  So what is held is within s / 2 of x up to |x| =
+ * 69120, and beyond it is 64512.  A block with a value that is not finite is
+ * held as NaN.  Held values are exact in bf16 and fp16.
+ *
+ *  - head_dim is 32, 64, 96 or 128, the page size a multiple of 16.
+ *  - A page of one head is page_size head_dim 9/8 bytes, in an order of the
+ *    library's own, at 16-byte aligned strides; its slots may be written in any
+ *    order and again, by slnr_page_append4.  slnr_page_copy4 copies pages.
+ *  - Queries, new keys and values are bf16 or fp16 (dtype: slnr_dtype), and so
+ *    are the outputs; products, sums and maxima are fp32.  The softmax weights
+ *    are rounded once before their product with the values, to fp16 (to bf16
+ *    where a request has more than 32 query rows a key head and the queries are
+ *    bf16).  Of a row of bf16 queries, columns below 2^-28 of its largest are
+ *    rounded by 2^-39 of that.
+ *  - What the section above says of tokens, positions, slots, tables, waits and
+ *    validate mode holds here too.
+ */
+typedef struct slnr_cache4 {
+  int32_t npages, page_size, nheads, head_dim;
+  int64_t page_stride, head_stride; /* bytes, multiples of 16 */
+  void *data;
+} slnr_cache4;
+
+slnr_status slnr_page_append4(const slnr_cache4 *cache, const slnr_pages *pages, const slnr_rows *k,
+                              const slnr_rows *v, int32_t dtype, const slnr_opts *opts);
+
+/* k and v [n][page_size][nheads][head_dim], packed: what pages ids[0 .. n) stand
+ * for (ids NULL: pages 0 .. n); zeros for an id that is no page (validate:
+ * SLNR_ERR_INDEX where it is not negative).  Slots that were not written have
+ * any value. */
+slnr_status slnr_page_values4(const slnr_cache4 *cache, const int32_t *ids, int32_t n, void *k, void *v, int32_t dtype,
+                              const slnr_opts *opts);
+
+/* Attention of the new tokens over all pages of their requests, as
+ * slnr_paged_attention. */
+slnr_status slnr_paged_attention4_workspace(const slnr_cache4 *cache, const slnr_pages *pages, int32_t nheads_q,
+                                            const slnr_opts *opts, size_t *bytes);
+slnr_status slnr_paged_attention4(const slnr_rows *q, int32_t nheads_q, const slnr_cache4 *cache,
+                                  const slnr_pages *pages, int32_t dtype, float scale, void *out, float *lse,
+                                  const slnr_opts *opts);
+
+/* ======================================================================
+ * Whole pages between the steps
+ *
+ * Requests may share pages: those that are full, so that no step writes them.
+ * A table [nreq][width] with lens[nreq] says what requests hold: of request r
+ * the first ceil(lens[r] / page size) entries of its row.  No counts of users
+ * are kept; the calls look at the tables.  Entries that are no pages are
+ * skipped (validate: SLNR_ERR_INDEX), lengths below 0 are 0, those past a row's
+ * end the row's.  A step of a program that serves requests takes its free pages
+ * from slnr_page_free's list.  The calls need a workspace (256 bytes) in
+ * validate mode only. */
+
+/* Pages src[i] of `from` to pages dst[i] of `to`, i < n: keys, values, and the
+ * summaries where both have them.  Entries that are no pages (-1) are skipped
+ * (validate: SLNR_ERR_INDEX where they are past the last one).  No page may be
+ * in dst twice, nor in src and dst of one call over one cache.  The caches have
+ * one page size, width, number of heads and type; their strides may differ. */
+slnr_status slnr_page_copy(const slnr_cache *to, const slnr_cache *from, const int32_t *src, const int32_t *dst,
+                           int32_t n, const slnr_opts *opts);
+slnr_status slnr_page_copy4(const slnr_cache4 *to, const slnr_cache4 *from, const int32_t *src, const int32_t *dst,
+                            int32_t n, const slnr_opts *opts);
+
+/* Requests that go on from others: child i of n from request parent[i] (another
+ * number: a request without keys).  out_table[n][width] (packed; not table
+ * itself) and out_lens[n] are the children's.  They share their parents' full
+ * pages.  A last page that is not full stays with the first child of its parent;
+ * each further child gets the next page of free_pages, and src[i] and dst[i]
+ * (-1 where nothing is to be copied) name the copy that slnr_page_copy has to
+ * make.  used[0] = pages taken; where free_pages is too short dst[i] and the
+ * entry are -1 (validate: SLNR_ERR_INDEX for a parent past the last request
+ * only).  Entries of a row behind its pages are -1.  n <= 65536. */
+slnr_status slnr_page_fork(int32_t nreq, const int32_t *lens, const int32_t *table, int64_t table_stride,
+                           int32_t width, int32_t page_size, const int32_t *parent, int32_t n,
+                           const int32_t *free_pages, int32_t nfree, int32_t *out_table, int32_t *out_lens,
+                           int32_t *src, int32_t *dst, int32_t *used, const slnr_opts *opts);
+
+/* The pages that no request holds: free_pages[npages] in ascending order, -1
+ * behind them, and count[0] of them.  First lens[drop[i]] = 0 for i < ndrop
+ * (entries that are no requests are skipped).  npages <= 8388608. */
+slnr_status slnr_page_free(int32_t nreq, int32_t *lens, const int32_t *table, int64_t table_stride, int32_t width,
+                           int32_t page_size, const int32_t *drop, int32_t ndrop, int32_t npages, int32_t *free_pages,
+                           int32_t *count, const slnr_opts *opts);
+
+/* The pages in use to the front: of used[0] pages that requests hold, those at
+ * used[0] and behind move to the places before it that none holds, in order.
+ * src and dst [npages / 2] name the copies that slnr_page_copy has to make, -1
+ * behind them; ids[npages] is each page's new number, -1 where none holds it;
+ * out_table[nreq][width] (packed; not table itself) the tables with the new
+ * numbers, -1 behind a row's pages.  npages <= 8388608. */
+slnr_status slnr_page_compact(int32_t nreq, const int32_t *lens, const int32_t *table, int64_t table_stride,
+                              int32_t width, int32_t page_size, int32_t npages, int32_t *out_table, int32_t *src,
+                              int32_t *dst, int32_t *ids, int32_t *used, const slnr_opts *opts);
+
 /* ---- per-launch timing (instrumentation) --------------------------------
  * With timing enabled, each call on the calling thread records a CUDA event on
  * opts->stream before each of its phases (a named step of one or two kernel

@@ -67,6 +67,12 @@ class slnr_cache(ctypes.Structure):
                 ("v", ctypes.c_void_p), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
+class slnr_cache4(ctypes.Structure):
+    _fields_ = [("npages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("nheads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("data", ctypes.c_void_p)]
+
+
 class slnr_rows(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p), ("stride_tok", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
 
@@ -75,6 +81,7 @@ class slnr_rows(ctypes.Structure):
 _P, _I32, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)
 _CSR, _CSF, _OPT = ctypes.POINTER(slnr_csr), ctypes.POINTER(slnr_csf3), ctypes.POINTER(slnr_opts)
 _PG, _CA, _RO = ctypes.POINTER(slnr_pages), ctypes.POINTER(slnr_cache), ctypes.POINTER(slnr_rows)
+_C4, _I64 = ctypes.POINTER(slnr_cache4), ctypes.c_int64
 SIGNATURES = {
     "slnr_spmm_gemm_workspace": ([_CSR, _I32, _I32, _OPT, _SZ], ctypes.c_int),
     "slnr_sddmm_spmm_workspace": ([_CSR, _I32, _I32, _OPT, _SZ], ctypes.c_int),
@@ -100,6 +107,15 @@ SIGNATURES = {
     "slnr_selected_attention_workspace": ([_CA, _PG, _I32, _I32, _OPT, _SZ], ctypes.c_int),
     "slnr_paged_attention": ([_RO, _I32, _CA, _PG, ctypes.c_float, _P, _P, _OPT], ctypes.c_int),
     "slnr_selected_attention": ([_RO, _I32, _CA, _PG, _P, _I32, ctypes.c_float, _P, _P, _OPT], ctypes.c_int),
+    "slnr_page_append4": ([_C4, _PG, _RO, _RO, _I32, _OPT], ctypes.c_int),
+    "slnr_page_values4": ([_C4, _P, _I32, _P, _P, _I32, _OPT], ctypes.c_int),
+    "slnr_paged_attention4_workspace": ([_C4, _PG, _I32, _OPT, _SZ], ctypes.c_int),
+    "slnr_paged_attention4": ([_RO, _I32, _C4, _PG, _I32, ctypes.c_float, _P, _P, _OPT], ctypes.c_int),
+    "slnr_page_copy": ([_CA, _CA, _P, _P, _I32, _OPT], ctypes.c_int),
+    "slnr_page_copy4": ([_C4, _C4, _P, _P, _I32, _OPT], ctypes.c_int),
+    "slnr_page_fork": ([_I32, _P, _P, _I64, _I32, _I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _P, _OPT], ctypes.c_int),
+    "slnr_page_free": ([_I32, _P, _P, _I64, _I32, _I32, _P, _I32, _I32, _P, _P, _OPT], ctypes.c_int),
+    "slnr_page_compact": ([_I32, _P, _P, _I64, _I32, _I32, _I32, _P, _P, _P, _P, _P, _OPT], ctypes.c_int),
     "slnr_set_wait_limit": ([ctypes.c_int64], ctypes.c_int),
     "slnr_peak_ffma": ([_P, ctypes.POINTER(ctypes.c_double)], ctypes.c_int),
     "slnr_peak_tf32": ([_P, ctypes.POINTER(ctypes.c_double)], ctypes.c_int),
@@ -598,8 +614,8 @@ def run(op: str, B, dense: dict, **kw):
 
 # ---- the paged cache (paged.py; imported on first use: it needs torch) ---------------------
 
-_PAGED = ("PageTables", "PagedCache", "page_tables", "page_append", "page_select", "paged_attention",
-          "selected_attention")
+_PAGED = ("PageTables", "PagedCache", "PagedCache4", "page_tables", "page_append", "page_values", "page_select",
+          "paged_attention", "selected_attention", "page_copy", "page_fork", "page_free", "page_compact")
 
 
 def __getattr__(name):

@@ -1,0 +1,65 @@
+// Keys and values held in 4 bits (slab4.h): their way back to 16 bits.
+#pragma once
+
+#include "paged.cuh"
+#include "slab4.h"
+
+namespace slnr {
+
+#ifdef __CUDACC__
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
+  return r;
+}
+
+// The four pairs of a word as fp16: 16 + n (pairs 0 and 2) and 256 + n (1 and 3).
+__device__ __forceinline__ void raw_pairs(uint32_t x, uint32_t (&r)[4]) {
+  const uint32_t y = __byte_perm(x, 0, 0x2301);
+  r[0] = and_or(x, 0x03c003c0u, 0x4c004c00u);
+  r[1] = and_or(x, 0x003c003cu, 0x5c005c00u);
+  r[2] = and_or(y, 0x03c003c0u, 0x4c004c00u);
+  r[3] = and_or(y, 0x003c003cu, 0x5c005c00u);
+}
+
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Two scales as what (16 + n) and (256 + n) are multiplied by and added to for code
+// s / 128.  All exact: s / 128 is a whole multiple of 2^-24, 264 s / 128 has 10
+// significant bits and is below 2^15.  (264 s itself would pass fp16's largest number.)
+struct ScalePair {
+  uint32_t s, o16, o256;
+};
+__device__ __forceinline__ ScalePair scale_pair(uint32_t fp16x2) {
+  ScalePair p;
+  p.s = hmul2(fp16x2, 0x20002000u);   // 2^-7
+  p.o16 = hmul2(p.s, 0xce00ce00u);    // -24
+  p.o256 = hmul2(p.s, 0xdc20dc20u);   // -264
+  return p;
+}
+// Byte `i` of x as the fp16 number that it stands for, twice.
+__device__ __forceinline__ uint32_t scale_twice(uint32_t x, int i) {
+  return __byte_perm(x, 0, 0x0404 | (i << 12) | (i << 4)) >> 1;
+}
+// Bytes `i` and `j` side by side, the first in the lower half.
+__device__ __forceinline__ uint32_t scales_of(uint32_t x, int i, int j) {
+  return __byte_perm(x, 0, 0x0404 | (j << 12) | (i << 4)) >> 1;
+}
+#endif
+
+// pages4.cu
+cudaError_t launch_page_append4(const PagesView& p, const Cache4View& c, const RowsView& k, const RowsView& v, int dtype,
+                                cudaStream_t s);
+cudaError_t launch_page_values4(const Cache4View& c, const int32_t* pages, int n, void* k, void* v, int dtype,
+                                cudaStream_t s);
+
+}  // namespace slnr

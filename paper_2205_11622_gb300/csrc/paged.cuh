@@ -36,6 +36,14 @@ struct CacheView {
   float* scales;
 };
 
+// The cache (slnr_cache4); strides in bytes.
+struct Cache4View {
+  uint8_t* data;
+  int64_t page, head;
+  int npages, nheads, width;
+  Divisor slots;  // of a page
+};
+
 #ifdef __CUDACC__
 // Page of a slot.
 __device__ __forceinline__ int page_of(int slot, const CacheView& c) { return c.page.div(slot); }
@@ -88,6 +96,7 @@ struct AttnArgs {
   const int32_t* picked;  // selected attention: [ntok][nheads][npicked]
   int npicked;
   AttnPlan plan;
+  Cache4View c4;  // with data: keys and values in 4 bits; c then has sizes alone
 };
 
 // Launches that follow one another in a call: the next grid may start once every

@@ -1,0 +1,705 @@
+// Attention of new tokens over a cache in 4 bits, rows of a few tokens at a time:
+// the kernel of single tokens and of short chunks (32 query rows of a key head).
+//
+//   o = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q.k_j - m),  m = max_j scale q.k_j
+//
+// over the keys j that the row sees, in one pass.  Bound by memory, 9/16 of a byte
+// a value, if no more than 3 instructions of a lane go into each value: an SM takes
+// 24 bytes, 43 values, a cycle, and has 128 lanes for them.  So:
+//   - Keys are the rows of both products (S^T = K Q^T, O^T = V^T P^T), 16 at a time,
+//     and the query rows their columns, 8 at a time: 8 query rows cost half of what
+//     16 would.  P^T is turned from the one product's result into the other's
+//     operand by the matrix transpose of a warp.
+//   - A pair of codes becomes a pair of fp16 numbers by one logical instruction and one
+//     multiplication and addition, with the scale (cache4.cuh).  Held values / 128 are
+//     exact in fp16 whatever type wrote them; queries of bf16 are taken as fp16
+//     times a power of two of their row, weights as fp16 against 2^-12 of the
+//     maximum, which is followed when it grew by 2^3, so none passes 2^15, and what
+//     is lost of n small ones is n 2^-37 of the largest at most.
+//   - A slab of 16 slots lies as its lanes read it: 16-byte loads without bank
+//     conflicts, no shuffles.
+//   - Each warp has a ring of slabs of its own, filled by bulk copies that its own lanes
+//     issue and wait for: no barrier of the block inside of an item.
+//
+// The units (32 keys) of all requests and key heads, one after another, are cut into
+// equal shares, one a block; its warps take them in turn.  Items that a cut goes
+// through are joined by k_paged4_join.
+#include <type_traits>
+
+#include "cache4.cuh"
+#include "launch.h"
+#include "mma16.cuh"
+#include "paged4.cuh"
+#include "tcgen05.cuh"
+
+namespace slnr {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kStages = 3;
+constexpr int kUnit = 2 * kSlab;  // keys of a stage
+constexpr float kBelow = 12.f, kGrow = 3.f;
+
+size_t smem_bytes(int width, int rows) {
+  const int w = width <= 64 ? 64 : 128;
+  return (size_t)kWarps * kStages * 2 * slab_bytes(width) + (size_t)kWarps * rows * (w + 4) * 4;
+}
+
+__device__ __forceinline__ void copy_bulk(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(tc::smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ void expect(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(tc::smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(tc::smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+constexpr long long kShortLimit = 1 << 20;  // cycles; a try_wait may sleep for longer than a limit below that
+
+// Waits for the phase of that parity; false after `limit` cycles.
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, long long limit) {
+  const bool sleeps = limit >= kShortLimit;
+  if (sleeps ? tc::mbar_try_wait(bar, parity) : test(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!(sleeps ? tc::mbar_try_wait(bar, parity) : test(bar, parity)))
+    if (clock64() - t0 > limit) return false;
+  return true;
+}
+
+__device__ __forceinline__ void lds4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void lds2(uint32_t& a, uint32_t& b, uint32_t at) {
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t lds1(uint32_t at) {
+  uint32_t r;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(at) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint32_t lds_half(uint32_t at) {
+  uint16_t r;
+  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(r) : "r"(at) : "memory");
+  return r;
+}
+// An 8 x 8 matrix of 16-bit values, a pair of a row's neighbours a lane, turned.
+__device__ __forceinline__ uint32_t turned(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ float2 to_float2(uint32_t x);
+template <>
+__device__ __forceinline__ float2 to_float2<__nv_bfloat16>(uint32_t x) {
+  return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+}
+template <>
+__device__ __forceinline__ float2 to_float2<__half>(uint32_t x) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&x));
+}
+
+// What a block knows of a request.
+struct Request {
+  int r, q0, qn, keys, units;  // its first token, tokens, keys, units of 32 keys (0: no tokens)
+};
+__device__ __forceinline__ int units_of(int qn, int keys) {
+  return qn > 0 ? (keys > 0 ? (keys - 1) / kUnit + 1 : 1) : 0;
+}
+__device__ __forceinline__ Request request(const PagesView& p, int r) {
+  Request q{r, 0, 0, 0, 0};
+  if (r < p.nreq) {
+    q.q0 = __ldg(p.q_pos + r);
+    q.qn = __ldg(p.q_pos + r + 1) - q.q0;
+    q.keys = max(__ldg(p.k_len + r), 0);
+    q.units = units_of(q.qn, q.keys);
+  }
+  return q;
+}
+
+// Units of all requests (of one key head) before request `upto`, or of the requests
+// before the one that holds unit `at` of `heads` heads each, which goes to r (a whole
+// warp; nreq: past the last one).
+__device__ __forceinline__ int64_t units_before(const PagesView& p, int heads, int64_t at, int& r) {
+  const int lane = threadIdx.x & 31;
+  int64_t before = 0;
+  for (int r0 = 0; r0 < p.nreq; r0 += 32) {
+    const int i = r0 + lane;
+    const int mine = i < p.nreq ? units_of(__ldg(p.q_pos + i + 1) - __ldg(p.q_pos + i), __ldg(p.k_len + i)) : 0;
+    int64_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, (before + sum) * heads > at);
+    if (past) {
+      const int from = __ffs(past) - 1;
+      r = r0 + from;
+      return before + __shfl_sync(0xffffffffu, sum - mine, from);
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  r = p.nreq;
+  return before;
+}
+
+// The part of an item that a block works on: units [u0, u1) of request q.r and head h.
+struct Part {
+  Request q;
+  int h, u0, u1;
+  int64_t left;  // units of the share behind it
+};
+__device__ __forceinline__ void clip(Part& s, int64_t left) {
+  s.u1 = (int)(s.q.units - s.u0 < left ? s.q.units : s.u0 + left);
+  s.left = left - (s.u1 - s.u0);
+}
+// The next one; its left is below 0 where there is none.
+__device__ __forceinline__ void advance(const Attn4Args& a, Part& s) {
+  if (s.left <= 0) {
+    s.left = -1;
+    return;
+  }
+  if (++s.h == a.c.nheads) {
+    s.h = 0;
+    do s.q = request(a.p, s.q.r + 1);
+    while (s.q.units == 0 && s.q.r < a.p.nreq);
+    if (s.q.r >= a.p.nreq) {  // not met: the shares end with the last item
+      s.left = -1;
+      return;
+    }
+  }
+  s.u0 = 0;
+  clip(s, s.left);
+}
+
+struct Shared {
+  uint64_t full[kWarps][kStages];
+  float2 ml[kWarps][32];  // a warp's (reference, sum) of each row
+  int failed[kWarps];
+};
+
+template <typename T, int W, int NT>
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : NT == 2 ? 2 : 1)
+k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
+  constexpr int WORDS = W / 32;  // of a key, a lane: its columns are 8 WORDS t ..
+  constexpr int MT = W / 16;
+  extern __shared__ __align__(128) unsigned char raw[];
+  __shared__ Shared sh;
+  const PagesView& p = a.p;
+  const Cache4View& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int G = a.group.d, D = c.width, slab = slab_bytes(D);
+  let_next_start();
+
+  // the block's share
+  int r;
+  const int64_t total = units_before(p, c.nheads, INT64_MAX, r) * c.nheads;
+  const int64_t most = (total + a.least - 1) / a.least;
+  const int n = (int)(most < gridDim.x ? most : gridDim.x);
+  if (blockIdx.x >= n) {
+    if (blockIdx.x == 0 && tid == 0) a.shares[a.nblocks] = make_int4(0, 0, 0, 0);
+    return;
+  }
+  const int64_t lo = total / n * blockIdx.x + total % n * blockIdx.x / n;
+  const int64_t hi = total / n * (blockIdx.x + 1) + total % n * (blockIdx.x + 1) / n;
+  Part s;
+  {
+    const int64_t in = lo - units_before(p, c.nheads, lo, r) * c.nheads;
+    s.q = request(p, r);
+    s.h = (int)(in / s.q.units);
+    s.u0 = (int)(in - (int64_t)s.h * s.q.units);
+    clip(s, hi - lo);
+  }
+  if (tid == 0) {
+    a.shares[blockIdx.x] = make_int4(s.q.r, s.h, s.u0, 0);
+    if (blockIdx.x == 0) a.shares[a.nblocks] = make_int4(n, 0, 0, 0);
+  }
+
+  uint64_t* full = sh.full[warp];
+  if (lane < kStages) tc::mbar_init(full + lane, 1);
+  tc::fence_mbar_init();
+  __syncwarp();
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(raw) + warp * kStages * 2 * slab;
+  float* rows = reinterpret_cast<float*>(raw + kWarps * kStages * 2 * slab);
+
+  // The copies run ahead of the work: at unit cu of part cs, whose pages (one a lane of the first two) were looked up
+  // before.
+  Part cs = s;
+  int cu = cs.u0 + warp, issued = 0, id = -1;
+  const bool whole = c.slots.d % kUnit == 0;  // both slabs of a unit lie in one page, one after another
+  auto look_up = [&] {
+    while (cs.left >= 0 && cu >= cs.u1) {
+      advance(a, cs);
+      cu = cs.u0 + warp;
+    }
+    id = -1;
+    if (cs.left < 0 || lane > 1) return;
+    const int key = cu * kUnit + lane * kSlab;
+    if (key < cs.q.keys) {
+      const int i = c.slots.div(key);
+      if (i < p.width) id = __ldg(p.table + cs.q.r * p.table_stride + i);
+    }
+  };
+  auto issue = [&] {  // into the stage of unit `issued` of this warp
+    if (cs.left < 0) return;
+    const int key = cu * kUnit + lane * kSlab;
+    const bool on = (unsigned)id < (unsigned)c.npages;
+    const uint32_t both = __ballot_sync(0xffffffffu, on);
+    uint64_t* bar = full + issued % kStages;
+    const uint32_t dst = ring + issued % kStages * 2 * slab;
+    if (lane == 0) expect(bar, __popc(both) * slab);
+    __syncwarp();
+    if (on && !(whole && lane == 1 && (both & 1))) {
+      const int page_slot = key - c.slots.div(key) * c.slots.d;
+      const uint8_t* src = c.data + id * c.page + cs.h * c.head + (int64_t)(page_slot / kSlab) * slab;
+      copy_bulk(dst + lane * slab, src, whole && both == 3 ? 2 * slab : slab, bar);
+    }
+    ++issued;
+    cu += kWarps;
+    look_up();
+  };
+  look_up();
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) issue();
+
+  int taken = 0;
+  bool ok = true;
+  for (; s.left >= 0; advance(a, s)) {
+    const Request& q = s.q;
+    const int n_rows = min(q.qn * G, 8 * NT);
+    const int first = q.keys - q.qn;  // position of its first token (lengths below 0 are 0: all tokens see nothing)
+    // query fragments, and what a row's scores are multiplied by: log2 e scale, 128 of the held values, its power of two
+    uint32_t qf[NT][2 * WORDS][2];
+    float f[NT][2], m[NT][2], l[NT][2];
+    int pos[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int x = 8 * nt + g;
+      const bool on = x < n_rows;
+      const int tok = on ? a.group.div(x) : 0, gg = on ? x - tok * G : 0;
+      const T* row = (const T*)a.q.p + (int64_t)(q.q0 + tok) * a.q.tok + (int64_t)(s.h * G + gg) * a.q.head + 8 * WORDS * t;
+      uint4 raw_q[WORDS];
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w)
+        raw_q[w] = on && 8 * (WORDS * t + w) < D ? __ldg(reinterpret_cast<const uint4*>(row) + w) : make_uint4(0, 0, 0, 0);
+      float factor = a.scale * 1.4426950408889634f;
+      if constexpr (std::is_same<T, __half>::value) {
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+          qf[nt][2 * w][0] = raw_q[w].x;
+          qf[nt][2 * w][1] = raw_q[w].y;
+          qf[nt][2 * w + 1][0] = raw_q[w].z;
+          qf[nt][2 * w + 1][1] = raw_q[w].w;
+        }
+        factor *= 128.f;
+      } else {
+        uint32_t top = 0;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+          const uint32_t e[4] = {raw_q[w].x, raw_q[w].y, raw_q[w].z, raw_q[w].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = max(top, max(e[i] & 0x7fffu, (e[i] >> 16) & 0x7fffu));
+        }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // the row times 2^(14 - e), e the exponent of its largest value, which is below 2^15 then: in two steps, as either
+        // power alone may not be a number.  Zeros, infinities and NaN: times 1.
+        const int ex = top == 0 || top >= 0x7f80u ? 14 : max((int)(top >> 7), 1) - 127;
+        const float up = __uint_as_float((uint32_t)(127 + (14 - ex) / 2) << 23);
+        const float up2 = __uint_as_float((uint32_t)(127 + (14 - ex) - (14 - ex) / 2) << 23);
+        factor = factor * (128.f / up) / up2;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+          const uint32_t e[4] = {raw_q[w].x, raw_q[w].y, raw_q[w].z, raw_q[w].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 y = to_float2<__nv_bfloat16>(e[i]);
+            qf[nt][2 * w + i / 2][i & 1] = Half2<__half>::pack(y.x * up * up2, y.y * up * up2);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {  // of the columns that this lane has of the products
+        f[nt][i] = __shfl_sync(0xffffffffu, factor, 4 * (2 * t + i));
+        const int y = 8 * nt + 2 * t + i;
+        pos[nt][i] = y < n_rows ? first + a.group.div(y) : INT32_MAX;
+        m[nt][i] = -INFINITY;
+        l[nt][i] = 0.f;
+      }
+    }
+    float o[MT][NT][4];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) o[i][j][0] = o[i][j][1] = o[i][j][2] = o[i][j][3] = 0.f;
+
+    for (int u = s.u0 + warp; u < s.u1; u += kWarps) {
+      const uint32_t stage = ring + taken % kStages * 2 * slab;
+      ok = ok && __all_sync(0xffffffffu, wait(full + taken % kStages, taken / kStages & 1, limit));
+      if (!ok) continue;  // no more copies are issued
+      const int key0 = u * kUnit;
+      const int slabs = q.keys - key0 > kSlab ? 2 : q.keys > key0 ? 1 : 0;
+      float x[2][NT][4];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) x[b][j][0] = x[b][j][1] = x[b][j][2] = x[b][j][3] = 0.f;
+        if (b < slabs) {
+          const uint32_t at = stage + b * slab;
+          uint32_t w0[WORDS] = {}, w1[WORDS] = {}, sc = 0;
+          if (8 * WORDS * t < D) {
+            const uint32_t from = at + (4 * (g >> 1) + (g & 1)) * (D / 2) + 4 * WORDS * t;
+            if constexpr (W == 128) {
+              lds4(w0, from);
+              lds4(w1, from + D);  // two slots on
+              sc = lds1(at + 8 * D + (g * (D / 32) + t) * 4);
+            } else {
+              lds2(w0[0], w0[1], from);
+              lds2(w1[0], w1[1], from + D);
+              sc = lds_half(at + 8 * D + (g * (D / 16) + t) * 2);
+            }
+          }
+          ScalePair s0, s1;
+#pragma unroll
+          for (int w = 0; w < WORDS; ++w) {
+            if (w % 2 == 0) {
+              s0 = scale_pair(scale_twice(sc, W == 128 ? w / 2 : 0));
+              s1 = scale_pair(scale_twice(sc, W == 128 ? 2 + w / 2 : 1));
+            }
+            uint32_t y0[4], y1[4];
+            raw_pairs(w0[w], y0);
+            raw_pairs(w1[w], y1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              y0[i] = hfma2(y0[i], s0.s, i & 1 ? s0.o256 : s0.o16);
+              y1[i] = hfma2(y1[i], s1.s, i & 1 ? s1.o256 : s1.o16);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t key[4] = {y0[2 * k], y1[2 * k], y0[2 * k + 1], y1[2 * k + 1]};
+#pragma unroll
+              for (int j = 0; j < NT; ++j) Half2<__half>::mma(x[b][j], key, qf[j][2 * w + k][0], qf[j][2 * w + k][1]);
+            }
+          }
+        }
+      }
+      // scores in units of log 2; -inf where the row does not see the key
+      const bool masked = key0 + kUnit - 1 > first;
+      bool grow = false;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float& y = x[b][j][2 * k + i];
+              y = __fmul_rn(y, f[j][i]);
+              const int key = key0 + b * kSlab + 4 * (g >> 1) + (g & 1) + 2 * k;
+              if (masked && (key > pos[j][i] || key >= q.keys)) y = -INFINITY;
+              top = fmaxf(top, y);
+            }
+          grow = grow || top - m[j][i] > kBelow + kGrow;
+        }
+      if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float top = fmaxf(fmaxf(x[0][j][i], x[0][j][2 + i]), fmaxf(x[1][j][i], x[1][j][2 + i]));
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            if (top - m[j][i] > kBelow + kGrow) {  // rounded up: no weight passes 2^kBelow, however large the maximum
+              const float to = __fsub_ru(top, kBelow), by = exp2_fast(m[j][i] - to);
+              m[j][i] = to;
+              l[j][i] *= by;
+#pragma unroll
+              for (int k = 0; k < MT; ++k) {
+                o[k][j][i] *= by;
+                o[k][j][2 + i] *= by;
+              }
+            }
+          }
+      }
+      uint32_t w[2][NT][2];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        float ref[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) ref[i] = m[j][i] == -INFINITY ? 0.f : m[j][i];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float w0 = exp2_fast(__fsub_rn(x[b][j][2 * k], ref[0]));
+            const float w1 = exp2_fast(__fsub_rn(x[b][j][2 * k + 1], ref[1]));
+            l[j][0] += w0;
+            l[j][1] += w1;
+            w[b][j][k] = turned(Half2<__half>::pack(w0, w1));
+          }
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if (b >= slabs) break;
+        const uint32_t at = stage + b * slab;
+        uint32_t v0[W / 32] = {}, v1[W / 32] = {}, sc = 0;  // W = 128: two words a slot; 64: one
+        if (W / 8 * g < D) {
+          if constexpr (W == 128) {
+            lds4(v0, at + 9 * D + lane * 16);
+            lds4(v1, at + 13 * D + lane * 16);
+            sc = lds1(at + 17 * D + g * 16 + 4 * t);
+          } else {
+            uint32_t v[4];
+            lds4(v, at + 9 * D + lane * 16);
+            v0[0] = v[0];
+            v0[1] = v[1];
+            v1[0] = v[2];
+            v1[1] = v[3];
+            sc = lds1(at + 17 * D + (g >> 1) * 16 + 4 * t);
+          }
+        }
+        const int left = q.keys - key0 - b * kSlab - 4 * t;  // slots past the last key hold anything: scales of 0
+        if (left < 4) sc &= left > 0 ? (1u << 8 * left) - 1 : 0u;
+        const ScalePair s0 = scale_pair(scales_of(sc, 0, 1)), s1 = scale_pair(scales_of(sc, 2, 3));
+#pragma unroll
+        for (int e = 0; e < W / 64; ++e) {
+          // slots 4 t and 4 t + 1, 4 t + 2 and 4 t + 3: of each pair the even columns, the odd ones
+          uint32_t y[4][4];
+          const uint32_t a0 = v0[e], a1 = v0[e + W / 64], b0 = v1[e], b1 = v1[e + W / 64];
+          raw_pairs(__byte_perm(a0, a1, 0x5410), y[0]);
+          raw_pairs(__byte_perm(a0, a1, 0x7632), y[1]);
+          raw_pairs(__byte_perm(b0, b1, 0x5410), y[2]);
+          raw_pairs(__byte_perm(b0, b1, 0x7632), y[3]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t val[4] = {hfma2(y[0][i], s0.s, i & 1 ? s0.o256 : s0.o16),
+                                     hfma2(y[1][i], s0.s, i & 1 ? s0.o256 : s0.o16),
+                                     hfma2(y[2][i], s1.s, i & 1 ? s1.o256 : s1.o16),
+                                     hfma2(y[3][i], s1.s, i & 1 ? s1.o256 : s1.o16)};
+#pragma unroll
+            for (int j = 0; j < NT; ++j) Half2<__half>::mma(o[4 * e + i][j], val, w[b][j][0], w[b][j][1]);
+          }
+        }
+      }
+      __syncwarp();  // the stage has been read
+      ++taken;
+      issue();
+    }
+
+    // the warps' sums, joined
+    if (!ok) {  // NaN, not what the memory held: no wait gives up unseen
+#pragma unroll
+      for (int j = 0; j < NT; ++j) m[j][0] = m[j][1] = l[j][0] = l[j][1] = __int_as_float(0x7fffffff);
+    }
+    float* mine = rows + warp * 8 * NT * (W + 4);
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) l[j][i] += __shfl_xor_sync(0xffffffffu, l[j][i], d);
+        const int y = 8 * j + 2 * t + i;
+        if (g == 0) sh.ml[warp][y] = make_float2(m[j][i], l[j][i]);
+        // columns 16 g .. (W = 128), 8 g ..
+#pragma unroll
+        for (int k = 0; k < MT; ++k)
+          *reinterpret_cast<float2*>(mine + y * (W + 4) + MT * 2 * g + 2 * k) = make_float2(o[k][j][i], o[k][j][2 + i]);
+      }
+    __syncthreads();
+    constexpr int PIECES = W / 8, ROWS = kThreads / PIECES;
+    const int col = tid % PIECES * 8;
+    const bool all = s.u0 == 0 && s.u1 == q.units;
+    for (int y = tid / PIECES; y < n_rows; y += ROWS) {
+      float mx = -INFINITY, sum = 0.f, acc[8] = {};
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) {
+        const float v = sh.ml[k][y].x;
+        mx = v != v ? v : fmaxf(mx, v);
+      }
+      const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) {
+        const float2 ml = sh.ml[k][y];
+        const float by = exp2_fast(ml.x - ref);
+        sum += by * ml.y;
+        const float4* z = reinterpret_cast<const float4*>(rows + (k * 8 * NT + y) * (W + 4) + col);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float4 v = z[e];
+          acc[4 * e] += by * v.x;
+          acc[4 * e + 1] += by * v.y;
+          acc[4 * e + 2] += by * v.z;
+          acc[4 * e + 3] += by * v.w;
+        }
+      }
+      const float inv = sum == 0.f ? 0.f : __fdividef(128.f, sum);  // no key: zeros
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = sum == 0.f ? 0.f : acc[e] * inv;
+      if (col >= D) continue;
+      if (all) {
+        const int tok = a.group.div(y);
+        const int64_t at = (int64_t)(q.q0 + tok) * c.nheads * G + s.h * G + y - tok * G;
+        const uint4 z = make_uint4(Half2<T>::pack(acc[0], acc[1]), Half2<T>::pack(acc[2], acc[3]),
+                                   Half2<T>::pack(acc[4], acc[5]), Half2<T>::pack(acc[6], acc[7]));
+        *reinterpret_cast<uint4*>((T*)a.out + at * D + col) = z;
+        if (col == 0 && a.lse) a.lse[at] = (mx + __log2f(sum)) * 0.6931471805599453f;
+      } else {
+        const int64_t at = (int64_t)(2 * blockIdx.x + (s.u0 == 0)) * (8 * NT) + y;
+        float4* z = reinterpret_cast<float4*>(a.part + at * D + col);
+        z[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        z[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        if (col == 0) a.part_ml[at] = make_float2(mx, sum);
+      }
+    }
+    __syncthreads();
+  }
+  if (lane == 0) sh.failed[warp] = !ok;
+  // the copies in flight end before the block does
+  if (!ok)
+    for (; taken < issued; ++taken) wait(full + taken % kStages, taken / kStages & 1, kWaitCycles);
+  __syncthreads();
+  if (tid == 0) {
+    int failed = 0;
+    for (int k = 0; k < kWarps; ++k) failed |= sh.failed[k];
+    if (failed) a.shares[blockIdx.x].w = 1;
+  }
+}
+
+// Items that cuts went through: o = sum 2^(m_part - m) l_part o_part / sum 2^(m_part - m) l_part
+// over their parts.  Block x: the item that share x + 1 begins inside of, if no share
+// before does; block y: a row of it.  Each of the 4 warps adds every fourth part in
+// their order, the warps' sums are added in theirs.
+template <typename T>
+__global__ void __launch_bounds__(128)
+k_paged4_join(const __grid_constant__ Attn4Args a, WsHeader* hdr) {
+  __shared__ float4 sums[4][32];
+  __shared__ float weights[4];
+  wait_for_previous();
+  const int n = a.shares[a.nblocks].x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && warp == 0) {
+    int failed = 0;
+    for (int i = lane; i < n; i += 32) failed |= a.shares[i].w;
+    failed = __any_sync(0xffffffffu, failed);
+    if (lane == 0) hdr->error = failed ? kErrTimeout : 0;
+  }
+  const int c0 = blockIdx.x + 1;
+  if (c0 >= n) return;
+  const int4 cut = a.shares[c0], before = a.shares[c0 - 1];
+  if (cut.z == 0 || (before.x == cut.x && before.y == cut.y && before.z > 0)) return;
+  const int G = a.group.d, D = a.c.width, y = blockIdx.y;
+  const int q0 = __ldg(a.p.q_pos + cut.x), n_rows = (__ldg(a.p.q_pos + cut.x + 1) - q0) * G;
+  if (y >= n_rows) return;
+  int c1 = c0 + 1;  // shares c0 .. c1 - 1 begin inside of the item
+  for (; c1 < n; ++c1) {
+    const int4 s = a.shares[c1];
+    if (s.x != cut.x || s.y != cut.y || s.z == 0) break;
+  }
+  const int parts = c1 - c0 + 1;
+  auto part = [&](int k) { return (int64_t)(2 * (c0 - 1 + k) + (k == 0)) * a.tile + y; };
+  float m = -INFINITY;
+  bool nan = false;
+  for (int k = lane; k < parts; k += 32) {
+    const float v = a.part_ml[part(k)].x;
+    nan = nan || v != v;
+    m = fmaxf(m, v);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (__any_sync(0xffffffffu, nan)) m = __int_as_float(0x7fffffff);
+  const float ref = m == -INFINITY ? 0.f : m;
+  const int col = 4 * lane;
+  float sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int k = warp; k < parts; k += 4) {
+    const int64_t at = part(k);
+    const float2 ml = a.part_ml[at];
+    const float f = exp2_fast(ml.x - ref) * ml.y;
+    sum += f;
+    if (col < D) {
+      const float4 x = *reinterpret_cast<const float4*>(a.part + at * D + col);
+      acc.x += f * x.x;
+      acc.y += f * x.y;
+      acc.z += f * x.z;
+      acc.w += f * x.w;
+    }
+  }
+  sums[warp][lane] = acc;
+  if (lane == 0) weights[warp] = sum;
+  __syncthreads();
+  if (warp > 0) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+    const float4 x = sums[w][lane];
+    sum += weights[w];
+    acc.x += x.x;
+    acc.y += x.y;
+    acc.z += x.z;
+    acc.w += x.w;
+  }
+  const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);  // the parts of a row without keys are zeros
+  const int tok = a.group.div(y);
+  const int64_t at = (int64_t)(q0 + tok) * a.c.nheads * G + cut.y * G + y - tok * G;
+  if (col < D) {
+    uint2 z;
+    z.x = Half2<T>::pack(acc.x * inv, acc.y * inv);
+    z.y = Half2<T>::pack(acc.z * inv, acc.w * inv);
+    *reinterpret_cast<uint2*>((T*)a.out + at * D + col) = z;
+  }
+  if (lane == 0 && a.lse) a.lse[at] = (m + __log2f(sum)) * 0.6931471805599453f;
+}
+
+template <typename T, int W, int NT>
+cudaError_t launch_rows(const Attn4Args& a, cudaStream_t s) {
+  auto kernel = k_paged4_rows<T, W, NT>;
+  static OncePerDevice once;
+  const cudaError_t e = once([&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(W, 8 * NT));
+  });
+  if (e != cudaSuccess) return e;
+  kernel<<<SLNR_COUNTED((unsigned)a.nblocks), kThreads, smem_bytes(a.c.width, 8 * NT), s>>>(a, wait_limit_cycles());
+  return cudaGetLastError();
+}
+
+template <typename T, int W>
+cudaError_t launch_rows_w(const Attn4Args& a, cudaStream_t s) {
+  switch (a.tile) {
+    case 8: return launch_rows<T, W, 1>(a, s);
+    case 16: return launch_rows<T, W, 2>(a, s);
+    default: return launch_rows<T, W, 4>(a, s);
+  }
+}
+
+template <typename T>
+cudaError_t launch_rows_t(const Attn4Args& a, cudaStream_t s) {
+  return a.c.width <= 64 ? launch_rows_w<T, 64>(a, s) : launch_rows_w<T, 128>(a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_paged4_rows(const Attn4Args& a, int dtype, cudaStream_t s) {
+  return dtype == SLNR_FP16 ? launch_rows_t<__half>(a, s) : launch_rows_t<__nv_bfloat16>(a, s);
+}
+
+cudaError_t launch_paged4_join(const Attn4Args& a, int dtype, WsHeader* hdr, cudaStream_t s) {
+  const dim3 grid((unsigned)a.nblocks, (unsigned)a.tile);
+  auto kernel = dtype == SLNR_FP16 ? k_paged4_join<__half> : k_paged4_join<__nv_bfloat16>;
+  return launch_next(kernel, SLNR_COUNTED(grid), dim3(128), 0, s, a, hdr);
+}
+
+}  // namespace slnr

@@ -1,10 +1,14 @@
 // C entry points of the paged cache (declared in include/slnr.h): argument
 // checks, workspace layout and launches.
 #include <cmath>
+#include <utility>
 
+#include "cache4.cuh"
 #include "call.h"
 #include "launch.h"
+#include "page_sets.cuh"
 #include "paged.cuh"
+#include "paged4.cuh"
 
 using namespace slnr;
 
@@ -121,6 +125,93 @@ slnr_status validated(const slnr_opts* o, Launch launch) {
   return SLNR_OK;
 }
 
+slnr_status check_type(int32_t dtype) {
+  if (dtype != SLNR_BF16 && dtype != SLNR_FP16) return fail(SLNR_ERR_UNSUPPORTED, "unknown type %d", (int)dtype);
+  return SLNR_OK;
+}
+
+// The sizes of a cache in 4 bits, for the checks that want no more.
+slnr_cache sizes(const slnr_cache4& c) {
+  slnr_cache s{};
+  s.npages = c.npages;
+  s.page_size = c.page_size;
+  s.nheads = c.nheads;
+  s.head_dim = c.head_dim;
+  return s;
+}
+
+slnr_status check_cache4(const slnr_cache4* c, bool pointers) {
+  if (!c) return fail(SLNR_ERR_NULL, "cache is NULL");
+  const slnr_cache s = sizes(*c);
+  SLNR_CHECK(check_cache(&s, false, false, false));
+  if (c->head_dim % 32 != 0)
+    return fail(SLNR_ERR_UNSUPPORTED, "head_dim = %d: 32, 64, 96 or 128 in 4 bits", (int)c->head_dim);
+  if (c->page_size % kSlab != 0)
+    return fail(SLNR_ERR_UNSUPPORTED, "page_size = %d: a multiple of %d in 4 bits", (int)c->page_size, kSlab);
+  if (c->page_stride < 0 || c->page_stride % 16 != 0 || c->head_stride < 0 || c->head_stride % 16 != 0)
+    return fail(SLNR_ERR_UNSUPPORTED, "cache strides %lld and %lld must be multiples of 16 bytes",
+                (long long)c->page_stride, (long long)c->head_stride);
+  if (pointers && c->npages > 0) {
+    if (!c->data) return fail(SLNR_ERR_NULL, "cache.data is NULL");
+    if (!aligned16(c->data)) return fail(SLNR_ERR_UNSUPPORTED, "cache.data must be 16-byte aligned");
+  }
+  return SLNR_OK;
+}
+
+Cache4View view(const slnr_cache4& c) {
+  return Cache4View{(uint8_t*)c.data, c.page_stride, c.head_stride, c.npages, c.nheads, c.head_dim, divisor(c.page_size)};
+}
+
+// What slnr_page_fork, _free and _compact are given of the requests.
+slnr_status check_tables(int32_t nreq, const int32_t* lens, const int32_t* table, int64_t table_stride, int32_t width,
+                         int32_t page_size, const slnr_opts* opts) {
+  SLNR_CHECK(check_paged_opts(opts));
+  if (nreq < 0 || width < 0 || table_stride < width)
+    return fail(SLNR_ERR_SHAPE, "negative size, or rows of table that overlap");
+  if (page_size <= 0) return fail(SLNR_ERR_SHAPE, "page_size = %d must be positive", (int)page_size);
+  if (nreq > 0 && (!lens || (width > 0 && !table))) return fail(SLNR_ERR_NULL, "lens or table is NULL");
+  return SLNR_OK;
+}
+
+slnr_status check_set(int32_t npages) {
+  if (npages < 0) return fail(SLNR_ERR_SHAPE, "npages = %d", (int)npages);
+  if (npages > kMaxSetPages)
+    return fail(SLNR_ERR_UNSUPPORTED, "npages = %d: at most %d", (int)npages, kMaxSetPages);
+  return SLNR_OK;
+}
+
+slnr_status check_copy(const int32_t* src, const int32_t* dst, int32_t n, const slnr_opts* opts) {
+  SLNR_CHECK(check_paged_opts(opts));
+  if (n < 0) return fail(SLNR_ERR_SHAPE, "n = %d", (int)n);
+  if (n > 0 && (!src || !dst)) return fail(SLNR_ERR_NULL, "src or dst is NULL");
+  return SLNR_OK;
+}
+
+// Adds a tensor of outer x inner rows of `row` bytes a page.  False: too many units for an int.
+bool add_part(CopyParts& c, const void* from, void* to, const int64_t (&f)[3], const int64_t (&t)[3], int64_t outer,
+              int64_t inner, int64_t row, int unit) {
+  const int64_t pieces = outer * inner * (row / unit);
+  if (pieces > INT32_MAX - kCopyItem) return false;
+  CopyPart& a = c.part[c.n++];
+  a = CopyPart{(const char*)from, (char*)to, f[0], t[0], f[1], t[1], f[2], t[2], divisor((int)inner),
+               divisor((int)(row / unit)), unit, (int)pieces, c.items};
+  const int64_t items = c.items + (pieces + kCopyItem - 1) / kCopyItem;
+  c.items = (int)items;
+  return items <= INT32_MAX;
+}
+
+slnr_status copy_pages(const CopyParts& c, const int32_t* src, const int32_t* dst, int32_t n, int32_t from_pages,
+                       int32_t to_pages, const slnr_opts* opts) {
+  cudaStream_t s = (cudaStream_t)opts->stream;
+  const TablesView none{0, 0, 0, divisor(1), nullptr, nullptr};
+  SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
+    return launch_validate_set(none, 0, src, n, from_pages, dst, to_pages, hdr, st);
+  }));
+  SLNR_LAUNCH("page_copy", launch_page_copy(c, src, dst, n, from_pages, to_pages, s));
+  timing_end(s);
+  return SLNR_OK;
+}
+
 constexpr int64_t kSms = 152;          // of one block of the tensor-core kernel, two of the row kernel's
 constexpr int64_t kMaxBlocks = 16384;  // splits stop here
 constexpr int64_t kMaxCluster = 16;
@@ -221,6 +312,17 @@ AttnLayout attn_layout(const slnr_cache& c, const slnr_pages& p, int32_t nheads_
   return l;
 }
 
+void place(AttnPlan& a, const AttnLayout& l, char* ws) {
+  a.part = (float*)(ws + l.part);
+  a.part_ml = (float2*)(ws + l.ml);
+  a.tiles = (int4*)(ws + l.tiles);
+  a.before = (int64_t*)(ws + l.before);
+  a.shares = (int2*)(ws + l.shares);
+  a.pages = (int32_t*)(ws + l.pages);
+  a.pickers = (uint32_t*)(ws + l.pickers);
+  a.npages = (int32_t*)(ws + l.npages);
+}
+
 slnr_status attention_workspace(const slnr_cache* cache, const slnr_pages* pages, int32_t nheads_q, int32_t npicked,
                                 const slnr_opts* opts, size_t* bytes) {
   if (!bytes) return fail(SLNR_ERR_NULL, "bytes is NULL");
@@ -257,14 +359,7 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   const AttnLayout l = attn_layout(*cache, *pages, nheads_q, a.plan);
   SLNR_CHECK(check_ws(opts, l.total));
   char* ws = (char*)opts->workspace;
-  a.plan.part = (float*)(ws + l.part);
-  a.plan.part_ml = (float2*)(ws + l.ml);
-  a.plan.tiles = (int4*)(ws + l.tiles);
-  a.plan.before = (int64_t*)(ws + l.before);
-  a.plan.shares = (int2*)(ws + l.shares);
-  a.plan.pages = (int32_t*)(ws + l.pages);
-  a.plan.pickers = (uint32_t*)(ws + l.pickers);
-  a.plan.npages = (int32_t*)(ws + l.npages);
+  place(a.plan, l, ws);
   cudaStream_t s = (cudaStream_t)opts->stream;
   SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
     return launch_validate_pages(a.p, a.c.npages, a.c.page, false, picked, npicked, a.c.nheads, hdr, st);
@@ -281,6 +376,89 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   if (tc && opts->validate) {
     int flag = 0;
     SLNR_CUDA(cudaMemcpyAsync(&flag, &((WsHeader*)ws)->error, sizeof(int), cudaMemcpyDeviceToHost, s));
+    SLNR_CUDA(cudaStreamSynchronize(s));
+    if (flag != 0) return fail(SLNR_ERR_TIMEOUT, "a bounded device-side wait gave up (flags 0x%x)", flag);
+  }
+  return SLNR_OK;
+}
+
+// Attention over a cache in 4 bits: calls with a request of more than 32 query rows
+// of a key head go to the tensor-core kernel, the others to the row kernel.
+AttnPlan attn4_chunk_plan(const slnr_pages& p, int64_t group) {
+  AttnPlan a{};
+  const int64_t requests = p.nreq < p.ntok ? p.nreq : p.ntok, tiles = p.ntok * group / kChunkRows + requests;
+  a.nsplit = 1;
+  a.tile = kChunkRows;
+  a.ntiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
+  return a;
+}
+
+bool rows4(const slnr_pages& p, int64_t group) { return p.max_q * group <= 32; }
+
+// Of the row kernel: rows of an item, blocks, and its workspace after the header.
+struct Rows4Layout {
+  int tile, nblocks;
+  size_t shares, part, ml, total;
+};
+Rows4Layout rows4_layout(const slnr_cache& c, const slnr_pages& p, int64_t group) {
+  Rows4Layout l;
+  const int64_t rows = p.max_q * group;
+  l.tile = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+  l.nblocks = (int)kSms * (l.tile == 8 ? 3 : l.tile == 16 ? 2 : 1);
+  l.shares = align256(sizeof(WsHeader));
+  l.part = align256(l.shares + (l.nblocks + 1) * sizeof(int4));
+  l.ml = align256(l.part + (size_t)2 * l.nblocks * l.tile * c.head_dim * sizeof(float));
+  l.total = align256(l.ml + (size_t)2 * l.nblocks * l.tile * sizeof(float2));
+  return l;
+}
+
+slnr_status attention4(const slnr_rows* q, int32_t nheads_q, const slnr_cache4* cache, const slnr_pages* pages,
+                       int32_t dtype, float scale, void* out, float* lse, const slnr_opts* opts) {
+  SLNR_CHECK(check_paged_opts(opts));
+  SLNR_CHECK(check_cache4(cache, true));
+  SLNR_CHECK(check_type(dtype));
+  const slnr_cache shape = sizes(*cache);
+  SLNR_CHECK(check_pages(pages, &shape, true, true, false));
+  SLNR_CHECK(check_heads(&shape, nheads_q));
+  SLNR_CHECK(check_rows("q", q, pages->ntok > 0));
+  if (!std::isfinite(scale)) return fail(SLNR_ERR_SHAPE, "scale must be finite");
+  if (pages->ntok == 0) return SLNR_OK;
+  if (!out) return fail(SLNR_ERR_NULL, "out is NULL");
+  if (!aligned16(out)) return fail(SLNR_ERR_UNSUPPORTED, "out must be 16-byte aligned");
+  const Divisor group = divisor(nheads_q / cache->nheads);
+  const Cache4View c4 = view(*cache);
+  const PagesView p = view(*pages);
+  cudaStream_t s = (cudaStream_t)opts->stream;
+  char* ws = (char*)opts->workspace;
+  WsHeader* hdr = (WsHeader*)ws;
+  const auto check = [&](WsHeader* h, cudaStream_t st) {
+    return launch_validate_pages(p, c4.npages, c4.slots, false, nullptr, 0, 0, h, st);
+  };
+  if (rows4(*pages, group.d)) {
+    const Rows4Layout l = rows4_layout(shape, *pages, group.d);
+    SLNR_CHECK(check_ws(opts, l.total));
+    SLNR_CHECK(validated(opts, check));
+    const Attn4Args a{p, c4, view(*q), group, scale, out, lse, l.tile, l.nblocks, 4, (int4*)(ws + l.shares),
+                      (float*)(ws + l.part), (float2*)(ws + l.ml)};
+    SLNR_LAUNCH("paged4_rows", launch_paged4_rows(a, dtype, s));
+    SLNR_LAUNCH("paged4_join", launch_paged4_join(a, dtype, hdr, s));
+  } else {
+    AttnArgs a{p, view(shape), view(*q), group, scale, out, lse, nullptr, 0, attn4_chunk_plan(*pages, group.d), c4};
+    if (a.plan.ntiles == INT32_MAX || (int64_t)a.plan.ntiles * cache->nheads > kMaxKeys ||
+        (int64_t)pages->max_q * group.d >= (int64_t(1) << 31))
+      return fail(SLNR_ERR_UNSUPPORTED, "too many rows or keys for one call");
+    const AttnLayout l = attn_layout(shape, *pages, nheads_q, a.plan);
+    SLNR_CHECK(check_ws(opts, l.total));
+    place(a.plan, l, ws);
+    SLNR_CHECK(validated(opts, check));
+    SLNR_LAUNCH("paged_plan", launch_paged_plan(a, hdr, s));
+    SLNR_LAUNCH("paged4_chunk", launch_paged_chunk(a, dtype, hdr, s));
+    SLNR_LAUNCH("paged_join", launch_paged_join(a, dtype, s));
+  }
+  timing_end(s);
+  if (opts->validate) {
+    int flag = 0;
+    SLNR_CUDA(cudaMemcpyAsync(&flag, &hdr->error, sizeof(int), cudaMemcpyDeviceToHost, s));
     SLNR_CUDA(cudaStreamSynchronize(s));
     if (flag != 0) return fail(SLNR_ERR_TIMEOUT, "a bounded device-side wait gave up (flags 0x%x)", flag);
   }
@@ -385,6 +563,194 @@ slnr_status slnr_selected_attention(const slnr_rows* q, int32_t nheads_q, const 
   if (npicked > kAttnMaxPicked) return fail(SLNR_ERR_UNSUPPORTED, "npicked = %d: at most %d", (int)npicked, kAttnMaxPicked);
   if (!picked) return fail(SLNR_ERR_NULL, "picked is NULL");
   return attention(q, nheads_q, cache, pages, picked, npicked, scale, out, lse, opts);
+}
+
+slnr_status slnr_page_append4(const slnr_cache4* cache, const slnr_pages* pages, const slnr_rows* k, const slnr_rows* v,
+                              int32_t dtype, const slnr_opts* opts) {
+  timing_begin();
+  SLNR_CHECK(check_paged_opts(opts));
+  SLNR_CHECK(check_cache4(cache, true));
+  SLNR_CHECK(check_type(dtype));
+  const slnr_cache shape = sizes(*cache);
+  SLNR_CHECK(check_pages(pages, &shape, true, true, true));
+  SLNR_CHECK(check_rows("k", k, pages->ntok > 0));
+  SLNR_CHECK(check_rows("v", v, pages->ntok > 0));
+  if (pages->ntok == 0) return SLNR_OK;
+  cudaStream_t s = (cudaStream_t)opts->stream;
+  const PagesView p = view(*pages);
+  const Cache4View c = view(*cache);
+  SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
+    return launch_validate_pages(p, c.npages, c.slots, true, nullptr, 0, 0, hdr, st);
+  }));
+  SLNR_LAUNCH("page_append4", launch_page_append4(p, c, view(*k), view(*v), dtype, s));
+  timing_end(s);
+  return SLNR_OK;
+}
+
+slnr_status slnr_page_values4(const slnr_cache4* cache, const int32_t* ids, int32_t n, void* k, void* v, int32_t dtype,
+                              const slnr_opts* opts) {
+  timing_begin();
+  SLNR_CHECK(check_paged_opts(opts));
+  SLNR_CHECK(check_cache4(cache, true));
+  SLNR_CHECK(check_type(dtype));
+  if (n < 0 || (!ids && n > cache->npages)) return fail(SLNR_ERR_SHAPE, "n = %d pages", (int)n);
+  if (n == 0) return SLNR_OK;
+  if (!k || !v) return fail(SLNR_ERR_NULL, "k or v is NULL");
+  if (!aligned16(k) || !aligned16(v)) return fail(SLNR_ERR_UNSUPPORTED, "k and v must be 16-byte aligned");
+  const int64_t page = (int64_t)cache->page_size * cache->nheads * (cache->head_dim / kBlockCols);
+  if (page > kMaxKeys || n * (page / 256 + 1) > INT32_MAX) return fail(SLNR_ERR_UNSUPPORTED, "too many values for one call");
+  cudaStream_t s = (cudaStream_t)opts->stream;
+  const TablesView none{0, 0, 0, divisor(1), nullptr, nullptr};
+  SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
+    return launch_validate_set(none, 0, ids, n, cache->npages, nullptr, 0, hdr, st);
+  }));
+  SLNR_LAUNCH("page_values4", launch_page_values4(view(*cache), ids, n, k, v, dtype, s));
+  timing_end(s);
+  return SLNR_OK;
+}
+
+slnr_status slnr_paged_attention4_workspace(const slnr_cache4* cache, const slnr_pages* pages, int32_t nheads_q,
+                                            const slnr_opts* opts, size_t* bytes) {
+  if (!bytes) return fail(SLNR_ERR_NULL, "bytes is NULL");
+  SLNR_CHECK(check_paged_opts(opts));
+  SLNR_CHECK(check_cache4(cache, false));
+  const slnr_cache shape = sizes(*cache);
+  SLNR_CHECK(check_pages(pages, &shape, false, true, false));
+  SLNR_CHECK(check_heads(&shape, nheads_q));
+  const int64_t group = nheads_q / cache->nheads;
+  *bytes = rows4(*pages, group) ? rows4_layout(shape, *pages, group).total
+                                : attn_layout(shape, *pages, nheads_q, attn4_chunk_plan(*pages, group)).total;
+  return SLNR_OK;
+}
+
+slnr_status slnr_paged_attention4(const slnr_rows* q, int32_t nheads_q, const slnr_cache4* cache, const slnr_pages* pages,
+                                  int32_t dtype, float scale, void* out, float* lse, const slnr_opts* opts) {
+  timing_begin();
+  return attention4(q, nheads_q, cache, pages, dtype, scale, out, lse, opts);
+}
+
+slnr_status slnr_page_copy(const slnr_cache* to, const slnr_cache* from, const int32_t* src, const int32_t* dst,
+                           int32_t n, const slnr_opts* opts) {
+  timing_begin();
+  SLNR_CHECK(check_copy(src, dst, n, opts));
+  for (const slnr_cache* c : {to, from}) {
+    const bool keys = c && c->k;
+    SLNR_CHECK(check_cache(c, keys, c && c->codes, true));
+    if (!keys && !c->codes && c->npages > 0) return fail(SLNR_ERR_NULL, "a cache without keys and summaries");
+  }
+  if (to->page_size != from->page_size || to->nheads != from->nheads || to->head_dim != from->head_dim ||
+      to->dtype != from->dtype)
+    return fail(SLNR_ERR_SHAPE, "caches of other pages, heads, widths or types");
+  if (to->npages > 0 && from->npages > 0 && !to->k != !from->k)
+    return fail(SLNR_ERR_NULL, "one of the caches has no keys");
+  if (n == 0 || to->npages == 0 || from->npages == 0) return SLNR_OK;
+  CopyParts c{};
+  const int64_t slots = from->page_size, heads = from->nheads, width = from->head_dim;
+  const auto bytes = [](const int64_t (&s)[3], int64_t (&b)[3]) {
+    for (int i = 0; i < 3; ++i) b[i] = 2 * s[i];
+  };
+  bool fits = true;
+  if (from->k) {
+    // heads outside where a page of the destination holds them one after another
+    for (int i = 0; i < 2; ++i) {
+      int64_t f[3], t[3];
+      bytes(i ? from->v_stride : from->k_stride, f);
+      bytes(i ? to->v_stride : to->k_stride, t);
+      const bool heads_first = t[2] > t[1];
+      if (heads_first) {
+        std::swap(f[1], f[2]);
+        std::swap(t[1], t[2]);
+      }
+      fits = fits && add_part(c, i ? from->v : from->k, i ? to->v : to->k, f, t, heads_first ? heads : slots,
+                              heads_first ? slots : heads, 2 * width, 16);
+    }
+  }
+  if (from->codes && to->codes) {
+    const int64_t code[3] = {heads * width, 0, 0}, scale[3] = {heads * 4, 0, 0};
+    fits = fits && add_part(c, from->codes, to->codes, code, code, 1, 1, heads * width, 8);
+    fits = fits && add_part(c, from->scales, to->scales, scale, scale, 1, 1, heads * 4, 4);
+  }
+  if (!fits) return fail(SLNR_ERR_UNSUPPORTED, "too large a page for one call");
+  return copy_pages(c, src, dst, n, from->npages, to->npages, opts);
+}
+
+slnr_status slnr_page_copy4(const slnr_cache4* to, const slnr_cache4* from, const int32_t* src, const int32_t* dst,
+                            int32_t n, const slnr_opts* opts) {
+  timing_begin();
+  SLNR_CHECK(check_copy(src, dst, n, opts));
+  SLNR_CHECK(check_cache4(to, true));
+  SLNR_CHECK(check_cache4(from, true));
+  if (to->page_size != from->page_size || to->nheads != from->nheads || to->head_dim != from->head_dim)
+    return fail(SLNR_ERR_SHAPE, "caches of other pages, heads or widths");
+  if (n == 0 || to->npages == 0 || from->npages == 0) return SLNR_OK;
+  CopyParts c{};
+  const int64_t f[3] = {from->page_stride, 0, from->head_stride}, t[3] = {to->page_stride, 0, to->head_stride};
+  if (!add_part(c, from->data, to->data, f, t, 1, from->nheads, (int64_t)from->page_size / kSlab * slab_bytes(from->head_dim),
+                16))
+    return fail(SLNR_ERR_UNSUPPORTED, "too large a page for one call");
+  return copy_pages(c, src, dst, n, from->npages, to->npages, opts);
+}
+
+slnr_status slnr_page_fork(int32_t nreq, const int32_t* lens, const int32_t* table, int64_t table_stride, int32_t width,
+                           int32_t page_size, const int32_t* parent, int32_t n, const int32_t* free_pages, int32_t nfree,
+                           int32_t* out_table, int32_t* out_lens, int32_t* src, int32_t* dst, int32_t* used,
+                           const slnr_opts* opts) {
+  timing_begin();
+  SLNR_CHECK(check_tables(nreq, lens, table, table_stride, width, page_size, opts));
+  if (n < 0 || nfree < 0) return fail(SLNR_ERR_SHAPE, "n = %d, nfree = %d", (int)n, (int)nfree);
+  if (n > kMaxForks) return fail(SLNR_ERR_UNSUPPORTED, "n = %d: at most %d", (int)n, kMaxForks);
+  if (!used) return fail(SLNR_ERR_NULL, "used is NULL");
+  if (n > 0 && (!parent || (width > 0 && !out_table) || !out_lens || !src || !dst))
+    return fail(SLNR_ERR_NULL, "an array of the children is NULL");
+  if (nfree > 0 && !free_pages) return fail(SLNR_ERR_NULL, "free_pages is NULL");
+  if (width > 0 && n > 0 && out_table == table) return fail(SLNR_ERR_UNSUPPORTED, "out_table is table");
+  cudaStream_t s = (cudaStream_t)opts->stream;
+  const TablesView t{nreq, width, table_stride, divisor(page_size), table, lens};
+  SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
+    return launch_validate_set(t, INT32_MAX, parent, n, nreq, nullptr, 0, hdr, st);
+  }));
+  SLNR_LAUNCH("page_fork",
+              launch_page_fork(t, parent, n, free_pages, nfree, out_table, out_lens, src, dst, used, s));
+  timing_end(s);
+  return SLNR_OK;
+}
+
+slnr_status slnr_page_free(int32_t nreq, int32_t* lens, const int32_t* table, int64_t table_stride, int32_t width,
+                           int32_t page_size, const int32_t* drop, int32_t ndrop, int32_t npages, int32_t* free_pages,
+                           int32_t* count, const slnr_opts* opts) {
+  timing_begin();
+  SLNR_CHECK(check_tables(nreq, lens, table, table_stride, width, page_size, opts));
+  SLNR_CHECK(check_set(npages));
+  if (ndrop < 0) return fail(SLNR_ERR_SHAPE, "ndrop = %d", (int)ndrop);
+  if (!count || (npages > 0 && !free_pages)) return fail(SLNR_ERR_NULL, "free_pages or count is NULL");
+  if (ndrop > 0 && !drop) return fail(SLNR_ERR_NULL, "drop is NULL");
+  cudaStream_t s = (cudaStream_t)opts->stream;
+  const TablesView t{nreq, width, table_stride, divisor(page_size), table, lens};
+  SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
+    return launch_validate_set(t, npages, drop, ndrop, nreq, nullptr, 0, hdr, st);
+  }));
+  SLNR_LAUNCH("page_free", launch_page_free(t, lens, drop, ndrop, npages, free_pages, count, s));
+  timing_end(s);
+  return SLNR_OK;
+}
+
+slnr_status slnr_page_compact(int32_t nreq, const int32_t* lens, const int32_t* table, int64_t table_stride,
+                              int32_t width, int32_t page_size, int32_t npages, int32_t* out_table, int32_t* src,
+                              int32_t* dst, int32_t* ids, int32_t* used, const slnr_opts* opts) {
+  timing_begin();
+  SLNR_CHECK(check_tables(nreq, lens, table, table_stride, width, page_size, opts));
+  SLNR_CHECK(check_set(npages));
+  if (!used || (npages > 0 && !ids) || (npages > 1 && (!src || !dst)) || (nreq > 0 && width > 0 && !out_table))
+    return fail(SLNR_ERR_NULL, "an output is NULL");
+  if (nreq > 0 && width > 0 && out_table == table) return fail(SLNR_ERR_UNSUPPORTED, "out_table is table");
+  cudaStream_t s = (cudaStream_t)opts->stream;
+  const TablesView t{nreq, width, table_stride, divisor(page_size), table, lens};
+  SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
+    return launch_validate_set(t, npages, nullptr, 0, 0, nullptr, 0, hdr, st);
+  }));
+  SLNR_LAUNCH("page_compact", launch_page_compact(t, npages, out_table, src, dst, ids, used, s));
+  timing_end(s);
+  return SLNR_OK;
 }
 
 }  // extern "C"

@@ -49,6 +49,7 @@
 // kernel, which reads every page once for every token, 1.29.
 #include <type_traits>
 
+#include "cache4.cuh"
 #include "launch.h"
 #include "mma16.cuh"
 #include "paged_tile.cuh"
@@ -150,6 +151,124 @@ __device__ __forceinline__ void meet(int id, int n) { asm volatile("bar.sync %0,
 __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
   return (uint32_t)((piece >> 3) * kBlock + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
 }
+
+// ---- keys and values in 4 bits (cache4.cuh): a load warp takes two slabs of each
+// 128 keys, its lanes 16-byte pieces of their codes, which become 16-bit rows of the
+// tile.  bf16 holds every value, fp16 every 128th part.
+
+__device__ __forceinline__ uint32_t fma_bf16(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+
+// A scale, ready for the words of its block.
+template <typename T>
+struct Unpack;
+template <>
+struct Unpack<__half> {
+  static constexpr float kTimes = 128.f;  // what products of the unpacked values lack
+  ScalePair p;
+  __device__ __forceinline__ explicit Unpack(uint32_t byte) : p(scale_pair(scale_twice(byte, 0))) {}
+  // 8 columns.
+  __device__ __forceinline__ uint4 word(uint32_t x) const {
+    uint32_t r[4];
+    raw_pairs(x, r);
+    return make_uint4(hfma2(r[0], p.s, p.o16), hfma2(r[1], p.s, p.o256), hfma2(r[2], p.s, p.o16), hfma2(r[3], p.s, p.o256));
+  }
+};
+template <>
+struct Unpack<__nv_bfloat16> {
+  static constexpr float kTimes = 1.f;
+  uint32_t s, off;
+  __device__ __forceinline__ explicit Unpack(uint32_t byte) {
+    const float f = __half2float(__ushort_as_half((unsigned short)(byte << 7)));
+    s = Half2<__nv_bfloat16>::pack(f, f);
+    off = Half2<__nv_bfloat16>::pack(-24.f * f, -24.f * f);
+  }
+  __device__ __forceinline__ uint4 word(uint32_t x) const {  // n as the fraction bits 6..3 of 16 + n
+    const uint32_t y = __byte_perm(x, 0, 0x2301);
+    return make_uint4(fma_bf16(and_or(x >> 3, 0x00780078u, 0x41804180u), s, off),
+                      fma_bf16(and_or(x << 1, 0x00780078u, 0x41804180u), s, off),
+                      fma_bf16(and_or(y >> 3, 0x00780078u, 0x41804180u), s, off),
+                      fma_bf16(and_or(y << 1, 0x00780078u, 0x41804180u), s, off));
+  }
+};
+
+__device__ __forceinline__ void sts16(uint32_t to, const uint4& x) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+
+// A lane's pieces of the codes of one slab, and the scales of their blocks.
+template <int W>
+struct Raw {
+  static constexpr int N = W / 64;
+  uint4 code[N];
+  uint32_t scale[N];  // a byte each: two (W = 128), or two or four (W = 64)
+
+  __device__ __forceinline__ void load(const uint8_t* slab, int width, bool value, int lane, int keys) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int i = lane + 32 * k;
+      code[k] = make_uint4(0, 0, 0, 0);
+      scale[k] = 0;
+      if (i >= width / 2 || keys <= 0) continue;
+      code[k] = __ldg(reinterpret_cast<const uint4*>(slab + (value ? 9 * width : 0)) + i);
+      if (value) {
+        const uint8_t* s = slab + 17 * width;
+        int slot;
+        if constexpr (W == 128) {
+          const int q = i >= width / 4, j = i - q * (width / 4);
+          slot = 4 * (j & 3) + 2 * q;
+          scale[k] = __ldg(reinterpret_cast<const uint16_t*>(s + (j >> 2) * 16 + slot));
+        } else {
+          slot = 4 * (i & 3);
+          scale[k] = __ldg(reinterpret_cast<const uint32_t*>(s + (i >> 3) * 16 + slot));
+        }
+        // slots past the last key hold anything: scales of 0
+        const int left = keys - slot;
+        if (left < 4) scale[k] &= left > 0 ? (1u << 8 * left) - 1 : 0u;
+      } else {
+        const int per = width / 32, slot = i / per, t = i - slot * per, g = 2 * (slot >> 2) + (slot & 1), half = (slot >> 1) & 1;
+        const uint8_t* s = slab + 8 * width;
+        if constexpr (W == 128) scale[k] = __ldg(reinterpret_cast<const uint16_t*>(s + (g * per + t) * 4 + half * 2));
+        else scale[k] = __ldg(s + (g * 2 * per + 2 * t) * 2 + half) | __ldg(s + (g * 2 * per + 2 * t + 1) * 2 + half) << 8;
+      }
+    }
+  }
+
+  // Rows first .. first + 15 of a tile at `tile`.
+  template <typename T>
+  __device__ __forceinline__ void store(uint32_t tile, int width, bool value, int lane, int first) const {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int i = lane + 32 * k;
+      if (i >= width / 2) continue;
+      const uint32_t w[4] = {code[k].x, code[k].y, code[k].z, code[k].w};
+      if (!value) {  // 32 columns of a key
+        const int per = width / 32, slot = i / per, t = i - slot * per;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const Unpack<T> u((scale[k] >> 8 * b) & 255);
+          sts16(tile + piece_at(first + slot, 4 * t + 2 * b), u.word(w[2 * b]));
+          sts16(tile + piece_at(first + slot, 4 * t + 2 * b + 1), u.word(w[2 * b + 1]));
+        }
+      } else if constexpr (W == 128) {  // 16 columns of two values
+        const int q = i >= width / 4, j = i - q * (width / 4), slot = 4 * (j & 3) + 2 * q, c = j >> 2;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const Unpack<T> u((scale[k] >> 8 * b) & 255);
+          sts16(tile + piece_at(first + slot + b, 2 * c), u.word(w[2 * b]));
+          sts16(tile + piece_at(first + slot + b, 2 * c + 1), u.word(w[2 * b + 1]));
+        }
+      } else {  // 8 columns of four values
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          sts16(tile + piece_at(first + 4 * (i & 3) + b, i >> 2), Unpack<T>((scale[k] >> 8 * b) & 255).word(w[b]));
+      }
+    }
+  }
+};
 
 // Two fp32 values in 64 bits: one instruction for both (0.62 ms where single ones
 // took 0.65).
@@ -475,10 +594,11 @@ __device__ __forceinline__ void each_item(const AttnArgs& a, F f) {
     f(item_of<SEL>(a, i, ntiles, i == from.x ? from.y : 0, i == to.x ? to.y : -1));
 }
 
-template <typename T, int W, bool SEL>
+template <typename T, int W, bool SEL, bool FOUR>
 __global__ void __launch_bounds__(kThreads, 1)
 k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   constexpr int PIECES = W / 8, NB = buffers<W>();
+  constexpr float TIMES = FOUR ? Unpack<T>::kTimes : 1.f;  // of the keys and of the values
   extern __shared__ unsigned char smem_raw[];
   __shared__ Shared bars;
   const PagesView& p = a.p;
@@ -531,6 +651,30 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       each_item<SEL>(a, [&](const Item& it) {
         if (it.steps == 0) return;
         const int32_t* table = p.table + it.r * p.table_stride;
+        Raw<FOUR ? W : 64> codes[2];  // 4 bits: of the warp's two slabs, loaded a half step ahead
+        int ids[2], next_ids[2];      // their pages, looked up another half step ahead
+        const int lw = lt >> 5;
+        auto find4 = [&](int j) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const int u = it.u0 + j * kChunkKeys + (2 * lw + b) * kSlab;
+            next_ids[b] = -1;
+            if (u < it.u1) {
+              const int i = c.page.div(u);
+              if (i < p.width) next_ids[b] = __ldg(table + i);
+            }
+          }
+        };
+        auto load4 = [&](int j, bool value) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const int u = it.u0 + j * kChunkKeys + (2 * lw + b) * kSlab;
+            const bool on = (unsigned)ids[b] < (unsigned)c.npages;
+            const int slab = on ? (u - c.page.div(u) * c.page.d) / kSlab : 0;
+            codes[b].load(a.c4.data + (on ? ids[b] * a.c4.page : 0) + it.h * a.c4.head + (int64_t)slab * slab_bytes(c.width),
+                          c.width, value, lane, on ? it.u1 - u : 0);
+          }
+        };
         const char* src_k = (const char*)c.k + 2 * (c.ks[2] * it.h + (col_on ? piece * 8 : 0));
         const char* src_v = (const char*)c.v + 2 * (c.vs[2] * it.h + (col_on ? piece * 8 : 0));
         const int segs = SEL ? (c.page.d < kChunkKeys ? kChunkKeys / c.page.d : 1) : 0;
@@ -551,7 +695,14 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           if (SEL) listed(j + 1);
         };
         if (SEL) listed(0);
-        find(0);
+        if constexpr (FOUR) {
+          find4(0);
+          ids[0] = next_ids[0];
+          ids[1] = next_ids[1];
+          load4(0, false);
+        } else {
+          find(0);
+        }
         for (int x = lt; x < it.tiles * kRows; x += kLoaders) {
           const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
           bars.row_q[x] = x < it.n ? 2 * ((it.q0 + tok) * a.q.tok + (it.h * G + g) * a.q.head) : -1;
@@ -580,6 +731,24 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         for (int i = 0; i < total; ++i) {
           const bool value = i & 1;  // K0 V0 K1 V1 ...
           const int j = i >> 1, b = (ring + i) % NB;
+          if constexpr (FOUR) {
+            ok = ok && wait_warp(&bars.empty[b], (((ring + i) / NB) & 1) ^ 1, failed, limit);
+            if (ok) {
+#pragma unroll
+              for (int n = 0; n < 2; ++n) codes[n].template store<T>(buffer(b), c.width, value, lane, (2 * lw + n) * kSlab);
+              tc::fence_proxy_async_smem();
+              tc::mbar_arrive(&bars.full[b]);
+              if (!value) {
+                load4(j, true);
+                find4(j + 1);
+              } else {
+                ids[0] = next_ids[0];
+                ids[1] = next_ids[1];
+                if (i + 1 < total) load4(j + 1, false);
+              }
+            }
+            continue;
+          }
           if (!value) {
             const bool on = (unsigned)id < (unsigned)c.npages;
             bars.row_k[j & 1][lt] = on ? 2 * (id * c.ks[0] + off * c.ks[1]) : -1;
@@ -740,7 +909,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t col_s = tmem + lanes + kColS + t * 128, col_o = tmem + lanes + kColO + t * 128;
     // scores are kept raw and take their factor inside the exponential; one that is not positive goes to them first
-    const float factor = a.scale * 1.4426950408889634f;
+    const float factor = a.scale * 1.4426950408889634f * TIMES;
     int done = 0, count = 0, ring = 0;
     bool ok = true;  // where a wait gave up the items go on without work, and their rows are NaN
     each_item<SEL>(a, [&](const Item& it) {
@@ -879,9 +1048,9 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           const float f = exp2_fast(m - b);
           f_other = exp2_fast(ml.x - b);
           l = l * f + ml.y * f_other;
-          f_other = l == 0.f ? 0.f : f_other * __fdividef(1.f, l);
+          f_other = l == 0.f ? 0.f : f_other * __fdividef(TIMES, l);
           m = top;
-          const float inv = l == 0.f ? 0.f : f * __fdividef(1.f, l);
+          const float inv = l == 0.f ? 0.f : f * __fdividef(TIMES, l);
           write_row<T, W>(a, it, bars, o, x, row, inv, f_other, m, l);
         } else {
 #pragma unroll
@@ -893,7 +1062,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           }
         }
       } else {
-        write_row<T, W>(a, it, bars, o, x, row, l == 0.f ? 0.f : __fdividef(1.f, l), 0.f, m, l);
+        write_row<T, W>(a, it, bars, o, x, row, l == 0.f ? 0.f : __fdividef(TIMES, l), 0.f, m, l);
       }
     });
   }
@@ -985,9 +1154,9 @@ k_paged_join(AttnArgs a) {
   }
 }
 
-template <typename T, int W, bool SEL>
+template <typename T, int W, bool SEL, bool FOUR>
 cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
-  auto kernel = k_paged_chunk<T, W, SEL>;
+  auto kernel = k_paged_chunk<T, W, SEL, FOUR>;
   static OncePerDevice once;
   cudaError_t e = once(
       [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<W>()); });
@@ -996,9 +1165,9 @@ cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
                      wait_limit_cycles());
 }
 
-template <typename T, bool SEL>
+template <typename T, bool SEL, bool FOUR = false>
 cudaError_t launch_w(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
-  return a.c.width <= 64 ? launch<T, 64, SEL>(a, hdr, s) : launch<T, 128, SEL>(a, hdr, s);
+  return a.c.width <= 64 ? launch<T, 64, SEL, FOUR>(a, hdr, s) : launch<T, 128, SEL, FOUR>(a, hdr, s);
 }
 
 }  // namespace
@@ -1016,6 +1185,8 @@ cudaError_t launch_paged_plan(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) 
 }
 
 cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s) {
+  if (a.c4.data)
+    return dtype == SLNR_FP16 ? launch_w<__half, false, true>(a, hdr, s) : launch_w<__nv_bfloat16, false, true>(a, hdr, s);
   if (a.picked) return dtype == SLNR_FP16 ? launch_w<__half, true>(a, hdr, s) : launch_w<__nv_bfloat16, true>(a, hdr, s);
   return dtype == SLNR_FP16 ? launch_w<__half, false>(a, hdr, s) : launch_w<__nv_bfloat16, false>(a, hdr, s);
 }

@@ -1,6 +1,7 @@
 """Attention over a paged key/value cache (include/slnr.h): block tables, the
 cache's writes, pages picked by a cheap score, and attention over all pages or
-the picked ones.
+the picked ones; a cache held in 4 bits; and whole pages between the steps of a
+program: forks of requests, copies, free pages, compaction.
 
 Like the expressions' wrappers these only marshal torch CUDA tensors into the
 C structures of the ABI; every step runs in the library's CUDA kernels.
@@ -15,7 +16,7 @@ from typing import Optional
 import torch
 
 from . import (SlnrError, _buffer, _capturing, _default_ws, _last_ws, _lock_of_others, _new_workspace, _query, _stream_ptr,
-               last_error, lib, slnr_cache, slnr_opts, slnr_pages, slnr_rows)
+               last_error, lib, slnr_cache, slnr_cache4, slnr_opts, slnr_pages, slnr_rows)
 
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
@@ -140,6 +141,42 @@ class PagedCache:
         object.__setattr__(self, "_sizes", (c.npages, c.page_size, c.nheads, c.head_dim, c.dtype))
 
 
+@dataclass(frozen=True, eq=False)
+class PagedCache4:
+    """Keys and values in 4 bits: data uint8 [pages, heads, page size / 16, 18 width], a CUDA tensor whose last two axes are
+    packed and whose strides are multiples of 16.  Width is 32, 64, 96 or 128; 9/16 byte a value.
+
+    page_append codes what it writes (blocks of 16 columns share a scale: include/slnr.h), paged_attention reads the codes,
+    page_values gives the values; what the bytes mean is the library's own.  Queries, keys and values may be bf16 or fp16,
+    whichever wrote the cache.  The tensor is held, and read and written by the calls that take the cache."""
+    data: torch.Tensor
+    page_size: int = field(init=False)
+    device: torch.device = field(init=False, repr=False)
+    _c: slnr_cache4 = field(init=False, repr=False)
+    _sizes: tuple = field(init=False, repr=False)
+
+    def __post_init__(self):
+        x = self.data
+        if x.dim() != 4 or x.dtype != torch.uint8 or not x.is_cuda or x.shape[3] not in (576, 1152, 1728, 2304):
+            raise ValueError("data must be a uint8 CUDA tensor [pages, heads, page size / 16, 18 width], width 32, 64, 96 or 128")
+        if x.stride(3) != 1 or (x.shape[2] > 1 and x.stride(2) != x.shape[3]):
+            raise ValueError("the last two axes of data must be packed")
+        npages, heads, slabs, row = x.shape
+        # an axis of one entry is never stepped along
+        c = slnr_cache4(npages, 16 * slabs, heads, row // 18, x.stride(0) if npages > 1 else 0,
+                        x.stride(1) if heads > 1 else 0, x.data_ptr())
+        self.__dict__.update(page_size=16 * slabs, device=x.device, _c=c, _sizes=(npages, 16 * slabs, heads, row // 18))
+
+    @classmethod
+    def empty(cls, npages, page_size, heads, width, device="cuda"):
+        """A cache of that many pages, slots of a page, heads and columns; its memory holds anything."""
+        if page_size < 16 or page_size % 16:
+            raise ValueError(f"page_size is {page_size}, not a multiple of 16")
+        if width not in (32, 64, 96, 128):
+            raise ValueError(f"width is {width}, not 32, 64, 96 or 128")
+        return cls(torch.empty((npages, heads, page_size // 16, 18 * width), dtype=torch.uint8, device=device))
+
+
 def _same_device(cache, tables, name):
     if tables.table.device != cache.device:
         raise ValueError(f"{name}: the tables are on {tables.table.device}, the cache is on {cache.device}")
@@ -227,9 +264,11 @@ def page_tables(new_len, old_len, table, free_pages, page_size, ntok, max_q=None
     return PageTables._of(c, table=table, q_pos=q_pos, k_len=k_len, req=req, slots=slots, max_q=max_q, max_k=max_k), used
 
 
-def page_append(cache: PagedCache, tables: PageTables, k, v, validate=False, workspace=None, stream=None):
+def page_append(cache: PagedCache | PagedCache4, tables: PageTables, k, v, validate=False, workspace=None, stream=None):
     """New keys and values [T, heads, width] to their slots, and the summaries of the pages that became full
-    (slnr_page_append); the cache's tensors are written in place."""
+    (slnr_page_append); the cache's tensors are written in place.  A PagedCache4 gets their codes (slnr_page_append4)."""
+    if type(cache) is PagedCache4:
+        return _append4(cache, tables, k, v, validate, workspace, stream)
     if cache.k is None or tables.slots is None:
         raise ValueError("page_append needs a cache with keys, and tables with slots")
     _same_device(cache, tables, "page_append")
@@ -240,11 +279,42 @@ def page_append(cache: PagedCache, tables: PageTables, k, v, validate=False, wor
           (cache.k, cache.v, cache.codes, cache.scales, k, v, *tables._tensors()))
 
 
+def _append4(cache, tables, k, v, validate, workspace, stream):
+    if tables.slots is None:
+        raise ValueError("page_append needs tables with slots")
+    _same_device(cache, tables, "page_append")
+    T, H, dt = tables.ntok, cache._c.nheads, k.dtype
+    args = (_byref(cache._c), _byref(tables._c), _byref(_rows(k, "k", cache, H, T)), _byref(_rows(v, "v", cache, H, T, dt)),
+            _TYPES[dt])
+    _call("slnr_page_append4", args, cache.device.index, 0, validate and T > 0, workspace, stream,
+          (cache.data, k, v, *tables._tensors()))
+
+
+def page_values(cache: PagedCache4, pages=None, dtype=torch.bfloat16, out=None, validate=False, workspace=None, stream=None):
+    """The values that pages of a cache in 4 bits stand for (slnr_page_values4): (k, v), each [pages, slots, heads, width]
+    of that type.  pages: int32 page numbers, of which those that are no pages give zeros (None: all).  out: (k, v)."""
+    if type(cache) is not PagedCache4:
+        raise ValueError("page_values needs a PagedCache4")
+    if dtype not in _TYPES:
+        raise ValueError("dtype must be bf16 or fp16")
+    c, dev = cache._c, cache.device
+    n = c.npages if pages is None else pages.shape[0] if pages.dim() == 1 else -1
+    at = None if pages is None else _ints(pages, "pages", (n,), dev)
+    shape = (n, c.page_size, c.nheads, c.head_dim)
+    if out is None:
+        k, v = _empty(shape, dtype, dev, stream), _empty(shape, dtype, dev, stream)
+    else:
+        k, v = (_checked(x, name, shape, dtype, dev) for x, name in zip(out, ("out k", "out v"), strict=True))
+    _call("slnr_page_values4", (_byref(c), at, n, k.data_ptr(), v.data_ptr(), _TYPES[dtype]), dev.index, 0,
+          validate and n > 0, workspace, stream, (cache.data, pages, k, v))
+    return k, v
+
+
 def page_select(q, cache: PagedCache, tables: PageTables, npicked, first=1, last=2, out=None, validate=False,
                 workspace=None, stream=None):
     """Pages for each new token and key head by the cheap score (slnr_page_select): int32 [T, heads, npicked], ascending,
     -1 behind.  The first `first` pages and the last `last` are always among them."""
-    if cache.codes is None:
+    if type(cache) is PagedCache4 or cache.codes is None:
         raise ValueError("page_select needs a cache with summaries")
     _same_device(cache, tables, "page_select")
     c, T = cache._c, tables.ntok
@@ -273,6 +343,29 @@ def _attention_bytes(cache, pages, heads_q, npicked):
     return _query("slnr_paged_attention_workspace", *args, _byref(o))
 
 
+@functools.lru_cache(maxsize=4096)
+def _attention4_bytes(cache, pages, heads_q):
+    """The same over a cache in 4 bits."""
+    return _query("slnr_paged_attention4_workspace", _byref(slnr_cache4(*cache)), _byref(slnr_pages(*pages, 0, pages[-1])),
+                  heads_q, _byref(slnr_opts()))
+
+
+def _attention4(q, cache, tables, scale, out, lse, validate, workspace, stream):
+    _same_device(cache, tables, "paged_attention")
+    c, T, dtype, device = cache._c, tables.ntok, q.dtype, cache.device
+    rows = _rows(q, "q", cache, None, T)
+    shape = q.shape
+    out = _empty(shape, dtype, device, stream) if out is None else _checked(out, "out", shape, dtype, device)
+    lse = _empty(shape[:2], torch.float32, device, stream) if lse is None else \
+        _checked(lse, "lse", shape[:2], torch.float32, device)
+    need = _attention4_bytes(cache._sizes, tables._sizes, shape[1]) if T else 0
+    args = (_byref(rows), shape[1], _byref(c), _byref(tables._c), _TYPES[dtype],
+            c.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr())
+    _call("slnr_paged_attention4", args, device.index, need, validate and T > 0, workspace, stream,
+          (q, cache.data, out, lse, *tables._tensors()))
+    return out, lse
+
+
 def _attention(name, q, cache, tables, picked, npicked, scale, out, lse, validate, workspace, stream):
     if cache.k is None:
         raise ValueError(f"{name} needs a cache with keys")
@@ -298,18 +391,105 @@ def _attention(name, q, cache, tables, picked, npicked, scale, out, lse, validat
     return out, lse
 
 
-def paged_attention(q, cache: PagedCache, tables: PageTables, scale=None, out=None, lse=None, validate=False,
+def paged_attention(q, cache: PagedCache | PagedCache4, tables: PageTables, scale=None, out=None, lse=None, validate=False,
                     workspace=None, stream=None):
     """Causal attention of the new tokens q [T, query heads, width] over all pages of their requests
-    (slnr_paged_attention): returns (out [T, query heads, width], lse fp32 [T, query heads]).  scale: width ** -0.5."""
+    (slnr_paged_attention): returns (out [T, query heads, width], lse fp32 [T, query heads]).  scale: width ** -0.5.
+    Over a PagedCache4 (slnr_paged_attention4) q may be bf16 or fp16; out has its type."""
+    if type(cache) is PagedCache4:
+        return _attention4(q, cache, tables, scale, out, lse, validate, workspace, stream)
     return _attention("slnr_paged_attention", q, cache, tables, None, 0, scale, out, lse, validate, workspace, stream)
 
 
 def selected_attention(q, cache: PagedCache, tables: PageTables, picked, scale=None, out=None, lse=None, validate=False,
                        workspace=None, stream=None):
     """paged_attention over the pages picked [T, heads, n] for each token and key head only (slnr_selected_attention)."""
+    if type(cache) is PagedCache4:
+        raise ValueError("selected_attention needs a 16-bit cache")
     n = picked.shape[-1] if picked.dim() == 3 else 0
     if n < 1:
         raise ValueError("picked must be [tokens, heads, pages], with one page at least")
     _ints(picked, "picked", (tables.ntok, cache._c.nheads, n), cache.device)
     return _attention("slnr_selected_attention", q, cache, tables, picked, n, scale, out, lse, validate, workspace, stream)
+
+
+# ---- whole pages between the steps -----------------------------------------------------------
+
+def _held_by(table, lens, page_size):
+    """(arguments of the tables, device): the checks that page_fork, page_free and page_compact share."""
+    R, width, stride = _table(table)
+    if page_size < 1:
+        raise ValueError(f"page_size is {page_size}")
+    return R, width, stride, _ints(lens, "lens", (R,), table.device), table.device
+
+
+def page_copy(cache: PagedCache | PagedCache4, src, dst, source=None, validate=False, workspace=None, stream=None):
+    """Pages src[i] to pages dst[i] (int32 [n]): keys, values and summaries, or codes (slnr_page_copy, slnr_page_copy4).
+    Entries of -1 are skipped.  No page may be in dst twice, nor in src and dst of one cache.  source: the cache that they
+    are copied from (None: cache itself), of the same kind, page size, heads and width."""
+    source = cache if source is None else source
+    if type(source) is not type(cache):
+        raise ValueError("cache and source must be of one kind")
+    dev, n = cache.device, src.shape[0] if src.dim() == 1 else -1
+    if source.device != dev:
+        raise ValueError(f"page_copy: the source is on {source.device}, the cache is on {dev}")
+    args = (_byref(cache._c), _byref(source._c), _ints(src, "src", (n,), dev), _ints(dst, "dst", (n,), dev), n)
+    if type(cache) is PagedCache4:
+        name, tensors = "slnr_page_copy4", (cache.data, source.data, src, dst)
+    else:
+        name = "slnr_page_copy"
+        tensors = (cache.k, cache.v, cache.codes, cache.scales, source.k, source.v, source.codes, source.scales, src, dst)
+    _call(name, args, dev.index, 0, validate and n > 0, workspace, stream, tensors)
+
+
+def page_fork(table, lens, parent, free_pages, page_size, validate=False, workspace=None, stream=None):
+    """Requests that go on from others (slnr_page_fork): child i from request parent[i] of table [R, width] and lens [R].
+
+    Returns (table [n, width], lens [n], src [n], dst [n], pages taken [1]) of the children; the old table and lengths are
+    not changed.  Full pages are shared; a last page that is not full stays with a parent's first child, and for the others
+    page_copy(cache, src, dst) has to copy it, in every cache that the tables are of."""
+    R, width, stride, at_lens, dev = _held_by(table, lens, page_size)
+    n, nfree = parent.shape[0] if parent.dim() == 1 else -1, free_pages.shape[0]
+    at_parent, at_free = _ints(parent, "parent", (n,), dev), _ints(free_pages, "free_pages", (nfree,), dev)
+    out = _empty((n, width), torch.int32, dev, stream)
+    ints = _empty(3 * n + 1, torch.int32, dev, stream)
+    out_lens, src, dst, used = ints.split_with_sizes((n, n, n, 1))
+    at = ints.data_ptr()
+    _call("slnr_page_fork", (R, at_lens, table.data_ptr(), stride, width, page_size, at_parent, n, at_free, nfree,
+                             out.data_ptr(), at, at + 4 * n, at + 8 * n, at + 12 * n),
+          dev.index, 0, validate, workspace, stream, (table, lens, parent, free_pages))
+    return out, out_lens, src, dst, used
+
+
+def page_free(table, lens, npages, page_size, drop=None, validate=False, workspace=None, stream=None):
+    """The pages that no request of table [R, width] and lens [R] holds (slnr_page_free): (free_pages [npages], ascending, -1
+    behind them; how many [1]).  First lens is set to 0, in place, for the requests in drop (int32)."""
+    R, width, stride, at_lens, dev = _held_by(table, lens, page_size)
+    ndrop = 0 if drop is None else drop.shape[0] if drop.dim() == 1 else -1
+    at_drop = None if drop is None else _ints(drop, "drop", (ndrop,), dev)
+    if npages < 0:
+        raise ValueError(f"npages is {npages}")
+    ints = _empty(npages + 1, torch.int32, dev, stream)
+    free_pages, count = ints.split_with_sizes((npages, 1))
+    at = ints.data_ptr()
+    _call("slnr_page_free", (R, at_lens, table.data_ptr(), stride, width, page_size, at_drop, ndrop, npages, at,
+                             at + 4 * npages), dev.index, 0, validate, workspace, stream, (table, lens, drop))
+    return free_pages, count
+
+
+def page_compact(table, lens, npages, page_size, validate=False, workspace=None, stream=None):
+    """The pages that requests hold to the front of a cache of npages (slnr_page_compact): (table [R, width] with the new
+    numbers, src and dst [npages // 2], new number of each page [npages] or -1, pages in use [1]).  page_copy(cache, src,
+    dst) has to make the copies in every cache that the tables are of; the old table is not changed."""
+    R, width, stride, at_lens, dev = _held_by(table, lens, page_size)
+    if npages < 0:
+        raise ValueError(f"npages is {npages}")
+    half = npages // 2
+    out = _empty((R, width), torch.int32, dev, stream)
+    ints = _empty(2 * half + npages + 1, torch.int32, dev, stream)
+    src, dst, ids, used = ints.split_with_sizes((half, half, npages, 1))
+    at = ints.data_ptr()
+    _call("slnr_page_compact", (R, at_lens, table.data_ptr(), stride, width, page_size, npages, out.data_ptr(), at,
+                                at + 4 * half, at + 8 * half, at + 8 * half + 4 * npages),
+          dev.index, 0, validate, workspace, stream, (table, lens))
+    return out, src, dst, ids, used
