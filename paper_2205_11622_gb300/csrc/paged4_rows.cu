@@ -46,14 +46,6 @@ size_t smem_bytes(int width, int rows) {
   return (size_t)kWarps * kStages * 2 * slab_bytes(width) + (size_t)kWarps * rows * (w + 4) * 4;
 }
 
-__device__ __forceinline__ void copy_bulk(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(src), "r"(bytes), "r"(tc::smem_u32(bar))
-               : "memory");
-}
-__device__ __forceinline__ void expect(uint64_t* bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(tc::smem_u32(bar)), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ bool test(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -260,12 +252,12 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
     const uint32_t both = __ballot_sync(0xffffffffu, on);
     uint64_t* bar = full + issued % kStages;
     const uint32_t dst = ring + issued % kStages * 2 * slab;
-    if (lane == 0) expect(bar, __popc(both) * slab);
+    if (lane == 0) tc::mbar_expect(bar, __popc(both) * slab);
     __syncwarp();
     if (on && !(whole && lane == 1 && (both & 1))) {
       const int page_slot = key - c.slots.div(key) * c.slots.d;
       const uint8_t* src = c.data + id * c.page + cs.h * c.head + (int64_t)(page_slot / kSlab) * slab;
-      copy_bulk(dst + lane * slab, src, whole && both == 3 ? 2 * slab : slab, bar);
+      tc::copy_bulk(dst + lane * slab, src, whole && both == 3 ? 2 * slab : slab, bar);
     }
     ++issued;
     cu += kWarps;

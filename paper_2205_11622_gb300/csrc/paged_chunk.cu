@@ -92,15 +92,36 @@ struct Shared {
   uint64_t q_full, q_empty, s_full[2], p_full[2], o_full, full[8], empty[8], drained;
   uint32_t tmem;
   int failed;
-  int64_t row_k[2][kChunkKeys], row_v[2][kChunkKeys];  // bytes from the head's first row to each key's; -1: zeros
-  int64_t row_q[2 * kRows];                            // the same of the item's query rows
-  uint32_t listed[8][kSegments * (1 + kMaxWords)];  // selected: a step's pages, then who picked each
+  int64_t row_q[2 * kRows];  // bytes from the head's first row to each of the item's query rows; -1: zeros
   // one tile an item: 16 columns of the second warpgroup's O, its maxima and sums
   float other[16][kRows];
   float2 other_ml[kRows];
 };
+template <bool FOUR>
+struct LoadShared : Shared {
+  int64_t row_k[2][kChunkKeys], row_v[2][kChunkKeys];  // the same to each key of a step
+  uint32_t listed[8][kSegments * (1 + kMaxWords)];     // selected: a step's pages, then who picked each
+};
 
-static_assert(smem_bytes<128>() + sizeof(Shared) <= (size_t)227 * 1024, "shared memory of a block");
+// Keys and values in 4 bits: the seven warps beside the softmax and MMA warps unpack
+// them, each with a ring of slabs' keys (or values) of its own beside the tiles.
+constexpr int kUnpackWarps = 7;
+constexpr int kStepSlabs = kChunkKeys / kSlab;
+template <int W>
+constexpr int raw_stages() { return W == 128 ? 2 : 4; }
+template <int W>
+constexpr int raw_bytes() { return 9 * W; }  // of a stage
+template <>
+struct LoadShared<true> : Shared {
+  uint64_t raw_full[kUnpackWarps][4];
+};
+template <int W, bool FOUR>
+constexpr size_t block_bytes() {
+  return smem_bytes<W>() + (FOUR ? (size_t)kUnpackWarps * raw_stages<W>() * raw_bytes<W>() : 0);
+}
+
+static_assert(block_bytes<128, false>() + sizeof(LoadShared<false>) <= (size_t)227 * 1024, "shared memory of a block");
+static_assert(block_bytes<128, true>() + sizeof(LoadShared<true>) <= (size_t)227 * 1024, "shared memory of a block");
 
 // One poll that does not sleep.
 __device__ __forceinline__ bool test(uint64_t* bar, uint32_t parity) {
@@ -184,87 +205,129 @@ struct Unpack<__nv_bfloat16> {
   __device__ __forceinline__ explicit Unpack(uint32_t byte) {
     const float f = __half2float(__ushort_as_half((unsigned short)(byte << 7)));
     s = Half2<__nv_bfloat16>::pack(f, f);
-    off = Half2<__nv_bfloat16>::pack(-24.f * f, -24.f * f);
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(off) : "r"(s), "r"(0xc220c220u));  // -40
   }
-  __device__ __forceinline__ uint4 word(uint32_t x) const {  // n as the fraction bits 6..3 of 16 + n
+  __device__ __forceinline__ uint4 word(uint32_t x) const {  // n as the fraction bits 5..2 of 32 + n
     const uint32_t y = __byte_perm(x, 0, 0x2301);
-    return make_uint4(fma_bf16(and_or(x >> 3, 0x00780078u, 0x41804180u), s, off),
-                      fma_bf16(and_or(x << 1, 0x00780078u, 0x41804180u), s, off),
-                      fma_bf16(and_or(y >> 3, 0x00780078u, 0x41804180u), s, off),
-                      fma_bf16(and_or(y << 1, 0x00780078u, 0x41804180u), s, off));
+    return make_uint4(fma_bf16(and_or(x >> 4, 0x003c003cu, 0x42004200u), s, off),
+                      fma_bf16(and_or(x, 0x003c003cu, 0x42004200u), s, off),
+                      fma_bf16(and_or(y >> 4, 0x003c003cu, 0x42004200u), s, off),
+                      fma_bf16(and_or(y, 0x003c003cu, 0x42004200u), s, off));
   }
 };
 
+__device__ __forceinline__ uint32_t lds_u32(uint32_t at) {
+  uint32_t r;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(at) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint32_t lds_u16(uint32_t at) {
+  uint16_t r;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r) : "r"(at) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint32_t lds_u8(uint32_t at) {
+  uint32_t r;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(r) : "r"(at) : "memory");
+  return r;
+}
+__device__ __forceinline__ void lds4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
 __device__ __forceinline__ void sts16(uint32_t to, const uint4& x) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
 }
 
-// A lane's pieces of the codes of one slab, and the scales of their blocks.
+// Where a lane's pieces of a slab are, in the codes and in a tile of its first row,
+// for keys and values.  The words of a piece are written in an order by t (turn) in
+// which the eight lanes of a 128-byte store touch every bank once.
 template <int W>
-struct Raw {
+struct Places {
   static constexpr int N = W / 64;
-  uint4 code[N];
-  uint32_t scale[N];  // a byte each: two (W = 128), or two or four (W = 64)
+  int k_scale[N], v_scale[N], k_to[N], v_to[N];
+  int k_turn, v_turn, v_slot[N];
 
-  __device__ __forceinline__ void load(const uint8_t* slab, int width, bool value, int lane, int keys) {
+  __device__ __forceinline__ Places(int width, int lane) {
+    const int per = width / 32;
+    k_turn = W == 128 ? (lane % per) >> 1 : 0;  // per is 4, or 3 where the second piece has it from its own t
+    v_turn = W == 128 ? (lane & 3) >> 1 : lane & 2;
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int i = lane + 32 * k;
-      code[k] = make_uint4(0, 0, 0, 0);
-      scale[k] = 0;
-      if (i >= width / 2 || keys <= 0) continue;
-      code[k] = __ldg(reinterpret_cast<const uint4*>(slab + (value ? 9 * width : 0)) + i);
-      if (value) {
-        const uint8_t* s = slab + 17 * width;
-        int slot;
-        if constexpr (W == 128) {
-          const int q = i >= width / 4, j = i - q * (width / 4);
-          slot = 4 * (j & 3) + 2 * q;
-          scale[k] = __ldg(reinterpret_cast<const uint16_t*>(s + (j >> 2) * 16 + slot));
-        } else {
-          slot = 4 * (i & 3);
-          scale[k] = __ldg(reinterpret_cast<const uint32_t*>(s + (i >> 3) * 16 + slot));
-        }
-        // slots past the last key hold anything: scales of 0
-        const int left = keys - slot;
-        if (left < 4) scale[k] &= left > 0 ? (1u << 8 * left) - 1 : 0u;
+    for (int n = 0; n < N; ++n) {
+      const int i = lane + 32 * n;
+      int slot = i / per;
+      const int t = i - slot * per, g = 2 * (slot >> 2) + (slot & 1), half = (slot >> 1) & 1;
+      k_scale[n] = 8 * width + (W == 128 ? (g * per + t) * 4 + half * 2 : (g * 2 * per + 2 * t) * 2 + half);
+      k_to[n] = piece_at(slot, 4 * t);
+      if constexpr (W == 128) {
+        const int q = i >= width / 4, j = i - q * (width / 4);
+        slot = 4 * (j & 3) + 2 * q;
+        v_scale[n] = 8 * width + (j >> 2) * 16 + slot;
+        v_to[n] = piece_at(slot, 2 * (j >> 2));
       } else {
-        const int per = width / 32, slot = i / per, t = i - slot * per, g = 2 * (slot >> 2) + (slot & 1), half = (slot >> 1) & 1;
-        const uint8_t* s = slab + 8 * width;
-        if constexpr (W == 128) scale[k] = __ldg(reinterpret_cast<const uint16_t*>(s + (g * per + t) * 4 + half * 2));
-        else scale[k] = __ldg(s + (g * 2 * per + 2 * t) * 2 + half) | __ldg(s + (g * 2 * per + 2 * t + 1) * 2 + half) << 8;
+        slot = 4 * (i & 3);
+        v_scale[n] = 8 * width + (i >> 3) * 16 + slot;
+        v_to[n] = piece_at(slot, i >> 2);
       }
+      v_slot[n] = slot;
+    }
+  }
+};
+
+// Codes and scales of the keys (or values) of a slab in shared memory, a lane's.
+template <int W>
+struct Codes {
+  static constexpr int N = W / 64;
+  uint32_t w[N][4], scale[N];
+
+  // keys: slots of it that are keys; the others hold anything, and their values become 0 (their scores are dropped)
+  __device__ __forceinline__ void load(uint32_t raw, const Places<W>& at, int width, bool value, int lane, int keys) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      w[n][0] = w[n][1] = w[n][2] = w[n][3] = scale[n] = 0;
+      if (keys <= 0 || lane + 32 * n >= width / 2) continue;
+      lds4(w[n], raw + 16 * (lane + 32 * n));
+      if (W == 128) scale[n] = lds_u16(raw + (value ? at.v_scale[n] : at.k_scale[n]));
+      else if (value) scale[n] = lds_u32(raw + at.v_scale[n]);
+      else scale[n] = lds_u8(raw + at.k_scale[n]) | lds_u8(raw + at.k_scale[n] + 2) << 8;
+      const int left = keys - at.v_slot[n];
+      if (value && left < 4) scale[n] &= left > 0 ? (1u << 8 * left) - 1 : 0u;
     }
   }
 
-  // Rows first .. first + 15 of a tile at `tile`.
+  // To 16 rows of a tile.
   template <typename T>
-  __device__ __forceinline__ void store(uint32_t tile, int width, bool value, int lane, int first) const {
+  __device__ __forceinline__ void store(uint32_t tile, const Places<W>& at, int width, bool value, int lane) const {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int i = lane + 32 * k;
-      if (i >= width / 2) continue;
-      const uint32_t w[4] = {code[k].x, code[k].y, code[k].z, code[k].w};
-      if (!value) {  // 32 columns of a key
-        const int per = width / 32, slot = i / per, t = i - slot * per;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const Unpack<T> u((scale[k] >> 8 * b) & 255);
-          sts16(tile + piece_at(first + slot, 4 * t + 2 * b), u.word(w[2 * b]));
-          sts16(tile + piece_at(first + slot, 4 * t + 2 * b + 1), u.word(w[2 * b + 1]));
-        }
-      } else if constexpr (W == 128) {  // 16 columns of two values
-        const int q = i >= width / 4, j = i - q * (width / 4), slot = 4 * (j & 3) + 2 * q, c = j >> 2;
+    for (int n = 0; n < N; ++n) {
+      if (lane + 32 * n >= width / 2) break;
+      const uint32_t* x = w[n];
+      if (!value) {  // 32 columns of a key: word i to piece 4 t + i
+        const uint32_t to = tile + at.k_to[n];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          const Unpack<T> u((scale[k] >> 8 * b) & 255);
-          sts16(tile + piece_at(first + slot + b, 2 * c), u.word(w[2 * b]));
-          sts16(tile + piece_at(first + slot + b, 2 * c + 1), u.word(w[2 * b + 1]));
+          const int bb = b ^ at.k_turn;
+          const Unpack<T> u((scale[n] >> 8 * bb) & 255);
+          sts16(to ^ (bb << 5), u.word(at.k_turn ? x[2 * (b ^ 1)] : x[2 * b]));
+          sts16(to ^ (bb << 5) ^ 16, u.word(at.k_turn ? x[2 * (b ^ 1) + 1] : x[2 * b + 1]));
         }
-      } else {  // 8 columns of four values
+      } else if constexpr (W == 128) {  // 16 columns of two values, in rows that differ in their last bit
+        const uint32_t to = tile + at.v_to[n];
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-          sts16(tile + piece_at(first + 4 * (i & 3) + b, i >> 2), Unpack<T>((scale[k] >> 8 * b) & 255).word(w[b]));
+        for (int b = 0; b < 2; ++b) {
+          const Unpack<T> u((scale[n] >> 8 * b) & 255);
+          const uint32_t row = (to ^ (b << 4)) + b * 128;
+          sts16(row ^ (at.v_turn << 4), u.word(at.v_turn ? x[2 * b + 1] : x[2 * b]));
+          sts16(row ^ (at.v_turn << 4) ^ 16, u.word(at.v_turn ? x[2 * b] : x[2 * b + 1]));
+        }
+      } else {  // 8 columns of four values, in rows that differ in their last two bits
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int r = b ^ at.v_turn;
+          sts16(tile + (at.v_to[n] ^ (r << 4)) + r * 128, Unpack<T>((scale[n] >> 8 * r) & 255).word(at.v_turn ? x[b ^ 2] : x[b]));
+        }
       }
     }
   }
@@ -600,7 +663,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   constexpr int PIECES = W / 8, NB = buffers<W>();
   constexpr float TIMES = FOUR ? Unpack<T>::kTimes : 1.f;  // of the keys and of the values
   extern __shared__ unsigned char smem_raw[];
-  __shared__ Shared bars;
+  __shared__ LoadShared<FOUR> bars;
   const PagesView& p = a.p;
   const CacheView& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -619,9 +682,11 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       tc::mbar_init(&bars.p_full[t], kWarpArrivals);
     }
     for (int b = 0; b < NB; ++b) {
-      tc::mbar_init(&bars.full[b], kLoaders);
+      tc::mbar_init(&bars.full[b], FOUR ? kStepSlabs : kLoaders);
       tc::mbar_init(&bars.empty[b], 1);
     }
+    if constexpr (FOUR)
+      for (int i = 0; i < kUnpackWarps * 4; ++i) tc::mbar_init(&bars.raw_full[i / 4][i % 4], 1);
     bars.failed = 0;
     tc::fence_mbar_init();
   }
@@ -640,7 +705,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   // Counters run on from item to item: ring steps, steps of each tile, items with keys.
   if (warp >= kLoadWarp) {
     regs_down<kOtherRegs>();
-    if (warp < kMmaWarp) {
+    if (warp < kMmaWarp || (FOUR && warp > kMmaWarp)) {
       // ---- loads ----
       constexpr int ROWS = kLoaders / PIECES;  // rows of a pass: a multiple of 8, so a thread's swizzle is fixed
       const int lt = tid - 32 * kLoadWarp, piece = lt % PIECES, row0 = lt / PIECES;
@@ -648,31 +713,45 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const uint32_t at = piece_at(row0, piece);
       int ring = 0, count = 0;
       bool ok = true;  // where a wait gave up the loops go on without copies: their warps meet at barriers
+      constexpr int NR = raw_stages<W>();
+      const int lw = warp < kMmaWarp ? warp - kLoadWarp : warp - kLoadWarp - 1;
+      [[maybe_unused]] const uint32_t raw = buffer(NB) + lw * NR * raw_bytes<W>();
+      [[maybe_unused]] const Places<W> places(c.width, lane);
+      int raw_sent = 0, raw_read = 0, next_id = -1;
+      uint32_t there = 0;
       each_item<SEL>(a, [&](const Item& it) {
         if (it.steps == 0) return;
         const int32_t* table = p.table + it.r * p.table_stride;
-        Raw<FOUR ? W : 64> codes[2];  // 4 bits: of the warp's two slabs, loaded a half step ahead
-        int ids[2], next_ids[2];      // their pages, looked up another half step ahead
-        const int lw = lt >> 5;
-        auto find4 = [&](int j) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int u = it.u0 + j * kChunkKeys + (2 * lw + b) * kSlab;
-            next_ids[b] = -1;
-            if (u < it.u1) {
-              const int i = c.page.div(u);
-              if (i < p.width) next_ids[b] = __ldg(table + i);
-            }
+        // 4 bits: the slabs' keys and values in the order of the half steps (K0 V0 K1 V1 ...), eight a half step, of which the
+        // warp takes every seventh: its k-th is number lw + 7 k, whose codes a bulk copy brings to stage raw_sent % NR.  Bit s
+        // of `there`: those of stage s were copied (else there are no such keys).
+        [[maybe_unused]] auto key_of = [&](int q) { return it.u0 + (q >> 4) * kChunkKeys + (q & 7) * kSlab; };
+        [[maybe_unused]] auto find4 = [&](int q) {
+          const int u = key_of(q);
+          next_id = -1;
+          if (lane == 0 && u < it.u1) {
+            const int i = c.page.div(u);
+            if (i < p.width) next_id = __ldg(table + i);
           }
         };
-        auto load4 = [&](int j, bool value) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int u = it.u0 + j * kChunkKeys + (2 * lw + b) * kSlab;
-            const bool on = (unsigned)ids[b] < (unsigned)c.npages;
-            const int slab = on ? (u - c.page.div(u) * c.page.d) / kSlab : 0;
-            codes[b].load(a.c4.data + (on ? ids[b] * a.c4.page : 0) + it.h * a.c4.head + (int64_t)slab * slab_bytes(c.width),
-                          c.width, value, lane, on ? it.u1 - u : 0);
+        [[maybe_unused]] auto send4 = [&](int q) {
+          if constexpr (FOUR) {
+            const int s = raw_sent % NR, id4 = next_id;
+            find4(q + kUnpackWarps);
+            const bool on = (unsigned)id4 < (unsigned)c.npages;
+            if (lane == 0) {
+              uint64_t* bar = &bars.raw_full[lw][s];
+              tc::mbar_expect(bar, on ? 9 * c.width : 0);
+              if (on) {
+                const int u = key_of(q), slab = (u - c.page.div(u) * c.page.d) / kSlab;
+                tc::copy_bulk(raw + s * raw_bytes<W>(),
+                              a.c4.data + id4 * a.c4.page + it.h * a.c4.head + (int64_t)slab * slab_bytes(c.width) +
+                                  (q & 8 ? 9 * c.width : 0),
+                              9 * c.width, bar);
+              }
+            }
+            there = (there & ~(1u << s)) | (uint32_t)__shfl_sync(0xffffffffu, (int)on, 0) << s;
+            ++raw_sent;
           }
         };
         const char* src_k = (const char*)c.k + 2 * (c.ks[2] * it.h + (col_on ? piece * 8 : 0));
@@ -696,19 +775,19 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         };
         if (SEL) listed(0);
         if constexpr (FOUR) {
-          find4(0);
-          ids[0] = next_ids[0];
-          ids[1] = next_ids[1];
-          load4(0, false);
+          find4(lw);
+          for (int q = lw; ok && q < min(NR * kUnpackWarps, 2 * it.steps * kStepSlabs); q += kUnpackWarps) send4(q);
         } else {
           find(0);
         }
-        for (int x = lt; x < it.tiles * kRows; x += kLoaders) {
-          const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
-          bars.row_q[x] = x < it.n ? 2 * ((it.q0 + tok) * a.q.tok + (it.h * G + g) * a.q.head) : -1;
+        if (!FOUR || warp < kMmaWarp) {
+          for (int x = lt; x < it.tiles * kRows; x += kLoaders) {
+            const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
+            bars.row_q[x] = x < it.n ? 2 * ((it.q0 + tok) * a.q.tok + (it.h * G + g) * a.q.head) : -1;
+          }
+          meet(1, kLoaders);
+          ok = ok && wait_warp(&bars.q_empty, (count & 1) ^ 1, failed, limit);
         }
-        meet(1, kLoaders);
-        ok = ok && wait_warp(&bars.q_empty, (count & 1) ^ 1, failed, limit);
         constexpr int BATCH = kChunkKeys / ROWS / 2;  // offsets are read ahead of the copies that wait for them
         auto copy_rows = [&](uint32_t dst, const char* src, const int64_t* rows) {
 #pragma unroll
@@ -723,58 +802,65 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
             }
           }
         };
-        if (ok)
+        if (ok && (!FOUR || warp < kMmaWarp)) {
           for (int t = 0; t < it.tiles; ++t)
             copy_rows(q_tile(t), (const char*)a.q.p + (col_on ? piece * 16 : 0), bars.row_q + t * kRows);
-        if (ok) copy_arrive(&bars.q_full);
+          copy_arrive(&bars.q_full);
+        }
         const int total = 2 * it.steps;
-        for (int i = 0; i < total; ++i) {
-          const bool value = i & 1;  // K0 V0 K1 V1 ...
-          const int j = i >> 1, b = (ring + i) % NB;
-          if constexpr (FOUR) {
-            ok = ok && wait_warp(&bars.empty[b], (((ring + i) / NB) & 1) ^ 1, failed, limit);
-            if (ok) {
-#pragma unroll
-              for (int n = 0; n < 2; ++n) codes[n].template store<T>(buffer(b), c.width, value, lane, (2 * lw + n) * kSlab);
-              tc::fence_proxy_async_smem();
-              tc::mbar_arrive(&bars.full[b]);
-              if (!value) {
-                load4(j, true);
-                find4(j + 1);
-              } else {
-                ids[0] = next_ids[0];
-                ids[1] = next_ids[1];
-                if (i + 1 < total) load4(j + 1, false);
-              }
-            }
-            continue;
-          }
-          if (!value) {
-            const bool on = (unsigned)id < (unsigned)c.npages;
-            bars.row_k[j & 1][lt] = on ? 2 * (id * c.ks[0] + off * c.ks[1]) : -1;
-            bars.row_v[j & 1][lt] = on ? 2 * (id * c.vs[0] + off * c.vs[1]) : -1;
-            find(j + 1);
-            meet(1, kLoaders);
-          }
-          ok = ok && wait_warp(&bars.empty[b], (((ring + i) / NB) & 1) ^ 1, failed, limit);
-          if (SEL && ok && !value && lt < segs * (1 + a.plan.words)) {  // with K: the step's pages and their pickers
-            const int g = lt < segs ? lt : (lt - segs) / a.plan.words, u = it.u0 + j * kChunkKeys + g * c.page.d;
-            const bool on = u < it.u1;
-            const int64_t e = it.list + (on ? c.page.div(u) : 0);
-            copy4(tc::smem_u32(&bars.listed[(ring / 2 + j) % NB][lt]),
-                  lt < segs ? (const void*)(a.plan.pages + e)
-                            : (const void*)(a.plan.pickers + e * a.plan.words + (lt - segs) % a.plan.words), on);
-          }
-          if (ok) {
-            copy_rows(buffer(b), value ? src_v : src_k, value ? bars.row_v[j & 1] : bars.row_k[j & 1]);
-            copy_arrive(&bars.full[b]);
+        if constexpr (FOUR) {
+          for (int q = lw; ok && q < total * kStepSlabs; q += kUnpackWarps) {
+            const int i = ring + q / kStepSlabs, b = i % NB, s = raw_read % NR;
+            const bool value = q & kStepSlabs;
+            ok = wait_warp(&bars.raw_full[lw][s], (raw_read / NR) & 1, failed, limit);
+            ok = ok && wait_warp(&bars.empty[b], ((i / NB) & 1) ^ 1, failed, limit);
+            if (!ok) break;
+            ++raw_read;
+            Codes<W> codes;
+            codes.load(raw + s * raw_bytes<W>(), places, c.width, value, lane, (there >> s) & 1 ? it.u1 - key_of(q) : 0);
+            codes.template store<T>(buffer(b) + (q & 7) * kSlab * 128, places, c.width, value, lane);
+            tc::fence_proxy_async_smem();
+            arrive_warp(&bars.full[b]);  // the stage has been read
+            if (q + NR * kUnpackWarps < total * kStepSlabs) send4(q + NR * kUnpackWarps);
           }
         }
-        meet(1, kLoaders);  // the offsets are read before the next item's are written
+        for (int i = 0; !FOUR && i < total; ++i) {
+          const bool value = i & 1;  // K0 V0 K1 V1 ...
+          const int j = i >> 1, b = (ring + i) % NB;
+          if constexpr (!FOUR) {
+            if (!value) {
+              const bool on = (unsigned)id < (unsigned)c.npages;
+              bars.row_k[j & 1][lt] = on ? 2 * (id * c.ks[0] + off * c.ks[1]) : -1;
+              bars.row_v[j & 1][lt] = on ? 2 * (id * c.vs[0] + off * c.vs[1]) : -1;
+              find(j + 1);
+              meet(1, kLoaders);
+            }
+            ok = ok && wait_warp(&bars.empty[b], (((ring + i) / NB) & 1) ^ 1, failed, limit);
+            if (SEL && ok && !value && lt < segs * (1 + a.plan.words)) {  // with K: the step's pages and their pickers
+              const int g = lt < segs ? lt : (lt - segs) / a.plan.words, u = it.u0 + j * kChunkKeys + g * c.page.d;
+              const bool on = u < it.u1;
+              const int64_t e = it.list + (on ? c.page.div(u) : 0);
+              copy4(tc::smem_u32(&bars.listed[(ring / 2 + j) % NB][lt]),
+                    lt < segs ? (const void*)(a.plan.pages + e)
+                              : (const void*)(a.plan.pickers + e * a.plan.words + (lt - segs) % a.plan.words), on);
+            }
+            if (ok) {
+              copy_rows(buffer(b), value ? src_v : src_k, value ? bars.row_v[j & 1] : bars.row_k[j & 1]);
+              copy_arrive(&bars.full[b]);
+            }
+          }
+        }
+        if (!FOUR || warp < kMmaWarp) meet(1, kLoaders);  // the offsets are read before the next item's are written
         ring += total;
         ++count;
       });
       asm volatile("cp.async.wait_all;" ::: "memory");
+      if constexpr (FOUR) {  // copies in flight end before the block does
+        const long long t0 = clock64();
+        for (; raw_read < raw_sent; ++raw_read)
+          while (!tc::mbar_try_wait(&bars.raw_full[lw][raw_read % NR], (raw_read / NR) & 1))
+            if (clock64() - t0 > kWaitCycles) break;
+      }
     } else if (warp == kMmaWarp) {
       // ---- products ----
       const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
@@ -945,7 +1031,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         // selected: bit g: the row's token picked the page of keys 16 g .. 16 g + 15.  Groups that it did not pick are
         // left out of the maximum and get weights of 2^-inf; the slots past the token in its own page are dropped.
         uint32_t picked = 0;
-        if (SEL) {
+        if constexpr (SEL) {
           const uint32_t* listed = bars.listed[(ring / 2 + j) % NB];
           bool own = false;
           for (int i = 0; i < segs; ++i) {
@@ -1159,9 +1245,9 @@ cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
   auto kernel = k_paged_chunk<T, W, SEL, FOUR>;
   static OncePerDevice once;
   cudaError_t e = once(
-      [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<W>()); });
+      [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)block_bytes<W, FOUR>()); });
   if (e != cudaSuccess) return e;
-  return launch_next(kernel, SLNR_COUNTED(dim3(kChunkBlocks)), dim3(kThreads), smem_bytes<W>(), s, a, hdr,
+  return launch_next(kernel, SLNR_COUNTED(dim3(kChunkBlocks)), dim3(kThreads), block_bytes<W, FOUR>(), s, a, hdr,
                      wait_limit_cycles());
 }
 
