@@ -61,7 +61,7 @@ namespace {
 constexpr int kRows = 128;              // of a tile
 constexpr int kLoadWarp = 8;            // warps 0-7: softmax
 constexpr int kLoaders = 128;
-constexpr int kMmaWarp = 12;            // 13-15 only complete its warpgroup
+constexpr int kMmaWarp = 12;            // 13-15 only complete its warpgroup (4 bits: below)
 constexpr int kThreads = 512;
 constexpr int kSoftRegs = 192, kOtherRegs = 64;  // of 128 a thread at launch
 static_assert(2 * (kSoftRegs + kOtherRegs) <= 4 * 128, "register shares of the four warpgroups");
@@ -103,21 +103,23 @@ struct LoadShared : Shared {
   uint32_t listed[8][kSegments * (1 + kMaxWords)];     // selected: a step's pages, then who picked each
 };
 
-// Keys and values in 4 bits: the seven warps beside the softmax and MMA warps unpack
-// them, each with a ring of slabs' keys (or values) of its own beside the tiles.
-constexpr int kUnpackWarps = 7;
+// Keys and values in 4 bits: one warp copies their codes to a ring of half steps (128
+// keys, then their values) beside the tiles, six unpack them.
+constexpr int kCopyWarp = 13;
+constexpr int kUnpackWarps = 6;  // 8-11, 14, 15
 constexpr int kStepSlabs = kChunkKeys / kSlab;
 template <int W>
 constexpr int raw_stages() { return W == 128 ? 2 : 4; }
 template <int W>
-constexpr int raw_bytes() { return 9 * W; }  // of a stage
+constexpr int raw_bytes() { return kStepSlabs * 9 * W; }  // of a stage
 template <>
 struct LoadShared<true> : Shared {
-  uint64_t raw_full[kUnpackWarps][4];
+  uint64_t raw_full[4], raw_empty[4];
+  uint32_t there[4];  // bit i: slab i of the stage was copied; else there are no such keys
 };
 template <int W, bool FOUR>
 constexpr size_t block_bytes() {
-  return smem_bytes<W>() + (FOUR ? (size_t)kUnpackWarps * raw_stages<W>() * raw_bytes<W>() : 0);
+  return smem_bytes<W>() + (FOUR ? (size_t)raw_stages<W>() * raw_bytes<W>() : 0);
 }
 
 static_assert(block_bytes<128, false>() + sizeof(LoadShared<false>) <= (size_t)227 * 1024, "shared memory of a block");
@@ -282,18 +284,22 @@ struct Codes {
   static constexpr int N = W / 64;
   uint32_t w[N][4], scale[N];
 
-  // keys: slots of it that are keys; the others hold anything, and their values become 0 (their scores are dropped)
+  // keys: slots of it that are keys; the others hold anything, and their scales become 0 (of keys, only where there are
+  // none: their scores are dropped)
   __device__ __forceinline__ void load(uint32_t raw, const Places<W>& at, int width, bool value, int lane, int keys) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      w[n][0] = w[n][1] = w[n][2] = w[n][3] = scale[n] = 0;
-      if (keys <= 0 || lane + 32 * n >= width / 2) continue;
+      if (lane + 32 * n >= width / 2) break;
       lds4(w[n], raw + 16 * (lane + 32 * n));
       if (W == 128) scale[n] = lds_u16(raw + (value ? at.v_scale[n] : at.k_scale[n]));
       else if (value) scale[n] = lds_u32(raw + at.v_scale[n]);
       else scale[n] = lds_u8(raw + at.k_scale[n]) | lds_u8(raw + at.k_scale[n] + 2) << 8;
-      const int left = keys - at.v_slot[n];
-      if (value && left < 4) scale[n] &= left > 0 ? (1u << 8 * left) - 1 : 0u;
+    }
+    if (keys >= kSlab) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int left = value ? keys - at.v_slot[n] : keys > 0 ? kSlab : 0;
+      if (left < 4) scale[n] &= left > 0 ? (1u << 8 * left) - 1 : 0u;
     }
   }
 
@@ -682,11 +688,14 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       tc::mbar_init(&bars.p_full[t], kWarpArrivals);
     }
     for (int b = 0; b < NB; ++b) {
-      tc::mbar_init(&bars.full[b], FOUR ? kStepSlabs : kLoaders);
+      tc::mbar_init(&bars.full[b], FOUR ? kUnpackWarps : kLoaders);
       tc::mbar_init(&bars.empty[b], 1);
     }
     if constexpr (FOUR)
-      for (int i = 0; i < kUnpackWarps * 4; ++i) tc::mbar_init(&bars.raw_full[i / 4][i % 4], 1);
+      for (int i = 0; i < 4; ++i) {
+        tc::mbar_init(&bars.raw_full[i], 1);
+        tc::mbar_init(&bars.raw_empty[i], kUnpackWarps);
+      }
     bars.failed = 0;
     tc::fence_mbar_init();
   }
@@ -705,7 +714,57 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   // Counters run on from item to item: ring steps, steps of each tile, items with keys.
   if (warp >= kLoadWarp) {
     regs_down<kOtherRegs>();
-    if (warp < kMmaWarp || (FOUR && warp > kMmaWarp)) {
+    if (FOUR && warp == kCopyWarp) {
+      // ---- codes of 4 bits: lane i of the first eight slab i of each half step ----
+      if constexpr (FOUR) {
+        constexpr int NR = raw_stages<W>();
+        const uint32_t raw = buffer(NB);
+        int sent = 0;
+        bool ok = true;
+        each_item<SEL>(a, [&](const Item& it) {
+          const int32_t* table = p.table + it.r * p.table_stride;
+          int next = -1;
+          auto find = [&](int j) {
+            const int u = it.u0 + j * kChunkKeys + lane * kSlab;
+            next = -1;
+            if (lane < kStepSlabs && u < it.u1) {
+              const int i = c.page.div(u);
+              if (i < p.width) next = __ldg(table + i);
+            }
+          };
+          find(0);
+          for (int j = 0; ok && j < it.steps; ++j) {
+            const int u = it.u0 + j * kChunkKeys + lane * kSlab;
+            const bool on = (unsigned)next < (unsigned)c.npages;
+            const uint8_t* src = a.c4.data;
+            if (on)
+              src += next * a.c4.page + it.h * a.c4.head + (int64_t)((u - c.page.div(u) * c.page.d) / kSlab) * slab_bytes(c.width);
+            const uint32_t mask = __ballot_sync(0xffffffffu, on);
+            find(j + 1);
+#pragma unroll
+            for (int value = 0; value < 2; ++value) {
+              const int s = sent % NR;
+              ok = ok && wait_warp(&bars.raw_empty[s], ((sent / NR) & 1) ^ 1, failed, limit);
+              if (!ok) break;
+              if (lane == 0) {
+                bars.there[s] = mask;
+                tc::mbar_expect(&bars.raw_full[s], __popc(mask) * 9 * c.width);
+              }
+              __syncwarp();
+              if (on)
+                tc::copy_bulk(raw + s * raw_bytes<W>() + lane * 9 * W, src + value * 9 * c.width, 9 * c.width,
+                              &bars.raw_full[s]);
+              ++sent;
+            }
+          }
+        });
+        // copies in flight end before the block does: the last of each stage
+        const long long t0 = clock64();
+        for (int i = sent > NR ? sent - NR : 0; i < sent; ++i)
+          while (!tc::mbar_try_wait(&bars.raw_full[i % NR], (i / NR) & 1))
+            if (clock64() - t0 > kWaitCycles) break;
+      }
+    } else if (warp < kMmaWarp || (FOUR && warp > kMmaWarp)) {
       // ---- loads ----
       constexpr int ROWS = kLoaders / PIECES;  // rows of a pass: a multiple of 8, so a thread's swizzle is fixed
       const int lt = tid - 32 * kLoadWarp, piece = lt % PIECES, row0 = lt / PIECES;
@@ -713,47 +772,12 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       const uint32_t at = piece_at(row0, piece);
       int ring = 0, count = 0;
       bool ok = true;  // where a wait gave up the loops go on without copies: their warps meet at barriers
-      constexpr int NR = raw_stages<W>();
-      const int lw = warp < kMmaWarp ? warp - kLoadWarp : warp - kLoadWarp - 1;
-      [[maybe_unused]] const uint32_t raw = buffer(NB) + lw * NR * raw_bytes<W>();
+      [[maybe_unused]] const int uw = warp < kMmaWarp ? warp - kLoadWarp : warp - kCopyWarp + 3;
       [[maybe_unused]] const Places<W> places(c.width, lane);
-      int raw_sent = 0, raw_read = 0, next_id = -1;
-      uint32_t there = 0;
+      [[maybe_unused]] int slab = uw;  // of the eight of a half step: every sixth of all is the warp's
       each_item<SEL>(a, [&](const Item& it) {
         if (it.steps == 0) return;
         const int32_t* table = p.table + it.r * p.table_stride;
-        // 4 bits: the slabs' keys and values in the order of the half steps (K0 V0 K1 V1 ...), eight a half step, of which the
-        // warp takes every seventh: its k-th is number lw + 7 k, whose codes a bulk copy brings to stage raw_sent % NR.  Bit s
-        // of `there`: those of stage s were copied (else there are no such keys).
-        [[maybe_unused]] auto key_of = [&](int q) { return it.u0 + (q >> 4) * kChunkKeys + (q & 7) * kSlab; };
-        [[maybe_unused]] auto find4 = [&](int q) {
-          const int u = key_of(q);
-          next_id = -1;
-          if (lane == 0 && u < it.u1) {
-            const int i = c.page.div(u);
-            if (i < p.width) next_id = __ldg(table + i);
-          }
-        };
-        [[maybe_unused]] auto send4 = [&](int q) {
-          if constexpr (FOUR) {
-            const int s = raw_sent % NR, id4 = next_id;
-            find4(q + kUnpackWarps);
-            const bool on = (unsigned)id4 < (unsigned)c.npages;
-            if (lane == 0) {
-              uint64_t* bar = &bars.raw_full[lw][s];
-              tc::mbar_expect(bar, on ? 9 * c.width : 0);
-              if (on) {
-                const int u = key_of(q), slab = (u - c.page.div(u) * c.page.d) / kSlab;
-                tc::copy_bulk(raw + s * raw_bytes<W>(),
-                              a.c4.data + id4 * a.c4.page + it.h * a.c4.head + (int64_t)slab * slab_bytes(c.width) +
-                                  (q & 8 ? 9 * c.width : 0),
-                              9 * c.width, bar);
-              }
-            }
-            there = (there & ~(1u << s)) | (uint32_t)__shfl_sync(0xffffffffu, (int)on, 0) << s;
-            ++raw_sent;
-          }
-        };
         const char* src_k = (const char*)c.k + 2 * (c.ks[2] * it.h + (col_on ? piece * 8 : 0));
         const char* src_v = (const char*)c.v + 2 * (c.vs[2] * it.h + (col_on ? piece * 8 : 0));
         const int segs = SEL ? (c.page.d < kChunkKeys ? kChunkKeys / c.page.d : 1) : 0;
@@ -774,12 +798,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
           if (SEL) listed(j + 1);
         };
         if (SEL) listed(0);
-        if constexpr (FOUR) {
-          find4(lw);
-          for (int q = lw; ok && q < min(NR * kUnpackWarps, 2 * it.steps * kStepSlabs); q += kUnpackWarps) send4(q);
-        } else {
-          find(0);
-        }
+        if constexpr (!FOUR) find(0);
         if (!FOUR || warp < kMmaWarp) {
           for (int x = lt; x < it.tiles * kRows; x += kLoaders) {
             const int tok = a.group.div(it.x0 + x), g = it.x0 + x - tok * G;
@@ -809,19 +828,23 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         }
         const int total = 2 * it.steps;
         if constexpr (FOUR) {
-          for (int q = lw; ok && q < total * kStepSlabs; q += kUnpackWarps) {
-            const int i = ring + q / kStepSlabs, b = i % NB, s = raw_read % NR;
-            const bool value = q & kStepSlabs;
-            ok = wait_warp(&bars.raw_full[lw][s], (raw_read / NR) & 1, failed, limit);
+          constexpr int NR = raw_stages<W>();
+          for (int i = ring; ok && i < ring + total; ++i) {
+            const int b = i % NB, s = i % NR, key0 = it.u0 + ((i - ring) >> 1) * kChunkKeys;
+            const bool value = (i - ring) & 1;
+            ok = wait_warp(&bars.raw_full[s], (i / NR) & 1, failed, limit);
             ok = ok && wait_warp(&bars.empty[b], ((i / NB) & 1) ^ 1, failed, limit);
             if (!ok) break;
-            ++raw_read;
-            Codes<W> codes;
-            codes.load(raw + s * raw_bytes<W>(), places, c.width, value, lane, (there >> s) & 1 ? it.u1 - key_of(q) : 0);
-            codes.template store<T>(buffer(b) + (q & 7) * kSlab * 128, places, c.width, value, lane);
+            const uint32_t there = bars.there[s], raw = buffer(NB) + s * raw_bytes<W>();
+            for (; slab < kStepSlabs; slab += kUnpackWarps) {
+              Codes<W> codes;
+              codes.load(raw + slab * 9 * W, places, c.width, value, lane, (there >> slab) & 1 ? it.u1 - key0 - slab * kSlab : 0);
+              codes.template store<T>(buffer(b) + slab * kSlab * 128, places, c.width, value, lane);
+            }
+            slab -= kStepSlabs;
             tc::fence_proxy_async_smem();
-            arrive_warp(&bars.full[b]);  // the stage has been read
-            if (q + NR * kUnpackWarps < total * kStepSlabs) send4(q + NR * kUnpackWarps);
+            arrive_warp(&bars.full[b]);
+            if (lane == 0) tc::mbar_arrive(&bars.raw_empty[s]);
           }
         }
         for (int i = 0; !FOUR && i < total; ++i) {
@@ -855,12 +878,6 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
         ++count;
       });
       asm volatile("cp.async.wait_all;" ::: "memory");
-      if constexpr (FOUR) {  // copies in flight end before the block does
-        const long long t0 = clock64();
-        for (; raw_read < raw_sent; ++raw_read)
-          while (!tc::mbar_try_wait(&bars.raw_full[lw][raw_read % NR], (raw_read / NR) & 1))
-            if (clock64() - t0 > kWaitCycles) break;
-      }
     } else if (warp == kMmaWarp) {
       // ---- products ----
       const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
