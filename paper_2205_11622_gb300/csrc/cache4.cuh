@@ -7,44 +7,38 @@
 namespace slnr {
 
 #ifdef __CUDACC__
-__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t bits) {
+// x & MASK | bits.
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t bits) {
   uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "n"(MASK), "r"(bits));
   return r;
 }
 
-// The four pairs of a word as fp16: 16 + n (pairs 0 and 2) and 256 + n (1 and 3).
+// The four pairs of a word as fp16: (16 + n) / 128 (pairs 0 and 2) and (256 + n) / 128 (1 and 3).
 __device__ __forceinline__ void raw_pairs(uint32_t x, uint32_t (&r)[4]) {
   const uint32_t y = __byte_perm(x, 0, 0x2301);
-  r[0] = and_or(x, 0x03c003c0u, 0x4c004c00u);
-  r[1] = and_or(x, 0x003c003cu, 0x5c005c00u);
-  r[2] = and_or(y, 0x03c003c0u, 0x4c004c00u);
-  r[3] = and_or(y, 0x003c003cu, 0x5c005c00u);
+  r[0] = and_or<0x03c003c0u>(x, 0x30003000u);
+  r[1] = and_or<0x003c003cu>(x, 0x40004000u);
+  r[2] = and_or<0x03c003c0u>(y, 0x30003000u);
+  r[3] = and_or<0x003c003cu>(y, 0x40004000u);
 }
 
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
+__device__ __forceinline__ uint32_t bits_of(const __half2& x) { return *reinterpret_cast<const uint32_t*>(&x); }
 __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t r;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-  return r;
-}
-__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
+  return bits_of(__hfma2(as_half2(a), as_half2(b), as_half2(c)));
 }
 
-// Two scales as what (16 + n) and (256 + n) are multiplied by and added to for code
-// s / 128.  All exact: s / 128 is a whole multiple of 2^-24, 264 s / 128 has 10
+// Two scales as what (16 + n) / 128 and (256 + n) / 128 are multiplied by and added to
+// for code s / 128.  All exact: s is a whole multiple of 2^-17, 264 s / 128 has 10
 // significant bits and is below 2^15.  (264 s itself would pass fp16's largest number.)
 struct ScalePair {
   uint32_t s, o16, o256;
 };
 __device__ __forceinline__ ScalePair scale_pair(uint32_t fp16x2) {
-  ScalePair p;
-  p.s = hmul2(fp16x2, 0x20002000u);   // 2^-7
-  p.o16 = hmul2(p.s, 0xce00ce00u);    // -24
-  p.o256 = hmul2(p.s, 0xdc20dc20u);   // -264
-  return p;
+  const __half2 s = as_half2(fp16x2);
+  return {fp16x2, bits_of(__hmul2(s, __float2half2_rn(-24.f / 128))), bits_of(__hmul2(s, __float2half2_rn(-264.f / 128)))};
 }
 // Byte `i` of x as the fp16 number that it stands for, twice.
 __device__ __forceinline__ uint32_t scale_twice(uint32_t x, int i) {

@@ -37,8 +37,9 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kStages = 3;
-constexpr int kUnit = 2 * kSlab;  // keys of a stage
+constexpr int kStages = 2;
+constexpr int kUnit = 2 * kSlab;   // keys of a stage
+constexpr int kBatch = 16;         // units whose pages a warp looks up at once
 constexpr float kBelow = 12.f, kGrow = 3.f;
 
 size_t smem_bytes(int width, int rows) {
@@ -92,17 +93,34 @@ __device__ __forceinline__ uint32_t turned(uint32_t x) {
   return r;
 }
 
+// Two fp32 values in 64 bits: one instruction for both.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 template <typename T>
 __device__ __forceinline__ float2 to_float2(uint32_t x);
 template <>
 __device__ __forceinline__ float2 to_float2<__nv_bfloat16>(uint32_t x) {
   return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
 }
-template <>
-__device__ __forceinline__ float2 to_float2<__half>(uint32_t x) {
-  return __half22float2(*reinterpret_cast<const __half2*>(&x));
-}
-
 // What a block knows of a request.
 struct Request {
   int r, q0, qn, keys, units;  // its first token, tokens, keys, units of 32 keys (0: no tokens)
@@ -177,14 +195,24 @@ __device__ __forceinline__ void advance(const Attn4Args& a, Part& s) {
   clip(s, s.left);
 }
 
+// How far the copies of a warp are: its next unit, and the batch that it is sending.
+// Here, as registers are short: looked at once a unit.
+struct Ahead {
+  Part part;
+  int unit;
+  uint32_t have;               // bit l: src[l] is a slab that is there
+  const uint8_t* src[2 * kBatch];  // of unit i of the batch, slab k: at 2 i + k
+};
 struct Shared {
+  Ahead ahead[kWarps];
+  Part part[kWarps];  // that the warp works on
   uint64_t full[kWarps][kStages];
   float2 ml[kWarps][32];  // a warp's (reference, sum) of each row
   int failed[kWarps];
 };
 
 template <typename T, int W, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : NT == 2 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 2 : 1)
 k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   constexpr int WORDS = W / 32;  // of a key, a lane: its columns are 8 WORDS t ..
   constexpr int MT = W / 16;
@@ -227,55 +255,70 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(raw) + warp * kStages * 2 * slab;
   float* rows = reinterpret_cast<float*>(raw + kWarps * kStages * 2 * slab);
 
-  // The copies run ahead of the work: at unit cu of part cs, whose pages (one a lane of the first two) were looked up
-  // before.
-  Part cs = s;
-  int cu = cs.u0 + warp, issued = 0, id = -1;
+  // The copies run ahead of the work, a batch of up to 16 units of one part at a time.
+  Ahead& ahead = sh.ahead[warp];
   const bool whole = c.slots.d % kUnit == 0;  // both slabs of a unit lie in one page, one after another
+  int units = 0, done = 0, issued = 0;        // of the batch; of all
   auto look_up = [&] {
+    Part cs = ahead.part;
+    int cu = ahead.unit;
     while (cs.left >= 0 && cu >= cs.u1) {
       advance(a, cs);
       cu = cs.u0 + warp;
     }
-    id = -1;
-    if (cs.left < 0 || lane > 1) return;
-    const int key = cu * kUnit + lane * kSlab;
-    if (key < cs.q.keys) {
+    units = cs.left < 0 ? 0 : min((cs.u1 - cu - 1) / kWarps + 1, kBatch);
+    done = 0;
+    const int key = (cu + kWarps * (lane >> 1)) * kUnit + (lane & 1) * kSlab;
+    int id = -1, at = 0;
+    if ((lane >> 1) < units && key < cs.q.keys) {
       const int i = c.slots.div(key);
+      at = (int)((unsigned)(key - i * c.slots.d) / kSlab);
       if (i < p.width) id = __ldg(p.table + cs.q.r * p.table_stride + i);
     }
-  };
-  auto issue = [&] {  // into the stage of unit `issued` of this warp
-    if (cs.left < 0) return;
-    const int key = cu * kUnit + lane * kSlab;
     const bool on = (unsigned)id < (unsigned)c.npages;
-    const uint32_t both = __ballot_sync(0xffffffffu, on);
-    uint64_t* bar = full + issued % kStages;
-    const uint32_t dst = ring + issued % kStages * 2 * slab;
-    if (lane == 0) tc::mbar_expect(bar, __popc(both) * slab);
-    __syncwarp();
-    if (on && !(whole && lane == 1 && (both & 1))) {
-      const int page_slot = key - c.slots.div(key) * c.slots.d;
-      const uint8_t* src = c.data + id * c.page + cs.h * c.head + (int64_t)(page_slot / kSlab) * slab;
-      tc::copy_bulk(dst + lane * slab, src, whole && both == 3 ? 2 * slab : slab, bar);
+    const uint32_t have = __ballot_sync(0xffffffffu, on);
+    if (on) ahead.src[lane] = c.data + id * c.page + cs.h * c.head + (int64_t)at * slab;
+    if (lane == 0) {
+      ahead.part = cs;
+      ahead.unit = cu + kWarps * units;
+      ahead.have = have;
     }
-    ++issued;
-    cu += kWarps;
-    look_up();
+    __syncwarp();
   };
-  look_up();
+  auto issue = [&](int stage) {
+    if (done == units) look_up();
+    if (units == 0) return;
+    if ((lane >> 1) == done) {
+      const uint32_t both = (ahead.have >> 2 * done) & 3;
+      uint64_t* bar = full + stage;
+      if ((lane & 1) == 0) tc::mbar_expect(bar, __popc(both) * slab);
+      __syncwarp(3u << (2 * done));
+      if ((both >> (lane & 1) & 1) && !(whole && lane & 1 && both == 3))
+        tc::copy_bulk(ring + (stage * 2 + (lane & 1)) * slab, ahead.src[lane], whole && both == 3 ? 2 * slab : slab, bar);
+    }
+    ++done;
+    ++issued;
+  };
+  if (lane == 0) {
+    ahead.part = s;
+    ahead.unit = s.u0 + warp;
+    sh.part[warp] = s;
+  }
+  __syncwarp();
 #pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) issue();
+  for (int i = 0; i < kStages; ++i) issue(i);
 
-  int taken = 0;
+  int taken = 0, stage_i = 0;
+  uint32_t phase = 0;
   bool ok = true;
-  for (; s.left >= 0; advance(a, s)) {
+  while (s.left >= 0) {
     const Request& q = s.q;
     const int n_rows = min(q.qn * G, 8 * NT);
     const int first = q.keys - q.qn;  // position of its first token (lengths below 0 are 0: all tokens see nothing)
     // query fragments, and what a row's scores are multiplied by: log2 e scale, 128 of the held values, its power of two
     uint32_t qf[NT][2 * WORDS][2];
-    float f[NT][2], m[NT][2], l[NT][2];
+    float f[NT][2], m[NT][2];
+    uint64_t l[NT];  // a pair of fp32
     int pos[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -329,8 +372,8 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
         const int y = 8 * nt + 2 * t + i;
         pos[nt][i] = y < n_rows ? first + a.group.div(y) : INT32_MAX;
         m[nt][i] = -INFINITY;
-        l[nt][i] = 0.f;
       }
+      l[nt] = 0;
     }
     float o[MT][NT][4];
 #pragma unroll
@@ -338,116 +381,114 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) o[i][j][0] = o[i][j][1] = o[i][j][2] = o[i][j][3] = 0.f;
 
-    for (int u = s.u0 + warp; u < s.u1; u += kWarps) {
-      const uint32_t stage = ring + taken % kStages * 2 * slab;
-      ok = ok && __all_sync(0xffffffffu, wait(full + taken % kStages, taken / kStages & 1, limit));
-      if (!ok) continue;  // no more copies are issued
-      const int key0 = u * kUnit;
-      const int slabs = q.keys - key0 > kSlab ? 2 : q.keys > key0 ? 1 : 0;
+    // a unit's scores, weights and outputs; FULL: both slabs, every key seen by every row
+    auto unit = [&](auto full_unit, int key0, uint32_t stage) {
+      constexpr bool FULL = decltype(full_unit)::value;
+      const int slabs = FULL ? 2 : q.keys - key0 > kSlab ? 2 : q.keys > key0 ? 1 : 0;
       float x[2][NT][4];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) x[b][j][0] = x[b][j][1] = x[b][j][2] = x[b][j][3] = 0.f;
-        if (b < slabs) {
-          const uint32_t at = stage + b * slab;
-          uint32_t w0[WORDS] = {}, w1[WORDS] = {}, sc = 0;
-          if (8 * WORDS * t < D) {
-            const uint32_t from = at + (4 * (g >> 1) + (g & 1)) * (D / 2) + 4 * WORDS * t;
-            if constexpr (W == 128) {
-              lds4(w0, from);
-              lds4(w1, from + D);  // two slots on
-              sc = lds1(at + 8 * D + (g * (D / 32) + t) * 4);
-            } else {
-              lds2(w0[0], w0[1], from);
-              lds2(w1[0], w1[1], from + D);
-              sc = lds_half(at + 8 * D + (g * (D / 16) + t) * 2);
-            }
+        if (!FULL && b >= slabs) continue;
+        const uint32_t at = stage + b * slab;
+        uint32_t w0[WORDS] = {}, w1[WORDS] = {}, sc = 0;
+        if (8 * WORDS * t < D) {
+          const uint32_t from = at + (4 * (g >> 1) + (g & 1)) * (D / 2) + 4 * WORDS * t;
+          if constexpr (W == 128) {
+            lds4(w0, from);
+            lds4(w1, from + D);  // two slots on
+            sc = lds1(at + 8 * D + (g * (D / 32) + t) * 4);
+          } else {
+            lds2(w0[0], w0[1], from);
+            lds2(w1[0], w1[1], from + D);
+            sc = lds_half(at + 8 * D + (g * (D / 16) + t) * 2);
           }
-          ScalePair s0, s1;
+        }
+        ScalePair s0, s1;
 #pragma unroll
-          for (int w = 0; w < WORDS; ++w) {
-            if (w % 2 == 0) {
-              s0 = scale_pair(scale_twice(sc, W == 128 ? w / 2 : 0));
-              s1 = scale_pair(scale_twice(sc, W == 128 ? 2 + w / 2 : 1));
-            }
-            uint32_t y0[4], y1[4];
-            raw_pairs(w0[w], y0);
-            raw_pairs(w1[w], y1);
+        for (int w = 0; w < WORDS; ++w) {
+          if (w % 2 == 0) {
+            s0 = scale_pair(scale_twice(sc, W == 128 ? w / 2 : 0));
+            s1 = scale_pair(scale_twice(sc, W == 128 ? 2 + w / 2 : 1));
+          }
+          uint32_t y0[4], y1[4];
+          raw_pairs(w0[w], y0);
+          raw_pairs(w1[w], y1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              y0[i] = hfma2(y0[i], s0.s, i & 1 ? s0.o256 : s0.o16);
-              y1[i] = hfma2(y1[i], s1.s, i & 1 ? s1.o256 : s1.o16);
-            }
+          for (int i = 0; i < 4; ++i) {
+            y0[i] = hfma2(y0[i], s0.s, i & 1 ? s0.o256 : s0.o16);
+            y1[i] = hfma2(y1[i], s1.s, i & 1 ? s1.o256 : s1.o16);
+          }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const uint32_t key[4] = {y0[2 * k], y1[2 * k], y0[2 * k + 1], y1[2 * k + 1]};
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t key[4] = {y0[2 * k], y1[2 * k], y0[2 * k + 1], y1[2 * k + 1]};
 #pragma unroll
-              for (int j = 0; j < NT; ++j) Half2<__half>::mma(x[b][j], key, qf[j][2 * w + k][0], qf[j][2 * w + k][1]);
-            }
+            for (int j = 0; j < NT; ++j) Half2<__half>::mma(x[b][j], key, qf[j][2 * w + k][0], qf[j][2 * w + k][1]);
           }
         }
       }
-      // scores in units of log 2; -inf where the row does not see the key
-      const bool masked = key0 + kUnit - 1 > first;
+      // scores in units of log 2; -inf where the row does not see the key.  [i]: slab i / 2, key i % 2 of the lane's
+      uint64_t y[NT][4];
+      float top[NT][2];
       bool grow = false;
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
+      for (int j = 0; j < NT; ++j) {
+        float2 z[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float top = -INFINITY;
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              float& y = x[b][j][2 * k + i];
-              y = __fmul_rn(y, f[j][i]);
-              const int key = key0 + b * kSlab + 4 * (g >> 1) + (g & 1) + 2 * k;
-              if (masked && (key > pos[j][i] || key >= q.keys)) y = -INFINITY;
-              top = fmaxf(top, y);
-            }
-          grow = grow || top - m[j][i] > kBelow + kGrow;
+        for (int i = 0; i < 4; ++i) {
+          y[j][i] = mul2(pack2(x[i >> 1][j][2 * (i & 1)], x[i >> 1][j][2 * (i & 1) + 1]), pack2(f[j][0], f[j][1]));
+          z[i] = unpack2(y[j][i]);
+          if constexpr (!FULL) {
+            const int key = key0 + (i >> 1) * kSlab + 4 * (g >> 1) + (g & 1) + 2 * (i & 1);
+            if (key > pos[j][0] || key >= q.keys) z[i].x = -INFINITY;
+            if (key > pos[j][1] || key >= q.keys) z[i].y = -INFINITY;
+            y[j][i] = pack2(z[i].x, z[i].y);
+          }
         }
+        top[j][0] = fmaxf(fmaxf(z[0].x, z[1].x), fmaxf(z[2].x, z[3].x));
+        top[j][1] = fmaxf(fmaxf(z[0].y, z[1].y), fmaxf(z[2].y, z[3].y));
+        grow = grow || top[j][0] - m[j][0] > kBelow + kGrow || top[j][1] - m[j][1] > kBelow + kGrow;
+      }
       if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int j = 0; j < NT; ++j) {
+          float by[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float top = fmaxf(fmaxf(x[0][j][i], x[0][j][2 + i]), fmaxf(x[1][j][i], x[1][j][2 + i]));
+            float most = top[j][i];
 #pragma unroll
-            for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            if (top - m[j][i] > kBelow + kGrow) {  // rounded up: no weight passes 2^kBelow, however large the maximum
-              const float to = __fsub_ru(top, kBelow), by = exp2_fast(m[j][i] - to);
+            for (int d = 4; d < 32; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            by[i] = 1.f;
+            if (most - m[j][i] > kBelow + kGrow) {  // rounded up: no weight passes 2^kBelow, however large the maximum
+              const float to = __fsub_ru(most, kBelow);
+              by[i] = exp2_fast(m[j][i] - to);
               m[j][i] = to;
-              l[j][i] *= by;
+            }
 #pragma unroll
-              for (int k = 0; k < MT; ++k) {
-                o[k][j][i] *= by;
-                o[k][j][2 + i] *= by;
-              }
+            for (int k = 0; k < MT; ++k) {
+              o[k][j][i] *= by[i];
+              o[k][j][2 + i] *= by[i];
             }
           }
+          l[j] = mul2(l[j], pack2(by[0], by[1]));
+        }
       }
       uint32_t w[2][NT][2];
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        float ref[2];
+        const uint64_t ref = pack2(m[j][0] == -INFINITY ? 0.f : -m[j][0], m[j][1] == -INFINITY ? 0.f : -m[j][1]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) ref[i] = m[j][i] == -INFINITY ? 0.f : m[j][i];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float w0 = exp2_fast(__fsub_rn(x[b][j][2 * k], ref[0]));
-            const float w1 = exp2_fast(__fsub_rn(x[b][j][2 * k + 1], ref[1]));
-            l[j][0] += w0;
-            l[j][1] += w1;
-            w[b][j][k] = turned(Half2<__half>::pack(w0, w1));
-          }
+        for (int i = 0; i < 4; ++i) {
+          const float2 z = unpack2(add2(y[j][i], ref));
+          const float w0 = exp2_fast(z.x), w1 = exp2_fast(z.y);
+          l[j] = add2(l[j], pack2(w0, w1));
+          w[i >> 1][j][i & 1] = turned(Half2<__half>::pack(w0, w1));
+        }
       }
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        if (b >= slabs) break;
+        if (!FULL && b >= slabs) break;
         const uint32_t at = stage + b * slab;
         uint32_t v0[W / 32] = {}, v1[W / 32] = {}, sc = 0;  // W = 128: two words a slot; 64: one
         if (W / 8 * g < D) {
@@ -465,48 +506,64 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
             sc = lds1(at + 17 * D + (g >> 1) * 16 + 4 * t);
           }
         }
-        const int left = q.keys - key0 - b * kSlab - 4 * t;  // slots past the last key hold anything: scales of 0
-        if (left < 4) sc &= left > 0 ? (1u << 8 * left) - 1 : 0u;
+        if constexpr (!FULL) {
+          const int left = q.keys - key0 - b * kSlab - 4 * t;  // slots past the last key hold anything: scales of 0
+          if (left < 4) sc &= left > 0 ? (1u << 8 * left) - 1 : 0u;
+        }
         const ScalePair s0 = scale_pair(scales_of(sc, 0, 1)), s1 = scale_pair(scales_of(sc, 2, 3));
 #pragma unroll
         for (int e = 0; e < W / 64; ++e) {
           // slots 4 t and 4 t + 1, 4 t + 2 and 4 t + 3: of each pair the even columns, the odd ones
-          uint32_t y[4][4];
+          uint32_t r[4][4];
           const uint32_t a0 = v0[e], a1 = v0[e + W / 64], b0 = v1[e], b1 = v1[e + W / 64];
-          raw_pairs(__byte_perm(a0, a1, 0x5410), y[0]);
-          raw_pairs(__byte_perm(a0, a1, 0x7632), y[1]);
-          raw_pairs(__byte_perm(b0, b1, 0x5410), y[2]);
-          raw_pairs(__byte_perm(b0, b1, 0x7632), y[3]);
+          raw_pairs(__byte_perm(a0, a1, 0x5410), r[0]);
+          raw_pairs(__byte_perm(a0, a1, 0x7632), r[1]);
+          raw_pairs(__byte_perm(b0, b1, 0x5410), r[2]);
+          raw_pairs(__byte_perm(b0, b1, 0x7632), r[3]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t val[4] = {hfma2(y[0][i], s0.s, i & 1 ? s0.o256 : s0.o16),
-                                     hfma2(y[1][i], s0.s, i & 1 ? s0.o256 : s0.o16),
-                                     hfma2(y[2][i], s1.s, i & 1 ? s1.o256 : s1.o16),
-                                     hfma2(y[3][i], s1.s, i & 1 ? s1.o256 : s1.o16)};
+            const uint32_t val[4] = {hfma2(r[0][i], s0.s, i & 1 ? s0.o256 : s0.o16),
+                                     hfma2(r[1][i], s0.s, i & 1 ? s0.o256 : s0.o16),
+                                     hfma2(r[2][i], s1.s, i & 1 ? s1.o256 : s1.o16),
+                                     hfma2(r[3][i], s1.s, i & 1 ? s1.o256 : s1.o16)};
 #pragma unroll
             for (int j = 0; j < NT; ++j) Half2<__half>::mma(o[4 * e + i][j], val, w[b][j][0], w[b][j][1]);
           }
         }
       }
+    };
+    for (int u = s.u0 + warp, end = s.u1; u < end; u += kWarps) {
+      ok = ok && __all_sync(0xffffffffu, wait(full + stage_i, phase, limit));
+      if (!ok) continue;  // no more copies are issued
+      const int key0 = u * kUnit;
+      const uint32_t stage = ring + stage_i * 2 * slab;
+      if (key0 + kUnit - 1 <= first) unit(std::true_type(), key0, stage);
+      else unit(std::false_type(), key0, stage);
       __syncwarp();  // the stage has been read
+      issue(stage_i);
       ++taken;
-      issue();
+      if (++stage_i == kStages) {
+        stage_i = 0;
+        phase ^= 1;
+      }
     }
+    s = sh.part[warp];
 
     // the warps' sums, joined
     if (!ok) {  // NaN, not what the memory held: no wait gives up unseen
 #pragma unroll
-      for (int j = 0; j < NT; ++j) m[j][0] = m[j][1] = l[j][0] = l[j][1] = __int_as_float(0x7fffffff);
+      for (int j = 0; j < NT; ++j) m[j][0] = m[j][1] = __int_as_float(0x7fffffff), l[j] = pack2(m[j][0], m[j][0]);
     }
     float* mine = rows + warp * 8 * NT * (W + 4);
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        float sum = i ? unpack2(l[j]).y : unpack2(l[j]).x;
 #pragma unroll
-        for (int d = 4; d < 32; d *= 2) l[j][i] += __shfl_xor_sync(0xffffffffu, l[j][i], d);
+        for (int d = 4; d < 32; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int y = 8 * j + 2 * t + i;
-        if (g == 0) sh.ml[warp][y] = make_float2(m[j][i], l[j][i]);
+        if (g == 0) sh.ml[warp][y] = make_float2(m[j][i], sum);
         // columns 16 g .. (W = 128), 8 g ..
 #pragma unroll
         for (int k = 0; k < MT; ++k)
@@ -559,6 +616,9 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
       }
     }
     __syncthreads();
+    advance(a, s);
+    if (lane == 0) sh.part[warp] = s;
+    __syncwarp();
   }
   if (lane == 0) sh.failed[warp] = !ok;
   // the copies in flight end before the block does

@@ -404,7 +404,7 @@ Rows4Layout rows4_layout(const slnr_cache& c, const slnr_pages& p, int64_t group
   Rows4Layout l;
   const int64_t rows = p.max_q * group;
   l.tile = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
-  l.nblocks = (int)kSms * (l.tile == 8 ? 3 : l.tile == 16 ? 2 : 1);
+  l.nblocks = (int)kSms * (l.tile == 8 ? 4 : l.tile == 16 ? 2 : 1);
   l.shares = align256(sizeof(WsHeader));
   l.part = align256(l.shares + (l.nblocks + 1) * sizeof(int4));
   l.ml = align256(l.part + (size_t)2 * l.nblocks * l.tile * c.head_dim * sizeof(float));

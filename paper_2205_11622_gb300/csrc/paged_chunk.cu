@@ -211,10 +211,10 @@ struct Unpack<__nv_bfloat16> {
   }
   __device__ __forceinline__ uint4 word(uint32_t x) const {  // n as the fraction bits 5..2 of 32 + n
     const uint32_t y = __byte_perm(x, 0, 0x2301);
-    return make_uint4(fma_bf16(and_or(x >> 4, 0x003c003cu, 0x42004200u), s, off),
-                      fma_bf16(and_or(x, 0x003c003cu, 0x42004200u), s, off),
-                      fma_bf16(and_or(y >> 4, 0x003c003cu, 0x42004200u), s, off),
-                      fma_bf16(and_or(y, 0x003c003cu, 0x42004200u), s, off));
+    return make_uint4(fma_bf16(and_or<0x003c003cu>(x >> 4, 0x42004200u), s, off),
+                      fma_bf16(and_or<0x003c003cu>(x, 0x42004200u), s, off),
+                      fma_bf16(and_or<0x003c003cu>(y >> 4, 0x42004200u), s, off),
+                      fma_bf16(and_or<0x003c003cu>(y, 0x42004200u), s, off));
   }
 };
 

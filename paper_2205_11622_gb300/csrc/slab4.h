@@ -19,7 +19,7 @@
 // half the odd ones, a half's four n at
 //   n0: bits 9..6   n1: bits 5..2   n2: bits 1..0 and 15..14   n3: bits 13..10
 // so that n0 and n1, and after a swap of a half's bytes n2 and n3, are fraction bits
-// of 16 + n (exponent bits of 16) and 256 + n (of 256).
+// of 16 + n (exponent bits of 16) and 256 + n (of 256), or of the 128th part of these.
 //
 // A page of one head is a run of slabs of 16 slots, each 18 width bytes: codes of
 // the keys (8 width bytes), their scales (width), codes of the values, their
