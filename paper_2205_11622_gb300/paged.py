@@ -451,14 +451,15 @@ def page_fork(table, lens, parent, free_pages, page_size, validate=False, worksp
     R, width, stride, at_lens, dev = _held_by(table, lens, page_size)
     n, nfree = parent.shape[0] if parent.dim() == 1 else -1, free_pages.shape[0]
     at_parent, at_free = _ints(parent, "parent", (n,), dev), _ints(free_pages, "free_pages", (nfree,), dev)
-    out = _empty((n, width), torch.int32, dev, stream)
-    ints = _empty(3 * n + 1, torch.int32, dev, stream)
-    out_lens, src, dst, used = ints.split_with_sizes((n, n, n, 1))
-    at = ints.data_ptr()
-    _call("slnr_page_fork", (R, at_lens, table.data_ptr(), stride, width, page_size, at_parent, n, at_free, nfree,
-                             out.data_ptr(), at, at + 4 * n, at + 8 * n, at + 12 * n),
+    cells = n * width
+    ints = _empty(cells + 3 * n + 1, torch.int32, dev, stream)
+    out, out_lens, src, dst, used = ints.split_with_sizes((cells, n, n, n, 1))
+    at, row = ints.data_ptr(), 4 * n
+    at_out = at + 4 * cells
+    _call("slnr_page_fork", (R, at_lens, table.data_ptr(), stride, width, page_size, at_parent, n, at_free, nfree, at,
+                             at_out, at_out + row, at_out + 2 * row, at_out + 3 * row),
           dev.index, 0, validate, workspace, stream, (table, lens, parent, free_pages))
-    return out, out_lens, src, dst, used
+    return out.view(n, width), out_lens, src, dst, used
 
 
 def page_free(table, lens, npages, page_size, drop=None, validate=False, workspace=None, stream=None):
@@ -485,11 +486,12 @@ def page_compact(table, lens, npages, page_size, validate=False, workspace=None,
     if npages < 0:
         raise ValueError(f"npages is {npages}")
     half = npages // 2
-    out = _empty((R, width), torch.int32, dev, stream)
-    ints = _empty(2 * half + npages + 1, torch.int32, dev, stream)
-    src, dst, ids, used = ints.split_with_sizes((half, half, npages, 1))
+    cells = R * width
+    ints = _empty(cells + 2 * half + npages + 1, torch.int32, dev, stream)
+    out, src, dst, ids, used = ints.split_with_sizes((cells, half, half, npages, 1))
     at = ints.data_ptr()
-    _call("slnr_page_compact", (R, at_lens, table.data_ptr(), stride, width, page_size, npages, out.data_ptr(), at,
-                                at + 4 * half, at + 8 * half, at + 8 * half + 4 * npages),
+    at_src = at + 4 * cells
+    _call("slnr_page_compact", (R, at_lens, table.data_ptr(), stride, width, page_size, npages, at, at_src,
+                                at_src + 4 * half, at_src + 8 * half, at_src + 8 * half + 4 * npages),
           dev.index, 0, validate, workspace, stream, (table, lens))
-    return out, src, dst, ids, used
+    return out.view(R, width), src, dst, ids, used

@@ -47,7 +47,7 @@ def held(lens, table, page):
 
 # requests, columns, page size, pages
 SIZES = [(1, 1, 1, 1), (1, 0, 16, 3), (3, 4, 16, 40), (7, 300, 5, 3001), (65, 33, 64, 2500), (700, 9, 16, 7000),
-         (2, 2000, 16, 100_000), (40, 600, 128, 600_001)]
+         (2, 2000, 16, 100_000), (40, 600, 128, 600_001), (30, 100, 16, 1_100_003)]
 
 
 @pytest.mark.parametrize("R,width,page,npages", SIZES)
