@@ -1,6 +1,7 @@
 // Keys and values held in 4 bits (slab4.h): their way back to 16 bits.
 #pragma once
 
+#include "mma16.cuh"
 #include "paged.cuh"
 #include "slab4.h"
 
@@ -48,6 +49,45 @@ __device__ __forceinline__ uint32_t scale_twice(uint32_t x, int i) {
 __device__ __forceinline__ uint32_t scales_of(uint32_t x, int i, int j) {
   return __byte_perm(x, 0, 0x0404 | (j << 12) | (i << 4)) >> 1;
 }
+__device__ __forceinline__ uint32_t fma_bf16(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+
+// A scale, ready for the words of its block, whose values it makes: bf16 holds every
+// value, fp16 every 128th part.
+template <typename T>
+struct Unpack;
+template <>
+struct Unpack<__half> {
+  static constexpr float kTimes = 128.f;  // what the unpacked values lack
+  ScalePair p;
+  __device__ __forceinline__ explicit Unpack(uint32_t byte) : p(scale_pair(scale_twice(byte, 0))) {}
+  // 8 columns.
+  __device__ __forceinline__ uint4 word(uint32_t x) const {
+    uint32_t r[4];
+    raw_pairs(x, r);
+    return make_uint4(hfma2(r[0], p.s, p.o16), hfma2(r[1], p.s, p.o256), hfma2(r[2], p.s, p.o16), hfma2(r[3], p.s, p.o256));
+  }
+};
+template <>
+struct Unpack<__nv_bfloat16> {
+  static constexpr float kTimes = 1.f;
+  uint32_t s, off;
+  __device__ __forceinline__ explicit Unpack(uint32_t byte) {
+    const float f = __half2float(__ushort_as_half((unsigned short)(byte << 7)));
+    s = Half2<__nv_bfloat16>::pack(f, f);
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(off) : "r"(s), "r"(0xc220c220u));  // -40
+  }
+  __device__ __forceinline__ uint4 word(uint32_t x) const {  // n as the fraction bits 5..2 of 32 + n
+    const uint32_t y = __byte_perm(x, 0, 0x2301);
+    return make_uint4(fma_bf16(and_or<0x003c003cu>(x >> 4, 0x42004200u), s, off),
+                      fma_bf16(and_or<0x003c003cu>(x, 0x42004200u), s, off),
+                      fma_bf16(and_or<0x003c003cu>(y >> 4, 0x42004200u), s, off),
+                      fma_bf16(and_or<0x003c003cu>(y, 0x42004200u), s, off));
+  }
+};
 #endif
 
 // pages4.cu

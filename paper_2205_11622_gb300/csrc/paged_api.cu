@@ -579,6 +579,8 @@ slnr_status slnr_page_append4(const slnr_cache4* cache, const slnr_pages* pages,
   cudaStream_t s = (cudaStream_t)opts->stream;
   const PagesView p = view(*pages);
   const Cache4View c = view(*cache);
+  if (((int64_t)p.ntok + 7) / 8 * c.nheads * (c.width / 32) > INT32_MAX)  // warps
+    return fail(SLNR_ERR_UNSUPPORTED, "too many tokens and heads for one call");
   SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {
     return launch_validate_pages(p, c.npages, c.slots, true, nullptr, 0, 0, hdr, st);
   }));
@@ -598,7 +600,8 @@ slnr_status slnr_page_values4(const slnr_cache4* cache, const int32_t* ids, int3
   if (!k || !v) return fail(SLNR_ERR_NULL, "k or v is NULL");
   if (!aligned16(k) || !aligned16(v)) return fail(SLNR_ERR_UNSUPPORTED, "k and v must be 16-byte aligned");
   const int64_t page = (int64_t)cache->page_size * cache->nheads * (cache->head_dim / kBlockCols);
-  if (page > kMaxKeys || n * (page / 256 + 1) > INT32_MAX) return fail(SLNR_ERR_UNSUPPORTED, "too many values for one call");
+  if (page > kMaxKeys || n * (page / 256 + 1) > INT32_MAX)  // 16 columns a thread, 256 threads a block
+    return fail(SLNR_ERR_UNSUPPORTED, "too many values for one call");
   cudaStream_t s = (cudaStream_t)opts->stream;
   const TablesView none{0, 0, 0, divisor(1), nullptr, nullptr};
   SLNR_CHECK(validated(opts, [&](WsHeader* hdr, cudaStream_t st) {

@@ -177,46 +177,7 @@ __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
 
 // ---- keys and values in 4 bits (cache4.cuh): a load warp takes two slabs of each
 // 128 keys, its lanes 16-byte pieces of their codes, which become 16-bit rows of the
-// tile.  bf16 holds every value, fp16 every 128th part.
-
-__device__ __forceinline__ uint32_t fma_bf16(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t r;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-  return r;
-}
-
-// A scale, ready for the words of its block.
-template <typename T>
-struct Unpack;
-template <>
-struct Unpack<__half> {
-  static constexpr float kTimes = 128.f;  // what products of the unpacked values lack
-  ScalePair p;
-  __device__ __forceinline__ explicit Unpack(uint32_t byte) : p(scale_pair(scale_twice(byte, 0))) {}
-  // 8 columns.
-  __device__ __forceinline__ uint4 word(uint32_t x) const {
-    uint32_t r[4];
-    raw_pairs(x, r);
-    return make_uint4(hfma2(r[0], p.s, p.o16), hfma2(r[1], p.s, p.o256), hfma2(r[2], p.s, p.o16), hfma2(r[3], p.s, p.o256));
-  }
-};
-template <>
-struct Unpack<__nv_bfloat16> {
-  static constexpr float kTimes = 1.f;
-  uint32_t s, off;
-  __device__ __forceinline__ explicit Unpack(uint32_t byte) {
-    const float f = __half2float(__ushort_as_half((unsigned short)(byte << 7)));
-    s = Half2<__nv_bfloat16>::pack(f, f);
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(off) : "r"(s), "r"(0xc220c220u));  // -40
-  }
-  __device__ __forceinline__ uint4 word(uint32_t x) const {  // n as the fraction bits 5..2 of 32 + n
-    const uint32_t y = __byte_perm(x, 0, 0x2301);
-    return make_uint4(fma_bf16(and_or<0x003c003cu>(x >> 4, 0x42004200u), s, off),
-                      fma_bf16(and_or<0x003c003cu>(x, 0x42004200u), s, off),
-                      fma_bf16(and_or<0x003c003cu>(y >> 4, 0x42004200u), s, off),
-                      fma_bf16(and_or<0x003c003cu>(y, 0x42004200u), s, off));
-  }
-};
+// tile.
 
 __device__ __forceinline__ uint32_t lds_u32(uint32_t at) {
   uint32_t r;
