@@ -42,9 +42,10 @@ constexpr int kUnit = 2 * kSlab;   // keys of a stage
 constexpr int kBatch = 16;         // units whose pages a warp looks up at once
 constexpr float kBelow = 12.f, kGrow = 3.f;
 
-size_t smem_bytes(int width, int rows) {
+// Slabs, the item's queries (a warp's fragments), and the warps' sums of the rows of an item.
+size_t smem_bytes(int width, int tile, int rows) {
   const int w = width <= 64 ? 64 : 128;
-  return (size_t)kWarps * kStages * 2 * slab_bytes(width) + (size_t)kWarps * rows * (w + 4) * 4;
+  return (size_t)kWarps * kStages * 2 * slab_bytes(width) + (size_t)tile * w * 2 + (size_t)kWarps * rows * (w + 4) * 4;
 }
 
 __device__ __forceinline__ bool test(uint64_t* bar, uint32_t parity) {
@@ -212,10 +213,11 @@ struct Shared {
 };
 
 template <typename T, int W, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : 2)
 k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   constexpr int WORDS = W / 32;  // of a key, a lane: its columns are 8 WORDS t ..
   constexpr int MT = W / 16;
+  constexpr int SL = NT == 4 ? 1 : 2;  // slabs that are multiplied together: 32 rows have no registers for more
   extern __shared__ __align__(128) unsigned char raw[];
   __shared__ Shared sh;
   const PagesView& p = a.p;
@@ -253,7 +255,8 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   tc::fence_mbar_init();
   __syncwarp();
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(raw) + warp * kStages * 2 * slab;
-  float* rows = reinterpret_cast<float*>(raw + kWarps * kStages * 2 * slab);
+  const uint32_t queries = (uint32_t)__cvta_generic_to_shared(raw) + kWarps * kStages * 2 * slab + lane * 16;
+  float* rows = reinterpret_cast<float*>(raw + kWarps * kStages * 2 * slab + 8 * NT * W * 2);
 
   // The copies run ahead of the work, a batch of up to 16 units of one part at a time.
   Ahead& ahead = sh.ahead[warp];
@@ -313,10 +316,10 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   bool ok = true;
   while (s.left >= 0) {
     const Request& q = s.q;
-    const int n_rows = min(q.qn * G, 8 * NT);
+    const int n_rows = min(q.qn * G, a.rows);
     const int first = q.keys - q.qn;  // position of its first token (lengths below 0 are 0: all tokens see nothing)
-    // query fragments, and what a row's scores are multiplied by: log2 e scale, 128 of the held values, its power of two
-    uint32_t qf[NT][2 * WORDS][2];
+    // query fragments to shared memory (registers are short), by the first warp; and what a row's scores are multiplied by:
+    // log2 e scale, 128 of the held values, its power of two
     float f[NT][2], m[NT][2];
     uint64_t l[NT];  // a pair of fp32
     int pos[NT][2];
@@ -332,13 +335,6 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
         raw_q[w] = on && 8 * (WORDS * t + w) < D ? __ldg(reinterpret_cast<const uint4*>(row) + w) : make_uint4(0, 0, 0, 0);
       float factor = a.scale * 1.4426950408889634f;
       if constexpr (std::is_same<T, __half>::value) {
-#pragma unroll
-        for (int w = 0; w < WORDS; ++w) {
-          qf[nt][2 * w][0] = raw_q[w].x;
-          qf[nt][2 * w][1] = raw_q[w].y;
-          qf[nt][2 * w + 1][0] = raw_q[w].z;
-          qf[nt][2 * w + 1][1] = raw_q[w].w;
-        }
         factor *= 128.f;
       } else {
         uint32_t top = 0;
@@ -358,14 +354,20 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
         factor = factor * (128.f / up) / up2;
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) {
-          const uint32_t e[4] = {raw_q[w].x, raw_q[w].y, raw_q[w].z, raw_q[w].w};
+          uint32_t* e = &raw_q[w].x;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float2 y = to_float2<__nv_bfloat16>(e[i]);
-            qf[nt][2 * w + i / 2][i & 1] = Half2<__half>::pack(y.x * up * up2, y.y * up * up2);
+            e[i] = Half2<__half>::pack(y.x * up * up2, y.y * up * up2);
           }
         }
       }
+      if (warp == 0)
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(queries + (nt * WORDS + w) * 512), "r"(raw_q[w].x),
+                       "r"(raw_q[w].y), "r"(raw_q[w].z), "r"(raw_q[w].w)
+                       : "memory");
 #pragma unroll
       for (int i = 0; i < 2; ++i) {  // of the columns that this lane has of the products
         f[nt][i] = __shfl_sync(0xffffffffu, factor, 4 * (2 * t + i));
@@ -375,19 +377,20 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
       }
       l[nt] = 0;
     }
+    __syncthreads();
     float o[MT][NT][4];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) o[i][j][0] = o[i][j][1] = o[i][j][2] = o[i][j][3] = 0.f;
 
-    // a unit's scores, weights and outputs; FULL: both slabs, every key seen by every row
+    // scores, weights and outputs of SL slabs; FULL: every key is there and seen by every row
     auto unit = [&](auto full_unit, int key0, uint32_t stage) {
       constexpr bool FULL = decltype(full_unit)::value;
-      const int slabs = FULL ? 2 : q.keys - key0 > kSlab ? 2 : q.keys > key0 ? 1 : 0;
-      float x[2][NT][4];
+      const int slabs = FULL ? SL : q.keys - key0 > kSlab ? 2 : q.keys > key0 ? 1 : 0;
+      float x[SL][NT][4];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < SL; ++b) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) x[b][j][0] = x[b][j][1] = x[b][j][2] = x[b][j][3] = 0.f;
         if (!FULL && b >= slabs) continue;
@@ -412,6 +415,9 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
             s0 = scale_pair(scale_twice(sc, W == 128 ? w / 2 : 0));
             s1 = scale_pair(scale_twice(sc, W == 128 ? 2 + w / 2 : 1));
           }
+          uint32_t qf[NT][4];
+#pragma unroll
+          for (int j = 0; j < NT; ++j) lds4(qf[j], queries + (j * WORDS + w) * 512);
           uint32_t y0[4], y1[4];
           raw_pairs(w0[w], y0);
           raw_pairs(w1[w], y1);
@@ -424,19 +430,19 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
           for (int k = 0; k < 2; ++k) {
             const uint32_t key[4] = {y0[2 * k], y1[2 * k], y0[2 * k + 1], y1[2 * k + 1]};
 #pragma unroll
-            for (int j = 0; j < NT; ++j) Half2<__half>::mma(x[b][j], key, qf[j][2 * w + k][0], qf[j][2 * w + k][1]);
+            for (int j = 0; j < NT; ++j) Half2<__half>::mma(x[b][j], key, qf[j][2 * k], qf[j][2 * k + 1]);
           }
         }
       }
       // scores in units of log 2; -inf where the row does not see the key.  [i]: slab i / 2, key i % 2 of the lane's
-      uint64_t y[NT][4];
+      uint64_t y[NT][2 * SL];
       float top[NT][2];
       bool grow = false;
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        float2 z[4];
+        float2 z[2 * SL];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2 * SL; ++i) {
           y[j][i] = mul2(pack2(x[i >> 1][j][2 * (i & 1)], x[i >> 1][j][2 * (i & 1) + 1]), pack2(f[j][0], f[j][1]));
           z[i] = unpack2(y[j][i]);
           if constexpr (!FULL) {
@@ -446,8 +452,12 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
             y[j][i] = pack2(z[i].x, z[i].y);
           }
         }
-        top[j][0] = fmaxf(fmaxf(z[0].x, z[1].x), fmaxf(z[2].x, z[3].x));
-        top[j][1] = fmaxf(fmaxf(z[0].y, z[1].y), fmaxf(z[2].y, z[3].y));
+        top[j][0] = fmaxf(z[0].x, z[1].x);
+        top[j][1] = fmaxf(z[0].y, z[1].y);
+        if constexpr (SL == 2) {
+          top[j][0] = fmaxf(top[j][0], fmaxf(z[2].x, z[3].x));
+          top[j][1] = fmaxf(top[j][1], fmaxf(z[2].y, z[3].y));
+        }
         grow = grow || top[j][0] - m[j][0] > kBelow + kGrow || top[j][1] - m[j][1] > kBelow + kGrow;
       }
       if (__any_sync(0xffffffffu, grow)) {
@@ -474,12 +484,12 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
           l[j] = mul2(l[j], pack2(by[0], by[1]));
         }
       }
-      uint32_t w[2][NT][2];
+      uint32_t w[SL][NT][2];
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
         const uint64_t ref = pack2(m[j][0] == -INFINITY ? 0.f : -m[j][0], m[j][1] == -INFINITY ? 0.f : -m[j][1]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2 * SL; ++i) {
           const float2 z = unpack2(add2(y[j][i], ref));
           const float w0 = exp2_fast(z.x), w1 = exp2_fast(z.y);
           l[j] = add2(l[j], pack2(w0, w1));
@@ -487,7 +497,7 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
         }
       }
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < SL; ++b) {
         if (!FULL && b >= slabs) break;
         const uint32_t at = stage + b * slab;
         uint32_t v0[W / 32] = {}, v1[W / 32] = {}, sc = 0;  // W = 128: two words a slot; 64: one
@@ -537,8 +547,11 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
       if (!ok) continue;  // no more copies are issued
       const int key0 = u * kUnit;
       const uint32_t stage = ring + stage_i * 2 * slab;
-      if (key0 + kUnit - 1 <= first) unit(std::true_type(), key0, stage);
-      else unit(std::false_type(), key0, stage);
+#pragma unroll
+      for (int b = 0; b < 2; b += SL) {
+        if (key0 + (b + SL) * kSlab - 1 <= first) unit(std::true_type(), key0 + b * kSlab, stage + b * slab);
+        else unit(std::false_type(), key0 + b * kSlab, stage + b * slab);
+      }
       __syncwarp();  // the stage has been read
       issue(stage_i);
       ++taken;
@@ -554,7 +567,7 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) m[j][0] = m[j][1] = __int_as_float(0x7fffffff), l[j] = pack2(m[j][0], m[j][0]);
     }
-    float* mine = rows + warp * 8 * NT * (W + 4);
+    float* mine = rows + warp * a.rows * (W + 4);
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -564,6 +577,7 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
         for (int d = 4; d < 32; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int y = 8 * j + 2 * t + i;
         if (g == 0) sh.ml[warp][y] = make_float2(m[j][i], sum);
+        if (y >= n_rows) continue;
         // columns 16 g .. (W = 128), 8 g ..
 #pragma unroll
         for (int k = 0; k < MT; ++k)
@@ -586,7 +600,7 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
         const float2 ml = sh.ml[k][y];
         const float by = exp2_fast(ml.x - ref);
         sum += by * ml.y;
-        const float4* z = reinterpret_cast<const float4*>(rows + (k * 8 * NT + y) * (W + 4) + col);
+        const float4* z = reinterpret_cast<const float4*>(rows + (k * a.rows + y) * (W + 4) + col);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float4 v = z[e];
@@ -721,10 +735,10 @@ cudaError_t launch_rows(const Attn4Args& a, cudaStream_t s) {
   auto kernel = k_paged4_rows<T, W, NT>;
   static OncePerDevice once;
   const cudaError_t e = once([&] {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(W, 8 * NT));
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(W, 8 * NT, 8 * NT));
   });
   if (e != cudaSuccess) return e;
-  kernel<<<SLNR_COUNTED((unsigned)a.nblocks), kThreads, smem_bytes(a.c.width, 8 * NT), s>>>(a, wait_limit_cycles());
+  kernel<<<SLNR_COUNTED((unsigned)a.nblocks), kThreads, smem_bytes(a.c.width, a.tile, a.rows), s>>>(a, wait_limit_cycles());
   return cudaGetLastError();
 }
 
@@ -743,6 +757,12 @@ cudaError_t launch_rows_t(const Attn4Args& a, cudaStream_t s) {
 }
 
 }  // namespace
+
+int paged4_blocks(int width, int tile, int rows) {
+  const int by_registers = tile == 8 ? 4 : 2;
+  const int by_memory = (int)((size_t)228 * 1024 / (smem_bytes(width, tile, rows) + sizeof(Shared) + 1024));
+  return 152 * (by_registers < by_memory ? by_registers : by_memory);
+}
 
 cudaError_t launch_paged4_rows(const Attn4Args& a, int dtype, cudaStream_t s) {
   return dtype == SLNR_FP16 ? launch_rows_t<__half>(a, s) : launch_rows_t<__nv_bfloat16>(a, s);

@@ -397,14 +397,14 @@ bool rows4(const slnr_pages& p, int64_t group) { return p.max_q * group <= 32; }
 
 // Of the row kernel: rows of an item, blocks, and its workspace after the header.
 struct Rows4Layout {
-  int tile, nblocks;
+  int tile, rows, nblocks;
   size_t shares, part, ml, total;
 };
 Rows4Layout rows4_layout(const slnr_cache& c, const slnr_pages& p, int64_t group) {
   Rows4Layout l;
-  const int64_t rows = p.max_q * group;
-  l.tile = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
-  l.nblocks = (int)kSms * (l.tile == 8 ? 4 : l.tile == 16 ? 2 : 1);
+  l.rows = (int)(p.max_q * group);
+  l.tile = l.rows <= 8 ? 8 : l.rows <= 16 ? 16 : 32;
+  l.nblocks = paged4_blocks(c.head_dim, l.tile, l.rows);
   l.shares = align256(sizeof(WsHeader));
   l.part = align256(l.shares + (l.nblocks + 1) * sizeof(int4));
   l.ml = align256(l.part + (size_t)2 * l.nblocks * l.tile * c.head_dim * sizeof(float));
@@ -438,7 +438,7 @@ slnr_status attention4(const slnr_rows* q, int32_t nheads_q, const slnr_cache4* 
     const Rows4Layout l = rows4_layout(shape, *pages, group.d);
     SLNR_CHECK(check_ws(opts, l.total));
     SLNR_CHECK(validated(opts, check));
-    const Attn4Args a{p, c4, view(*q), group, scale, out, lse, l.tile, l.nblocks, 4, (int4*)(ws + l.shares),
+    const Attn4Args a{p, c4, view(*q), group, scale, out, lse, l.tile, l.rows, l.nblocks, 4, (int4*)(ws + l.shares),
                       (float*)(ws + l.part), (float2*)(ws + l.ml)};
     SLNR_LAUNCH("paged4_rows", launch_paged4_rows(a, dtype, s));
     SLNR_LAUNCH("paged4_join", launch_paged4_join(a, dtype, hdr, s));
