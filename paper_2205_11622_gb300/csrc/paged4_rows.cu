@@ -212,10 +212,11 @@ struct Shared {
   int failed[kWarps];
 };
 
-template <typename T, int W, int NT>
+template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : 2)
 k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
-  constexpr int WORDS = W / 32;  // of a key, a lane: its columns are 8 WORDS t ..
+  constexpr int W = D <= 64 ? 64 : 128;  // of the products
+  constexpr int WORDS = W / 32;          // of a key, a lane: its columns are 8 WORDS t ..
   constexpr int MT = W / 16;
   constexpr int SL = NT == 4 ? 1 : 2;  // slabs that are multiplied together: 32 rows have no registers for more
   extern __shared__ __align__(128) unsigned char raw[];
@@ -223,7 +224,8 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   const PagesView& p = a.p;
   const Cache4View& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int G = a.group.d, D = c.width, slab = slab_bytes(D);
+  constexpr int slab = slab_bytes(D);
+  const int G = a.group.d;
   let_next_start();
 
   // the block's share
@@ -730,30 +732,35 @@ k_paged4_join(const __grid_constant__ Attn4Args a, WsHeader* hdr) {
   if (lane == 0 && a.lse) a.lse[at] = (m + __log2f(sum)) * 0.6931471805599453f;
 }
 
-template <typename T, int W, int NT>
+template <typename T, int D, int NT>
 cudaError_t launch_rows(const Attn4Args& a, cudaStream_t s) {
-  auto kernel = k_paged4_rows<T, W, NT>;
+  auto kernel = k_paged4_rows<T, D, NT>;
   static OncePerDevice once;
   const cudaError_t e = once([&] {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(W, 8 * NT, 8 * NT));
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(D, 8 * NT, 8 * NT));
   });
   if (e != cudaSuccess) return e;
-  kernel<<<SLNR_COUNTED((unsigned)a.nblocks), kThreads, smem_bytes(a.c.width, a.tile, a.rows), s>>>(a, wait_limit_cycles());
+  kernel<<<SLNR_COUNTED((unsigned)a.nblocks), kThreads, smem_bytes(D, a.tile, a.rows), s>>>(a, wait_limit_cycles());
   return cudaGetLastError();
 }
 
-template <typename T, int W>
-cudaError_t launch_rows_w(const Attn4Args& a, cudaStream_t s) {
+template <typename T, int D>
+cudaError_t launch_rows_d(const Attn4Args& a, cudaStream_t s) {
   switch (a.tile) {
-    case 8: return launch_rows<T, W, 1>(a, s);
-    case 16: return launch_rows<T, W, 2>(a, s);
-    default: return launch_rows<T, W, 4>(a, s);
+    case 8: return launch_rows<T, D, 1>(a, s);
+    case 16: return launch_rows<T, D, 2>(a, s);
+    default: return launch_rows<T, D, 4>(a, s);
   }
 }
 
 template <typename T>
 cudaError_t launch_rows_t(const Attn4Args& a, cudaStream_t s) {
-  return a.c.width <= 64 ? launch_rows_w<T, 64>(a, s) : launch_rows_w<T, 128>(a, s);
+  switch (a.c.width) {
+    case 32: return launch_rows_d<T, 32>(a, s);
+    case 64: return launch_rows_d<T, 64>(a, s);
+    case 96: return launch_rows_d<T, 96>(a, s);
+    default: return launch_rows_d<T, 128>(a, s);
+  }
 }
 
 }  // namespace
