@@ -97,7 +97,7 @@ struct Shared {
   float other[16][kRows];
   float2 other_ml[kRows];
 };
-template <bool FOUR>
+template <bool CODES>
 struct LoadShared : Shared {
   int64_t row_k[2][kChunkKeys], row_v[2][kChunkKeys];  // the same to each key of a step
   uint32_t listed[8][kSegments * (1 + kMaxWords)];     // selected: a step's pages, then who picked each
@@ -117,9 +117,9 @@ struct LoadShared<true> : Shared {
   uint64_t raw_full[4], raw_empty[4];
   uint32_t there[4];  // bit i: slab i of the stage was copied; else there are no such keys
 };
-template <int W, bool FOUR>
+template <int W, bool CODES>
 constexpr size_t block_bytes() {
-  return smem_bytes<W>() + (FOUR ? (size_t)raw_stages<W>() * raw_bytes<W>() : 0);
+  return smem_bytes<W>() + (CODES ? (size_t)raw_stages<W>() * raw_bytes<W>() : 0);
 }
 
 static_assert(block_bytes<128, false>() + sizeof(LoadShared<false>) <= (size_t)227 * 1024, "shared memory of a block");
@@ -207,14 +207,14 @@ __device__ __forceinline__ void sts16(uint32_t to, const uint4& x) {
 // Where a lane's pieces of a slab are, in the codes and in a tile of its first row,
 // for keys and values.  The words of a piece are written in an order by t (turn) in
 // which the eight lanes of a 128-byte store touch every bank once.
-template <int W>
+template <int D>
 struct Places {
-  static constexpr int N = W / 64;
+  static constexpr int W = D <= 64 ? 64 : 128, N = W / 64;
   int k_scale[N], v_scale[N], k_to[N], v_to[N];
   int k_turn, v_turn, v_slot[N];
 
-  __device__ __forceinline__ Places(int width, int lane) {
-    const int per = width / 32;
+  __device__ __forceinline__ explicit Places(int lane) {
+    constexpr int per = D / 32;
     k_turn = W == 128 ? (lane % per) >> 1 : 0;  // per is 4, or 3 where the second piece has it from its own t
     v_turn = W == 128 ? (lane & 3) >> 1 : lane & 2;
 #pragma unroll
@@ -222,16 +222,16 @@ struct Places {
       const int i = lane + 32 * n;
       int slot = i / per;
       const int t = i - slot * per, g = 2 * (slot >> 2) + (slot & 1), half = (slot >> 1) & 1;
-      k_scale[n] = 8 * width + (W == 128 ? (g * per + t) * 4 + half * 2 : (g * 2 * per + 2 * t) * 2 + half);
+      k_scale[n] = 8 * D + (W == 128 ? (g * per + t) * 4 + half * 2 : (g * 2 * per + 2 * t) * 2 + half);
       k_to[n] = piece_at(slot, 4 * t);
       if constexpr (W == 128) {
-        const int q = i >= width / 4, j = i - q * (width / 4);
+        const int q = i >= D / 4, j = i - q * (D / 4);
         slot = 4 * (j & 3) + 2 * q;
-        v_scale[n] = 8 * width + (j >> 2) * 16 + slot;
+        v_scale[n] = 8 * D + (j >> 2) * 16 + slot;
         v_to[n] = piece_at(slot, 2 * (j >> 2));
       } else {
         slot = 4 * (i & 3);
-        v_scale[n] = 8 * width + (i >> 3) * 16 + slot;
+        v_scale[n] = 8 * D + (i >> 3) * 16 + slot;
         v_to[n] = piece_at(slot, i >> 2);
       }
       v_slot[n] = slot;
@@ -240,17 +240,17 @@ struct Places {
 };
 
 // Codes and scales of the keys (or values) of a slab in shared memory, a lane's.
-template <int W>
+template <int D>
 struct Codes {
-  static constexpr int N = W / 64;
+  static constexpr int W = D <= 64 ? 64 : 128, N = W / 64;
   uint32_t w[N][4], scale[N];
 
   // keys: slots of it that are keys; the others hold anything, and their scales become 0 (of keys, only where there are
   // none: their scores are dropped)
-  __device__ __forceinline__ void load(uint32_t raw, const Places<W>& at, int width, bool value, int lane, int keys) {
+  __device__ __forceinline__ void load(uint32_t raw, const Places<D>& at, bool value, int lane, int keys) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      if (lane + 32 * n >= width / 2) break;
+      if (lane + 32 * n >= D / 2) break;
       lds4(w[n], raw + 16 * (lane + 32 * n));
       if (W == 128) scale[n] = lds_u16(raw + (value ? at.v_scale[n] : at.k_scale[n]));
       else if (value) scale[n] = lds_u32(raw + at.v_scale[n]);
@@ -266,10 +266,10 @@ struct Codes {
 
   // To 16 rows of a tile.
   template <typename T>
-  __device__ __forceinline__ void store(uint32_t tile, const Places<W>& at, int width, bool value, int lane) const {
+  __device__ __forceinline__ void store(uint32_t tile, const Places<D>& at, bool value, int lane) const {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      if (lane + 32 * n >= width / 2) break;
+      if (lane + 32 * n >= D / 2) break;
       const uint32_t* x = w[n];
       if (!value) {  // 32 columns of a key: word i to piece 4 t + i
         const uint32_t to = tile + at.k_to[n];
@@ -624,13 +624,15 @@ __device__ __forceinline__ void each_item(const AttnArgs& a, F f) {
     f(item_of<SEL>(a, i, ntiles, i == from.x ? from.y : 0, i == to.x ? to.y : -1));
 }
 
-template <typename T, int W, bool SEL, bool FOUR>
+// FOUR: width of a cache in 4 bits, or 0.
+template <typename T, int W, bool SEL, int FOUR>
 __global__ void __launch_bounds__(kThreads, 1)
 k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
   constexpr int PIECES = W / 8, NB = buffers<W>();
+  constexpr int D = FOUR ? FOUR : W;
   constexpr float TIMES = FOUR ? Unpack<T>::kTimes : 1.f;  // of the keys and of the values
   extern __shared__ unsigned char smem_raw[];
-  __shared__ LoadShared<FOUR> bars;
+  __shared__ LoadShared<(FOUR > 0)> bars;
   const PagesView& p = a.p;
   const CacheView& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -699,7 +701,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
             const bool on = (unsigned)next < (unsigned)c.npages;
             const uint8_t* src = a.c4.data;
             if (on)
-              src += next * a.c4.page + it.h * a.c4.head + (int64_t)((u - c.page.div(u) * c.page.d) / kSlab) * slab_bytes(c.width);
+              src += next * a.c4.page + it.h * a.c4.head + (int64_t)((u - c.page.div(u) * c.page.d) / kSlab) * slab_bytes(D);
             const uint32_t mask = __ballot_sync(0xffffffffu, on);
             find(j + 1);
 #pragma unroll
@@ -709,11 +711,11 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
               if (!ok) break;
               if (lane == 0) {
                 bars.there[s] = mask;
-                tc::mbar_expect(&bars.raw_full[s], __popc(mask) * 9 * c.width);
+                tc::mbar_expect(&bars.raw_full[s], __popc(mask) * 9 * D);
               }
               __syncwarp();
               if (on)
-                tc::copy_bulk(raw + s * raw_bytes<W>() + lane * 9 * W, src + value * 9 * c.width, 9 * c.width,
+                tc::copy_bulk(raw + s * raw_bytes<W>() + lane * 9 * D, src + value * 9 * D, 9 * D,
                               &bars.raw_full[s]);
               ++sent;
             }
@@ -734,7 +736,7 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
       int ring = 0, count = 0;
       bool ok = true;  // where a wait gave up the loops go on without copies: their warps meet at barriers
       [[maybe_unused]] const int uw = warp < kMmaWarp ? warp - kLoadWarp : warp - kCopyWarp + 3;
-      [[maybe_unused]] const Places<W> places(c.width, lane);
+      [[maybe_unused]] const Places<D> places(lane);
       [[maybe_unused]] int slab = uw;  // of the eight of a half step: every sixth of all is the warp's
       each_item<SEL>(a, [&](const Item& it) {
         if (it.steps == 0) return;
@@ -798,9 +800,9 @@ k_paged_chunk(AttnArgs a, WsHeader* hdr, long long limit) {
             if (!ok) break;
             const uint32_t there = bars.there[s], raw = buffer(NB) + s * raw_bytes<W>();
             for (; slab < kStepSlabs; slab += kUnpackWarps) {
-              Codes<W> codes;
-              codes.load(raw + slab * 9 * W, places, c.width, value, lane, (there >> slab) & 1 ? it.u1 - key0 - slab * kSlab : 0);
-              codes.template store<T>(buffer(b) + slab * kSlab * 128, places, c.width, value, lane);
+              Codes<D> codes;
+              codes.load(raw + slab * 9 * D, places, value, lane, (there >> slab) & 1 ? it.u1 - key0 - slab * kSlab : 0);
+              codes.template store<T>(buffer(b) + slab * kSlab * 128, places, value, lane);
             }
             slab -= kStepSlabs;
             tc::fence_proxy_async_smem();
@@ -1218,20 +1220,30 @@ k_paged_join(AttnArgs a) {
   }
 }
 
-template <typename T, int W, bool SEL, bool FOUR>
+template <typename T, int W, bool SEL, int FOUR>
 cudaError_t launch(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
   auto kernel = k_paged_chunk<T, W, SEL, FOUR>;
   static OncePerDevice once;
   cudaError_t e = once(
-      [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)block_bytes<W, FOUR>()); });
+      [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)block_bytes<W, (FOUR > 0)>()); });
   if (e != cudaSuccess) return e;
-  return launch_next(kernel, SLNR_COUNTED(dim3(kChunkBlocks)), dim3(kThreads), block_bytes<W, FOUR>(), s, a, hdr,
+  return launch_next(kernel, SLNR_COUNTED(dim3(kChunkBlocks)), dim3(kThreads), block_bytes<W, (FOUR > 0)>(), s, a, hdr,
                      wait_limit_cycles());
 }
 
-template <typename T, bool SEL, bool FOUR = false>
+template <typename T, bool SEL>
 cudaError_t launch_w(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
-  return a.c.width <= 64 ? launch<T, 64, SEL, FOUR>(a, hdr, s) : launch<T, 128, SEL, FOUR>(a, hdr, s);
+  return a.c.width <= 64 ? launch<T, 64, SEL, 0>(a, hdr, s) : launch<T, 128, SEL, 0>(a, hdr, s);
+}
+
+template <typename T>
+cudaError_t launch_4(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) {
+  switch (a.c.width) {
+    case 32: return launch<T, 64, false, 32>(a, hdr, s);
+    case 64: return launch<T, 64, false, 64>(a, hdr, s);
+    case 96: return launch<T, 128, false, 96>(a, hdr, s);
+    default: return launch<T, 128, false, 128>(a, hdr, s);
+  }
 }
 
 }  // namespace
@@ -1250,7 +1262,7 @@ cudaError_t launch_paged_plan(const AttnArgs& a, WsHeader* hdr, cudaStream_t s) 
 
 cudaError_t launch_paged_chunk(const AttnArgs& a, int dtype, WsHeader* hdr, cudaStream_t s) {
   if (a.c4.data)
-    return dtype == SLNR_FP16 ? launch_w<__half, false, true>(a, hdr, s) : launch_w<__nv_bfloat16, false, true>(a, hdr, s);
+    return dtype == SLNR_FP16 ? launch_4<__half>(a, hdr, s) : launch_4<__nv_bfloat16>(a, hdr, s);
   if (a.picked) return dtype == SLNR_FP16 ? launch_w<__half, true>(a, hdr, s) : launch_w<__nv_bfloat16, true>(a, hdr, s);
   return dtype == SLNR_FP16 ? launch_w<__half, false>(a, hdr, s) : launch_w<__nv_bfloat16, false>(a, hdr, s);
 }
