@@ -104,7 +104,9 @@ struct LoadShared : Shared {
 };
 
 // Keys and values in 4 bits: one warp copies their codes to a ring of half steps (128
-// keys, then their values) beside the tiles, six unpack them.
+// keys, then their values) beside the tiles, six unpack them, every sixth of all slabs
+// each.  The ring is handed over by half steps, of which each of the six reads: none can
+// be a turn of the ring ahead of another, whose turns it tells apart by parity alone.
 constexpr int kCopyWarp = 13;
 constexpr int kUnpackWarps = 6;  // 8-11, 14, 15
 constexpr int kStepSlabs = kChunkKeys / kSlab;

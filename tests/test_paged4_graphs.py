@@ -224,6 +224,23 @@ def test_rows_whose_waits_gave_up(slnr, lens, heads):
     assert (gave_up > 0 or max(n for n, _ in lens) < 10 and lens[0][1] < 20000) and not bad.any() and flags == 0
 
 
+@pytest.mark.parametrize("lens", [[(1, 9000), (1, 3)], [(8, 3000)], [(90, 700), (1, 50)], [(300, 2000)]])
+@pytest.mark.parametrize("D", [32, 64, 96, 128])
+def test_no_wait_runs_out_unseen(slnr, lens, D):
+    """Right results alone do not show a wait that gave up where nothing depended on it: it takes two seconds."""
+    b = P.Batch4(slnr, lens, 16, 4, 1, D, seed=83)
+    args = (b.q.cuda(), b.cache(), b.tables())
+    slnr.paged_attention(*args)
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    torch.cuda.synchronize()
+    start.record()
+    for _ in range(3):
+        slnr.paged_attention(*args)
+    end.record()
+    torch.cuda.synchronize()
+    assert start.elapsed_time(end) < 500
+
+
 def test_no_flag_on_memory_that_held_others(slnr):
     for lens in ([(1, 40)], [(0, 5), (1, 700)], [(1, 9000), (8, 3)], [(100, 300)]):
         b, ws = P.Batch4(slnr, lens, 16, 4, 1, 64, seed=80), slnr.Workspace()
