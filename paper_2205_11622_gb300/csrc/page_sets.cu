@@ -10,7 +10,8 @@ namespace {
 // Copies.  An item is 256 units of a page's tensor (4 KB of 16-byte units), and a
 // warp's: 8 loads a lane in flight, then 8 stores.  Warp g of W takes items g, g +
 // W, ... of all pages; its lanes look at 32 of them at once for the ones whose
-// entries name pages, so that long lists of which few are used cost little.
+// entries name pages, so that long lists of which few are used cost little.  600 pages of
+// 64 slots, 8 heads of 128 (315 MB in and out) 52 us, 6.0 TB/s.
 constexpr int kCopyThreads = 256;
 
 template <typename U>
@@ -69,7 +70,7 @@ k_page_copy(const __grid_constant__ CopyParts c, const int32_t* src, const int32
 // Sets of pages: one cluster of 16 blocks.  Each block has a sixteenth of the
 // pages, a bit each, in its shared memory, and reads a sixteenth of the tables.  Up to
 // 2^20 pages a block sets the bits of what it reads in a set of all pages of its own,
-// and the sets are joined (512 requests of 150k pages in all 27 -> 12 us); above, where
+// and the sets are joined (512 requests, 150k pages, 27 -> 16 us); above, where
 // those do not fit, it sets them where they belong.  Counts go through shared memory
 // too, so one launch does it, without a workspace, and lists come out in the pages' order.
 constexpr int kSetThreads = 1024;

@@ -3,9 +3,9 @@
 //
 //   o = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q.k_j - m),  m = max_j scale q.k_j
 //
-// over the keys j that the row sees, in one pass.  Bound by memory, 9/16 of a byte
-// a value, if no more than 3 instructions of a lane go into each value: an SM takes
-// 24 bytes, 43 values, a cycle, and has 128 lanes for them.  So:
+// over the keys j that the row sees, in one pass.  At the rate of memory an SM takes 24
+// bytes, 43 values of 9/16 of a byte, a cycle, and has 128 lanes for them: 3 instructions
+// of a lane a value, and no more than one in two of them logical.  So:
 //   - Keys are the rows of both products (S^T = K Q^T, O^T = V^T P^T), 16 at a time,
 //     and the query rows their columns, 8 at a time: 8 query rows cost half of what
 //     16 would.  P^T is turned from the one product's result into the other's
@@ -20,10 +20,24 @@
 //     conflicts, no shuffles.
 //   - Each warp has a ring of slabs of its own, filled by bulk copies that its own lanes
 //     issue and wait for: no barrier of the block inside of an item.
+//   - What a warp knows of its copies and the queries' fragments are in shared memory, a
+//     kernel is for one width, and units that every row sees whole have code without masks:
+//     with 128 registers the compiler else makes values again that it had.
 //
 // The units (32 keys) of all requests and key heads, one after another, are cut into
 // equal shares, one a block; its warps take them in turn.  Items that a cut goes
 // through are joined by k_paged4_join.
+//
+// 64 single tokens over 9000 keys each, 32 query and 8 key heads of 128, bf16 (663 MB):
+// 126 us of kernel time, 5.3 TB/s, and a call of 132.  Bound by instructions: 289 of a warp
+// a slab, 2.3 a value, of which logical and byte-permuting ones take 54 % of their pipe's
+// time, fp16 ones 39 %, products 26 %; out of L2 alone it takes 3 % less.  What brought it
+// here (us a call, 64 tokens over 1001 to 32003 keys): 179 to begin with; 153 two values at a
+// time in the softmax, whole units without masks, look-ups of 16 units at once, 16 warps an
+// SM; 147 the copies' state in shared memory; 142 a kernel a width.  12 or 16 warps
+// an SM, two or three stages, 16 or 32 keys at once made no difference.  Of 17 to 32 rows a
+// warp takes a slab at a time (64 requests of 8 tokens 305 us; two slabs, with
+// registers spilled, 686; the tensor cores' kernel, as for 36 rows, 571).
 #include <type_traits>
 
 #include "cache4.cuh"
@@ -776,7 +790,7 @@ cudaError_t launch_paged4_rows(const Attn4Args& a, int dtype, cudaStream_t s) {
 }
 
 cudaError_t launch_paged4_join(const Attn4Args& a, int dtype, WsHeader* hdr, cudaStream_t s) {
-  const dim3 grid((unsigned)a.nblocks, (unsigned)a.tile);
+  const dim3 grid((unsigned)a.nblocks, (unsigned)a.rows);
   auto kernel = dtype == SLNR_FP16 ? k_paged4_join<__half> : k_paged4_join<__nv_bfloat16>;
   return launch_next(kernel, SLNR_COUNTED(grid), dim3(128), 0, s, a, hdr);
 }

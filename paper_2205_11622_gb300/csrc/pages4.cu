@@ -117,9 +117,10 @@ Group group(int width, int heads) {
 
 // A thread a block of 16 columns of one token's key and value of one head.  Per value
 // one instruction to make it fp32, one each for two values to take the quotient, the
-// whole number and the pair, one and a half to place it.  31k tokens of 8 heads of 128
-// (163 MB in and out) 37 us, 4.4 TB/s; a warp a token's blocks, whose codes of values
-// are 8 bytes of each sector, 44.
+// whole number and the pair, one and a half to place it.  32k tokens of 8 heads of 128
+// (168 MB in and out) 33 us, 5.1 TB/s, two thirds of the issue slots.  52 with each value limited to 7
+// in fp32 and a division; 38 with limits that only blocks with a value past 7 s took (one
+// block in 16: most warps have one).
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 k_page_append4(PagesView p, Cache4View c, RowsView kn, RowsView vn, Group gr, int warps) {
@@ -160,7 +161,7 @@ __device__ __forceinline__ void store_values(T* to, uint2 x, uint32_t byte, bool
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = bits_of(__hmul2(as_half2(e[i]), __float2half2_rn(Unpack<T>::kTimes)));
   }
-  if (aligned) {  // 32 bytes at once: a whole sector a lane (33 us for 31k slots where 16-byte stores took 39)
+  if (aligned) {  // 32 bytes at once: a whole sector a lane (26 us for 32k slots where 16-byte stores took 33)
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(y[0].x), "r"(y[0].y), "r"(y[0].z),
                  "r"(y[0].w), "r"(y[1].x), "r"(y[1].y), "r"(y[1].z), "r"(y[1].w)
                  : "memory");
