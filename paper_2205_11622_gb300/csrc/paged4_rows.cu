@@ -424,13 +424,12 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
             sc = lds_half(at + 8 * D + (g * (D / 16) + t) * 2);
           }
         }
-        ScalePair s0, s1;
+        // scales of the two keys side by side: of the first block, and of the second
+        const ScalePair sa = scale_pair(W == 128 ? (sc & 0x00ff00ffu) << 7 : scales_of(sc, 0, 1));
+        const ScalePair sb = W == 128 ? scale_pair((sc >> 1) & 0x7f807f80u) : sa;
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) {
-          if (w % 2 == 0) {
-            s0 = scale_pair(scale_twice(sc, W == 128 ? w / 2 : 0));
-            s1 = scale_pair(scale_twice(sc, W == 128 ? 2 + w / 2 : 1));
-          }
+          const ScalePair& s2 = w < 2 ? sa : sb;
           uint32_t qf[NT][4];
 #pragma unroll
           for (int j = 0; j < NT; ++j) lds4(qf[j], queries + (j * WORDS + w) * 512);
@@ -439,8 +438,9 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
           raw_pairs(w1[w], y1);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            y0[i] = hfma2(y0[i], s0.s, i & 1 ? s0.o256 : s0.o16);
-            y1[i] = hfma2(y1[i], s1.s, i & 1 ? s1.o256 : s1.o16);
+            const __half2 o = as_half2(i & 1 ? s2.o256 : s2.o16), m2 = as_half2(s2.s);
+            y0[i] = bits_of(__hfma2(as_half2(y0[i]), __low2half2(m2), __low2half2(o)));
+            y1[i] = bits_of(__hfma2(as_half2(y1[i]), __high2half2(m2), __high2half2(o)));
           }
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
