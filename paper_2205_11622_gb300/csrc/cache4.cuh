@@ -49,43 +49,49 @@ __device__ __forceinline__ uint32_t scale_twice(uint32_t x, int i) {
 __device__ __forceinline__ uint32_t scales_of(uint32_t x, int i, int j) {
   return __byte_perm(x, 0, 0x0404 | (j << 12) | (i << 4)) >> 1;
 }
-__device__ __forceinline__ uint32_t fma_bf16(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t r;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-  return r;
-}
-
-// A scale, ready for the words of its block, whose values it makes: bf16 holds every
-// value, fp16 every 128th part.
+// Scales of two blocks (bytes 0 and 1 of x), ready for the words of both, whose values
+// they make: bf16 holds every value, fp16 every 128th part.  A multiplication picks its
+// half of the pair by itself.
 template <typename T>
 struct Unpack;
 template <>
 struct Unpack<__half> {
   static constexpr float kTimes = 128.f;  // what the unpacked values lack
   ScalePair p;
-  __device__ __forceinline__ explicit Unpack(uint32_t byte) : p(scale_pair(scale_twice(byte, 0))) {}
-  // 8 columns.
+  __device__ __forceinline__ explicit Unpack(uint32_t x) : p(scale_pair(scales_of(x, 0, 1))) {}
+  // 8 columns of block SECOND.
+  template <bool SECOND>
   __device__ __forceinline__ uint4 word(uint32_t x) const {
     uint32_t r[4];
     raw_pairs(x, r);
-    return make_uint4(hfma2(r[0], p.s, p.o16), hfma2(r[1], p.s, p.o256), hfma2(r[2], p.s, p.o16), hfma2(r[3], p.s, p.o256));
+    auto value = [&](uint32_t n, uint32_t off) {
+      const __half2 s = as_half2(p.s), o = as_half2(off);
+      return bits_of(SECOND ? __hfma2(as_half2(n), __high2half2(s), __high2half2(o))
+                            : __hfma2(as_half2(n), __low2half2(s), __low2half2(o)));
+    };
+    return make_uint4(value(r[0], p.o16), value(r[1], p.o256), value(r[2], p.o16), value(r[3], p.o256));
   }
 };
 template <>
 struct Unpack<__nv_bfloat16> {
   static constexpr float kTimes = 1.f;
-  uint32_t s, off;
-  __device__ __forceinline__ explicit Unpack(uint32_t byte) {
-    const float f = __half2float(__ushort_as_half((unsigned short)(byte << 7)));
-    s = Half2<__nv_bfloat16>::pack(f, f);
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(off) : "r"(s), "r"(0xc220c220u));  // -40
+  __nv_bfloat162 s, off;
+  __device__ __forceinline__ explicit Unpack(uint32_t x) {
+    const float2 f = __half22float2(as_half2(scales_of(x, 0, 1)));
+    s = __floats2bfloat162_rn(f.x, f.y);
+    off = __hmul2(s, __float2bfloat162_rn(-40.f));
   }
+  template <bool SECOND>
   __device__ __forceinline__ uint4 word(uint32_t x) const {  // n as the fraction bits 5..2 of 32 + n
     const uint32_t y = __byte_perm(x, 0, 0x2301);
-    return make_uint4(fma_bf16(and_or<0x003c003cu>(x >> 4, 0x42004200u), s, off),
-                      fma_bf16(and_or<0x003c003cu>(x, 0x42004200u), s, off),
-                      fma_bf16(and_or<0x003c003cu>(y >> 4, 0x42004200u), s, off),
-                      fma_bf16(and_or<0x003c003cu>(y, 0x42004200u), s, off));
+    auto value = [&](uint32_t n) {
+      n = and_or<0x003c003cu>(n, 0x42004200u);
+      const __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162*>(&n);
+      const __nv_bfloat162 r = SECOND ? __hfma2(a, __high2bfloat162(s), __high2bfloat162(off))
+                                      : __hfma2(a, __low2bfloat162(s), __low2bfloat162(off));
+      return *reinterpret_cast<const uint32_t*>(&r);
+    };
+    return make_uint4(value(x >> 4), value(x), value(y >> 4), value(y));
   }
 };
 #endif

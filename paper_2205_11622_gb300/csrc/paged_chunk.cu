@@ -282,28 +282,29 @@ struct Codes {
       if (lane + 32 * n >= D / 2) break;
       const uint32_t* x = w[n];
       if (!value) {  // 32 columns of a key: word i to piece 4 t + i
-        const uint32_t to = tile + at.k_to[n];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const int bb = b ^ at.k_turn;
-          const Unpack<T> u((scale[n] >> 8 * bb) & 255);
-          sts16(to ^ (bb << 5), u.word(at.k_turn ? x[2 * (b ^ 1)] : x[2 * b]));
-          sts16(to ^ (bb << 5) ^ 16, u.word(at.k_turn ? x[2 * (b ^ 1) + 1] : x[2 * b + 1]));
-        }
+        const uint32_t to = tile + (at.k_to[n] ^ (at.k_turn << 5));
+        const Unpack<T> u(at.k_turn ? __byte_perm(scale[n], 0, 0x4401) : scale[n]);
+        sts16(to, u.template word<false>(at.k_turn ? x[2] : x[0]));
+        sts16(to ^ 16, u.template word<false>(at.k_turn ? x[3] : x[1]));
+        sts16(to ^ 32, u.template word<true>(at.k_turn ? x[0] : x[2]));
+        sts16(to ^ 48, u.template word<true>(at.k_turn ? x[1] : x[3]));
       } else if constexpr (W == 128) {  // 16 columns of two values, in rows that differ in their last bit
-        const uint32_t to = tile + at.v_to[n];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const Unpack<T> u((scale[n] >> 8 * b) & 255);
-          const uint32_t row = (to ^ (b << 4)) + b * 128;
-          sts16(row ^ (at.v_turn << 4), u.word(at.v_turn ? x[2 * b + 1] : x[2 * b]));
-          sts16(row ^ (at.v_turn << 4) ^ 16, u.word(at.v_turn ? x[2 * b] : x[2 * b + 1]));
-        }
+        const uint32_t to = tile + (at.v_to[n] ^ (at.v_turn << 4));
+        const Unpack<T> u(scale[n]);
+        sts16(to, u.template word<false>(at.v_turn ? x[1] : x[0]));
+        sts16(to ^ 16, u.template word<false>(at.v_turn ? x[0] : x[1]));
+        sts16((to ^ 16) + 128, u.template word<true>(at.v_turn ? x[3] : x[2]));
+        sts16(to + 128, u.template word<true>(at.v_turn ? x[2] : x[3]));
       } else {  // 8 columns of four values, in rows that differ in their last two bits
+        const uint32_t in_turn = at.v_turn ? __byte_perm(scale[n], 0, 0x1032) : scale[n];
+        const Unpack<T> u0(in_turn), u1(in_turn >> 16);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           const int r = b ^ at.v_turn;
-          sts16(tile + (at.v_to[n] ^ (r << 4)) + r * 128, Unpack<T>((scale[n] >> 8 * r) & 255).word(at.v_turn ? x[b ^ 2] : x[b]));
+          const uint32_t y = at.v_turn ? x[b ^ 2] : x[b];
+          const uint4 z = b == 0 ? u0.template word<false>(y) : b == 1 ? u0.template word<true>(y)
+                        : b == 2 ? u1.template word<false>(y) : u1.template word<true>(y);
+          sts16(tile + (at.v_to[n] ^ (r << 4)) + r * 128, z);
         }
       }
     }

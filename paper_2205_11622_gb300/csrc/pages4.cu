@@ -155,7 +155,7 @@ k_page_append4(PagesView p, Cache4View c, RowsView kn, RowsView vn, Group gr, in
 template <typename T>
 __device__ __forceinline__ void store_values(T* to, uint2 x, uint32_t byte, bool aligned) {
   const Unpack<T> u(byte);
-  uint4 y[2] = {u.word(x.x), u.word(x.y)};
+  uint4 y[2] = {u.template word<false>(x.x), u.template word<false>(x.y)};
   uint32_t* e = &y[0].x;
   if (Unpack<T>::kTimes != 1.f) {
 #pragma unroll
