@@ -154,31 +154,35 @@ __device__ __forceinline__ Request request(const PagesView& p, int r) {
   return q;
 }
 
-// Units of all requests (of one key head) before request `upto`, or of the requests
-// before the one that holds unit `at` of `heads` heads each, which goes to r (a whole
-// warp; nreq: past the last one).
-__device__ __forceinline__ int64_t units_before(const PagesView& p, int heads, int64_t at, int& r) {
-  const int lane = threadIdx.x & 31;
-  int64_t before = 0;
-  for (int r0 = 0; r0 < p.nreq; r0 += 32) {
-    const int i = r0 + lane;
-    const int mine = i < p.nreq ? units_of(__ldg(p.q_pos + i + 1) - __ldg(p.q_pos + i), __ldg(p.k_len + i)) : 0;
-    int64_t sum = mine;
+// Inclusive sum of the warp's units (of one key head) of requests r0 .. r0 + 31, a lane each.
+__device__ __forceinline__ int64_t units_of_32(const PagesView& p, int r0, int& mine) {
+  const int lane = threadIdx.x & 31, i = r0 + lane;
+  mine = i < p.nreq ? units_of(__ldg(p.q_pos + i + 1) - __ldg(p.q_pos + i), __ldg(p.k_len + i)) : 0;
+  int64_t sum = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += y;
-    }
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += y;
+  }
+  return sum;
+}
+// The request that holds unit `at` of `heads` heads each, and the units of one head
+// before it; first, first_mine: units_of_32 of request 0.
+__device__ __forceinline__ int find_unit(const PagesView& p, int heads, int64_t at, int64_t first, int first_mine,
+                                         int64_t& before) {
+  before = 0;
+  for (int r0 = 0; r0 < p.nreq; r0 += 32) {
+    int mine = first_mine;
+    const int64_t sum = r0 == 0 ? first : units_of_32(p, r0, mine);
     const unsigned past = __ballot_sync(0xffffffffu, (before + sum) * heads > at);
     if (past) {
       const int from = __ffs(past) - 1;
-      r = r0 + from;
-      return before + __shfl_sync(0xffffffffu, sum - mine, from);
+      before += __shfl_sync(0xffffffffu, sum - mine, from);
+      return r0 + from;
     }
     before += __shfl_sync(0xffffffffu, sum, 31);
   }
-  r = p.nreq;
-  return before;
+  return p.nreq;
 }
 
 // The part of an item that a block works on: units [u0, u1) of request q.r and head h.
@@ -243,8 +247,14 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   let_next_start();
 
   // the block's share
-  int r;
-  const int64_t total = units_before(p, c.nheads, INT64_MAX, r) * c.nheads;
+  int first_mine;
+  const int64_t first_sum = units_of_32(p, 0, first_mine);
+  int64_t total = __shfl_sync(0xffffffffu, first_sum, 31);
+  for (int r0 = 32; r0 < p.nreq; r0 += 32) {
+    int mine;
+    total += __shfl_sync(0xffffffffu, units_of_32(p, r0, mine), 31);
+  }
+  total *= c.nheads;
   const int64_t most = (total + a.least - 1) / a.least;
   const int n = (int)(most < gridDim.x ? most : gridDim.x);
   if (blockIdx.x >= n) {
@@ -255,8 +265,9 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   const int64_t hi = total / n * (blockIdx.x + 1) + total % n * (blockIdx.x + 1) / n;
   Part s;
   {
-    const int64_t in = lo - units_before(p, c.nheads, lo, r) * c.nheads;
-    s.q = request(p, r);
+    int64_t before;
+    s.q = request(p, find_unit(p, c.nheads, lo, first_sum, first_mine, before));
+    const int64_t in = lo - before * c.nheads;
     s.h = (int)(in / s.q.units);
     s.u0 = (int)(in - (int64_t)s.h * s.q.units);
     clip(s, hi - lo);
@@ -686,10 +697,15 @@ k_paged4_join(const __grid_constant__ Attn4Args a, WsHeader* hdr) {
   const int G = a.group.d, D = a.c.width, y = blockIdx.y;
   const int q0 = __ldg(a.p.q_pos + cut.x), n_rows = (__ldg(a.p.q_pos + cut.x + 1) - q0) * G;
   if (y >= n_rows) return;
-  int c1 = c0 + 1;  // shares c0 .. c1 - 1 begin inside of the item
-  for (; c1 < n; ++c1) {
-    const int4 s = a.shares[c1];
-    if (s.x != cut.x || s.y != cut.y || s.z == 0) break;
+  int c1 = c0 + 1;  // shares c0 .. c1 - 1 begin inside of the item; 32 at a look
+  for (uint32_t others = 0; others == 0;) {
+    bool same = false;
+    if (c1 + lane < n) {
+      const int4 s = a.shares[c1 + lane];
+      same = s.x == cut.x && s.y == cut.y && s.z != 0;
+    }
+    others = ~__ballot_sync(0xffffffffu, same);
+    c1 += others ? __ffs(others) - 1 : 32;
   }
   const int parts = c1 - c0 + 1;
   auto part = [&](int k) { return (int64_t)(2 * (c0 - 1 + k) + (k == 0)) * a.tile + y; };
