@@ -395,9 +395,13 @@ AttnPlan attn4_chunk_plan(const slnr_pages& p, int64_t group) {
 
 bool rows4(const slnr_pages& p, int64_t group) { return p.max_q * group <= 32; }
 
-// Of the row kernel: rows of an item, blocks, and its workspace after the header.
+// Of the row kernel: rows of an item, blocks, units of a block's share at least, and
+// its workspace after the header.  A unit is 32 keys, of which a block's four warps take
+// one each; long requests are cut into fewer shares, as each is one more part to join (us
+// of the GPU with 4, 8, 12 units: 500 keys of 8 heads 8.8, 9.5, 12.7; 4095 of 8 11.9,
+// 10.9, 13.5; 32768 of one head, 16 rows, 32.2, 22.7, 19.7).
 struct Rows4Layout {
-  int tile, rows, nblocks;
+  int tile, rows, nblocks, least;
   size_t shares, part, ml, total;
 };
 Rows4Layout rows4_layout(const slnr_cache& c, const slnr_pages& p, int64_t group) {
@@ -405,6 +409,7 @@ Rows4Layout rows4_layout(const slnr_cache& c, const slnr_pages& p, int64_t group
   l.rows = (int)(p.max_q * group);
   l.tile = l.rows <= 8 ? 8 : l.rows <= 16 ? 16 : 32;
   l.nblocks = paged4_blocks(c.head_dim, l.tile, l.rows);
+  l.least = p.max_k <= 2048 ? 4 : p.max_k <= 16384 ? 8 : 16;
   l.shares = align256(sizeof(WsHeader));
   l.part = align256(l.shares + (l.nblocks + 1) * sizeof(int4));
   l.ml = align256(l.part + (size_t)2 * l.nblocks * l.tile * c.head_dim * sizeof(float));
@@ -438,7 +443,7 @@ slnr_status attention4(const slnr_rows* q, int32_t nheads_q, const slnr_cache4* 
     const Rows4Layout l = rows4_layout(shape, *pages, group.d);
     SLNR_CHECK(check_ws(opts, l.total));
     SLNR_CHECK(validated(opts, check));
-    const Attn4Args a{p, c4, view(*q), group, scale, out, lse, l.tile, l.rows, l.nblocks, 4, (int4*)(ws + l.shares),
+    const Attn4Args a{p, c4, view(*q), group, scale, out, lse, l.tile, l.rows, l.nblocks, l.least, (int4*)(ws + l.shares),
                       (float*)(ws + l.part), (float2*)(ws + l.ml)};
     SLNR_LAUNCH("paged4_rows", launch_paged4_rows(a, dtype, s));
     SLNR_LAUNCH("paged4_join", launch_paged4_join(a, dtype, hdr, s));
