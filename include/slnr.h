@@ -405,12 +405,13 @@ slnr_status slnr_selected_attention(const slnr_rows *q, int32_t nheads_q, const 
  *  - head_dim is 32, 64, 96 or 128, the page size a multiple of 16.
  *  - A page of one head is page_size head_dim 9/8 bytes, in an order of the
  *    library's own, at 16-byte aligned strides; its slots may be written in any
- *    order and again, by slnr_page_append4.  slnr_page_copy4 copies pages.
+ *    order and again, by slnr_page_append4 (no slot twice in one call).
+ *    slnr_page_copy4 copies pages.
  *  - Queries, new keys and values are bf16 or fp16 (dtype: slnr_dtype), and so
  *    are the outputs; products, sums and maxima are fp32.  The softmax weights
  *    are rounded once before their product with the values, to fp16 (to bf16
  *    where a request has more than 32 query rows a key head and the queries are
- *    bf16).  Of a row of bf16 queries, columns below 2^-28 of its largest are
+ *    bf16).  Of a row of bf16 queries, columns below 2^-28 of its largest may be
  *    rounded by 2^-39 of that.
  *  - What the section above says of tokens, positions, slots, tables, waits and
  *    validate mode holds here too.
@@ -477,7 +478,10 @@ slnr_status slnr_page_fork(int32_t nreq, const int32_t *lens, const int32_t *tab
 
 /* The pages that no request holds: free_pages[npages] in ascending order, -1
  * behind them, and count[0] of them.  First lens[drop[i]] = 0 for i < ndrop
- * (entries that are no requests are skipped).  npages <= 8388608. */
+ * (entries that are no requests are skipped).  slnr_page_tables and
+ * slnr_page_fork take the list whole: where its pages run out entries and slots
+ * are -1 (validate mode of slnr_page_tables looks at its length alone).  npages
+ * <= 8388608. */
 slnr_status slnr_page_free(int32_t nreq, int32_t *lens, const int32_t *table, int64_t table_stride, int32_t width,
                            int32_t page_size, const int32_t *drop, int32_t ndrop, int32_t npages, int32_t *free_pages,
                            int32_t *count, const slnr_opts *opts);

@@ -29,15 +29,16 @@
 // through are joined by k_paged4_join.
 //
 // 64 single tokens over 9000 keys each, 32 query and 8 key heads of 128, bf16 (663 MB):
-// 126 us of kernel time, 5.3 TB/s, and a call of 132.  Bound by instructions: 289 of a warp
-// a slab, 2.3 a value, of which logical and byte-permuting ones take 54 % of their pipe's
-// time, fp16 ones 39 %, products 26 %; out of L2 alone it takes 3 % less.  What brought it
-// here (us a call, 64 tokens over 1001 to 32003 keys): 179 to begin with; 153 two values at a
-// time in the softmax, whole units without masks, look-ups of 16 units at once, 16 warps an
-// SM; 147 the copies' state in shared memory; 142 a kernel a width.  12 or 16 warps
-// an SM, two or three stages, 16 or 32 keys at once made no difference.  Of 17 to 32 rows a
-// warp takes a slab at a time (64 requests of 8 tokens 305 us; two slabs, with
-// registers spilled, 686; the tensor cores' kernel, as for 36 rows, 571).
+// 119 us of kernel time, 5.6 TB/s, and a call of 124.  Bound by instructions: 281 of a warp
+// a slab, 2.2 a value, of which logical and byte-permuting ones take 56 % of their pipe's
+// time, fp16 ones 40 %, products 27 %.  What brought it here (us a call, 64 tokens over 1001
+// to 32003 keys): 179 to begin with; 153 two values at a time in the softmax, whole units
+// without masks, look-ups of 16 units at once, 16 warps an SM; 147 the copies' state in
+// shared memory; 142 a kernel a width; 136 the scales of two keys side by side, halves of
+// which the multiplications pick by themselves.  12 or 16 warps an SM, two or three stages, 16
+// or 32 keys at once made no difference, nor did keys out of L2 alone (3 % less).  Of 17 to
+// 32 rows a warp takes a slab at a time (64 requests of 8 tokens 290 us; two slabs, with
+// registers spilled, 686; the tensor cores' kernel, as for 36 rows, 523).
 #include <type_traits>
 
 #include "cache4.cuh"

@@ -107,14 +107,14 @@ struct LoadShared : Shared {
 // keys, then their values) beside the tiles, six unpack them, every sixth of all slabs
 // each.  The ring is handed over by half steps, of which each of the six reads: none can
 // be a turn of the ring ahead of another, whose turns it tells apart by parity alone.
-// 4096 tokens over 16384 keys, 32 query and 8 key heads of 128, bf16: 738 us of kernel time,
-// 1.30 PFLOP/s, where 16 bits take 630: a half step's slabs take the six warps 1.8k
-// cycles, its products and weights 1.65k (621 us in all if nothing were unpacked).  What
-// brought it there (us a call): 1976 four warps that loaded codes themselves; 1289 bulk
-// copies to rings of the warps' own; 1166 instructions and bank conflicts fewer; 986 seven
-// warps; 776 one of them copying for the others, all by half steps; 753 a kernel a width.
-// fp16 for both products where queries are bf16, whose codes take 9 instructions a word and
-// not 11, made O's rescaling so frequent that it took 823.
+// 4096 tokens over 16384 keys, 32 query and 8 key heads of 128, bf16: 719 us of kernel time,
+// 1.34 PFLOP/s, where 16 bits take 630: the slabs of a half step take the six warps longer
+// than its products and weights (621 us in all if nothing were unpacked).  What brought it
+// there (us a call): 1976 four warps that loaded codes themselves; 1289 bulk copies to rings
+// of the warps' own; 1166 fewer instructions and bank conflicts; 986 seven warps; 776 one of
+// them copying for the others, all by half steps; 753 a kernel a width; 736 the scales of two
+// blocks at once.  fp16 for both products where queries are bf16, whose codes take 9 instructions
+// a word and not 11, made O's rescaling so frequent that it took 823.
 constexpr int kCopyWarp = 13;
 constexpr int kUnpackWarps = 6;  // 8-11, 14, 15
 constexpr int kStepSlabs = kChunkKeys / kSlab;
