@@ -79,6 +79,34 @@ def test_append_and_values(slnr, dtype, D, H, page):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_every_largest_value(slnr, dtype):
+    """Each finite number as the largest of a block, beside halves of its scale's steps and numbers next to them."""
+    g = torch.Generator().manual_seed(2)
+    m = torch.arange(0, 0x7f80 if dtype == BF16 else 0x7c00, dtype=torch.int16).view(dtype)
+    step = P.held(torch.cat([m[:, None]] + [torch.zeros_like(m)[:, None]] * 15, 1))[:, :1] / 7  # the scale, or less of a step
+    n = torch.randint(-7, 7, (len(m), 14), generator=g).double() + 0.5
+    rest = (n * step).clamp(-m[:, None].double(), m[:, None].double()).to(dtype)
+    rest[:, ::3] = (rest[:, ::3].view(torch.int16) + 1).view(dtype)
+    rest = torch.where(rest.double().abs() <= m[:, None].double(), rest, torch.zeros_like(rest))
+    x = torch.cat([m[:, None], rest, -m[:, None]], dim=1)
+    page, H, D = 64, 2, 64
+    per = H * D // 16
+    T = -(-len(m) // per)
+    x = torch.cat([x, torch.zeros((T * per - len(m), 16), dtype=dtype)]).reshape(T, H, D)
+    npages = -(-T // page)
+    k = torch.zeros((npages * page, H, D), dtype=dtype)
+    k[:T] = x
+    k = k.reshape(npages, page, H, D)
+    cache = P.written(slnr, k, -k, torch.arange(npages, dtype=torch.int32)[None], [T], npages, page, H, D)
+    for got, want in zip(slnr.page_values(cache, dtype=dtype), (x, -x)):
+        same(got.reshape(-1, H, D)[:T], P.held(want))
+    off = (P.held(x) - x.double()).abs().reshape(-1, 16)[:len(m)]
+    scale = P.SCALES[P.np.searchsorted(P.SCALES * 7.5, m.double().numpy().clip(max=7.5 * P.MOST))]
+    ordinary = m.double() <= 7.5 * P.MOST
+    assert (off[ordinary] <= torch.from_numpy(scale)[ordinary][:, None] / 2).all()  # as the format promises
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
 def test_values_of_some_pages(slnr, dtype):
     """Pages in any order, twice, and entries that are none; the values are exact in both types."""
     g = torch.Generator().manual_seed(3)
