@@ -196,7 +196,16 @@ __device__ __forceinline__ void clip(Part& s, int64_t left) {
   s.u1 = (int)(s.q.units - s.u0 < left ? s.q.units : s.u0 + left);
   s.left = left - (s.u1 - s.u0);
 }
-// The next one; its left is below 0 where there is none.
+// The first request behind r with new tokens, 32 at a look (a whole warp; nreq: none).
+__device__ __forceinline__ int next_request(const PagesView& p, int r) {
+  for (int r0 = r + 1; r0 < p.nreq; r0 += 32) {
+    const int i = r0 + (threadIdx.x & 31);
+    const unsigned on = __ballot_sync(0xffffffffu, i < p.nreq && __ldg(p.q_pos + i + 1) > __ldg(p.q_pos + i));
+    if (on) return r0 + __ffs(on) - 1;
+  }
+  return p.nreq;
+}
+// The next part (a whole warp); its left is below 0 where there is none.
 __device__ __forceinline__ void advance(const Attn4Args& a, Part& s) {
   if (s.left <= 0) {
     s.left = -1;
@@ -204,9 +213,9 @@ __device__ __forceinline__ void advance(const Attn4Args& a, Part& s) {
   }
   if (++s.h == a.c.nheads) {
     s.h = 0;
-    do s.q = request(a.p, s.q.r + 1);
-    while (s.q.units == 0 && s.q.r < a.p.nreq);
-    if (s.q.r >= a.p.nreq) {  // not met: the shares end with the last item
+    s.q = request(a.p, s.q.r + 1);
+    if (s.q.units == 0) s.q = request(a.p, next_request(a.p, s.q.r));
+    if (s.q.units == 0) {  // not met: the shares end with the last item
       s.left = -1;
       return;
     }

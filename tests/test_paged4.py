@@ -166,6 +166,17 @@ def test_lengths(slnr, lens, heads, D, page, first):
     b.check(slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), validate=True), b.attention(D ** -0.5))
 
 
+@pytest.mark.parametrize("heads", [(4, 2), (24, 1)])
+def test_few_of_many_requests_have_tokens(slnr, heads):
+    """Long runs of requests without new tokens, at the ends too, before and behind long and short ones."""
+    g = torch.Generator().manual_seed(12)
+    lens = [(0, int(torch.randint(0, 40, (1,), generator=g))) for _ in range(1500)]
+    for r, n in ((31, 900), (32, 17), (64, 1), (500, 3000), (501, 0), (1130, 64), (1467, 333)):
+        lens[r] = (1, n)
+    b = P.Batch4(slnr, lens, 16, *heads, 64, seed=13)
+    b.check(slnr.paged_attention(b.q.cuda(), b.cache(), b.tables(), validate=True), b.attention(0.125))
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP16])
 @pytest.mark.parametrize("heads", [(7, 1), (12, 1), (32, 1), (33, 1), (64, 2), (512, 1)])
 def test_many_query_heads(slnr, dtype, heads):
