@@ -155,31 +155,46 @@ __device__ __forceinline__ Request request(const PagesView& p, int r) {
   return q;
 }
 
-// Inclusive sum of the warp's units (of one key head) of requests r0 .. r0 + 31, a lane each.
-__device__ __forceinline__ int64_t units_of_32(const PagesView& p, int r0, int& mine) {
-  const int lane = threadIdx.x & 31, i = r0 + lane;
-  mine = i < p.nreq ? units_of(__ldg(p.q_pos + i + 1) - __ldg(p.q_pos + i), __ldg(p.k_len + i)) : 0;
-  int64_t sum = mine;
+// Units (of one key head) of requests r0 .. r0 + 127, four neighbours a lane.  Every warp
+// reads the lengths of all requests (4096 of one token and 100 keys 302 us of the GPU, 20000
+// of 20 keys 494; 32 at a time 375 and 962).  A part of them a thread, joined by the block,
+// took 270 and 262, but left the compiler with a slower loop for everyone (64 tokens over
+// 9000 keys 121 -> 125).
+struct Units {
+  int n[4];
+  __device__ __forceinline__ Units(const PagesView& p, int r0) {
+    const int r = r0 + 4 * (threadIdx.x & 31);
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += y;
+    for (int i = 0; i < 4; ++i)
+      n[i] = r + i < p.nreq ? units_of(__ldg(p.q_pos + r + i + 1) - __ldg(p.q_pos + r + i), __ldg(p.k_len + r + i)) : 0;
   }
-  return sum;
-}
+  __device__ __forceinline__ int64_t sum() const { return (int64_t)n[0] + n[1] + n[2] + n[3]; }
+};
 // The request that holds unit `at` of `heads` heads each, and the units of one head
-// before it; first, first_mine: units_of_32 of request 0.
-__device__ __forceinline__ int find_unit(const PagesView& p, int heads, int64_t at, int64_t first, int first_mine,
-                                         int64_t& before) {
+// before it (a whole warp); first: of requests 0 .. 127.
+__device__ __forceinline__ int find_unit(const PagesView& p, int heads, int64_t at, const Units& first, int64_t& before) {
+  const int lane = threadIdx.x & 31;
   before = 0;
-  for (int r0 = 0; r0 < p.nreq; r0 += 32) {
-    int mine = first_mine;
-    const int64_t sum = r0 == 0 ? first : units_of_32(p, r0, mine);
+  for (int r0 = 0; r0 < p.nreq; r0 += 128) {
+    const Units u = r0 == 0 ? first : Units(p, r0);
+    int64_t sum = u.sum();
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
     const unsigned past = __ballot_sync(0xffffffffu, (before + sum) * heads > at);
     if (past) {
       const int from = __ffs(past) - 1;
-      before += __shfl_sync(0xffffffffu, sum - mine, from);
-      return r0 + from;
+      before += __shfl_sync(0xffffffffu, sum - u.sum(), from);
+      int r = r0 + 4 * from;
+      for (int i = 0; i < 3; ++i) {
+        const int64_t next = before + __shfl_sync(0xffffffffu, i == 0 ? u.n[0] : i == 1 ? u.n[1] : u.n[2], from);
+        if (next * heads > at) break;
+        before = next;
+        ++r;
+      }
+      return r;
     }
     before += __shfl_sync(0xffffffffu, sum, 31);
   }
@@ -257,13 +272,12 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   let_next_start();
 
   // the block's share
-  int first_mine;
-  const int64_t first_sum = units_of_32(p, 0, first_mine);
-  int64_t total = __shfl_sync(0xffffffffu, first_sum, 31);
-  for (int r0 = 32; r0 < p.nreq; r0 += 32) {
-    int mine;
-    total += __shfl_sync(0xffffffffu, units_of_32(p, r0, mine), 31);
-  }
+  const Units first_units(p, 0);
+  int64_t total = first_units.sum();
+#pragma unroll 2
+  for (int r0 = 128; r0 < p.nreq; r0 += 128) total += Units(p, r0).sum();
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
   total *= c.nheads;
   const int64_t most = (total + a.least - 1) / a.least;
   const int n = (int)(most < gridDim.x ? most : gridDim.x);
@@ -276,7 +290,7 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   Part s;
   {
     int64_t before;
-    s.q = request(p, find_unit(p, c.nheads, lo, first_sum, first_mine, before));
+    s.q = request(p, find_unit(p, c.nheads, lo, first_units, before));
     const int64_t in = lo - before * c.nheads;
     s.h = (int)(in / s.q.units);
     s.u0 = (int)(in - (int64_t)s.h * s.q.units);
