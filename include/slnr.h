@@ -414,7 +414,8 @@ slnr_status slnr_selected_attention(const slnr_rows *q, int32_t nheads_q, const 
  *    bf16).  Of a row of bf16 queries, columns below 2^-28 of its largest may be
  *    rounded by 2^-39 of that.
  *  - What the section above says of tokens, positions, slots, tables, waits and
- *    validate mode holds here too.
+ *    validate mode holds here too; keys and values behind an entry that is no
+ *    page are zeros (without opts->validate, which refuses them).
  */
 typedef struct slnr_cache4 {
   int32_t npages, page_size, nheads, head_dim;

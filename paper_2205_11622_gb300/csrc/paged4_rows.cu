@@ -102,6 +102,15 @@ __device__ __forceinline__ uint32_t lds_half(uint32_t at) {
   asm volatile("ld.shared.b16 %0, [%1];" : "=h"(r) : "r"(at) : "memory");
   return r;
 }
+// Zeros for the scales of a slab's keys and values.
+template <int D>
+__device__ __forceinline__ void no_scales(uint32_t slab) {
+#pragma unroll 1
+  for (int i = 0; i < D; i += 16) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(slab + 8 * D + i), "r"(0) : "memory");
+    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(slab + 17 * D + i), "r"(0) : "memory");
+  }
+}
 // An 8 x 8 matrix of 16-bit values, a pair of a row's neighbours a lane, turned.
 __device__ __forceinline__ uint32_t turned(uint32_t x) {
   uint32_t r;
@@ -245,6 +254,7 @@ struct Ahead {
   Part part;
   int unit;
   uint32_t have;               // bit l: src[l] is a slab that is there
+  uint32_t lost;               // bit l: it has keys, but the table names no page for them
   const uint8_t* src[2 * kBatch];  // of unit i of the batch, slab k: at 2 i + k
 };
 struct Shared {
@@ -324,18 +334,20 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
     done = 0;
     const int key = (cu + kWarps * (lane >> 1)) * kUnit + (lane & 1) * kSlab;
     int id = -1, at = 0;
-    if ((lane >> 1) < units && key < cs.q.keys) {
+    const bool keys = (lane >> 1) < units && key < cs.q.keys;
+    if (keys) {
       const int i = c.slots.div(key);
       at = (int)((unsigned)(key - i * c.slots.d) / kSlab);
       if (i < p.width) id = __ldg(p.table + cs.q.r * p.table_stride + i);
     }
     const bool on = (unsigned)id < (unsigned)c.npages;
-    const uint32_t have = __ballot_sync(0xffffffffu, on);
+    const uint32_t have = __ballot_sync(0xffffffffu, on), lost = __ballot_sync(0xffffffffu, keys && !on);
     if (on) ahead.src[lane] = c.data + id * c.page + cs.h * c.head + (int64_t)at * slab;
     if (lane == 0) {
       ahead.part = cs;
       ahead.unit = cu + kWarps * units;
       ahead.have = have;
+      ahead.lost = lost;
     }
     __syncwarp();
   };
@@ -343,8 +355,13 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
     if (done == units) look_up();
     if (units == 0) return;
     if ((lane >> 1) == done) {
-      const uint32_t both = (ahead.have >> 2 * done) & 3;
+      const uint32_t both = (ahead.have >> 2 * done) & 3, lost = (ahead.lost >> 2 * done) & 3;
       uint64_t* bar = full + stage;
+      if (lost) {  // such slabs are zeros: without their scales what the stage held last is none
+        if (lost >> (lane & 1) & 1) no_scales<D>(ring + (stage * 2 + (lane & 1)) * slab);
+        tc::fence_proxy_async_smem();  // before the stage's next copies
+        __syncwarp(3u << (2 * done));
+      }
       if ((lane & 1) == 0) tc::mbar_expect(bar, __popc(both) * slab);
       __syncwarp(3u << (2 * done));
       if ((both >> (lane & 1) & 1) && !(whole && lane & 1 && both == 3))
