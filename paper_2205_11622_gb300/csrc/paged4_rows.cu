@@ -172,10 +172,10 @@ __device__ __forceinline__ Request request(const PagesView& p, int r) {
 struct Units {
   int n[4];
   __device__ __forceinline__ Units(const PagesView& p, int r0) {
-    const int r = r0 + 4 * (threadIdx.x & 31);
+    const unsigned r = item(r0, 4 * (threadIdx.x & 31));
+    const int32_t *q = p.q_pos + r, *k = p.k_len + r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      n[i] = r + i < p.nreq ? units_of(__ldg(p.q_pos + r + i + 1) - __ldg(p.q_pos + r + i), __ldg(p.k_len + r + i)) : 0;
+    for (int i = 0; i < 4; ++i) n[i] = r + i < (unsigned)p.nreq ? units_of(__ldg(q + i + 1) - __ldg(q + i), __ldg(k + i)) : 0;
   }
   __device__ __forceinline__ int64_t sum() const { return (int64_t)n[0] + n[1] + n[2] + n[3]; }
 };
@@ -184,7 +184,7 @@ struct Units {
 __device__ __forceinline__ int find_unit(const PagesView& p, int heads, int64_t at, const Units& first, int64_t& before) {
   const int lane = threadIdx.x & 31;
   before = 0;
-  for (int r0 = 0; r0 < p.nreq; r0 += 128) {
+  for (int r0 = 0; r0 < p.nreq; r0 = step_end(r0, 128, p.nreq)) {
     const Units u = r0 == 0 ? first : Units(p, r0);
     int64_t sum = u.sum();
 #pragma unroll
@@ -220,11 +220,11 @@ __device__ __forceinline__ void clip(Part& s, int64_t left) {
   s.u1 = (int)(s.q.units - s.u0 < left ? s.q.units : s.u0 + left);
   s.left = left - (s.u1 - s.u0);
 }
-// The first request behind r with new tokens, 32 at a look (a whole warp; nreq: none).
+// The first request behind r (at most nreq) with new tokens, 32 at a look (a whole warp; nreq: none).
 __device__ __forceinline__ int next_request(const PagesView& p, int r) {
-  for (int r0 = r + 1; r0 < p.nreq; r0 += 32) {
-    const int i = r0 + (threadIdx.x & 31);
-    const unsigned on = __ballot_sync(0xffffffffu, i < p.nreq && __ldg(p.q_pos + i + 1) > __ldg(p.q_pos + i));
+  for (int r0 = step_end(r, 1, p.nreq); r0 < p.nreq; r0 = step_end(r0, 32, p.nreq)) {
+    const int32_t* q = p.q_pos + item(r0, threadIdx.x & 31);
+    const unsigned on = __ballot_sync(0xffffffffu, inside(r0, threadIdx.x & 31, p.nreq) && __ldg(q + 1) > __ldg(q));
     if (on) return r0 + __ffs(on) - 1;
   }
   return p.nreq;
@@ -285,7 +285,7 @@ k_paged4_rows(const __grid_constant__ Attn4Args a, long long limit) {
   const Units first_units(p, 0);
   int64_t total = first_units.sum();
 #pragma unroll 2
-  for (int r0 = 128; r0 < p.nreq; r0 += 128) total += Units(p, r0).sum();
+  for (int r0 = 128; r0 < p.nreq; r0 = step_end(r0, 128, p.nreq)) total += Units(p, r0).sum();
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
   total *= c.nheads;

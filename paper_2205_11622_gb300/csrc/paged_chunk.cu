@@ -497,9 +497,9 @@ k_paged_plan(AttnArgs a, WsHeader* hdr) {
   wait_for_previous();
   if (tid == 0) hdr->error = 0;
   int ntiles = 0;
-  for (int r0 = 0; r0 < p.nreq; r0 += kPlanThreads) {
-    const int r = r0 + tid;
-    const int rows = r < p.nreq ? (__ldg(p.q_pos + r + 1) - __ldg(p.q_pos + r)) * G : 0;
+  for (int r0 = 0; r0 < p.nreq; r0 = step_end(r0, kPlanThreads, p.nreq)) {
+    const int32_t* q = p.q_pos + item(r0, tid);
+    const int rows = inside(r0, tid, p.nreq) ? (__ldg(q + 1) - __ldg(q)) * G : 0;
     int total;
     const int mine = tiles_of(rows, kChunkRows), sum = block_sum(mine, total, s_warp);
     s_first[tid] = sum - mine;

@@ -15,10 +15,10 @@ template <typename Parts>
 __device__ __forceinline__ void find_part(int nreq, int b, Parts parts, int& r, int& nth) {
   const int lane = threadIdx.x & 31;
   int before = 0;
-  for (int r0 = 0; r0 < nreq; r0 += 128) {
+  for (int r0 = 0; r0 < nreq; r0 = step_end(r0, 128, nreq)) {
     int n[4], mine = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) n[i] = r0 + 4 * lane + i < nreq ? parts(r0 + 4 * lane + i) : 0;
+    for (int i = 0; i < 4; ++i) n[i] = inside(r0, 4 * lane + i, nreq) ? parts(r0 + 4 * lane + i) : 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) mine += n[i];
     int sum = mine;
@@ -32,7 +32,7 @@ __device__ __forceinline__ void find_part(int nreq, int b, Parts parts, int& r, 
       const int from = __ffs(past) - 1;
       int at = b - before - (sum - mine), i = 0;  // the lane's own, where it is the one
       while (i < 3 && at >= n[i]) at -= n[i++];
-      r = __shfl_sync(0xffffffffu, r0 + 4 * lane + i, from);
+      r = __shfl_sync(0xffffffffu, (int)item(r0, 4 * lane + i), from);
       nth = __shfl_sync(0xffffffffu, at, from);
       return;
     }

@@ -34,9 +34,9 @@ k_page_tables(int nreq, const int32_t* __restrict__ new_len, const int32_t* __re
   const int t0 = blockIdx.x * kTablesTokens;
   const int t1 = step_end(t0, kTablesTokens, ntok);
   int tok_base = 0, pg_base = 0;
-  for (int r0 = 0; r0 < nreq; r0 += kTablesThreads) {
-    const int r = r0 + tid;
-    const bool on = r < nreq;
+  for (int r0 = 0; r0 < nreq; r0 = step_end(r0, kTablesThreads, nreq)) {
+    const unsigned r = item(r0, tid);
+    const bool on = inside(r0, tid, nreq);
     const int n = on ? max(new_len[r], 0) : 0, old = on ? max(old_len[r], 0) : 0;
     const int end = n > INT32_MAX - old ? INT32_MAX : old + n;
     const int take = clamped_div_up(end, page) - clamped_div_up(old, page);
@@ -80,7 +80,7 @@ k_page_tables(int nreq, const int32_t* __restrict__ new_len, const int32_t* __re
         if (s_tok[i + w] <= t) i += w;
       const int o = s_old[i], p = (int)((unsigned)o + (unsigned)t - (unsigned)s_tok[i]);
       int id = -1, off = 0;
-      if (p >= o && r0 + i < nreq) {
+      if (p >= o && inside(r0, i, nreq)) {
         const int held = clamped_div_up(o, page), n_page = page.div(p);
         off = p - n_page * page.d;
         if (n_page < held) {
@@ -264,7 +264,7 @@ __global__ void k_validate_lengths(int nreq, const int32_t* new_len, const int32
   if (threadIdx.x == 0) s_tok = s_pg = 0;
   __syncthreads();
   int bad = 0;
-  for (int r = threadIdx.x; r < nreq; r += blockDim.x) {
+  for (int64_t r = threadIdx.x; r < nreq; r += blockDim.x) {
     const long long n = new_len[r], o = old_len[r];
     if (n < 0 || o < 0 || n + o > (long long)width * page.d || n + o >= (1ll << 31)) {
       bad |= kErrPos;

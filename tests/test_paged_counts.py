@@ -1,0 +1,66 @@
+"""Calls over as many requests, tokens and entries of lists as an int counts: the steps of the kernels' loops end behind the
+last one (no GPU needed: the arrays of such a call take 8 GB each)."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2205_11622_gb300", "csrc")
+MOST = 2 ** 31 - 1
+SOURCES = sorted(f for f in os.listdir(CSRC) if re.match(r"page[ds_4]?.*\.cuh?$", f))
+
+WALK = """
+#include "range.h"
+// How often requests [r, end) are looked at, by lanes of `each` neighbours, `step` at a time; -1: one outside of them
+extern "C" long long walk(int r, int step, int each, int end) {
+  long long seen = 0;
+  for (int r0 = r; r0 < end; r0 = slnr::step_end(r0, step, end))
+    for (int lane = 0; lane < step / each; ++lane)
+      for (int i = 0; i < each; ++i)
+        if (slnr::inside(r0, each * lane + i, end)) {
+          if (slnr::item(r0, each * lane + i) >= (unsigned)end) return -1;
+          ++seen;
+        }
+  return seen;
+}
+"""
+
+
+def code(name):
+    with open(os.path.join(CSRC, name)) as f:
+        return re.sub(r"//[^\n]*", "", f.read())
+
+
+@pytest.fixture(scope="module")
+def walk(tmp_path_factory):
+    d = tmp_path_factory.mktemp("walk")
+    (d / "walk.cpp").write_text(WALK)
+    so = str(d / "walk.so")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, str(d / "walk.cpp"),
+                    "-o", so], check=True)
+    f = ctypes.CDLL(so).walk
+    f.restype = ctypes.c_longlong
+    return f
+
+
+@pytest.mark.parametrize("step,each", [(32, 1), (128, 4), (1024, 1)])
+@pytest.mark.parametrize("nreq", [0, 1, 127, 128, 5000, MOST - 1000, MOST - 1, MOST])
+def test_requests_are_looked_at_once(walk, step, each, nreq):
+    first = max(0, nreq - 3 * step - 1)
+    assert walk(first, step, each, nreq) == nreq - first
+
+
+def test_loops_over_requests_use_those_steps():
+    """A counter of requests that is an int is stepped by step_end and compared by inside: its sum with a step, or with a lane,
+    passes the largest int before it passes nreq."""
+    assert {"pages.cu", "paged4_rows.cu", "paged_chunk.cu", "paged_tile.cuh", "page_sets.cu"} <= set(SOURCES)
+    loops = 0
+    for name in SOURCES:
+        text = code(name)
+        for m in re.finditer(r"for \(\s*(?P<type>\w+) (?P<i>\w+) = [^;]*; (?P=i) < (?:\w+\.)?nreq; (?P<step>[^{;]*)\)", text):
+            loops += 1
+            assert m["type"] == "int64_t" or m["step"].startswith(m["i"] + " = step_end("), f"{name}: {m[0]}"
+        assert not re.search(r"\b(?:r0|r|i)\b \+ [^;=]*< (?:\w+\.)?nreq", text), name
+    assert loops >= 8
