@@ -227,7 +227,7 @@ k_page_free(TablesView t, int32_t* lens, const int32_t* __restrict__ drop, int n
   __shared__ SetShared sh;
   int* prefix = reinterpret_cast<int*>(bits + words);
   const int rank = (int)cluster_rank(), tid = threadIdx.x;
-  for (int i = rank * kSetThreads + tid; i < ndrop; i += kSetBlocks * kSetThreads) {
+  for (int64_t i = rank * kSetThreads + tid; i < ndrop; i += kSetBlocks * kSetThreads) {
     const int r = __ldg(drop + i);
     if ((unsigned)r < (unsigned)t.nreq) lens[r] = 0;
   }

@@ -64,3 +64,10 @@ def test_loops_over_requests_use_those_steps():
             assert m["type"] == "int64_t" or m["step"].startswith(m["i"] + " = step_end("), f"{name}: {m[0]}"
         assert not re.search(r"\b(?:r0|r|i)\b \+ [^;=]*< (?:\w+\.)?nreq", text), name
     assert loops >= 8
+
+
+def test_requests_that_end_are_counted_in_64_bits():
+    """page_free takes as many entries of drop as an int counts, 16384 a step: up to 2^31 - 1 of the same few requests."""
+    text = code("page_sets.cu")
+    loops = re.findall(r"for \((\w+) \w+ = [^;]*; \w+ < ndrop;", text)
+    assert loops and set(loops) == {"int64_t"}
