@@ -354,7 +354,8 @@ slnr_status slnr_page_tables(int32_t nreq, const int32_t *new_len, const int32_t
  * request's new tokens lie behind its older keys, k_len[r] of them in all.
  * Where cache->codes is not NULL, each page whose last slot is written gets its
  * summary, per head: m = the mean of its keys, scale = max|m| / 127, codes = m /
- * scale rounded to the nearest whole number (0 if scale is 0). */
+ * scale rounded to the nearest whole number (0 if scale is 0).  At most 2^31 -
+ * 2^16 tokens a call. */
 slnr_status slnr_page_append(const slnr_cache *cache, const slnr_pages *pages, const slnr_rows *k,
                              const slnr_rows *v, const slnr_opts *opts);
 

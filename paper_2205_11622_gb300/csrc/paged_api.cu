@@ -507,6 +507,8 @@ slnr_status slnr_page_append(const slnr_cache* cache, const slnr_pages* pages, c
   SLNR_CHECK(check_rows("k", k, pages->ntok > 0));
   SLNR_CHECK(check_rows("v", v, pages->ntok > 0));
   if (pages->ntok == 0) return SLNR_OK;
+  if (pages->ntok > kMaxKeys)  // a block's loops step past its last token
+    return fail(SLNR_ERR_UNSUPPORTED, "ntok = %d: at most %d", (int)pages->ntok, kMaxKeys);
   cudaStream_t s = (cudaStream_t)opts->stream;
   const PagesView p = view(*pages);
   const CacheView c = view(*cache);

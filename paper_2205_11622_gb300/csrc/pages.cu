@@ -71,8 +71,9 @@ k_page_tables(int nreq, const int32_t* __restrict__ new_len, const int32_t* __re
       k_len[r] = end;
     }
     __syncthreads();
-    const int lo = max(t0, tok_base), hi = min(t1, tok_end);
-    for (int t = lo + tid; t < hi; t += kTablesThreads) {
+    const int lo = max(t0, tok_base), here = max(min(t1, tok_end), lo) - lo;
+    for (int j = tid; j < here; j += kTablesThreads) {
+      const int t = lo + j;
       // the last request of this step that starts at or before t (the ones after it that start there too are empty)
       int i = 0;
 #pragma unroll
@@ -98,9 +99,10 @@ k_page_tables(int nreq, const int32_t* __restrict__ new_len, const int32_t* __re
     pg_base = pg_end;
   }
   // tokens that no request has
-  for (int t = max(t0, tok_base) + tid; t < t1; t += kTablesThreads) {
-    req[t] = -1;
-    slots[t] = -1;
+  const int rest = max(t0, tok_base);
+  for (int j = tid; j < t1 - rest; j += kTablesThreads) {
+    req[rest + j] = -1;
+    slots[rest + j] = -1;
   }
   if (blockIdx.x == 0 && tid == 0) {
     q_pos[nreq] = tok_base;

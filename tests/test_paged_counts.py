@@ -7,6 +7,9 @@ import subprocess
 
 import pytest
 
+import paper_2205_11622_gb300 as slnr
+from test_paged_abi import UNSUPPORTED, WORKSPACE, cache, opts, pages, rows
+
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2205_11622_gb300", "csrc")
 MOST = 2 ** 31 - 1
 SOURCES = sorted(f for f in os.listdir(CSRC) if re.match(r"page[ds_4]?.*\.cuh?$", f))
@@ -71,3 +74,24 @@ def test_requests_that_end_are_counted_in_64_bits():
     text = code("page_sets.cu")
     loops = re.findall(r"for \((\w+) \w+ = [^;]*; \w+ < ndrop;", text)
     assert loops and set(loops) == {"int64_t"}
+
+
+def test_tokens_of_tables_are_counted_from_a_blocks_first():
+    """page_tables takes as many tokens as an int counts: a block's loops count from its own first one, so that no sum with a
+    step passes the largest int."""
+    text, loops = code("pages.cu"), 0
+    text = text[text.index("k_page_tables(int nreq"):text.index("k_page_append(")]
+    for m in re.finditer(r"for \(int (\w+) = ([^;]*); ([^;]*); \1 \+= kTablesThreads\)", text):
+        loops += 1
+        assert m[2] == "tid" and not re.search(r"< (t1|hi|ntok)$", m[3]), m[0]
+    assert loops == 2
+
+
+def test_page_append_refuses_more_tokens_than_its_steps_count():
+    """A block steps by up to 1024 tokens, as an int."""
+    slnr.build()
+    lib, p = slnr.lib(), ctypes.byref
+    k = rows(tok=128)
+    for ntok, status in ((2 ** 31 - 2 ** 16, WORKSPACE), (2 ** 31 - 2 ** 16 + 1, UNSUPPORTED), (MOST, UNSUPPORTED)):
+        step = pages(ntok=ntok, max_q=1)
+        assert lib.slnr_page_append(p(cache()), p(step), p(k), p(k), p(opts(validate=1))) == status, slnr.last_error()
