@@ -470,9 +470,10 @@ slnr_status slnr_page_copy4(const slnr_cache4 *to, const slnr_cache4 *from, cons
  * pages.  A last page that is not full stays with the first child of its parent;
  * each further child gets the next page of free_pages, and src[i] and dst[i]
  * (-1 where nothing is to be copied) name the copy that slnr_page_copy has to
- * make.  used[0] = pages taken; where free_pages is too short dst[i] and the
- * entry are -1 (validate: SLNR_ERR_INDEX for a parent past the last request
- * only).  Entries of a row behind its pages are -1.  n <= 65536. */
+ * make; an entry there that is negative stays so for all.  used[0] = pages
+ * taken; where free_pages is too short dst[i] and the entry are -1 (validate:
+ * SLNR_ERR_INDEX for a parent past the last request only).  Entries of a row
+ * behind its pages are -1.  n <= 65536. */
 slnr_status slnr_page_fork(int32_t nreq, const int32_t *lens, const int32_t *table, int64_t table_stride,
                            int32_t width, int32_t page_size, const int32_t *parent, int32_t n,
                            const int32_t *free_pages, int32_t nfree, int32_t *out_table, int32_t *out_lens,

@@ -327,7 +327,8 @@ k_page_fork(TablesView t, const int32_t* __restrict__ parent, int n, const int32
   auto length = [&](int p) { return (unsigned)p < (unsigned)t.nreq ? max(__ldg(t.lens + p), 0) : 0; };
   for (int i = c0 + warp; i < c1; i += kSetThreads / 32) {
     const int p = __ldg(parent + i), len = length(p), full = t.page.div(len);
-    const bool part = len - full * t.page.d != 0 && full < t.width;
+    // a last page that is not full; an entry that is no page (free pages had run out) stays what it is
+    const bool part = len - full * t.page.d != 0 && full < t.width && __ldg(t.table + p * t.stride + full) >= 0;
     bool found = false;
     for (int j = 0; part && !found && j < i; j += 128) {
       bool same = false;
