@@ -324,7 +324,9 @@ k_page_fork(TablesView t, const int32_t* __restrict__ parent, int n, const int32
   __shared__ int s_dst[kForkChildren];  // 1 where the last page is copied, then the page that it goes to; -2: it is not
   const int rank = (int)cluster_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (n + kSetBlocks - 1) / kSetBlocks, c0 = min(rank * per, n), c1 = min(c0 + per, n);
-  auto length = [&](int p) { return (unsigned)p < (unsigned)t.nreq ? max(__ldg(t.lens + p), 0) : 0; };
+  const int64_t slots = (int64_t)t.width * t.page.d;
+  const int most = slots < INT32_MAX ? (int)slots : INT32_MAX;  // keys of a request
+  auto length = [&](int p) { return (unsigned)p < (unsigned)t.nreq ? min(max(__ldg(t.lens + p), 0), most) : 0; };
   for (int i = c0 + warp; i < c1; i += kSetThreads / 32) {
     const int p = __ldg(parent + i), len = length(p), full = t.page.div(len);
     // a last page that is not full; an entry that is no page (free pages had run out) stays what it is
