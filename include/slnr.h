@@ -303,7 +303,8 @@ typedef struct slnr_pages {
   int32_t ntok;         /* new tokens in all == q_pos[nreq] */
   int32_t max_q;        /* no request has more new tokens */
   int32_t max_k;        /* no request has more keys; <= width * page size, below 2^31 - 2^16 in whole pages.  The work is
-                           laid out by these two: bounds near the truth are faster, results do not depend on them */
+                           laid out by these two: bounds near the truth are faster.  Results depend on them by their
+                           rounding alone (which kernel takes the call) */
   int32_t width;        /* columns of table */
   int32_t reserved;     /* must be 0 */
   int64_t table_stride; /* from one row of table to the next */
@@ -411,9 +412,9 @@ slnr_status slnr_selected_attention(const slnr_rows *q, int32_t nheads_q, const 
  *  - Queries, new keys and values are bf16 or fp16 (dtype: slnr_dtype), and so
  *    are the outputs; products, sums and maxima are fp32.  The softmax weights
  *    are rounded once before their product with the values, to fp16 (to bf16
- *    where a request has more than 32 query rows a key head and the queries are
- *    bf16).  Of a row of bf16 queries, columns below 2^-28 of its largest may be
- *    rounded by 2^-39 of that.
+ *    where the queries are bf16 and max_q allows more than 32 query rows a key
+ *    head: max_q nheads_q / nheads > 32).  Of a row of bf16 queries, columns
+ *    below 2^-28 of its largest may be rounded by 2^-39 of that.
  *  - What the section above says of tokens, positions, slots, tables, waits and
  *    validate mode holds here too; keys and values behind an entry that is no
  *    page are zeros (without opts->validate, which refuses them).
@@ -471,9 +472,10 @@ slnr_status slnr_page_copy4(const slnr_cache4 *to, const slnr_cache4 *from, cons
  * each further child gets the next page of free_pages, and src[i] and dst[i]
  * (-1 where nothing is to be copied) name the copy that slnr_page_copy has to
  * make; an entry there that is negative stays so for all.  used[0] = pages
- * taken; where free_pages is too short dst[i] and the entry are -1 (validate:
- * SLNR_ERR_INDEX for a parent past the last request only).  Entries of a row
- * behind its pages are -1.  n <= 65536. */
+ * that they need; where free_pages has fewer dst[i] and the entry are -1
+ * (validate: SLNR_ERR_INDEX for a parent past the last request only).  Entries of a row
+ * behind its pages are -1.  n <= 65536; where few children share a parent the
+ * time grows with n squared (512 children 11 us, 4096 79, 65536 42 ms). */
 slnr_status slnr_page_fork(int32_t nreq, const int32_t *lens, const int32_t *table, int64_t table_stride,
                            int32_t width, int32_t page_size, const int32_t *parent, int32_t n,
                            const int32_t *free_pages, int32_t nfree, int32_t *out_table, int32_t *out_lens,

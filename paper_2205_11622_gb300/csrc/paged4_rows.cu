@@ -29,9 +29,13 @@
 // through are joined by k_paged4_join.
 //
 // 64 single tokens over 9000 keys each, 32 query and 8 key heads of 128, bf16 (663 MB):
-// 119 us of kernel time, 5.6 TB/s, and a call of 124.  Bound by instructions: 281 of a warp
-// a slab, 2.2 a value, of which logical and byte-permuting ones take 56 % of their pipe's
-// time, fp16 ones 40 %, products 27 %.  What brought it here (us a call, 64 tokens over 1001
+// 119 us of kernel time, 5.6 TB/s, and a call of 125.  No unit is full: 281 instructions of a
+// warp a slab, 2.2 a value, take 60 % of the issue slots, the logical and byte-permuting ones
+// 56 % of their pipe's time, fp16 ones 40 %, products 27 %, memory 70 %.  Of the four warps that
+// a scheduler has (registers allow no more) 1.3 are ready on average.  A warp's time is 21 % the
+// fixed delay of the instruction before in its chain (load, unpack, product, exponential,
+// transpose, product), 19 % another warp's turn, 17 % issuing, 16 % a pipe that another uses,
+// 11 % dispatch, 7 % global memory.  What brought it here (us a call, 64 tokens over 1001
 // to 32003 keys): 179 to begin with; 153 two values at a time in the softmax, whole units
 // without masks, look-ups of 16 units at once, 16 warps an SM; 147 the copies' state in
 // shared memory; 142 a kernel a width; 136 the scales of two keys side by side, halves of

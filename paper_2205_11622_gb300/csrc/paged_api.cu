@@ -382,8 +382,12 @@ slnr_status attention(const slnr_rows* q, int32_t nheads_q, const slnr_cache* ca
   return SLNR_OK;
 }
 
-// Attention over a cache in 4 bits: calls with a request of more than 32 query rows
-// of a key head go to the tensor-core kernel, the others to the row kernel.
+// Attention over a cache in 4 bits: calls whose bound max_q allows more than 32 query rows
+// of a key head go to the tensor-core kernel, the others to the row kernel, which has
+// registers for no more.  Up to there it is the faster one, whatever the number of requests
+// and keys (us a call by the row kernel and by the other, 32/8 heads of 128; 4, 16 and 32 rows
+// of each request: 1 request of 4096 keys 15, 17, 24 and 34-35; 1 of 32768 25, 27, 39 and 61-64;
+// 64 of 9000 125, 184, 290 and 517-520; 256 of 600 57, 93, 160 and 196-197).
 AttnPlan attn4_chunk_plan(const slnr_pages& p, int64_t group) {
   AttnPlan a{};
   const int64_t requests = p.nreq < p.ntok ? p.nreq : p.ntok, tiles = p.ntok * group / kChunkRows + requests;

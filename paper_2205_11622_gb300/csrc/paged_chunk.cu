@@ -185,9 +185,9 @@ __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
   return (uint32_t)((piece >> 3) * kBlock + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
 }
 
-// ---- keys and values in 4 bits (cache4.cuh): a load warp takes two slabs of each
-// 128 keys, its lanes 16-byte pieces of their codes, which become 16-bit rows of the
-// tile.
+// ---- keys and values in 4 bits (cache4.cuh): an unpacking warp takes every sixth
+// slab, its lanes 16-byte pieces of the slab's codes, which become 16-bit rows of
+// the tile.
 
 __device__ __forceinline__ uint32_t lds_u32(uint32_t at) {
   uint32_t r;

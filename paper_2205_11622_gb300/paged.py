@@ -50,10 +50,10 @@ class PageTables:
 
     table [R, width] (rows may be a slice of wider ones), q_pos [R + 1], k_len [R] (keys with the new tokens), req [T],
     slots [T] (page_append only).  max_q and max_k bound the new tokens and the keys of a request on the host.  The work
-    is laid out by them: a result does not depend on them, its time does.  One token over 4095 keys (32/8 heads of 128)
+    is laid out by them: a result depends on them by its rounding alone, its time in earnest.  One token over 4095 keys (32/8 heads of 128)
     takes 17 us of the GPU with max_k = 4095, 25 with 16384, 33 with 32768 and 52 with 131072; 64 single tokens over 581k
-    keys 421 with max_q = 1 and 658 with max_q = 64 (as chunks), page_select for them 52 and 263.  A captured call keeps
-    its bounds for every replay.  The tensors are held and read by each call that takes the tables.
+    keys 421 with max_q = 1 and 658 with max_q = 64 (as chunks), page_select for them 52 and 263; over a PagedCache4 127 with
+    max_q = 1, 306 with 8 and 543 with 9 or more (as chunks).  A captured call keeps its bounds for every replay.  The tensors are held and read by each call that takes the tables.
     """
     table: torch.Tensor
     q_pos: torch.Tensor
@@ -247,7 +247,8 @@ def page_tables(new_len, old_len, table, free_pages, page_size, ntok, max_q=None
     new_len, old_len [R]: new tokens, and keys already in the cache; free_pages: the pages to take from, in order; ntok
     = sum of new_len.  table [R, width] is written in place.  max_q and max_k go to the PageTables; the defaults, ntok and
     what a row of the table holds, are right for any lengths and wide for most (PageTables says what that costs): pass
-    max_q=1 where each request has one new token at most, and the longest request's keys as max_k where they are known."""
+    max_q=1 where each request has one new token at most, and the longest request's keys as max_k where they are known.
+    Where free pages run out the entries and slots of -1 are kept silently (validate refuses them)."""
     R, width, stride = _table(table)
     dev, n = table.device, free_pages.shape[0]
     ints = _empty(2 * R + 2 + 2 * ntok, torch.int32, dev, stream)
@@ -445,9 +446,10 @@ def page_copy(cache: PagedCache | PagedCache4, src, dst, source=None, validate=F
 def page_fork(table, lens, parent, free_pages, page_size, validate=False, workspace=None, stream=None):
     """Requests that go on from others (slnr_page_fork): child i from request parent[i] of table [R, width] and lens [R].
 
-    Returns (table [n, width], lens [n], src [n], dst [n], pages taken [1]) of the children; the old table and lengths are
+    Returns (table [n, width], lens [n], src [n], dst [n], pages needed [1]) of the children; the old table and lengths are
     not changed.  Full pages are shared; a last page that is not full stays with a parent's first child, and for the others
-    page_copy(cache, src, dst) has to copy it, in every cache that the tables are of."""
+    page_copy(cache, src, dst) has to copy it, in every cache that the tables are of.  Some hundred children take 10 us of
+    the GPU; of thousands with a parent each the time grows with their number squared (4096: 79 us, 65536: 42 ms)."""
     R, width, stride, at_lens, dev = _held_by(table, lens, page_size)
     n, nfree = parent.shape[0] if parent.dim() == 1 else -1, free_pages.shape[0]
     at_parent, at_free = _ints(parent, "parent", (n,), dev), _ints(free_pages, "free_pages", (nfree,), dev)
