@@ -475,7 +475,7 @@ slnr_status slnr_page_copy4(const slnr_cache4 *to, const slnr_cache4 *from, cons
  * that they need; where free_pages has fewer dst[i] and the entry are -1
  * (validate: SLNR_ERR_INDEX for a parent past the last request only).  Entries of a row
  * behind its pages are -1.  n <= 65536; where few children share a parent the
- * time grows with n squared (512 children 11 us, 4096 79, 65536 42 ms). */
+ * time grows with n squared (512 children 11 us, 4096 81, 65536 43 ms). */
 slnr_status slnr_page_fork(int32_t nreq, const int32_t *lens, const int32_t *table, int64_t table_stride,
                            int32_t width, int32_t page_size, const int32_t *parent, int32_t n,
                            const int32_t *free_pages, int32_t nfree, int32_t *out_table, int32_t *out_lens,

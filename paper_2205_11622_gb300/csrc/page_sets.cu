@@ -316,7 +316,7 @@ k_page_compact(TablesView t, int npages, int words, int32_t* out_table, int32_t*
 // has the same parent by looking (a warp a child, 128 at a time), which needs no
 // memory of the parents' number, and takes time with the children's number squared
 // where few of them share a parent (us of the GPU, of as many parents: 512 children
-// 11, 4096 79, 16384 837, 65536 42000; of one parent 9, 17, 42, 146).
+// 11, 4096 81, 16384 840, 65536 42600; of one parent 9, 17, 45, 157).
 constexpr int kForkChildren = kMaxForks / kSetBlocks;
 
 __global__ void __cluster_dims__(kSetBlocks, 1, 1) __launch_bounds__(kSetThreads)
